@@ -218,6 +218,121 @@ int nova_llm_decode_noalloc(const nova_llm* llm, const int32_t* ids, const int32
                             int max_blocks, int batch, int max_ctx, const nova_kv* kv, int32_t* next_ids,
                             float* logits, nova_stream_t stream);
 
+/* ------------------------------------------------------------------ operators over the paged cache
+ * Calls below the stages, for programs that batch, draft or move requests themselves.  One layer at
+ * a time, asynchronous on `stream`; device pointers are 16-byte aligned unless stated otherwise, and
+ * rows are [n_heads][head_dim] contiguous at a pitch of their own (a multiple of 16 bytes, so q, k
+ * and v may be views of one packed projection).  head_dim is 64 or 128.
+ *
+ * A cache layer of one of three types.  BF16 and F32 are a layer of a nova_kv pool.  E4M3 stores
+ * 8 bits per value: token t of a KV head is D OCP e4m3 numbers and one byte e + 127, the values
+ * being number * 2^e with the smallest e >= -100 that keeps |number| <= 448 (NaN and infinite values
+ * are stored as NaN).  Values read back are exact in bf16, and appending them again stores the same. */
+enum { NOVA_CACHE_BF16 = 0, NOVA_CACHE_F32 = 1, NOVA_CACHE_E4M3 = 2 };
+typedef struct {
+  void* k;          /* [num_blocks][n_kv][16][head_dim], 256-byte aligned */
+  void* v;          /* [num_blocks][n_kv][head_dim][16], 256-byte aligned */
+  uint8_t* k_exp;   /* E4M3: [num_blocks][n_kv][16]; else ignored */
+  uint8_t* v_exp;
+  int num_blocks, n_kv, head_dim, type;
+} nova_cache;
+/* Bytes of each of k and v of one layer (0 for invalid sizes); *exp_bytes (may be NULL): of each of
+ * k_exp and v_exp. */
+size_t nova_cache_bytes(int type, int num_blocks, int n_kv, int head_dim, size_t* exp_bytes);
+
+/* A batch of sequences over a cache and the rows (tokens) that each brings.  Row j of sequence b is
+ * row row_start[b] + j of the arrays and token ctx[b] + j of the sequence.  The arrays are read on
+ * the device when the kernels run; contents outside the stated bounds are clamped into them. */
+typedef struct {
+  const int32_t* row_start;  /* device int32 [batch + 1], ascending; NULL: max_rows rows each (rows == batch * max_rows) */
+  const int32_t* ctx;        /* device int32 [batch]: tokens in the cache before these rows; NULL: 0 */
+  const int32_t* tables;     /* device int32 [batch][max_blocks]: physical block of each 16 tokens; an
+                                entry outside the pool names no block: its tokens are neither written nor seen */
+  int max_blocks, batch;
+  int rows;                  /* rows of the arrays; those behind row_start[batch] are left as they were */
+  int max_rows;              /* upper bound of one sequence's rows; rows beyond it are left out */
+  int max_ctx;               /* upper bound of ctx[b] plus its rows, at most 16 * max_blocks */
+} nova_rows;
+
+/* Rotary embedding of the first `rot` dimensions (a multiple of 16, at most head_dim) of a head:
+ * pairs (c, c + rot/2), or (2c, 2c + 1) when interleaved, turned by position * f_c with
+ * f_c = theta^(-2c/rot).  Longer contexts: factor > 1 divides every f_c by it (linear interpolation);
+ * with orig_ctx > 0 only as far as f_c turns fewer than `beta` times over orig_ctx tokens, wholly at
+ * `alpha` turns and below (the "NTK-by-parts" interpolation of YaRN, arXiv 2309.00071, Eq. 18-20).
+ * Sines and cosines are multiplied by mscale.  Angles are formed in 64 bits. */
+typedef struct {
+  int rot, interleaved;
+  float theta, factor;
+  int orig_ctx;
+  float alpha, beta, mscale;
+} nova_rope;
+
+/* Append rows to a cache layer: q and k are rotated (rope NULL: not) at position pos[row] (device
+ * int32 [rows]; NULL: the token's number in its sequence), the rotated q goes to q_out, k and v into
+ * the cache (E4M3: quantised from the fp32 rotation, rounded once).
+ *  q, k, v: device, all of in_type (NOVA_ACT_BF16 / NOVA_ACT_F32), rows of n_q, n_kv and n_kv heads at
+ *           pitches in elements; q may be NULL (n_q 0): only k and v
+ *  q_out:   device, q_out_type; may be q itself (same type and pitch)
+ * No two rows may name the same slot of the same block (sequences that share a block append behind it). */
+int nova_kv_append(const nova_cache* cache, const nova_rows* rows, const nova_rope* rope, const int32_t* pos,
+                   int in_type, const void* q, int64_t q_pitch, int n_q, const void* k, int64_t k_pitch, const void* v,
+                   int64_t v_pitch, void* q_out, int q_out_type, int64_t q_out_pitch, nova_stream_t stream);
+
+/* Read cached rows back as dense rows of out_type: row j of sequence b is token slots[row] (device
+ * int32 [rows]; NULL: ctx[b] + j) of it.  Tokens of missing blocks read as zeros.  With the accepted
+ * tokens of a tree as slots, a following nova_kv_append (no rope) moves them behind the context. */
+int nova_kv_gather(const nova_cache* cache, const nova_rows* rows, const int32_t* slots, int out_type, void* k_out,
+                   int64_t k_pitch, void* v_out, int64_t v_pitch, nova_stream_t stream);
+
+/* Attention of each sequence's rows (drafted tokens, at most 64, already appended) over its cache:
+ * row j sees every token below ctx[b], and token ctx[b] + i where bit i of mask[row] is set
+ * (device uint64 [rows]; NULL: i <= j, a chain; one row per sequence is a decode step).  A row that
+ * sees nothing gets zeros; what a row does not see has no effect on it, whatever it holds.
+ *  q, out: device, bf16 (F32 with an F32 cache), n_q heads (a multiple of n_kv); scale is applied to q.k
+ *  ws:     device, nova_tree_attention_workspace_bytes(), 256-byte aligned; contents need not be kept
+ *          or cleared, but calls that may overlap in time need one each */
+size_t nova_tree_attention_workspace_bytes(const nova_cache* cache, const nova_rows* rows, int n_q);
+int nova_tree_attention(const nova_cache* cache, const nova_rows* rows, const uint64_t* mask, const void* q, int64_t q_pitch,
+                        int n_q, float scale, void* out, int64_t out_pitch, void* ws, size_t ws_bytes,
+                        nova_stream_t stream);
+
+/* ------------------------------------------------------------------ log probabilities
+ * From rows of logits (device, NOVA_ACT_BF16 / NOVA_ACT_F32, pitch in elements, any alignment of
+ * their element; as the LLM calls return them), in fp32:
+ *  given_lp[row][i] = log p(given[row][i]) (device int32 [rows][n_given]; -infinity for ids outside the
+ *                     vocabulary), n_given 0: none
+ *  entropy[row]     = -sum p log p; may be NULL
+ *  top_lp, top_ids[row][n_top]: the most likely tokens, descending, equal ones by the lower id (NaN
+ *                     counts as the largest); n_top <= 32 and <= vocab, 0: none
+ * A logit of -infinity has probability 0.  A row with a NaN or +infinity, or with nothing but
+ * -infinity, has NaN for every log probability of a token and for its entropy.  vocab <= 2^21.
+ *  ws: device, nova_logprobs_workspace_bytes(), 256-byte aligned, as for nova_tree_attention */
+size_t nova_logprobs_workspace_bytes(int rows, int vocab, int n_top);
+int nova_logprobs(const void* logits, int type, int64_t pitch, int rows, int vocab, const int32_t* given, int n_given,
+                  float* given_lp, float* entropy, int n_top, float* top_lp, int32_t* top_ids, void* ws,
+                  size_t ws_bytes, nova_stream_t stream);
+
+/* ------------------------------------------------------------------ LLM on a cache of any type
+ * nova_llm_prefill into a pool of nova_cache layers (cache describes layer 0; layer l's arrays follow
+ * at l times their size): the prompt's attention reads K and V as computed, the cache keeps them in
+ * its type.  The cache type is BF16 or E4M3 for a bf16 model, F32 for an fp32 one. */
+int nova_llm_prefill_cache(const nova_llm* llm, const void* vis, int n_vis, const int32_t* ids, int n_text,
+                           const int32_t* block_table, const nova_cache* cache, int32_t* next_id, float* logits,
+                           void* ws, size_t ws_bytes, nova_stream_t stream);
+
+/* One decode step over drafted tokens (speculative decoding): the rows' tokens ids run through the
+ * model together, each layer appending their K and V behind its sequence's context and attending by
+ * mask, as nova_kv_append and nova_tree_attention do.  One row per sequence is a plain decode step.
+ *  ids, pos: device int32 [rows], rows <= 32: tokens and their rotary positions
+ *  mask:     device uint64 [rows] or NULL (chains)
+ *  next_ids [rows], logits [rows][vocab] or NULL: as for nova_llm_decode, one per row
+ * The sequences keep only the tokens that the caller accepts: the rest of the slots are overwritten
+ * by the next step's rows. */
+size_t nova_llm_verify_workspace_bytes(const nova_llm* llm, const nova_cache* cache, const nova_rows* rows);
+int nova_llm_verify(const nova_llm* llm, const int32_t* ids, const int32_t* pos, const uint64_t* mask,
+                    const nova_rows* rows, const nova_cache* cache, int32_t* next_ids, float* logits, void* ws,
+                    size_t ws_bytes, nova_stream_t stream);
+
 /* ------------------------------------------------------------------ linear co-run study
  * The two-linear experiment behind the paper's choice of inter-CU partitioning (Sec. 3.2.1, its
  * linear co-run table, and Sec. 3.2.3): one linear layer out[M, N] += x[M, K] w[N, K]^T

@@ -19,7 +19,8 @@ BUILD = os.path.join(ROOT, "_build")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = os.environ.get("NOVA_ARCH", "gfx950")
 
-SOURCES = ["k_gemm.hip", "k_gemv.hip", "k_attn.hip", "k_decattn.hip", "k_misc.hip", "nova_abi.cpp"]
+SOURCES = ["k_gemm.hip", "k_gemv.hip", "k_attn.hip", "k_decattn.hip", "k_misc.hip", "k_cache.hip",
+           "k_tree.hip", "k_logits.hip", "nova_abi.cpp"]
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-munsafe-fp-atomics",
          # packed fp32 instructions stay disabled (the compiler would otherwise emit them from float2 code)
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

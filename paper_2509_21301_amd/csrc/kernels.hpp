@@ -198,4 +198,62 @@ hipError_t embed_rows(const T* vis, int n_vis, const int* ids, int n_ids, const 
 hipError_t argmax_rows(const float* logits, int B, int V, int* out, hipStream_t s);
 hipError_t cu_probe(hipStream_t s, uint32_t* out, int n);
 
+// ---- operators on the paged cache and on logits
+enum CacheType { CACHE_BF16 = 0, CACHE_F32 = 1, CACHE_E4M3 = 2 };
+// One layer's pool: k [num_blocks][n_kv][16][D], v [num_blocks][n_kv][D][16]; an e4m3 pool also keeps, per
+// token and head, the exponent byte e + 127 of its scale 2^e: [num_blocks][n_kv][16] each.
+struct CachePool {
+  void* k; void* v;
+  uint8_t* k_exp; uint8_t* v_exp;
+  int num_blocks, n_kv, D, type;
+};
+// The new rows of a batch of sequences over their cached tokens: rows row_start[b] .. row_start[b+1] - 1
+// are tokens ctx[b], ctx[b] + 1, ... of sequence b (row_start null: max_rows rows each; ctx null: 0).
+struct BatchRows {
+  const int* row_start; const int* ctx; const int* tables;
+  int max_blocks, batch, rows, max_rows, max_ctx;
+};
+struct AppendArgs {
+  CachePool c;
+  BatchRows r;
+  const int* pos;                       // rotary position of each row (null: its token number)
+  const void* q; const void* k; const void* v; long q_row, k_row, v_row; int n_q;   // q null: none
+  void* q_out; long q_out_row;
+  bool in_f32, q_out_f32;
+  int rot; bool interleaved;            // rotated dimensions (0: none)
+  float mscale;                         // factor of the sines and cosines
+  double turns[64];                     // turns of a pair per position: inverse frequency / 2 pi
+};
+hipError_t kv_append(const AppendArgs& p, int cus, hipStream_t s);
+struct GatherArgs {
+  CachePool c;
+  BatchRows r;
+  const int* slots;                     // token number of each row (null: ctx[b], ctx[b] + 1, ...)
+  void* k; void* v; long k_row, v_row;
+  bool out_f32;
+};
+hipError_t kv_gather(const GatherArgs& p, hipStream_t s);
+struct TreeArgs {
+  CachePool c;
+  BatchRows r;                          // max_rows <= 64
+  const unsigned long long* mask;       // drafted tokens each row sees (null: those up to its own)
+  const void* q; long q_row; int n_q;   // bf16 (f32 beside an f32 cache)
+  float scale;
+  void* out; long out_row;
+  float* partial;                       // tree_partial_floats() floats
+};
+size_t tree_partial_floats(int type, int n_kv, int n_q, int D, int batch, int rows, int max_rows, int max_ctx, int cus);
+hipError_t tree_attention(const TreeArgs& p, int cus, hipStream_t s);
+struct LogprobArgs {
+  const void* logits; bool f32; long stride;
+  int rows, vocab;
+  const int* given; int n_given; float* given_lp;      // [rows][n_given]
+  float* entropy;                                       // [rows] or null
+  int n_top; float* top_lp; int* top_ids;               // [rows][n_top]
+  float* part_sum; unsigned long long* part_top;        // logprobs_part_sizes()
+};
+bool logprobs_fits(int vocab, int n_top);
+void logprobs_part_sizes(int rows, int vocab, int n_top, size_t* sum_floats, size_t* top_keys);
+hipError_t logprobs(const LogprobArgs& p, hipStream_t s);
+
 }  // namespace nova

@@ -4,6 +4,7 @@
 #include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -688,6 +689,215 @@ DecodeBufs<T> decode_bufs(const nova_llm* m, int B, int max_ctx, void* base) {
 }
 }  // namespace
 
+// ------------------------------------------------------------------ operators over the paged cache
+namespace {
+int device_cus() { return g.cus > 0 ? g.cus : 256; }
+
+size_t cache_elem(int type) { return type == NOVA_CACHE_BF16 ? 2 : type == NOVA_CACHE_F32 ? 4 : type == NOVA_CACHE_E4M3 ? 1 : 0; }
+
+// Layer l of a pool whose layer 0 is `c`.
+nova::CachePool pool_layer(const nova_cache& c, int l) {
+  const size_t tokens = (size_t)c.num_blocks * c.n_kv * 16, bytes = tokens * c.head_dim * cache_elem(c.type);
+  const bool q8 = c.type == NOVA_CACHE_E4M3;
+  return nova::CachePool{(char*)c.k + l * bytes, (char*)c.v + l * bytes, q8 ? c.k_exp + l * tokens : nullptr,
+                         q8 ? c.v_exp + l * tokens : nullptr, c.num_blocks, c.n_kv, c.head_dim, c.type};
+}
+nova::BatchRows batch_rows(const nova_rows& r) {
+  return nova::BatchRows{r.row_start, r.ctx, r.tables, r.max_blocks, r.batch, r.rows, r.max_rows, r.max_ctx};
+}
+
+inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+inline bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
+
+int check_cache(const nova_cache* c) {
+  if (!c) return fail(NOVA_EINVAL, "null cache");
+  if (cache_elem(c->type) == 0) return fail(NOVA_EINVAL, "unknown cache type %d", c->type);
+  if (c->num_blocks <= 0 || c->n_kv <= 0) return fail(NOVA_EINVAL, "cache: non-positive sizes");
+  if (c->head_dim != 64 && c->head_dim != 128) return fail(NOVA_EUNSUPPORTED, "cache head_dim %d (supported: 64, 128)", c->head_dim);
+  if (!c->k || !c->v || !aligned(c->k) || !aligned(c->v)) return fail(NOVA_EINVAL, "cache k and v must be non-null and 256-byte aligned");
+  if (c->type == NOVA_CACHE_E4M3 && (!c->k_exp || !c->v_exp || !aligned16(c->k_exp) || !aligned16(c->v_exp)))
+    return fail(NOVA_EINVAL, "an e4m3 cache needs k_exp and v_exp, 16-byte aligned");
+  return NOVA_OK;
+}
+
+// `tokens`: rows are tokens ctx[b] + j, so that max_rows of them fit in max_ctx.
+int check_rows(const nova_rows* r, bool tokens) {
+  if (!r) return fail(NOVA_EINVAL, "null rows");
+  if (r->batch <= 0 || r->batch > 65535 || r->rows < 0 || r->max_rows <= 0 || r->max_blocks <= 0 || r->max_ctx <= 0)
+    return fail(NOVA_EINVAL, "rows: batch must be 1..65535, rows >= 0, max_rows, max_blocks and max_ctx positive");
+  if (!r->tables || !aligned4(r->tables) || !aligned4(r->row_start) || !aligned4(r->ctx))
+    return fail(NOVA_EINVAL, "rows: tables is null, or an array is misaligned");
+  if (!r->row_start && (int64_t)r->batch * r->max_rows != r->rows)
+    return fail(NOVA_EINVAL, "rows: without row_start, rows must be batch * max_rows");
+  if (tokens && r->max_rows > r->max_ctx) return fail(NOVA_EINVAL, "rows: max_rows %d above max_ctx %d", r->max_rows, r->max_ctx);
+  if (((int64_t)r->max_ctx + 15) / 16 > r->max_blocks) return fail(NOVA_ENOKV, "max_ctx %d exceeds the block table width %d", r->max_ctx, r->max_blocks);
+  return NOVA_OK;
+}
+
+// Rows of `heads` heads of D elements of `elem` bytes.
+int check_matrix(const char* what, const void* p, int64_t pitch, int heads, int D, size_t elem) {
+  if (!p || !aligned16(p)) return fail(NOVA_EINVAL, "%s must be non-null and 16-byte aligned", what);
+  if (pitch < (int64_t)heads * D || (pitch * elem) % 16) return fail(NOVA_EINVAL, "%s: pitch %lld below a row or no multiple of 16 bytes", what, (long long)pitch);
+  return NOVA_OK;
+}
+inline bool act_ok(int t) { return t == NOVA_ACT_BF16 || t == NOVA_ACT_F32; }
+inline size_t act_elem(int t) { return t == NOVA_ACT_F32 ? 4 : 2; }
+
+int check_rope(const nova_rope* r, int D) {
+  if (r->rot < 0 || r->rot > D || r->rot % 16) return fail(NOVA_EINVAL, "rope: rot %d must be a multiple of 16 up to head_dim", r->rot);
+  if (!(r->theta > 0.f) || !(r->factor > 0.f) || !std::isfinite(r->theta) || !std::isfinite(r->factor) || !std::isfinite(r->mscale))
+    return fail(NOVA_EINVAL, "rope: theta and factor must be positive, mscale finite");
+  if (r->orig_ctx < 0 || (r->orig_ctx > 0 && !(r->beta > r->alpha))) return fail(NOVA_EINVAL, "rope: orig_ctx must be >= 0 and beta above alpha");
+  return NOVA_OK;
+}
+void set_rope(nova::AppendArgs& a, const nova_rope& r) {
+  const double two_pi = 6.283185307179586;
+  a.rot = r.rot;
+  a.interleaved = r.interleaved != 0;
+  a.mscale = r.mscale;
+  for (int c = 0; c < r.rot / 2; ++c) {
+    const double f = std::pow((double)r.theta, -2.0 * c / r.rot);
+    double g = f / r.factor;
+    if (r.orig_ctx > 0) {
+      const double keep = std::min(1.0, std::max(0.0, (r.orig_ctx * f / two_pi - r.alpha) / ((double)r.beta - r.alpha)));
+      g = keep * f + (1.0 - keep) * g;
+    }
+    a.turns[c] = g / two_pi;
+  }
+}
+}  // namespace
+
+extern "C" size_t nova_cache_bytes(int type, int num_blocks, int n_kv, int head_dim, size_t* exp_bytes) {
+  if (exp_bytes) *exp_bytes = 0;
+  if (cache_elem(type) == 0 || num_blocks <= 0 || n_kv <= 0 || (head_dim != 64 && head_dim != 128)) return 0;
+  const size_t tokens = (size_t)num_blocks * n_kv * 16;
+  if (exp_bytes && type == NOVA_CACHE_E4M3) *exp_bytes = tokens;
+  return tokens * head_dim * cache_elem(type);
+}
+
+extern "C" int nova_kv_append(const nova_cache* cache, const nova_rows* rows, const nova_rope* rope, const int32_t* pos,
+                              int in_type, const void* q, int64_t q_pitch, int n_q, const void* k, int64_t k_pitch,
+                              const void* v, int64_t v_pitch, void* q_out, int q_out_type, int64_t q_out_pitch,
+                              nova_stream_t stream) {
+  if (int rc = check_cache(cache)) return rc;
+  if (int rc = check_rows(rows, true)) return rc;
+  if (rope)
+    if (int rc = check_rope(rope, cache->head_dim)) return rc;
+  if (!act_ok(in_type) || (q && !act_ok(q_out_type))) return fail(NOVA_EINVAL, "types must be NOVA_ACT_BF16 or NOVA_ACT_F32");
+  if (!aligned4(pos)) return fail(NOVA_EINVAL, "pos is misaligned");
+  if (rows->rows == 0) return NOVA_OK;
+  const int D = cache->head_dim;
+  if (int rc = check_matrix("k", k, k_pitch, cache->n_kv, D, act_elem(in_type))) return rc;
+  if (int rc = check_matrix("v", v, v_pitch, cache->n_kv, D, act_elem(in_type))) return rc;
+  if (q) {
+    if (n_q <= 0) return fail(NOVA_EINVAL, "q without heads");
+    if (int rc = check_matrix("q", q, q_pitch, n_q, D, act_elem(in_type))) return rc;
+    if (int rc = check_matrix("q_out", q_out, q_out_pitch, n_q, D, act_elem(q_out_type))) return rc;
+    if (q_out == q && (q_out_type != in_type || q_out_pitch != q_pitch)) return fail(NOVA_EINVAL, "q_out over q needs the same type and pitch");
+  }
+  hipStream_t s = (hipStream_t)stream;
+  nova::AppendArgs a{};
+  a.c = pool_layer(*cache, 0);
+  a.r = batch_rows(*rows);
+  a.pos = pos;
+  a.q = q, a.k = k, a.v = v, a.q_row = q_pitch, a.k_row = k_pitch, a.v_row = v_pitch, a.n_q = q ? n_q : 0;
+  a.q_out = q_out, a.q_out_row = q_out_pitch;
+  a.in_f32 = in_type == NOVA_ACT_F32, a.q_out_f32 = q && q_out_type == NOVA_ACT_F32;
+  if (rope) set_rope(a, *rope);
+  CALL(NOVA_KIND_MISC, s, nova::kv_append(a, device_cus(), s));
+  return NOVA_OK;
+}
+
+extern "C" int nova_kv_gather(const nova_cache* cache, const nova_rows* rows, const int32_t* slots, int out_type, void* k_out,
+                              int64_t k_pitch, void* v_out, int64_t v_pitch, nova_stream_t stream) {
+  if (int rc = check_cache(cache)) return rc;
+  if (int rc = check_rows(rows, slots == nullptr)) return rc;
+  if (!act_ok(out_type)) return fail(NOVA_EINVAL, "out_type must be NOVA_ACT_BF16 or NOVA_ACT_F32");
+  if (!aligned4(slots)) return fail(NOVA_EINVAL, "slots is misaligned");
+  if (rows->rows == 0) return NOVA_OK;
+  if (int rc = check_matrix("k_out", k_out, k_pitch, cache->n_kv, cache->head_dim, act_elem(out_type))) return rc;
+  if (int rc = check_matrix("v_out", v_out, v_pitch, cache->n_kv, cache->head_dim, act_elem(out_type))) return rc;
+  hipStream_t s = (hipStream_t)stream;
+  const nova::GatherArgs a{pool_layer(*cache, 0), batch_rows(*rows), slots, k_out, v_out, k_pitch, v_pitch, out_type == NOVA_ACT_F32};
+  CALL(NOVA_KIND_MISC, s, nova::kv_gather(a, s));
+  return NOVA_OK;
+}
+
+namespace {
+int check_tree(const nova_cache* cache, const nova_rows* rows, int n_q) {
+  if (int rc = check_cache(cache)) return rc;
+  if (int rc = check_rows(rows, true)) return rc;
+  if (rows->max_rows > 64) return fail(NOVA_EUNSUPPORTED, "%d drafted tokens of one sequence (at most 64)", rows->max_rows);
+  if (n_q <= 0 || n_q % cache->n_kv) return fail(NOVA_EINVAL, "n_q %d must be a positive multiple of n_kv %d", n_q, cache->n_kv);
+  if ((int64_t)rows->max_rows * n_q > (1 << 20)) return fail(NOVA_EUNSUPPORTED, "n_q %d is too large", n_q);
+  return NOVA_OK;
+}
+}  // namespace
+
+extern "C" size_t nova_tree_attention_workspace_bytes(const nova_cache* cache, const nova_rows* rows, int n_q) {
+  if (check_tree(cache, rows, n_q)) return 0;
+  return align256(nova::tree_partial_floats(cache->type, cache->n_kv, n_q, cache->head_dim, rows->batch, rows->rows, rows->max_rows,
+                                            rows->max_ctx, device_cus()) * sizeof(float));
+}
+
+extern "C" int nova_tree_attention(const nova_cache* cache, const nova_rows* rows, const uint64_t* mask, const void* q, int64_t q_pitch,
+                                   int n_q, float scale, void* out, int64_t out_pitch, void* ws, size_t ws_bytes, nova_stream_t stream) {
+  if (int rc = check_tree(cache, rows, n_q)) return rc;
+  if (rows->rows == 0) return NOVA_OK;
+  const size_t elem = cache->type == NOVA_CACHE_F32 ? 4 : 2;
+  if (int rc = check_matrix("q", q, q_pitch, n_q, cache->head_dim, elem)) return rc;
+  if (int rc = check_matrix("out", out, out_pitch, n_q, cache->head_dim, elem)) return rc;
+  if ((uintptr_t)mask & 7) return fail(NOVA_EINVAL, "mask must be 8-byte aligned");
+  if (!std::isfinite(scale)) return fail(NOVA_EINVAL, "scale must be finite");
+  const size_t need = nova_tree_attention_workspace_bytes(cache, rows, n_q);
+  if (ws_bytes < need) return fail(NOVA_ENOSPACE, "workspace %zu < required %zu bytes", ws_bytes, need);
+  if (need > 0 && (!ws || !aligned(ws))) return fail(NOVA_EINVAL, "null or misaligned workspace");
+  hipStream_t s = (hipStream_t)stream;
+  const nova::TreeArgs a{pool_layer(*cache, 0), batch_rows(*rows), (const unsigned long long*)mask, q, q_pitch, n_q, scale, out, out_pitch, (float*)ws};
+  const int cus = std::min(stream_cus(s) > 0 ? stream_cus(s) : device_cus(), device_cus());
+  CALL(NOVA_KIND_DECODE_ATTN, s, nova::tree_attention(a, cus, s));
+  return NOVA_OK;
+}
+
+// ------------------------------------------------------------------ log probabilities
+namespace {
+size_t logprobs_bytes(int rows, int vocab, int n_top, size_t* sums) {
+  size_t f = 0, k = 0;
+  nova::logprobs_part_sizes(rows, vocab, n_top, &f, &k);
+  *sums = align256(f * sizeof(float));
+  return *sums + align256(k * 8);
+}
+}  // namespace
+
+extern "C" size_t nova_logprobs_workspace_bytes(int rows, int vocab, int n_top) {
+  size_t sums;
+  if (rows <= 0 || vocab <= 0 || n_top < 0 || n_top > vocab || !nova::logprobs_fits(vocab, n_top)) return 0;
+  return logprobs_bytes(rows, vocab, n_top, &sums);
+}
+
+extern "C" int nova_logprobs(const void* logits, int type, int64_t pitch, int rows, int vocab, const int32_t* given, int n_given,
+                             float* given_lp, float* entropy, int n_top, float* top_lp, int32_t* top_ids, void* ws,
+                             size_t ws_bytes, nova_stream_t stream) {
+  if (!act_ok(type)) return fail(NOVA_EINVAL, "type must be NOVA_ACT_BF16 or NOVA_ACT_F32");
+  if (rows < 0 || vocab <= 0 || n_given < 0 || n_top < 0 || n_top > vocab) return fail(NOVA_EINVAL, "logprobs: sizes out of range");
+  if (!nova::logprobs_fits(vocab, n_top)) return fail(NOVA_EUNSUPPORTED, "vocab %d with %d alternatives (at most 2^21 and 32)", vocab, n_top);
+  if (rows == 0) return NOVA_OK;
+  if (!logits || (uintptr_t)logits % act_elem(type) || pitch < vocab) return fail(NOVA_EINVAL, "logits null or misaligned, or pitch below vocab");
+  if (n_given > 0 && (!given || !given_lp || !aligned4(given) || !aligned4(given_lp))) return fail(NOVA_EINVAL, "given and given_lp must be non-null and aligned");
+  if (n_top > 0 && (!top_lp || !top_ids || !aligned4(top_lp) || !aligned4(top_ids))) return fail(NOVA_EINVAL, "top_lp and top_ids must be non-null and aligned");
+  if (!aligned4(entropy)) return fail(NOVA_EINVAL, "entropy is misaligned");
+  if ((int64_t)rows * ((vocab + 2047) / 2048) > 0x7fffffffLL) return fail(NOVA_EUNSUPPORTED, "%d rows of %d logits are too many for one call", rows, vocab);
+  size_t sums;
+  const size_t need = logprobs_bytes(rows, vocab, n_top, &sums);
+  if (ws_bytes < need) return fail(NOVA_ENOSPACE, "workspace %zu < required %zu bytes", ws_bytes, need);
+  if (!ws || !aligned(ws)) return fail(NOVA_EINVAL, "null or misaligned workspace");
+  hipStream_t s = (hipStream_t)stream;
+  const nova::LogprobArgs a{logits, type == NOVA_ACT_F32, pitch, rows, vocab, given, n_given, given_lp, entropy, n_top, top_lp, top_ids,
+                            (float*)ws, (unsigned long long*)((char*)ws + sums)};
+  CALL(NOVA_KIND_MISC, s, nova::logprobs(a, s));
+  return NOVA_OK;
+}
+
 extern "C" size_t nova_llm_prefill_workspace_bytes(const nova_llm* m, int seq) {
   if (!m || seq <= 0) return 0;
   return m->d.cfg.act == NOVA_ACT_F32 ? prefill_ws<float>(m, seq, nullptr) : prefill_ws<bf16_t>(m, seq, nullptr);
@@ -699,9 +909,10 @@ extern "C" size_t nova_llm_decode_workspace_bytes(const nova_llm* m, int batch, 
 }
 
 namespace {
+// `pool`: the cache is a nova_cache pool (kv is null then).
 template <typename T>
 int llm_prefill_t(const nova_llm* m, const T* vis, int n_vis, const int* ids, int n_text, const int* table,
-                  const nova_kv* kv, int* next_id, float* logits_out, void* ws, hipStream_t s) {
+                  const nova_kv* kv, const nova_cache* pool, int* next_id, float* logits_out, void* ws, hipStream_t s) {
   const nova_llm_config& c = m->d.cfg;
   const int S = n_vis + n_text, H = c.hidden, D = c.head_dim, qd = c.n_q * D;
   const int skp = round_up(S, 64);
@@ -717,7 +928,7 @@ int llm_prefill_t(const nova_llm* m, const T* vis, int n_vis, const int* ids, in
   float* split_ws = w.take<float>(split_floats);
   const int n_cnt = c.n_q * ((S + 127) / 128);
   unsigned* att_cnt = w.take<unsigned>((size_t)n_cnt);
-  const size_t kv_layer = (size_t)kv->num_blocks * c.n_kv * c.block * D;
+  const size_t kv_layer = kv ? (size_t)kv->num_blocks * c.n_kv * c.block * D : 0;
   const int cus = stream_cus(s);
   // every projection may cut K into slices when its tiles cannot fill the stream's compute units
   auto with_split = [&](GemmArgs p) {
@@ -747,8 +958,8 @@ int llm_prefill_t(const nova_llm* m, const T* vis, int n_vis, const int* ids, in
   for (int l = 0; l < c.layers; ++l) {
     const char* lw = (const char*)m->d.layers + (size_t)l * m->lay.bytes;
     auto W = [&](int i) { return (const bf16_t*)(lw + m->lay.off[i]); };
-    T* kp = (T*)kv->k + l * kv_layer;
-    T* vp = (T*)kv->v + l * kv_layer;
+    T* kp = kv ? (T*)kv->k + l * kv_layer : nullptr;
+    T* vp = kv ? (T*)kv->v + l * kv_layer : nullptr;
     // The last layer writes every position's K and V, but past its attention only the last row is read
     // (the head takes row S - 1): its queries are the last block's, and its O and MLP projections and
     // norm run on that row: 3% of a 28-layer prefill (1500 tokens 19.33 -> 18.68 ms, of which the GEMM tiles
@@ -760,8 +971,16 @@ int llm_prefill_t(const nova_llm* m, const T* vis, int n_vis, const int* ids, in
       const GemmArgs p = with_split(GemmArgs{a, H, W(1), H, S, m->qkvw, H, nullptr, qkv, m->qkvw, nullptr, 0});
       CALL(NOVA_KIND_GEMM, s, (nova::gemm<T, T>(p, nova::EPI_STORE, s)));
     }
-    CALL(NOVA_KIND_MISC, s, nova::qkv_prefill<T>(qkv, S, 1, c.n_q, c.n_kv, D, c.rope_theta, 0, vt, skp, kp, vp, table,
+    CALL(NOVA_KIND_MISC, s, nova::qkv_prefill<T>(qkv, S, 1, c.n_q, c.n_kv, D, c.rope_theta, 0, vt, skp, kp, vp, kv ? table : nullptr,
                                                   c.block, s, att_cnt, n_cnt));
+    if (pool) {
+      nova::AppendArgs p{};
+      p.c = pool_layer(*pool, l);
+      p.r = nova::BatchRows{nullptr, nullptr, table, (S + c.block - 1) / c.block, 1, S, S, S};
+      p.k = qkv + qd, p.v = qkv + qd + c.n_kv * D, p.k_row = p.v_row = m->qkvw;
+      p.in_f32 = sizeof(T) == 4;
+      CALL(NOVA_KIND_MISC, s, nova::kv_append(p, cus, s));
+    }
     {
       nova::AttnArgs p{qkv, m->qkvw, 0, qkv + qd, m->qkvw, 0, vt, skp, att, qd, 0, S, S, c.n_q, c.n_kv, 1, 1};
       // the K slices' buffer is free between the QKV and O projections: the attention's key ranges keep
@@ -798,13 +1017,35 @@ int llm_prefill_t(const nova_llm* m, const T* vis, int n_vis, const int* ids, in
   return NOVA_OK;
 }
 
+// A decode step over drafted tokens: B rows of several sequences on a cache of any type.
+struct Verify {
+  const nova_rows* rows;
+  const nova_cache* pool;
+  const uint64_t* mask;
+};
+// Its buffers beside a decode step's of as many rows: the rotated q and the attention's partials.
+template <typename T>
+struct VerifyBufs { T* q; float* part; size_t used; };
+template <typename T>
+VerifyBufs<T> verify_bufs(const nova_llm* m, const nova_cache* pool, const nova_rows* r, void* base) {
+  const nova_llm_config& c = m->d.cfg;
+  Carve w(base);
+  w.used = decode_bufs<T>(m, r->rows, 1, nullptr).used;
+  VerifyBufs<T> v;
+  v.q = w.take<T>((size_t)r->rows * c.n_q * c.head_dim);
+  v.part = w.take<float>(nova::tree_partial_floats(pool->type, c.n_kv, c.n_q, c.head_dim, r->batch, r->rows, r->max_rows, r->max_ctx, device_cus()));
+  v.used = w.used;
+  return v;
+}
+
 template <typename T>
 int llm_decode_t(const nova_llm* m, const int* ids, const int* pos, const int* tables, int max_blocks, int B, int max_ctx,
-                 const nova_kv* kv, int* next_ids, float* logits_out, void* ws, hipStream_t s) {
+                 const nova_kv* kv, const Verify* vf, int* next_ids, float* logits_out, void* ws, hipStream_t s) {
   const nova_llm_config& c = m->d.cfg;
   const int H = c.hidden, D = c.head_dim, qd = c.n_q * D;
-  const DecodeBufs<T> d = decode_bufs<T>(m, B, max_ctx, ws);
-  const size_t kv_layer = (size_t)kv->num_blocks * c.n_kv * c.block * D;
+  const DecodeBufs<T> d = decode_bufs<T>(m, B, vf ? 1 : max_ctx, ws);
+  const VerifyBufs<T> vb = vf ? verify_bufs<T>(m, vf->pool, vf->rows, ws) : VerifyBufs<T>{};
+  const size_t kv_layer = kv ? (size_t)kv->num_blocks * c.n_kv * c.block * D : 0;
   const bool f32 = sizeof(T) == 4;
   const int tiles = H / 64;
   const int cus = stream_cus(s);
@@ -814,7 +1055,24 @@ int llm_decode_t(const nova_llm* m, const int* ids, const int* pos, const int* t
     return (const bf16_t*)((const char*)m->d.layers + (size_t)l * m->lay.bytes + m->lay.off[i]);
   };
   const bf16_t* final_gain = (const bf16_t*)(hw + m->head.off[0]);
+  // the QKV projection's output: split-K slabs for the fused attention, finished rows for a verify step
+  float* qkv_out = sp_qkv > 1 && !vf ? nullptr : d.qkv;
   auto attention_block = [&](int l) -> int {
+    if (vf) {
+      nova::AppendArgs a{};
+      a.c = pool_layer(*vf->pool, l);
+      a.r = batch_rows(*vf->rows);
+      a.pos = pos;
+      a.q = d.qkv, a.k = d.qkv + qd, a.v = d.qkv + qd + c.n_kv * D;
+      a.q_row = a.k_row = a.v_row = m->qkvw, a.n_q = c.n_q;
+      a.q_out = vb.q, a.q_out_row = qd;
+      a.in_f32 = true, a.q_out_f32 = f32;
+      set_rope(a, nova_rope{D, 0, c.rope_theta, 1.f, 0, 1.f, 32.f, 1.f});
+      CALL(NOVA_KIND_MISC, s, nova::kv_append(a, cus, s));
+      nova::TreeArgs t{a.c, a.r, (const unsigned long long*)vf->mask, vb.q, qd, c.n_q, 1.0f / sqrtf((float)D), d.att, qd, vb.part};
+      CALL(NOVA_KIND_DECODE_ATTN, s, nova::tree_attention(t, cus, s));
+      return (int)NOVA_OK;
+    }
     T* kp = (T*)kv->k + l * kv_layer;
     T* vp = (T*)kv->v + l * kv_layer;
     nova::DecAttnArgs p{sp_qkv > 1 ? d.part : d.qkv, sp_qkv, d.rope, kp, vp, tables, max_blocks, pos, d.att, d.apart,
@@ -837,7 +1095,7 @@ int llm_decode_t(const nova_llm* m, const int* ids, const int* pos, const int* t
     for (int l = 0; l < c.layers; ++l) {
       auto W = [&](int i) { return layer_w(l, i); };
       {
-        GemvArgs p{d.a, H, W(1), H, B, m->qkvw, H, sp_qkv > 1 ? nullptr : d.qkv, m->qkvw, d.part, nullptr};
+        GemvArgs p{d.a, H, W(1), H, B, m->qkvw, H, qkv_out, m->qkvw, d.part, nullptr};
         p.cus = cus;
         p.ss_in = ss(2 * l), p.ss_parts = tiles, p.eps = c.eps;
         CALL(NOVA_KIND_GEMV, s, (nova::gemv<T, float>(p, nova::EPI_STORE, s)));
@@ -883,7 +1141,7 @@ int llm_decode_t(const nova_llm* m, const int* ids, const int* pos, const int* t
     for (int l = 0; l < c.layers; ++l) {
       auto W = [&](int i) { return layer_w(l, i); };
       {
-        GemvArgs p{d.a, H, W(1), H, B, m->qkvw, H, sp_qkv > 1 ? nullptr : d.qkv, m->qkvw, d.part, nullptr};
+        GemvArgs p{d.a, H, W(1), H, B, m->qkvw, H, qkv_out, m->qkvw, d.part, nullptr};
         p.cus = cus;
         p.ss_in = ss(2 * l), p.ss_parts = tiles, p.eps = c.eps;
         CALL(NOVA_KIND_GEMV, s, (nova::gemv<T, float>(p, nova::EPI_STORE, s)));
@@ -937,8 +1195,8 @@ extern "C" int nova_llm_prefill(const nova_llm* m, const void* vis, int n_vis, c
   if (ws_bytes < need) return fail(NOVA_ENOSPACE, "workspace %zu < required %zu bytes", ws_bytes, need);
   hipStream_t s = (hipStream_t)stream;
   return m->d.cfg.act == NOVA_ACT_F32
-             ? llm_prefill_t<float>(m, (const float*)vis, n_vis, ids, n_text, table, kv, next_id, logits, ws, s)
-             : llm_prefill_t<bf16_t>(m, (const bf16_t*)vis, n_vis, ids, n_text, table, kv, next_id, logits, ws, s);
+             ? llm_prefill_t<float>(m, (const float*)vis, n_vis, ids, n_text, table, kv, nullptr, next_id, logits, ws, s)
+             : llm_prefill_t<bf16_t>(m, (const bf16_t*)vis, n_vis, ids, n_text, table, kv, nullptr, next_id, logits, ws, s);
 }
 
 namespace {
@@ -958,8 +1216,8 @@ int decode_dispatch(const nova_llm* m, const int32_t* ids, const int32_t* pos, c
                     int batch, int max_ctx, const nova_kv* kv, int32_t* next_ids, float* logits, void* ws,
                     hipStream_t s) {
   return m->d.cfg.act == NOVA_ACT_F32
-             ? llm_decode_t<float>(m, ids, pos, tables, max_blocks, batch, max_ctx, kv, next_ids, logits, ws, s)
-             : llm_decode_t<bf16_t>(m, ids, pos, tables, max_blocks, batch, max_ctx, kv, next_ids, logits, ws, s);
+             ? llm_decode_t<float>(m, ids, pos, tables, max_blocks, batch, max_ctx, kv, nullptr, next_ids, logits, ws, s)
+             : llm_decode_t<bf16_t>(m, ids, pos, tables, max_blocks, batch, max_ctx, kv, nullptr, next_ids, logits, ws, s);
 }
 }  // namespace
 
@@ -971,6 +1229,58 @@ extern "C" int nova_llm_decode(const nova_llm* m, const int32_t* ids, const int3
   const size_t need = nova_llm_decode_workspace_bytes(m, batch, max_ctx);
   if (ws_bytes < need) return fail(NOVA_ENOSPACE, "workspace %zu < required %zu bytes", ws_bytes, need);
   return decode_dispatch(m, ids, pos, tables, max_blocks, batch, max_ctx, kv, next_ids, logits, ws, (hipStream_t)stream);
+}
+
+// ------------------------------------------------------------------ LLM on a cache of any type
+namespace {
+int check_model_cache(const nova_llm* m, const nova_cache* c) {
+  if (!m) return fail(NOVA_EINVAL, "null model");
+  if (int rc = check_cache(c)) return rc;
+  if (c->n_kv != m->d.cfg.n_kv || c->head_dim != m->d.cfg.head_dim)
+    return fail(NOVA_EINVAL, "cache of %d heads of %d, the model has %d of %d", c->n_kv, c->head_dim, m->d.cfg.n_kv, m->d.cfg.head_dim);
+  if ((c->type == NOVA_CACHE_F32) != (m->d.cfg.act == NOVA_ACT_F32))
+    return fail(NOVA_EUNSUPPORTED, "an fp32 model takes an F32 cache, a bf16 model BF16 or E4M3");
+  return NOVA_OK;
+}
+}  // namespace
+
+extern "C" int nova_llm_prefill_cache(const nova_llm* m, const void* vis, int n_vis, const int32_t* ids, int n_text,
+                                      const int32_t* table, const nova_cache* cache, int32_t* next_id, float* logits, void* ws,
+                                      size_t ws_bytes, nova_stream_t stream) {
+  if (int rc = check_model_cache(m, cache)) return rc;
+  if (n_vis < 0 || n_text < 0 || (int64_t)n_vis + n_text <= 0) return fail(NOVA_EINVAL, "empty prompt");
+  if ((n_vis > 0 && (!vis || !aligned(vis))) || (n_text > 0 && !ids) || !table || !next_id || !ws || !aligned(ws))
+    return fail(NOVA_EINVAL, "null or misaligned pointer");
+  const int S = n_vis + n_text;
+  if ((S + 15) / 16 > cache->num_blocks) return fail(NOVA_ENOKV, "prompt needs more blocks than the pool holds");
+  const size_t need = nova_llm_prefill_workspace_bytes(m, S);
+  if (ws_bytes < need) return fail(NOVA_ENOSPACE, "workspace %zu < required %zu bytes", ws_bytes, need);
+  hipStream_t s = (hipStream_t)stream;
+  return m->d.cfg.act == NOVA_ACT_F32
+             ? llm_prefill_t<float>(m, (const float*)vis, n_vis, ids, n_text, table, nullptr, cache, next_id, logits, ws, s)
+             : llm_prefill_t<bf16_t>(m, (const bf16_t*)vis, n_vis, ids, n_text, table, nullptr, cache, next_id, logits, ws, s);
+}
+
+extern "C" size_t nova_llm_verify_workspace_bytes(const nova_llm* m, const nova_cache* cache, const nova_rows* rows) {
+  if (check_model_cache(m, cache) || check_tree(cache, rows, m->d.cfg.n_q) || rows->rows < 1 || rows->rows > 32) return 0;
+  return m->d.cfg.act == NOVA_ACT_F32 ? verify_bufs<float>(m, cache, rows, nullptr).used : verify_bufs<bf16_t>(m, cache, rows, nullptr).used;
+}
+
+extern "C" int nova_llm_verify(const nova_llm* m, const int32_t* ids, const int32_t* pos, const uint64_t* mask, const nova_rows* rows,
+                               const nova_cache* cache, int32_t* next_ids, float* logits, void* ws, size_t ws_bytes, nova_stream_t stream) {
+  if (int rc = check_model_cache(m, cache)) return rc;
+  if (int rc = check_tree(cache, rows, m->d.cfg.n_q)) return rc;
+  if (rows->rows < 1 || rows->rows > 32) return fail(NOVA_EINVAL, "%d rows outside 1..32", rows->rows);
+  if (!ids || !pos || !next_ids) return fail(NOVA_EINVAL, "null pointer");
+  if ((uintptr_t)mask & 7) return fail(NOVA_EINVAL, "mask must be 8-byte aligned");
+  if (!ws || !aligned(ws)) return fail(NOVA_EINVAL, "null or misaligned workspace");
+  const size_t need = nova_llm_verify_workspace_bytes(m, cache, rows);
+  if (ws_bytes < need) return fail(NOVA_ENOSPACE, "workspace %zu < required %zu bytes", ws_bytes, need);
+  const Verify vf{rows, cache, mask};
+  hipStream_t s = (hipStream_t)stream;
+  return m->d.cfg.act == NOVA_ACT_F32
+             ? llm_decode_t<float>(m, ids, pos, nullptr, 0, rows->rows, 1, nullptr, &vf, next_ids, logits, ws, s)
+             : llm_decode_t<bf16_t>(m, ids, pos, nullptr, 0, rows->rows, 1, nullptr, &vf, next_ids, logits, ws, s);
 }
 
 // ------------------------------------------------------------------ allocation-free decode

@@ -18,6 +18,7 @@ LIB_PATH = os.path.join(_HERE, "libnova.so")
 OK, EINVAL, ENOKV, EHIP, EUNSUPPORTED, ENOSPACE = 0, -1, -2, -3, -4, -5
 STAGE_ENCODE, STAGE_PREFILL, STAGE_DECODE = 0, 1, 2
 ACT_BF16, ACT_F32 = 0, 1
+CACHE_BF16, CACHE_F32, CACHE_E4M3 = 0, 1, 2
 KIND_GEMM, KIND_ATTN, KIND_GEMV, KIND_DECODE_ATTN, KIND_MISC = 0, 1, 2, 3, 4
 KIND_NAMES = {KIND_GEMM: "gemm", KIND_ATTN: "attention", KIND_GEMV: "thin_gemm", KIND_DECODE_ATTN: "decode_attention",
               KIND_MISC: "misc"}
@@ -54,6 +55,21 @@ class KvC(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("num_blocks", C.c_int)]
 
 
+class CacheC(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_exp", C.c_void_p), ("v_exp", C.c_void_p),
+                ("num_blocks", C.c_int), ("n_kv", C.c_int), ("head_dim", C.c_int), ("type", C.c_int)]
+
+
+class RowsC(C.Structure):
+    _fields_ = [("row_start", C.c_void_p), ("ctx", C.c_void_p), ("tables", C.c_void_p), ("max_blocks", C.c_int),
+                ("batch", C.c_int), ("rows", C.c_int), ("max_rows", C.c_int), ("max_ctx", C.c_int)]
+
+
+class RopeC(C.Structure):
+    _fields_ = [("rot", C.c_int), ("interleaved", C.c_int), ("theta", C.c_float), ("factor", C.c_float),
+                ("orig_ctx", C.c_int), ("alpha", C.c_float), ("beta", C.c_float), ("mscale", C.c_float)]
+
+
 # symbol -> (restype, argtypes); mirrors include/nova.h
 _SIG = {
     "nova_last_error": (C.c_char_p, []),
@@ -82,6 +98,22 @@ _SIG = {
                                   C.POINTER(KvC), C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "nova_llm_decode_noalloc": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int,
                                           C.POINTER(KvC), C.c_void_p, C.c_void_p, C.c_void_p]),
+    "nova_cache_bytes": (C.c_size_t, [C.c_int, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_size_t)]),
+    "nova_kv_append": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int64, C.c_int,
+                                 C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int, C.c_int64, C.c_void_p]),
+    "nova_kv_gather": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                 C.c_void_p]),
+    "nova_tree_attention_workspace_bytes": (C.c_size_t, [C.c_void_p, C.c_void_p, C.c_int]),
+    "nova_tree_attention": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int, C.c_float,
+                                      C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "nova_logprobs_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int, C.c_int]),
+    "nova_logprobs": (C.c_int, [C.c_void_p, C.c_int, C.c_int64, C.c_int, C.c_int, C.c_void_p, C.c_int, C.c_void_p,
+                                C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "nova_llm_prefill_cache": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p,
+                                         C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "nova_llm_verify_workspace_bytes": (C.c_size_t, [C.c_void_p, C.c_void_p, C.c_void_p]),
+    "nova_llm_verify": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                  C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "nova_linear": (C.c_int, [C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p]),
     "nova_make_cu_mask": (C.c_int, [C.c_int, C.c_int, C.POINTER(C.c_uint32)]),
     "nova_set_stage_partition": (C.c_int, [C.c_int, C.POINTER(C.c_uint32), C.c_int, C.POINTER(C.c_void_p)]),
@@ -379,6 +411,11 @@ class Llm:
         ws = self._workspace("prefill", lib.nova_llm_prefill_workspace_bytes(self.h, n_vis + n_text), stream)
         if next_id is None:
             next_id = torch.empty(1, dtype=torch.int32, device=self.device)
+        if isinstance(kv, Cache):
+            kv._check_layers(self.cfg.layers)
+            _check(lib.nova_llm_prefill_cache(self.h, _ptr(vis), n_vis, _ptr(ids), n_text, _ptr(table), kv.layer(0),
+                                              _ptr(next_id), _ptr(logits), _ptr(ws), ws.numel(), _stream(stream)))
+            return next_id
         _check(lib.nova_llm_prefill(self.h, _ptr(vis), n_vis, _ptr(ids), n_text, _ptr(table), C.byref(kv.c),
                                     _ptr(next_id), _ptr(logits), _ptr(ws), ws.numel(), _stream(stream)))
         return next_id
@@ -394,6 +431,24 @@ class Llm:
                                    _stream(stream)))
         return next_ids
 
+    def verify(self, ids, pos, rows, cache, mask=None, next_ids=None, logits=None, stream=None):
+        """A decode step over drafted tokens on a ``Cache``: ids, pos int32 [rows.rows] (at most 32 rows), ``mask``
+        int64 [rows] as for ``tree_attention``; the greedy id after every row.  One row per sequence decodes."""
+        cache._check_layers(self.cfg.layers)
+        for what, t, dt in (("ids", ids, torch.int32), ("pos", pos, torch.int32), ("mask", mask, torch.int64)):
+            _check_vector(what, t, dt, rows.rows)
+        if logits is not None and (logits.dtype != torch.float32 or not logits.is_contiguous() or
+                                   logits.shape != (rows.rows, self.cfg.vocab)):
+            raise ValueError(f"logits must be contiguous float32 {(rows.rows, self.cfg.vocab)}")
+        n = lib.nova_llm_verify_workspace_bytes(self.h, cache.layer(0), rows.ref)
+        ws = self._workspace("verify", max(n, 256), stream)
+        if next_ids is None:
+            next_ids = torch.empty(rows.rows, dtype=torch.int32, device=self.device)
+        _check_vector("next_ids", next_ids, torch.int32, rows.rows)
+        _check(lib.nova_llm_verify(self.h, _ptr(ids), _ptr(pos), _ptr(mask), rows.ref, cache.layer(0), _ptr(next_ids),
+                                   _ptr(logits), _ptr(ws), ws.numel(), _stream(stream)))
+        return next_ids
+
     def decode_noalloc(self, ids, pos, tables, kv, max_ctx, next_ids, logits=None, stream=None):
         """The same step with the library's static scratch as workspace (no allocation in the
         library; outputs are the caller's)."""
@@ -406,6 +461,242 @@ class Llm:
         if h is not None and h.value and lib is not None:
             lib.nova_llm_destroy(h)
             self.h = None
+
+
+# ----------------------------------------------------------------------------- operators over the paged cache
+_CACHE_DTYPE = {CACHE_BF16: torch.bfloat16, CACHE_F32: torch.float32, CACHE_E4M3: torch.uint8}
+_ACT = {torch.bfloat16: ACT_BF16, torch.float32: ACT_F32}
+
+
+def _check_vector(what, t, dtype, n):
+    if t is not None and (t.dtype != dtype or t.dim() != 1 or t.shape[0] < n or not t.is_contiguous()):
+        raise ValueError(f"{what} must be a contiguous {dtype} vector of {n} entries, got {t.dtype} {tuple(t.shape)}")
+
+
+def _check_rows_of(what, t, rows, heads, d):
+    """Rows [rows, heads, d], heads and dimensions contiguous; returns (type, pitch)."""
+    act = _ACT.get(t.dtype)
+    if act is None:
+        raise ValueError(f"{what} must be bfloat16 or float32, got {t.dtype}")
+    if t.dim() != 3 or t.shape != (rows, heads, d) or t.stride(2) != 1 or (heads > 1 and t.stride(1) != d):
+        raise ValueError(f"{what} must be rows {(rows, heads, d)} with contiguous heads, got {tuple(t.shape)} strides {t.stride()}")
+    return act, t.stride(0) if rows > 1 else heads * d
+
+
+def _check_device(ref, *tensors):
+    """Every tensor lives on ``ref``'s device, which is the current one (the library launches there)."""
+    dev = ref.device
+    for t in tensors:
+        if t is not None and t.device != dev:
+            raise ValueError(f"tensors on {t.device} and {dev}")
+    if not ref.is_cuda or dev.index != torch.cuda.current_device():
+        raise ValueError(f"tensors on {dev}, which is not the current device")
+
+
+class _On:
+    """Allocate on the stream that a call runs on, so that memory freed after the call is reused behind it."""
+
+    def __init__(self, stream):
+        self.stream = stream
+
+    def empty(self, shape, dtype, device):
+        if self.stream is None:
+            return torch.empty(shape, dtype=dtype, device=device)
+        with torch.cuda.stream(self.stream):
+            return torch.empty(shape, dtype=dtype, device=device)
+
+
+class Cache:
+    """Paged K/V pool of ``layers`` layers: CACHE_BF16 or CACHE_F32 (a ``KvPool``'s layout) or CACHE_E4M3 (8 bits per
+    value and a power-of-two scale per token and head).  ``k`` [layers, num_blocks, n_kv, 16, head_dim], ``v``
+    [layers, num_blocks, n_kv, head_dim, 16], ``k_exp``, ``v_exp`` [layers, num_blocks, n_kv, 16] (E4M3)."""
+
+    def __init__(self, num_blocks, n_kv, head_dim, type=CACHE_E4M3, layers=1, device="cuda"):
+        if type not in _CACHE_DTYPE:
+            raise ValueError(f"unknown cache type {type}")
+        if lib.nova_cache_bytes(type, num_blocks, n_kv, head_dim, None) == 0 or layers < 1:
+            raise ValueError(f"unsupported cache: {layers} layers of {num_blocks} blocks, {n_kv} heads of {head_dim}")
+        k = torch.zeros(layers, num_blocks, n_kv, 16, head_dim, dtype=_CACHE_DTYPE[type], device=device)
+        v = torch.zeros(layers, num_blocks, n_kv, head_dim, 16, dtype=_CACHE_DTYPE[type], device=device)
+        e = (None, None)
+        if type == CACHE_E4M3:
+            e = tuple(torch.full((layers, num_blocks, n_kv, 16), 127, dtype=torch.uint8, device=device) for _ in "kv")
+        self._own(k, v, *e)
+
+    @classmethod
+    def of(cls, k, v, k_exp=None, v_exp=None):
+        """A cache on tensors in hand, with or without the layer dimension (a ``KvPool``'s k5 and v5, say)."""
+        self = cls.__new__(cls)
+        self._own(*(t if t is None or t.dim() == n else t.unsqueeze(0) for t, n in ((k, 5), (v, 5), (k_exp, 4), (v_exp, 4))))
+        return self
+
+    def _own(self, k, v, k_exp, v_exp):
+        types = {t: n for n, t in _CACHE_DTYPE.items()}
+        if k.dtype not in types or v.dtype != k.dtype or k.dim() != 5 or k.shape[3] != 16:
+            raise ValueError(f"k must be bfloat16, float32 or uint8 [layers, blocks, n_kv, 16, head_dim], got {k.dtype} {tuple(k.shape)}")
+        layers, nb, n_kv, _, d = k.shape
+        if v.shape != (layers, nb, n_kv, d, 16) or not k.is_contiguous() or not v.is_contiguous():
+            raise ValueError(f"k and v must be contiguous, v {(layers, nb, n_kv, d, 16)}: got {tuple(v.shape)}")
+        self.type = types[k.dtype]
+        if self.type == CACHE_E4M3:
+            for t in (k_exp, v_exp):
+                if t is None or t.dtype != torch.uint8 or t.shape != (layers, nb, n_kv, 16) or not t.is_contiguous():
+                    raise ValueError(f"an 8-bit cache needs contiguous uint8 k_exp and v_exp {(layers, nb, n_kv, 16)}")
+        else:
+            k_exp = v_exp = None
+        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        self.num_blocks, self.n_kv, self.head_dim, self.layers = nb, n_kv, d, layers
+        self.dtype = torch.float32 if self.type == CACHE_F32 else torch.bfloat16      # of q and the attention's output
+        e = [(None, None) if k_exp is None else (_ptr(k_exp[i]), _ptr(v_exp[i])) for i in range(layers)]
+        self._c = [CacheC(_ptr(k[i]), _ptr(v[i]), *e[i], nb, n_kv, d, self.type) for i in range(layers)]
+        self._ref = [C.addressof(c) for c in self._c]
+
+    def layer(self, i):
+        return self._ref[i]
+
+    def _check_layers(self, n):
+        if self.layers != n:
+            raise ValueError(f"a cache of {self.layers} layers for a model of {n}")
+
+
+class Rows:
+    """Which rows of a call belong to which sequence: ``row_start`` int32 [batch + 1] (None: max_rows rows each), ``ctx``
+    int32 [batch] tokens cached before them (None: 0), ``tables`` int32 [batch, max_blocks].  Row j of sequence b is
+    its token ctx[b] + j.  ``rows``, ``max_rows`` (of one sequence) and ``max_ctx`` (cached and new tokens of one
+    sequence) bound what the device arrays may hold when a call runs; the arrays may change between calls."""
+
+    def __init__(self, row_start, ctx, tables, rows=None, max_rows=1, max_ctx=None):
+        if tables.dtype != torch.int32 or tables.dim() != 2 or not tables.is_contiguous():
+            raise ValueError(f"tables must be contiguous int32 [batch, max_blocks], got {tables.dtype} {tuple(tables.shape)}")
+        batch, max_blocks = tables.shape
+        if rows is None:
+            if row_start is not None:
+                raise ValueError("rows is needed beside row_start")
+            rows = batch * max_rows
+        if max_ctx is None:
+            max_ctx = 16 * max_blocks
+        for what, t, n in (("row_start", row_start, batch + 1), ("ctx", ctx, batch)):
+            _check_vector(what, t, torch.int32, n)
+            if t is not None and t.device != tables.device:
+                raise ValueError(f"{what} on {t.device}, tables on {tables.device}")
+        self.row_start, self.ctx, self.tables = row_start, ctx, tables
+        self.batch, self.rows, self.max_rows, self.max_ctx = batch, rows, max_rows, max_ctx
+        self._c = RowsC(_ptr(row_start), _ptr(ctx), _ptr(tables), max_blocks, batch, rows, max_rows, max_ctx)
+        self.ref = C.addressof(self._c)
+        self._ws = {}
+
+    def _tree_bytes(self, cache, n_q):
+        """Workspace of an attention over these rows (its sizes are fixed, so it is asked for once)."""
+        key = (cache.type, cache.n_kv, cache.head_dim, n_q)
+        n = self._ws.get(key)
+        if n is None:
+            n = self._ws[key] = lib.nova_tree_attention_workspace_bytes(cache.layer(0), self.ref, n_q)
+        return n
+
+
+class Rope:
+    """Rotary embedding of the first ``rot`` dimensions, half-split or ``interleaved`` pairs; ``factor`` and
+    ``orig_ctx`` (with ``alpha``, ``beta``) scale it for longer contexts, ``mscale`` multiplies sines and cosines."""
+
+    def __init__(self, rot, theta=10000.0, interleaved=False, factor=1.0, orig_ctx=0, alpha=1.0, beta=32.0, mscale=1.0):
+        self._c = RopeC(rot, int(interleaved), theta, factor, orig_ctx, alpha, beta, mscale)
+        self.ref = C.addressof(self._c)
+
+
+def kv_append(cache, rows, k, v, q=None, pos=None, rope=None, q_out=None, layer=0, stream=None):
+    """Rotate q and k (``rope`` None: not) at ``pos`` (int32 [rows]; None: the rows' token numbers) and write k and v
+    behind their sequences' contexts in ``cache``, in its type.  k, v [rows, n_kv, head_dim], q [rows, n_q, head_dim],
+    bf16 or fp32, may be views of one packed projection.  Returns the rotated q (``q_out``, which may be q itself)."""
+    n, d = rows.rows, cache.head_dim
+    _check_device(cache.k, rows.tables, k, v, q, pos, q_out)
+    act, k_pitch = _check_rows_of("k", k, n, cache.n_kv, d)
+    act_v, v_pitch = _check_rows_of("v", v, n, cache.n_kv, d)
+    _check_vector("pos", pos, torch.int32, n)
+    n_q = q_pitch = out_pitch = act_out = 0
+    act_q = act
+    if q is not None:
+        n_q = q.shape[1] if q.dim() == 3 else 0
+        act_q, q_pitch = _check_rows_of("q", q, n, n_q, d)
+        if q_out is None:
+            q_out = _On(stream).empty((n, n_q, d), q.dtype, q.device)
+        act_out, out_pitch = _check_rows_of("q_out", q_out, n, n_q, d)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    if act_v != act or act_q != act:
+        raise ValueError("q, k and v must have one type")
+    _check(lib.nova_kv_append(cache.layer(layer), rows.ref, rope.ref if rope is not None else None, _ptr(pos), act, _ptr(q), q_pitch,
+                              n_q, k.data_ptr(), k_pitch, v.data_ptr(), v_pitch, _ptr(q_out), act_out, out_pitch, _stream(stream)))
+    return q_out
+
+
+def kv_gather(cache, rows, slots=None, k_out=None, v_out=None, dtype=torch.bfloat16, layer=0, stream=None):
+    """Cached rows as dense K and V [rows, n_kv, head_dim] in ``dtype``: the sequences' tokens ctx[b] + j, or ``slots``
+    (int32 [rows], token numbers in the row's sequence).  Rows behind the last sequence are left as they were."""
+    n, d = rows.rows, cache.head_dim
+    _check_vector("slots", slots, torch.int32, n)
+    on = _On(stream)
+    if k_out is None:
+        k_out = on.empty((n, cache.n_kv, d), dtype, cache.k.device)
+    if v_out is None:
+        v_out = on.empty((n, cache.n_kv, d), dtype, cache.k.device)
+    _check_device(cache.k, rows.tables, slots, k_out, v_out)
+    act, k_pitch = _check_rows_of("k_out", k_out, n, cache.n_kv, d)
+    act_v, v_pitch = _check_rows_of("v_out", v_out, n, cache.n_kv, d)
+    if act != act_v:
+        raise ValueError("k_out and v_out must have one type")
+    _check(lib.nova_kv_gather(cache.layer(layer), rows.ref, _ptr(slots), act, k_out.data_ptr(), k_pitch, v_out.data_ptr(), v_pitch,
+                              _stream(stream)))
+    return k_out, v_out
+
+
+def tree_attention(cache, rows, q, mask=None, out=None, scale=None, layer=0, stream=None):
+    """Attention of each sequence's rows (at most 64 drafted tokens, appended before) over its cache: a row sees the
+    context and the drafted tokens i whose bit i is set in ``mask`` (int64 [rows]; None: those up to its own).
+    q [rows, n_q, head_dim] in ``cache.dtype``; returns ``out`` of the same shape and type."""
+    n, d = rows.rows, cache.head_dim
+    _check_device(cache.k, rows.tables, q, mask, out)
+    _check_vector("mask", mask, torch.int64, n)
+    n_q = q.shape[1] if q.dim() == 3 else 0
+    act, q_pitch = _check_rows_of("q", q, n, n_q, d)
+    on = _On(stream)
+    if out is None:
+        out = on.empty((n, n_q, d), q.dtype, q.device)
+    act_out, out_pitch = _check_rows_of("out", out, n, n_q, d)
+    if q.dtype != cache.dtype or act_out != act:
+        raise ValueError(f"q and out must be {cache.dtype}")
+    nbytes = rows._tree_bytes(cache, n_q)
+    ws = on.empty(nbytes, torch.uint8, q.device) if nbytes else None
+    _check(lib.nova_tree_attention(cache.layer(layer), rows.ref, _ptr(mask), q.data_ptr(), q_pitch, n_q,
+                                   d ** -0.5 if scale is None else scale, out.data_ptr(), out_pitch, _ptr(ws), nbytes, _stream(stream)))
+    return out
+
+
+def logprobs(logits, given=None, n_top=0, stream=None):
+    """Of logit rows [rows, vocab] (fp32 or bf16): (log probabilities of ``given`` int32 [rows, n] or None, entropies
+    [rows], the ``n_top`` (at most 32) largest log probabilities [rows, n_top] and their ids, or None)."""
+    act = _ACT.get(logits.dtype)
+    if act is None or logits.dim() != 2 or logits.stride(1) != 1:
+        raise ValueError(f"logits must be float32 or bfloat16 [rows, vocab] with contiguous rows, got {logits.dtype} {tuple(logits.shape)}")
+    if n_top < 0:
+        raise ValueError(f"n_top {n_top} is negative")
+    rows, vocab = logits.shape
+    n_given = 0
+    if given is not None:
+        if given.dtype != torch.int32 or given.dim() != 2 or given.shape[0] != rows or not given.is_contiguous():
+            raise ValueError(f"given must be contiguous int32 [{rows}, n], got {given.dtype} {tuple(given.shape)}")
+        n_given = given.shape[1]
+    _check_device(logits, given)
+    on, dev = _On(stream), logits.device
+    n_top = min(n_top, vocab)
+    lp = on.empty((rows, n_given), torch.float32, dev) if given is not None else None
+    entropy = on.empty((rows,), torch.float32, dev)
+    top_lp = on.empty((rows, n_top), torch.float32, dev) if n_top else None
+    top_ids = on.empty((rows, n_top), torch.int32, dev) if n_top else None
+    nbytes = lib.nova_logprobs_workspace_bytes(rows, vocab, n_top)
+    ws = on.empty(max(nbytes, 256), torch.uint8, dev)
+    _check(lib.nova_logprobs(logits.data_ptr(), act, logits.stride(0) if rows > 1 else vocab, rows, vocab, _ptr(given), n_given, _ptr(lp),
+                             entropy.data_ptr(), n_top, _ptr(top_lp), _ptr(top_ids), ws.data_ptr(), ws.numel(), _stream(stream)))
+    return lp, entropy, top_lp, top_ids
 
 
 # ----------------------------------------------------------------------------- linear co-run study
