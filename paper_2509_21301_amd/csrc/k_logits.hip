@@ -1,9 +1,13 @@
 // Log probabilities from rows of logits: of given tokens, the entropy of the distribution, and the most
 // likely tokens.  With m the row's maximum, S = sum e^(x - m) and T = sum e^(x - m) (x - m):
-//   log p_t = x_t - m - log S,   entropy = log S - T / S,
-// sums in fp32 over parts of the row whose lanes keep a maximum of their own, so every e^(x - m) is at
-// most 1 and T / S loses nothing to cancellation.  The logits are read once; bound by HBM for a batch
-// of vocabulary rows, by launches and latency for one.
+//   log p_t = x_t - m - log S,   entropy = log S - T / S.
+// One pass: every lane keeps a maximum, S and T of its own (fp32; every e^(x - m) is at most 1 and T / S
+// loses nothing to cancellation), joined at the end.  For the most likely tokens the pass keeps the
+// maximum of every 16 consecutive logits: the n_top largest logits (equal ones by the lower id) lie in
+// the n_top groups of largest maximum (equal ones by the lower group), whatever ties there are, because
+// each better group holds a better logit.  So a selection among vocab / 16 numbers and n_top groups
+// read again give them exactly.  A short row is one workgroup and one launch; a long one is cut into
+// parts that a second kernel joins.  Bound by HBM for many rows, by launches and latency for one.
 #include <algorithm>
 
 #include "common.hpp"
@@ -11,10 +15,13 @@
 
 namespace nova {
 
-constexpr int LP_EPL = 32;                 // logits of a lane at a time
+constexpr int LP_EPL = 16;                 // logits of a lane at a time
 constexpr int LP_CHUNK = 64 * LP_EPL;      // of a wave
-constexpr int LP_MAX_PARTS = 1024;
+constexpr int LP_GROUP = 16;               // consecutive logits with one maximum
+constexpr int LP_ONE = 8;                  // chunks of a row that one workgroup takes
+constexpr int LP_MAX_PARTS = 512;
 constexpr int LP_MAX_TOP = 32;
+constexpr int LP_CAND = 2048;              // candidates that are ranked by counting
 
 // An unsigned number that orders as the values do: -0 equals 0, NaN is above infinity; 0 is no value's.
 NOVA_DEV uint32_t order_key(float x) {
@@ -23,235 +30,364 @@ NOVA_DEV uint32_t order_key(float x) {
   return (u >> 31) ? ~u : u | 0x80000000u;
 }
 NOVA_DEV float key_value(uint32_t k) { return __uint_as_float((k >> 31) ? k & 0x7FFFFFFFu : ~k); }
-// Larger first, equal values by the lower id.
+// Larger first, equal values by the lower id; 0: none.
 NOVA_DEV unsigned long long rank_key(uint32_t key, int id) { return ((unsigned long long)key << 32) | (0xFFFFFFFFu - (uint32_t)id); }
 
-template <typename T> NOVA_DEV void load_logits(const T* row, int i0, int vocab, float* x) {
-  constexpr int N = 16 / sizeof(T);        // i0: the lane's first logit, N of them
-  if (i0 + N <= vocab && ((uintptr_t)(row + i0) & 15) == 0) {
-    const uint4 w = *reinterpret_cast<const uint4*>(row + i0);
-    const uint32_t a[4] = {w.x, w.y, w.z, w.w};
+// N = 16 / sizeof(T) logits from i0 on, where row + i0 is 16-byte aligned; -infinity outside the row.
+template <typename T> NOVA_DEV void load_logits(const T* row, long i0, int vocab, float* x) {
+  constexpr int N = 16 / sizeof(T);
+  if (i0 >= 0 && i0 + N <= vocab) {
+    const u32x4 w = *reinterpret_cast<const u32x4*>(row + i0);
 #pragma unroll
     for (int e = 0; e < N; ++e)
-      x[e] = sizeof(T) == 4 ? __uint_as_float(a[e]) : __uint_as_float((e & 1) ? a[e / 2] & 0xFFFF0000u : a[e / 2] << 16);
+      x[e] = sizeof(T) == 4 ? __uint_as_float(w[e & 3]) : __uint_as_float((e & 1) ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
   } else {
 #pragma unroll
-    for (int e = 0; e < N; ++e) x[e] = i0 + e < vocab ? to_f<T>(row[i0 + e]) : -INFINITY;
+    for (int e = 0; e < N; ++e) x[e] = i0 + e >= 0 && i0 + e < vocab ? to_f<T>(row[i0 + e]) : -INFINITY;
   }
 }
 
-// m, S, T of two sets of logits together.
+// m, S, T of a set of logits.
 struct LogSum { float m, s, t; };
-NOVA_DEV LogSum log_sum_join(const LogSum& a, float m) {
-  // a's sums taken to the maximum m >= a.m
+// a's sums taken to a maximum m >= a.m.
+NOVA_DEV LogSum log_sum_at(const LogSum& a, float m) {
   if (a.m == m || a.s == 0.f) return LogSum{m, a.s, a.t};
   const float d = a.m - m, f = __expf(d);
   return LogSum{m, f * a.s, f > 0.f ? f * (a.t + d * a.s) : 0.f * a.t};
 }
+NOVA_DEV LogSum log_sum_join(const LogSum& a, const LogSum& b) {
+  const float m = fmaxf(a.m, b.m);
+  const LogSum x = log_sum_at(a, m), y = log_sum_at(b, m);
+  return LogSum{m, x.s + y.s, x.t + y.t};
+}
 NOVA_DEV LogSum log_sum_wave(const LogSum& a) {
   const float m = wave_max(a.m);
-  const LogSum j = log_sum_join(a, m);
+  const LogSum j = log_sum_at(a, m);
   return LogSum{m, wave_sum(j.s), wave_sum(j.t)};
 }
 
-// The k largest keys of a wave's values, sorted, to out[0 .. k) (0 where there are fewer).  x: the lane's
-// values, idx(j): the id of its j-th (-1: none).  The k-th largest of the lanes' maxima bounds the k-th
-// largest value from below and is found by bisection with ballots; the values that reach it (k or a few
-// more) are packed into LDS and ranked by counting.  With too many equal ones, k rounds of a wave maximum.
-template <typename F>
-NOVA_DEV void wave_top(const uint32_t (&key)[LP_EPL], F idx, int k, unsigned long long* sm, unsigned long long* out) {
-  const int lane = threadIdx.x & 63;
-  uint32_t best = 0;
-#pragma unroll
-  for (int j = 0; j < LP_EPL; ++j) best = max(best, key[j]);
-  uint32_t tau = 0;                        // largest number that at least k lanes' maxima reach
-#pragma unroll 1
-  for (int bit = 31; bit >= 0; --bit) {
-    const uint32_t trial = tau | (1u << bit);
-    const int c = __popcll(__ballot(best >= trial));
-    if (c >= k) tau = trial;
-    if (c == k) break;
+// The logit of the thread's first given token, requested before the sums are known.
+template <typename T> NOVA_DEV float given_logit(const LogprobArgs& p, int r, int i) {
+  const int id = i < p.n_given ? p.given[(long)r * p.n_given + i] : -1;
+  return (unsigned)id < (unsigned)p.vocab ? to_f<T>(reinterpret_cast<const T*>(p.logits)[r * p.stride + id]) : -INFINITY;
+}
+// What a row's sums say; `x`: given_logit() of the thread's first.  Called by every thread of a workgroup.
+template <typename T>
+NOVA_DEV float row_sums(const LogprobArgs& p, int r, const LogSum& a, float x) {
+  // nothing but -infinity: no distribution
+  const float log_s = a.s == 0.f ? __uint_as_float(0x7FC00000u) : logf(a.s);
+  if (threadIdx.x == 0 && p.entropy) p.entropy[r] = log_s - a.t / a.s;
+  for (int i = threadIdx.x; i < p.n_given; i += blockDim.x) {
+    if (i >= (int)blockDim.x) x = given_logit<T>(p, r, i);
+    const int id = p.given[(long)r * p.n_given + i];
+    p.given_lp[(long)r * p.n_given + i] = (unsigned)id < (unsigned)p.vocab ? x - a.m - log_s : -INFINITY;
   }
-  tau = max(tau, 1u);
-  int n = 0;
-#pragma unroll
-  for (int j = 0; j < LP_EPL; ++j) n += __popcll(__ballot(key[j] >= tau));
-  if (n <= 64) {
-    int at = 0;
-#pragma unroll
-    for (int j = 0; j < LP_EPL; ++j) {
-      const unsigned long long m = __ballot(key[j] >= tau);
-      if (key[j] >= tau) sm[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0))] = rank_key(key[j], idx(j));
-      at += __popcll(m);
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    const unsigned long long mine = lane < n ? sm[lane] : 0;
-    int rank = 0;
-    for (int i = 0; i < n; ++i) rank += sm[i] > mine;
-    if (lane < n && rank < k) out[rank] = mine;
-    if (lane >= n && lane < k) out[lane] = 0;
-    return;
-  }
-  unsigned long long last = ~0ull;
-#pragma unroll 1
-  for (int r = 0; r < k; ++r) {
-    unsigned long long top = 0;
-#pragma unroll
-    for (int j = 0; j < LP_EPL; ++j) {
-      const unsigned long long c = key[j] ? rank_key(key[j], idx(j)) : 0;
-      if (c < last && c > top) top = c;
-    }
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) {
-      const unsigned long long c = __shfl_xor(top, o, 64);
-      top = c > top ? c : top;
-    }
-    if (lane == 0) out[r] = top;
-    if (top) last = top;                   // 0: every value is taken, and the rest of the list is 0
-    else last = 0;
-  }
+  return log_s;
 }
 
-// Wave (part of a row): chunks of 2048 logits, 32 per lane in registers; one chunk with n_top > 0.
-template <typename T>
-__global__ void __launch_bounds__(256) logprobs_part_kernel(LogprobArgs p, int parts, int chunks) {
-  constexpr int N = 16 / sizeof(T);
-  __shared__ unsigned long long sm[4][64];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const long unit = (long)blockIdx.x * 4 + wave;
-  if (unit >= (long)p.rows * parts) return;
-  const int r = (int)(unit / parts), part = (int)(unit % parts);
+// The larger of two values, NaN where either is (one instruction for three on gfx950).
+NOVA_DEV float nan_max(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+// LDS of the selection.
+template <int W> struct TopShared {
+  unsigned long long cand[LP_CAND];
+  int group[LP_CAND], rank[LP_CAND];
+  float set[W][64];
+  int count[W], n, m;
+};
+
+// The n_top most likely tokens of a row whose groups have the maxima gmax[0 .. groups) (NaN if one is in it);
+// group g is logits 16 g - lead ...  Every thread of a workgroup of W waves.
+//  1. The groups are dealt to 64 sets (one per lane number).  The k-th largest of the sets' maxima bounds
+//     the k-th logit of the row from below, and few groups reach it: some 64 ln(64 / (64 - k)).
+//  2. Their logits that reach it are ranked by counting the larger ones.
+//  3. Where too many reach it (equal values, or the best ones side by side), and where the row holds a NaN,
+//     the k-th group is bisected exactly, on its maximum and its number, and the logits of the best k
+//     groups that are not below its maximum are ranked: at most 16 k.
+// A thread takes V groups at a time; the first AHEAD times V are requested before anything waits.
+template <typename T, int W, int V, int AHEAD>
+struct RowTop {
+  static constexpr int THREADS = 64 * W, STRIDE = THREADS * V;
+  const LogprobArgs& p;
+  const float* gmax;
+  int r, groups, lead;
+  float first[AHEAD][V];
+
+  NOVA_DEV void take(int g, float (&m)[V]) const {               // groups is a multiple of 64
+    if (g < groups) {
+      if constexpr (V == 4) {
+        const f32x4 v = *reinterpret_cast<const f32x4*>(gmax + g);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) m[q] = v[q];
+      } else {
+        m[0] = gmax[g];
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < V; ++q) m[q] = -INFINITY;
+    }
+  }
+  NOVA_DEV void request() {
+#pragma unroll
+    for (int e = 0; e < AHEAD; ++e) take(e * STRIDE + V * (int)threadIdx.x, first[e]);
+  }
+  // f(maximum, group) of the thread's groups, for the passes that are rare
+  template <typename F> NOVA_DEV void each(F f) {
+#pragma unroll 1
+    for (int g = V * (int)threadIdx.x; g < groups; g += STRIDE) {
+      float m[V];
+      take(g, m);
+#pragma unroll
+      for (int q = 0; q < V; ++q) f(m[q], g + q);
+    }
+  }
+  // The logits of the n groups in sm.group that are not below `least`, into sm.cand (those that fit): how many.
+  NOVA_DEV int logits_of(int n, uint32_t least, TopShared<W>& sm) {
+    const int tid = threadIdx.x;
+    const T* row = reinterpret_cast<const T*>(p.logits) + r * p.stride;
+    for (int i0 = 0; i0 < n * LP_GROUP; i0 += 4 * THREADS) {
+      float x[4];
+      int id[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {                               // requested together
+        const int i = i0 + u * THREADS + tid;
+        id[u] = i < n * LP_GROUP ? sm.group[i / LP_GROUP] * LP_GROUP - lead + i % LP_GROUP : -1;
+        if (id[u] >= p.vocab) id[u] = -1;
+        x[u] = id[u] >= 0 ? to_f<T>(row[id[u]]) : 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const uint32_t key = order_key(x[u]);
+        if (id[u] < 0 || key < least) continue;
+        const int to = atomicAdd(&sm.m, 1);
+        if (to < LP_CAND) {
+          sm.cand[to] = rank_key(key, id[u]);
+          sm.rank[to] = 0;
+        }
+      }
+    }
+    __syncthreads();
+    return sm.m;
+  }
+
+  NOVA_DEV void operator()(const LogSum& a, float log_s, TopShared<W>& sm) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, k = p.n_top;
+    float best = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < AHEAD; ++e)
+#pragma unroll
+      for (int q = 0; q < V; ++q) best = nan_max(best, first[e][q]);
+    if (groups > AHEAD * STRIDE) each([&](float m, int) { best = nan_max(best, m); });
+    sm.set[wave][lane] = best;
+    if (tid == 0) sm.n = sm.m = 0;
+    __syncthreads();
+    best = sm.set[0][lane];
+#pragma unroll
+    for (int w = 1; w < W; ++w) best = nan_max(best, sm.set[w][lane]);
+    const bool nan = __any(best != best);
+    int above = 0;                                                // sets with a larger maximum
+#pragma unroll
+    for (int l = 0; l < 64; ++l) above += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(best), l)) > best;
+    const float tau = -wave_max(above < k ? -best : -INFINITY);
+    int n = LP_CAND + 1;
+    if (!nan) {
+      auto put = [&](float m, int g) {
+        if (m >= tau) {
+          const int to = atomicAdd(&sm.n, 1);
+          if (to < LP_CAND) sm.group[to] = g;
+        }
+      };
+#pragma unroll
+      for (int e = 0; e < AHEAD; ++e)
+#pragma unroll
+        for (int q = 0; q < V; ++q)
+          if (e * STRIDE + V * tid + q < groups) put(first[e][q], e * STRIDE + V * tid + q);
+      if (groups > AHEAD * STRIDE)
+        each([&](float m, int g) {
+          if (g >= AHEAD * STRIDE) put(m, g);
+        });
+      __syncthreads();
+      n = sm.n;
+      if (n <= LP_CAND) n = logits_of(n, order_key(tau), sm);
+    }
+    if (n > LP_CAND) {
+      // the largest bound that k groups reach (there are 64 at least): exactly k, since keys differ
+      unsigned long long bound = 1;
+#pragma unroll 1
+      for (int bit = 63; bit >= 0; --bit) {
+        const unsigned long long trial = bound | (1ull << bit);
+        int c = 0;
+        each([&](float m, int g) { c += rank_key(order_key(m), g) >= trial; });
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) c += __shfl_xor(c, o, 64);
+        __syncthreads();
+        if (lane == 0) sm.count[wave] = c;
+        __syncthreads();
+        c = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) c += sm.count[w];
+        if (c >= k) bound = trial;
+      }
+      if (tid == 0) sm.n = sm.m = 0;
+      __syncthreads();
+      each([&](float m, int g) {
+        if (rank_key(order_key(m), g) >= bound) sm.group[atomicAdd(&sm.n, 1)] = g;
+      });
+      __syncthreads();
+      n = logits_of(k, (uint32_t)(bound >> 32), sm);
+    }
+    // a candidate's rank is the number of larger ones; `split` threads share a candidate
+    const int span = (n + 63) & ~63, split = max(1, THREADS / span), per = (n + split - 1) / split;
+    for (int t = tid; t < span * split; t += THREADS) {
+      const int i = t % span, j0 = t / span * per, j1 = min(j0 + per, n);
+      const unsigned long long c = i < n ? sm.cand[i] : ~0ull;
+      int x = 0;
+#pragma unroll 8
+      for (int j = j0; j < j1; ++j) x += sm.cand[j] > c;
+      if (i < n && x) atomicAdd(&sm.rank[i], x);
+    }
+    __syncthreads();
+    for (int i = tid; i < n; i += THREADS) {
+      const int at = sm.rank[i];
+      if (at >= k) continue;
+      p.top_lp[(long)r * k + at] = key_value((uint32_t)(sm.cand[i] >> 32)) - a.m - log_s;
+      p.top_ids[(long)r * k + at] = (int)(0xFFFFFFFFu - (uint32_t)sm.cand[i]);
+    }
+  }
+};
+
+// Workgroup (part of a row), its waves taking chunks of 1024 logits in turn, the next one's loads in
+// flight.  ONE: the part is the whole row, and the workgroup finishes it.
+template <typename T, bool ONE>
+__global__ void __launch_bounds__(256) logprobs_part_kernel(LogprobArgs p, int parts, int chunks, int groups) {
+  constexpr int N = 16 / sizeof(T), LPG = LP_GROUP / N;           // a load's logits, lanes that share a group
+  __shared__ LogSum sm[4];
+  __shared__ __align__(16) float sm_max[ONE ? LP_ONE * 64 : 4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r = ONE ? blockIdx.x : blockIdx.x / parts, part = ONE ? 0 : blockIdx.x % parts;
   const T* row = reinterpret_cast<const T*>(p.logits) + r * p.stride;
+  const int lead = (int)(((uintptr_t)row & 15) / sizeof(T));      // chunks start at the aligned address at or before the row
+  const int total = (p.vocab + lead + LP_CHUNK - 1) / LP_CHUNK;
+  const int c0 = part * chunks, c1 = min(c0 + chunks, total);
+  auto load = [&](int c, float (&x)[LP_EPL]) {
+#pragma unroll
+    for (int j = 0; j < LP_EPL; j += N) load_logits(row, (long)c * LP_CHUNK - lead + j * 64 + lane * N, p.vocab, x + j);
+  };
+  const float gx = ONE ? given_logit<T>(p, r, tid) : 0.f;
   LogSum a{-INFINITY, 0.f, 0.f};
-  for (int c = 0; c < chunks; ++c) {
-    const long c0 = ((long)part * chunks + c) * LP_CHUNK;
-    if (c0 >= p.vocab) break;
-    float x[LP_EPL];
+  float x[LP_EPL], next[LP_EPL];
+  if (c0 + wave < c1) load(c0 + wave, x);
+  for (int c = c0 + wave; c < c1; c += 4) {
+    if (c + 4 < c1) load(c + 4, next);
+    float top[LP_EPL / N], m = a.m;
 #pragma unroll
-    for (int j = 0; j < LP_EPL; j += N) load_logits(row, (int)min(c0 + j * 64 + lane * N, (long)p.vocab), p.vocab, x + j);
-    float m = a.m;
+    for (int j = 0; j < LP_EPL / N; ++j) {
+      top[j] = x[j * N];
 #pragma unroll
-    for (int j = 0; j < LP_EPL; ++j) m = fmaxf(m, x[j]);
-    a = log_sum_join(a, m);
+      for (int e = 1; e < N; ++e) top[j] = nan_max(top[j], x[j * N + e]);
+      m = fmaxf(m, top[j]);
+    }
+    if (p.n_top > 0) {                                            // lane LPG q + j writes group q of the j-th loads
+      float mine = 0.f;
+#pragma unroll
+      for (int j = 0; j < LP_EPL / N; ++j) {
+        float g = nan_max(top[j], __shfl_xor(top[j], 1, 64));
+        if (LPG == 4) g = nan_max(g, __shfl_xor(g, 2, 64));
+        if (lane % LPG == j) mine = g;
+      }
+      const int g = c * (LP_CHUNK / LP_GROUP) + lane % LPG * (64 / LPG) + lane / LPG;
+      if constexpr (ONE) sm_max[g] = mine;
+      else p.part_max[(long)r * groups + g] = mine;
+    }
+    a = log_sum_at(a, m);
     const float mu = m == -INFINITY ? 0.f : m;
 #pragma unroll
     for (int j = 0; j < LP_EPL; ++j) {
       const float d = x[j] - mu, e = __expf(d);
       a.s += e;
-      a.t += e == 0.f ? 0.f : e * d;
+      a.t += e * fmaxf(d, -200.f);                                // e is 0 there: -infinity adds 0
     }
+#pragma unroll
+    for (int j = 0; j < LP_EPL; ++j) x[j] = next[j];
+  }
+  a = log_sum_wave(a);
+  if (lane == 0) sm[wave] = a;
+  __syncthreads();
+  a = sm[0];
+#pragma unroll
+  for (int w = 1; w < 4; ++w) a = log_sum_join(a, sm[w]);
+  if constexpr (ONE) {
+    __shared__ TopShared<4> ts;
+    const float log_s = row_sums<T>(p, r, a, gx);
     if (p.n_top > 0) {
-      uint32_t key[LP_EPL];
-      auto idx = [&](int j) { return (int)(c0 + (j / N) * N * 64 + lane * N + j % N); };
-#pragma unroll
-      for (int j = 0; j < LP_EPL; ++j) key[j] = idx(j) < p.vocab ? order_key(x[j]) : 0;
-      wave_top(key, idx, p.n_top, sm[wave], p.part_top + unit * p.n_top);
+      RowTop<T, 4, 1, (LP_ONE * 64 + 255) / 256> top{p, sm_max, r, total * (LP_CHUNK / LP_GROUP), lead, {}};
+      top.request();
+      top(a, log_s, ts);
     }
+  } else if (tid == 0) {
+    reinterpret_cast<float4*>(p.part_sum)[blockIdx.x] = make_float4(a.m, a.s, a.t, 0.f);
   }
-  a = log_sum_wave(a);
-  if (lane == 0) reinterpret_cast<float4*>(p.part_sum)[unit] = make_float4(a.m, a.s, a.t, 0.f);
 }
 
-// Workgroup (row): the parts' sums joined, the given tokens' log probabilities, and the parts' sorted lists
-// merged: the k-th largest of their first entries bounds the k-th of all from below, so at most k lists
-// have entries that reach it; those are ranked by counting.
-template <typename T>
-__global__ void __launch_bounds__(256) logprobs_row_kernel(LogprobArgs p, int parts) {
-  __shared__ unsigned long long head[LP_MAX_PARTS], cand[LP_MAX_TOP * LP_MAX_TOP];
-  __shared__ float sm_m[4], sm_s[4], sm_t[4];
-  __shared__ unsigned long long tau;
-  __shared__ int n_cand;
-  const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, k = p.n_top;
-  const unsigned long long* lists = p.part_top + (long)r * parts * k;
-  if (tid == 0) { tau = 1; n_cand = 0; }
-  LogSum a{-INFINITY, 0.f, 0.f};
-  for (int i = tid; i < parts; i += 256) {
-    const float4 v = reinterpret_cast<const float4*>(p.part_sum)[(long)r * parts + i];
-    const LogSum b{v.x, v.y, v.z};
-    const float m = fmaxf(a.m, b.m);
-    const LogSum x = log_sum_join(a, m), y = log_sum_join(b, m);
-    a = LogSum{m, x.s + y.s, x.t + y.t};
-    if (k > 0) head[i] = lists[(long)i * k];
-  }
-  a = log_sum_wave(a);
-  if (lane == 0) { sm_m[wave] = a.m; sm_s[wave] = a.s; sm_t[wave] = a.t; }
-  __syncthreads();
-  const float m = fmaxf(fmaxf(sm_m[0], sm_m[1]), fmaxf(sm_m[2], sm_m[3]));
-  LogSum z{m, 0.f, 0.f};
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const LogSum j = log_sum_join(LogSum{sm_m[w], sm_s[w], sm_t[w]}, m);
-    z.s += j.s;
-    z.t += j.t;
-  }
-  // nothing but -infinity: no distribution
-  const float log_s = z.s == 0.f ? __uint_as_float(0x7FC00000u) : logf(z.s);
-  if (tid == 0 && p.entropy) p.entropy[r] = log_s - z.t / z.s;
+// Workgroup (row): the parts' sums joined, the most likely tokens from the groups' maxima.
+template <typename T, bool TOP>
+__global__ void __launch_bounds__(TOP ? 512 : 64) logprobs_join_kernel(LogprobArgs p, int parts, int groups) {
+  const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const T* row = reinterpret_cast<const T*>(p.logits) + r * p.stride;
-  for (int i = tid; i < p.n_given; i += 256) {
-    const int id = p.given[(long)r * p.n_given + i];
-    p.given_lp[(long)r * p.n_given + i] = (unsigned)id < (unsigned)p.vocab ? to_f<T>(row[id]) - m - log_s : -INFINITY;
+  const int lead = (int)(((uintptr_t)row & 15) / sizeof(T)), total = (p.vocab + lead + LP_CHUNK - 1) / LP_CHUNK;
+  const float gx = given_logit<T>(p, r, tid);
+  float4 v = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+  if (lane < parts) v = reinterpret_cast<const float4*>(p.part_sum)[(long)r * parts + lane];
+  RowTop<T, 8, 4, TOP ? 6 : 1> top{p, p.part_max + (long)r * groups, r, total * (LP_CHUNK / LP_GROUP), lead, {}};
+  if constexpr (TOP) top.request();
+  LogSum a{v.x, v.y, v.z};                                        // every wave the same: no barrier
+  for (int i = lane + 64; i < parts; i += 64) {
+    v = reinterpret_cast<const float4*>(p.part_sum)[(long)r * parts + i];
+    a = log_sum_join(a, LogSum{v.x, v.y, v.z});
   }
-  if (k == 0) return;
-  if (parts >= k) {
-    for (int i = tid; i < parts; i += 256) {
-      const unsigned long long h = head[i];
-      int rank = 0;
-      for (int j = 0; j < parts; ++j) rank += head[j] > h;
-      if (rank == k - 1 && h > 0) tau = h;
-    }
-  }
-  __syncthreads();
-  for (int i = tid; i < parts; i += 256) {
-    if (head[i] < tau) continue;
-    for (int j = 0; j < k; ++j) {
-      const unsigned long long c = lists[(long)i * k + j];
-      if (c < tau) break;
-      cand[atomicAdd(&n_cand, 1)] = c;
-    }
-  }
-  __syncthreads();
-  const int n = n_cand;
-  for (int i = tid; i < n; i += 256) {
-    const unsigned long long c = cand[i];
-    int rank = 0;
-    for (int j = 0; j < n; ++j) rank += cand[j] > c;
-    if (rank < k) {
-      p.top_lp[(long)r * k + rank] = key_value((uint32_t)(c >> 32)) - m - log_s;
-      p.top_ids[(long)r * k + rank] = (int)(0xFFFFFFFFu - (uint32_t)c);
-    }
+  a = log_sum_wave(a);
+  const float log_s = row_sums<T>(p, r, a, gx);
+  if constexpr (TOP) {
+    __shared__ TopShared<8> ts;
+    top(a, log_s, ts);
   }
 }
 
-struct LogprobPlan { int parts, chunks; };
-static LogprobPlan logprob_plan(int rows, int vocab, int n_top) {
-  LogprobPlan t;
-  const int chunks = (vocab + LP_CHUNK - 1) / LP_CHUNK;
-  t.chunks = 1;
-  if (n_top == 0) {                       // waves for the whole GPU, 16 on a compute unit
-    const long waves = (long)rows * chunks;
-    t.chunks = (int)std::min<long>(chunks, std::max<long>(1, waves / 4096));
-  }
-  t.parts = (chunks + t.chunks - 1) / t.chunks;
+// Parts of a row and the chunks of each.  A row of up to LP_ONE chunks is one workgroup.  Above, parts until
+// the GPU holds 16 waves on each of its 256 compute units, at least one chunk a wave.
+struct LogprobPlan { int parts, chunks, groups; };
+static LogprobPlan logprob_plan(int rows, int vocab) {
+  const int total = (vocab + 7 + LP_CHUNK - 1) / LP_CHUNK;       // an unaligned row starts up to 7 logits early
+  LogprobPlan t{1, total, total * (LP_CHUNK / LP_GROUP)};
+  if (total <= LP_ONE) return t;
+  const long per = std::max<long>(1, (long)rows * total / 4096);
+  t.chunks = (int)std::min<long>(total, per * 4);
+  t.chunks = std::max(t.chunks, (total + LP_MAX_PARTS - 1) / LP_MAX_PARTS);
+  t.parts = (total + t.chunks - 1) / t.chunks;
   return t;
 }
+static bool logprob_one(int vocab) { return (vocab + 7 + LP_CHUNK - 1) / LP_CHUNK <= LP_ONE; }
 
-bool logprobs_fits(int vocab, int n_top) { return n_top <= LP_MAX_TOP && vocab <= LP_MAX_PARTS * LP_CHUNK; }
+bool logprobs_fits(int vocab, int n_top) { return n_top <= LP_MAX_TOP && vocab <= 1 << 21; }
 
-void logprobs_part_sizes(int rows, int vocab, int n_top, size_t* sum_floats, size_t* top_keys) {
-  const LogprobPlan t = logprob_plan(rows, vocab, n_top);
-  *sum_floats = (size_t)rows * t.parts * 4;
-  *top_keys = (size_t)rows * t.parts * n_top;
+void logprobs_part_sizes(int rows, int vocab, int n_top, size_t* sum_floats, size_t* max_floats) {
+  const LogprobPlan t = logprob_plan(rows, vocab);
+  const bool one = logprob_one(vocab);
+  *sum_floats = one ? 0 : (size_t)rows * t.parts * 4;
+  *max_floats = one || n_top == 0 ? 0 : (size_t)rows * t.groups;
 }
 
 template <typename T> static hipError_t logprobs_launch(const LogprobArgs& p, hipStream_t s) {
-  const LogprobPlan t = logprob_plan(p.rows, p.vocab, p.n_top);
-  const long waves = (long)p.rows * t.parts;
-  hipLaunchKernelGGL((logprobs_part_kernel<T>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, p, t.parts, t.chunks);
+  const LogprobPlan t = logprob_plan(p.rows, p.vocab);
+  if (logprob_one(p.vocab)) {
+    hipLaunchKernelGGL((logprobs_part_kernel<T, true>), dim3(p.rows), dim3(256), 0, s, p, 1, t.chunks, t.groups);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((logprobs_part_kernel<T, false>), dim3((unsigned)((long)p.rows * t.parts)), dim3(256), 0, s, p, t.parts, t.chunks, t.groups);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((logprobs_row_kernel<T>), dim3(p.rows), dim3(256), 0, s, p, t.parts);
+  if (p.n_top > 0) hipLaunchKernelGGL((logprobs_join_kernel<T, true>), dim3(p.rows), dim3(512), 0, s, p, t.parts, t.groups);
+  else hipLaunchKernelGGL((logprobs_join_kernel<T, false>), dim3(p.rows), dim3(64), 0, s, p, t.parts, t.groups);
   return hipGetLastError();
 }
 

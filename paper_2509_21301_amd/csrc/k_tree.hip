@@ -31,49 +31,54 @@ template <typename CT, int D> struct TreeRaw {
   static constexpr int JN = TreeT<CT>::JN;
   static constexpr int KW = D * sizeof(CT) / 64;          // 16-byte words of a K row per lane
   static constexpr int VW = 4 * JN * sizeof(CT) / 16;     // of a V row
-  uint4 k[JN][KW];
-  uint4 v[D / 16][VW];
+  u32x4 k[JN][KW];
+  u32x4 v[D / 16][VW];
   float ks[JN];                                           // e4m3: scale of the lane's K rows
-  uint4 ve;                                               // e4m3: exponent bytes of the lane group's 16 tokens
+  u32x4 ve;                                               // e4m3: exponent bytes of the lane group's 16 tokens
   bool ok;                                                // the lane group's own block (V) exists
 };
 
-// The elements of a lane's V words that are not finite, a bit each (e4m3 has NaN only).
-template <typename CT, int VW> NOVA_DEV uint32_t v_odd(const uint4 (&v)[VW]) {
+// The elements of 16 bytes of V that are not finite, a bit each (e4m3 has NaN only).
+template <typename CT> NOVA_DEV uint32_t v_odd(u32x4 q) {
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
   uint32_t is = 0;
 #pragma unroll
-  for (int w = 0; w < 4 * VW; ++w) {
-    const uint32_t x = (w & 3) == 0 ? v[w / 4].x : (w & 3) == 1 ? v[w / 4].y : (w & 3) == 2 ? v[w / 4].z : v[w / 4].w;
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t x = w[i];
     if constexpr (sizeof(CT) == 4) {
-      is |= (x & 0x7F800000u) == 0x7F800000u ? 1u << w : 0u;
+      is |= (x & 0x7F800000u) == 0x7F800000u ? 1u << i : 0u;
     } else if constexpr (sizeof(CT) == 2) {
-      is |= (x & 0x7F80u) == 0x7F80u ? 1u << 2 * w : 0u;
-      is |= (x & 0x7F800000u) == 0x7F800000u ? 2u << 2 * w : 0u;
+      is |= (x & 0x7F80u) == 0x7F80u ? 1u << 2 * i : 0u;
+      is |= (x & 0x7F800000u) == 0x7F800000u ? 2u << 2 * i : 0u;
     } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) is |= ((x >> 8 * e) & 0x7Fu) == 0x7Fu ? 1u << (4 * w + e) : 0u;
+      for (int e = 0; e < 4; ++e) is |= ((x >> 8 * e) & 0x7Fu) == 0x7Fu ? 1u << (4 * i + e) : 0u;
     }
   }
   return is;
 }
-// Clears the elements of a lane's V words whose bit in `keep` is not set.
-template <typename CT, int VW> NOVA_DEV void v_keep(uint4 (&v)[VW], uint32_t keep) {
-  constexpr int EPW = 4 / sizeof(CT);
+// A V element where it is not finite (as a float), 0 elsewhere.
+template <typename CT> NOVA_DEV float odd_value(CT x) {
+  if constexpr (sizeof(CT) == 1) return (x.v & 0x7F) == 0x7F ? __uint_as_float(0x7FC00000u) : 0.f;
+  else return to_f<CT>(x);
+}
+// 16 bytes of V with the elements cleared whose bit in `keep` is not set.
+template <typename CT> NOVA_DEV u32x4 v_keep(u32x4 q, uint32_t keep) {
+  constexpr int EPW = 4 / sizeof(CT);                     // elements per dword
+  constexpr uint32_t one = sizeof(CT) == 4 ? ~0u : (1u << (8 * (sizeof(CT) & 3))) - 1u;
+  uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-  for (int w = 0; w < 4 * VW; ++w) {
+  for (int i = 0; i < 4; ++i) {
     uint32_t m = 0;
 #pragma unroll
-    for (int e = 0; e < EPW; ++e) {
-      constexpr uint32_t one = sizeof(CT) == 4 ? ~0u : (1u << (8 * (sizeof(CT) & 3))) - 1u;
-      m |= ((keep >> (w * EPW + e)) & 1u) ? one << (8 * sizeof(CT) * e % 32) : 0u;
-    }
-    uint32_t& x = (w & 3) == 0 ? v[w / 4].x : (w & 3) == 1 ? v[w / 4].y : (w & 3) == 2 ? v[w / 4].z : v[w / 4].w;
-    x &= m;
+    for (int e = 0; e < EPW; ++e) m |= ((keep >> (i * EPW + e)) & 1u) ? one << (8 * sizeof(CT) * e % 32) : 0u;
+    w[i] &= m;
   }
+  return u32x4{w[0], w[1], w[2], w[3]};
 }
 
 template <typename CT, int D, int NQ>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ > 2 ? 1 : 2)))
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
 tree_attn_kernel(TreeArgs p, int steps_per_split) {
   typedef typename TreeT<CT>::act T;
   typedef TreeRaw<CT, D> Raw;
@@ -133,7 +138,7 @@ tree_attn_kernel(TreeArgs p, int steps_per_split) {
 #pragma unroll
     for (int j = 0; j < JN; ++j) {
       // a lane's 16 bytes of word w: dimensions 64 w + 16 grp .. of e4m3, 32 w + 8 grp .. of bf16, 16 w + 4 grp .. of f32
-      const uint4* kr = reinterpret_cast<const uint4*>(reinterpret_cast<const CT*>(p.c.k) + (tok + 4 * j) * D) + grp;
+      const u32x4* kr = reinterpret_cast<const u32x4*>(reinterpret_cast<const CT*>(p.c.k) + (tok + 4 * j) * D) + grp;
 #pragma unroll
       for (int w = 0; w < Raw::KW; ++w) raw.k[j][w] = kr[4 * w];
       if constexpr (Q8) raw.ks[j] = exp_scale(p.c.k_exp[tok + 4 * j]);
@@ -147,8 +152,8 @@ tree_attn_kernel(TreeArgs p, int steps_per_split) {
 #pragma unroll
     for (int i = 0; i < ND; ++i)
 #pragma unroll
-      for (int w = 0; w < Raw::VW; ++w) raw.v[i][w] = reinterpret_cast<const uint4*>(vr + (size_t)16 * i * PAGE)[w];
-    if constexpr (Q8) raw.ve = *reinterpret_cast<const uint4*>(p.c.v_exp + tok);
+      for (int w = 0; w < Raw::VW; ++w) raw.v[i][w] = reinterpret_cast<const u32x4*>(vr + (size_t)16 * i * PAGE)[w];
+    if constexpr (Q8) raw.ve = *reinterpret_cast<const u32x4*>(p.c.v_exp + tok);
   };
   if (n_it > 0) {
     load_k(0);
@@ -182,7 +187,7 @@ tree_attn_kernel(TreeArgs p, int steps_per_split) {
   const float scale = p.scale * 1.4426950408889634f;
 
   // V^T P^T of one dimension block added to its accumulators: `v` the lane's words, `pt` P^T
-  auto add_pv = [&](const uint4 (&v)[Raw::VW], const auto& pt, f32x4 (&acc)[NQ]) {
+  auto add_pv = [&](const u32x4 (&v)[Raw::VW], const auto& pt, f32x4 (&acc)[NQ]) {
     if constexpr (F32) {
       float f[TPG];
       __builtin_memcpy(f, v, sizeof f);
@@ -191,7 +196,7 @@ tree_attn_kernel(TreeArgs p, int steps_per_split) {
 #pragma unroll
         for (int n = 0; n < NQ; ++n) acc[n] = mfma4(f[e], pt[n][e], acc[n]);
     } else if constexpr (Q8) {
-      const uint4 x = v[0];
+      const u32x4 x = v[0];
       const Frag8 a{{e4m3_pair<false>(x.x, 1.f), e4m3_pair<true>(x.x, 1.f), e4m3_pair<false>(x.y, 1.f), e4m3_pair<true>(x.y, 1.f)}};
       const Frag8 c{{e4m3_pair<false>(x.z, 1.f), e4m3_pair<true>(x.z, 1.f), e4m3_pair<false>(x.w, 1.f), e4m3_pair<true>(x.w, 1.f)}};
 #pragma unroll
@@ -218,7 +223,7 @@ tree_attn_kernel(TreeArgs p, int steps_per_split) {
       for (int n = 0; n < NQ; ++n) sc[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < Raw::KW; ++w) {
-        const uint4 x = raw.k[j][w];
+        const u32x4 x = raw.k[j][w];
         if constexpr (F32) {
           const float f[4] = {__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w)};
 #pragma unroll
@@ -257,18 +262,22 @@ tree_attn_kernel(TreeArgs p, int steps_per_split) {
       }
       // slots past the last token may hold anything: their V is cleared
 #pragma unroll
-      for (int i = 0; i < ND; ++i) v_keep<CT>(raw.v[i], (1u << valid) - 1u);
+      for (int i = 0; i < ND; ++i)
+#pragma unroll
+        for (int w = 0; w < Raw::VW; ++w) raw.v[i][w] = v_keep<CT>(raw.v[i][w], ((1u << valid) - 1u) >> (w * 16 / sizeof(CT)));
       // A drafted token's V that is not finite concerns the rows that see it and no other, and 0 times
       // infinity is not 0: such elements are cleared here too and added when the rows are written.
       if (mine + TPG > sr.ctx) {
         const uint32_t drafted = mine >= sr.ctx ? ~0u : ~0u << (sr.ctx - mine);
         uint32_t odd = 0;
 #pragma unroll
-        for (int i = 0; i < ND; ++i) {
-          const uint32_t is = v_odd<CT>(raw.v[i]) & drafted;
-          if (is) v_keep<CT>(raw.v[i], ~is);
-          odd |= is;
-        }
+        for (int i = 0; i < ND; ++i)
+#pragma unroll
+          for (int w = 0; w < Raw::VW; ++w) {
+            const uint32_t is = v_odd<CT>(raw.v[i][w]) & (drafted >> (w * 16 / sizeof(CT)));
+            if (is) raw.v[i][w] = v_keep<CT>(raw.v[i][w], ~is);
+            odd |= is;
+          }
         if (odd) sm_odd = 1;
       }
     }
@@ -290,12 +299,12 @@ tree_attn_kernel(TreeArgs p, int steps_per_split) {
       tmax = fmaxf(tmax, __shfl_xor(tmax, 32, 64));
       const float m_new = fmaxf(m_run[n], tmax);
       const float m_use = m_new == -INFINITY ? 0.f : m_new;      // nothing seen yet: every p is 0
-      const float corr = exp2f(m_run[n] - m_use);
+      const float corr = __builtin_amdgcn_exp2f(m_run[n] - m_use);
       m_run[n] = m_new;
       float rs = 0.f;
 #pragma unroll
       for (int e = 0; e < TPG; ++e) {
-        s[e] = exp2f(s[e] - m_use);
+        s[e] = __builtin_amdgcn_exp2f(s[e] - m_use);
         rs += s[e];
       }
       l_run[n] = l_run[n] * corr + rs;
@@ -362,7 +371,7 @@ tree_attn_kernel(TreeArgs p, int steps_per_split) {
       float L = 0.f, O = 0.f;
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        const float f = exp2f(sm_m[w][c] - mu);
+        const float f = __builtin_amdgcn_exp2f(sm_m[w][c] - mu);
         L += f * sm_l[w][c];
         O += f * sm_o[w][c][d];
       }
@@ -373,10 +382,7 @@ tree_attn_kernel(TreeArgs p, int steps_per_split) {
         for (int j = max(0, step0 * STEP - sr.ctx); j < min(sr.n, step1 * STEP - sr.ctx); ++j) {
           const int tok = sr.ctx + j, ph = page_of(p.r, p.c.num_blocks, b, tok / PAGE);
           if (!((see >> j) & 1) || ph < 0) continue;
-          const CT x = reinterpret_cast<const CT*>(p.c.v)[(((size_t)ph * n_kv + kvh) * D + d) * PAGE + tok % PAGE];
-          float v;
-          if constexpr (Q8) v = (x.v & 0x7F) == 0x7F ? __uint_as_float(0x7FC00000u) : 0.f;
-          else v = to_f<CT>(x);
+          const float v = odd_value<CT>(reinterpret_cast<const CT*>(p.c.v)[(((size_t)ph * n_kv + kvh) * D + d) * PAGE + tok % PAGE]);
           if (!(fabsf(v) < INFINITY)) O += v;
         }
       }
@@ -392,50 +398,374 @@ tree_attn_kernel(TreeArgs p, int steps_per_split) {
   }
 }
 
-// Joins the splits of one row and head: one wave, D / 64 dimensions per lane.
-template <typename T, int D>
-__global__ void __launch_bounds__(256) tree_combine_kernel(TreeArgs p, int nsplit, long row_heads) {
-  const int lane = threadIdx.x & 63;
-  const long rh = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (rh >= row_heads) return;
-  const long t = rh / p.n_q;
-  const int head = (int)(rh % p.n_q);
-  if (p.r.row_start) {                                   // rows of no sequence are left as they were
-    int lo = 0, hi = p.r.batch;
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (p.r.row_start[mid + 1] <= t) lo = mid + 1;
-      else hi = mid;
+// ------------------------------------------------------------------ many rows
+// Above 16 rows of a KV head the products outweigh the loads, and the waves share K and V: workgroup of
+// 4 waves x 32 rows, 64 tokens at a time staged in LDS as bf16 (8-bit ones are converted once for
+// the four waves), two buffers, so that a step costs one barrier and the next step's loads are in flight
+// during its products (32x32x16: S = K Q^T, O^T = V^T P^T).  S's rows are read in the order in which
+// lane half h then holds tokens 16 u + 8 h + e of each 32, the ones that it hands to the second product.
+// 16-byte pieces are swizzled by their row so that a read covers every bank once.
+template <typename CT, int D>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
+tree_wide_kernel(TreeArgs p, int steps_per_split) {
+  constexpr bool Q8 = sizeof(CT) == 1;
+  constexpr int STEP = 64, ND = D / 32, NS = D / 16;
+  constexpr int LW = STEP * D * sizeof(CT) / 16 / 256;            // 16-byte loads of a thread, for K and for V
+  constexpr int KPT = D * sizeof(CT) / 16;                        // of a K row
+  constexpr int VPT = PAGE * sizeof(CT) / 16;                     // of a V row of a block
+  // K [2][64 tokens][D] and V [2][D][64 tokens] in bf16, byte-addressed: the 16-byte piece c of a row sits at
+  // c ^ x(row), so pieces 2 n + h of a row are one address, of piece h, with n << 5 toggled
+  constexpr int KBUF = STEP * D * 2, VBUF = D * STEP * 2;
+  __shared__ __align__(1024) unsigned char smem[2 * KBUF + 2 * VBUF];
+  __shared__ __align__(16) float sm_vs[2][STEP + 64];
+  __shared__ int sm_odd;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n_kv = p.c.n_kv, G = p.n_q / n_kv;
+  const int split = blockIdx.x, kvh = blockIdx.y % n_kv, tile = blockIdx.y / n_kv, b = blockIdx.z;
+  const int col = lane & 31, half = lane >> 5;
+  const SeqRows sr = seq_rows(p.r, b);
+  const int nrow = sr.n * G, row0 = tile * 128;
+  if (row0 >= nrow) return;
+  const int total = sr.ctx + sr.n;
+  const int nsteps = (total + STEP - 1) / STEP;
+  const int step0 = split * steps_per_split, step1 = min(step0 + steps_per_split, nsteps);
+  const bool active = row0 + 32 * wave < nrow;
+  const int row = row0 + 32 * wave + col, rc = min(row, nrow - 1);
+  const int t = rc / G, head = kvh * G + rc % G;
+  const unsigned long long sees = p.mask ? p.mask[sr.r0 + t] : (2ull << t) - 1;
+  if (tid == 0) sm_odd = 0;
+
+  // Block ids of 16 steps at a time, one per lane (those that exist), the next 16 requested ahead: a
+  // step's loads wait for no table load.  A wave's u-th 16-byte load of K and of V lies in one block.
+  const int* table = p.r.tables + (size_t)b * p.r.max_blocks;
+  const int nblk = (total + PAGE - 1) / PAGE;
+  auto entries = [&](int step) -> int {
+    const int blk = 4 * step + lane;
+    const int ph = blk < min(nblk, p.r.max_blocks) ? table[blk] : -1;
+    return (unsigned)ph < (unsigned)p.c.num_blocks ? ph : -1;
+  };
+  int tl = entries(step0), tl_next = entries(step0 + 16);
+  constexpr int BB = D * sizeof(CT);                              // 16-byte pieces of a block's K, and of its V
+  constexpr int UB = 4 / LW;                                      // blocks that a load of the workgroup covers
+  const int wblk = __builtin_amdgcn_readfirstlane(tid / BB % UB), piece = tid % BB;
+  u32x4 rk[LW], rv[LW];
+  uint8_t rks[Q8 ? LW : 1], rvs[Q8 ? LW : 1];                     // exponent bytes: nothing waits for the loads here
+  unsigned exists = 0;                                            // of the loaded step's 4 blocks, a bit each
+  auto load = [&](int step) {
+    const int at = 4 * ((step - step0) & 15);
+    if (at == 0 && step != step0) {
+      tl = tl_next;
+      tl_next = entries(step + 16);
     }
-    if (lo >= p.r.batch) return;
-    const SeqRows sr = seq_rows(p.r, lo);
-    if (t < sr.r0 || t >= sr.r0 + sr.n) return;
+    exists = (unsigned)(__ballot(tl >= 0) >> at) & 15u;
+#pragma unroll
+    for (int u = 0; u < LW; ++u) {
+      const int ph = max(__builtin_amdgcn_readlane(tl, at + UB * u + wblk), 0);
+      const size_t blk = (size_t)ph * n_kv + kvh;
+      unsigned off = piece;
+      asm volatile("" : "+v"(off));                               // uniform base + 32-bit offset, not a 64-bit address kept per pool
+      rk[u] = (reinterpret_cast<const u32x4*>(p.c.k) + blk * BB)[off];
+      rv[u] = (reinterpret_cast<const u32x4*>(p.c.v) + blk * BB)[off];
+      if constexpr (Q8) {
+        rks[u] = (p.c.k_exp + blk * PAGE)[off / KPT];
+        rvs[u] = (p.c.v_exp + blk * PAGE)[off % PAGE];
+      }
+    }
+  };
+  auto keep_of = [&](int step) -> unsigned long long {            // tokens inside the sequence, in blocks that exist
+    const int left = total - step * STEP;
+    if (left >= STEP && exists == 15u) return ~0ull;
+    unsigned long long m = left >= 64 ? ~0ull : (1ull << left) - 1;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (!((exists >> j) & 1)) m &= ~(0xFFFFull << (16 * j));
+    return m;
+  };
+  auto kat = [&](int r, int c) { return r * (2 * D) + ((D == 128 ? c ^ (r & 15) : c ^ ((r >> 1) & 7)) << 4); };
+  auto vat = [&](int d, int c) { return d * (2 * STEP) + ((c ^ ((d >> 1) & 7)) << 4); };
+  auto masked_step = [&](int step, unsigned long long keep) { return (step + 1) * STEP > sr.ctx || keep != ~0ull; };
+  // Slots that hold no token are cleared, and drafted values that are not finite, which concern the rows
+  // that see them only, are added when the rows are written.
+  auto clean = [&](int step, unsigned long long keep) {
+#pragma unroll
+    for (int u = 0; u < LW; ++u) {
+      constexpr int N = 16 / sizeof(CT);
+      const int j = UB * u + wblk, t0 = PAGE * j + piece % VPT * N;
+      const int first = sr.ctx - (step * STEP + t0);              // its first drafted token
+      u32x4 v = v_keep<CT>(rv[u], (uint32_t)(keep >> t0));
+      const uint32_t odd = v_odd<CT>(v) & (first >= N ? 0u : ~0u << max(first, 0));
+      if (odd) {
+        v = v_keep<CT>(v, ~odd);
+        sm_odd = 1;
+      }
+      rv[u] = v;
+      if constexpr (Q8)
+        if (!((keep >> (PAGE * j + piece % PAGE)) & 1)) rvs[u] = 0;     // its scale may be anything: 0
+    }
+  };
+  // where the thread's first load goes; its u-th lies UB blocks on: 16 UB rows of K (the same x), 2 UB pieces of V
+  const int kw = kat(PAGE * wblk + piece / KPT, (Q8 ? 2 : 1) * (piece % KPT));
+  const int vw = 2 * KBUF + vat(piece / VPT, 2 * wblk + piece % VPT);
+  auto store = [&](int buf) {
+#pragma unroll
+    for (int u = 0; u < LW; ++u) {
+      const int ka = kw + buf * KBUF + u * UB * PAGE * 2 * D, va = (vw + buf * VBUF) ^ (u * UB << 5);
+      if constexpr (Q8) {
+        const u32x4 a = rk[u], v = rv[u];
+        const float s = exp_scale(rks[u]);
+        *reinterpret_cast<u32x4*>(smem + ka) = u32x4{e4m3_pair<false>(a.x, s), e4m3_pair<true>(a.x, s), e4m3_pair<false>(a.y, s), e4m3_pair<true>(a.y, s)};
+        *reinterpret_cast<u32x4*>(smem + (ka ^ 16)) = u32x4{e4m3_pair<false>(a.z, s), e4m3_pair<true>(a.z, s), e4m3_pair<false>(a.w, s), e4m3_pair<true>(a.w, s)};
+        *reinterpret_cast<u32x4*>(smem + va) = u32x4{e4m3_pair<false>(v.x, 1.f), e4m3_pair<true>(v.x, 1.f), e4m3_pair<false>(v.y, 1.f), e4m3_pair<true>(v.y, 1.f)};
+        *reinterpret_cast<u32x4*>(smem + (va ^ 16)) = u32x4{e4m3_pair<false>(v.z, 1.f), e4m3_pair<true>(v.z, 1.f), e4m3_pair<false>(v.w, 1.f), e4m3_pair<true>(v.w, 1.f)};
+        sm_vs[buf][piece < PAGE ? PAGE * (UB * u + wblk) + piece : STEP + lane] = exp_scale(rvs[u]);     // the others write nowhere
+      } else {
+        *reinterpret_cast<u32x4*>(smem + ka) = rk[u];
+        *reinterpret_cast<u32x4*>(smem + va) = rv[u];
+      }
+    }
+  };
+
+  if (step0 < step1) load(step0);
+  const bf16_t* qrow = reinterpret_cast<const bf16_t*>(p.q) + (sr.r0 + t) * p.q_row + head * D;
+  Frag8 qf[NS];
+#pragma unroll
+  for (int s = 0; s < NS; ++s) {
+    qf[s] = *reinterpret_cast<const Frag8*>(qrow + 16 * s + 8 * half);
+    if (p.scale < 0.f) {                                          // |scale| is folded into the exponent below
+#pragma unroll
+      for (int e = 0; e < 4; ++e) qf[s].w[e] ^= 0x80008000u;
+    }
   }
-  const float* part = p.partial + rh * nsplit * (D + 4);
+  f32x16 o[ND];
+#pragma unroll
+  for (int i = 0; i < ND; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;                           // l_run: of this lane half's tokens
+  const float scale = fmaxf(fabsf(p.scale) * 1.4426950408889634f, 1e-37f);   // not 0: -infinity stays what it is
+  __syncthreads();                                                // sm_odd is cleared
+  unsigned long long keep = 0;
+  if (step0 < step1) {
+    keep = keep_of(step0);
+    if (masked_step(step0, keep)) clean(step0, keep);
+    store(0);
+  }
+  __syncthreads();
+
+  // MFMA row m of S is token tau of its 32
+  const int tau = 16 * (col >> 4) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3);
+  // A step is two halves of 32 tokens, so that matrix and vector instructions of one wave run side by
+  // side: S of the second half beside the exponentials of the first, V^T P^T of the first beside those
+  // of the second, V^T P^T of the second beside the conversion of the next step.  The LDS reads of a
+  // product run 8 ahead of its MFMAs, 4 at a time.  The scheduler, left alone, does neither.
+  const int kr = kat(tau, half), vr = 2 * KBUF + vat(col, half);
+  auto k_read = [&](int buf, int x) {                             // x: 32-token half of the step and k-step
+    return *reinterpret_cast<const Frag8*>(smem + ((kr + buf * KBUF) ^ (x % NS << 5)) + x / NS * 32 * 2 * D);
+  };
+  auto v_read = [&](int buf, int x) {                             // x: 16 tokens and 32 dimensions
+    return *reinterpret_cast<const Frag8*>(smem + ((vr + buf * VBUF) ^ (x / ND << 5)) + x % ND * 32 * 2 * STEP);
+  };
+  constexpr int NK = 2 * NS, NF = NK + 4 * ND;                    // operands of a step: K's, then V's (NS == 2 ND)
+  Frag8 f[8];
+  auto read = [&](int buf, int x) {
+    if (x < NF) f[x & 7] = x < NK ? k_read(buf, x) : v_read(buf, x - NK);
+  };
+  // scores of one half: seen or not, and whether the running maximum has to move
+  auto hide = [&](f32x16& sc, uint32_t seen) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sc[r] = seen & (1u << (16 * (r >> 3) + (r & 7))) ? sc[r] : -INFINITY;
+  };
+  auto top_of = [&](const f32x16& sc) {
+    float m = sc[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) m = fmaxf(m, sc[r]);
+    return fmaxf(m, __shfl_xor(m, 32, 64)) * scale;
+  };
+  // p of elements e0 .. e0 + n - 1 of a half, packed as the second product's operand once 8 are there
+  float px[8], rs = 0.f;
+  auto expo = [&](const f32x16& sc, int buf, int h0, int e0, int n, float m, Frag8 (&pf)[2]) {
+#pragma unroll
+    for (int e = e0; e < e0 + n; ++e) {
+      px[e & 7] = __builtin_amdgcn_exp2f(fmaf(sc[e], scale, -m));
+      rs += px[e & 7];
+      if ((e & 7) != 7) continue;
+      const int h = e >> 3;                                       // 16 tokens
+      if constexpr (Q8) {
+        const float4 a = *reinterpret_cast<const float4*>(&sm_vs[buf][16 * (h0 + h) + 8 * half]);
+        const float4 c = *reinterpret_cast<const float4*>(&sm_vs[buf][16 * (h0 + h) + 8 * half + 4]);
+        px[0] *= a.x, px[1] *= a.y, px[2] *= a.z, px[3] *= a.w, px[4] *= c.x, px[5] *= c.y, px[6] *= c.z, px[7] *= c.w;
+      }
+#pragma unroll
+      for (int w = 0; w < 4; ++w) pf[h].w[w] = pack2(px[2 * w], px[2 * w + 1]);
+      // computed here, beside the MFMAs, and not where it is used
+      asm volatile("" : "+v"(pf[h].w[0]), "+v"(pf[h].w[1]), "+v"(pf[h].w[2]), "+v"(pf[h].w[3]));
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto base_of = [&]() { return m_run == -INFINITY ? 0.f : m_run; };   // nothing seen yet: every p is 0
+  for (int step = step0; step < step1; ++step) {
+    const int buf = (step - step0) & 1;
+    const bool more = step + 1 < step1;
+    const unsigned long long now = keep;
+    if (more) {
+      load(step + 1);
+      keep = keep_of(step + 1);
+    }
+    const bool next_masked = more && masked_step(step + 1, keep);
+    if (active) {
+      const bool masked = masked_step(step, now);
+      unsigned long long vis = ~0ull;
+      if (masked) {                                               // drafted tokens, the end, or a missing block
+        const int dr = step * STEP - sr.ctx;                      // the step's first token as a drafted one
+        vis = dr >= 64 ? 0ull : dr >= 0 ? sees >> dr : dr <= -64 ? ~0ull : (sees << -dr) | ((1ull << -dr) - 1);
+        vis = (vis & now) >> (8 * half);
+      }
+      f32x16 s0, s1;
+      Frag8 p0[2], p1[2];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s0[r] = s1[r] = 0.f;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) read(buf, x);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int x = 0; x < NS; ++x) {
+        s0 = mfma32(f[x & 7], qf[x], s0);
+        read(buf, x + 8);
+      }
+      if (masked) hide(s0, (uint32_t)vis);
+      // the sums move to a new maximum only when it exceeds theirs by 2^8: until then p is at most
+      // 2^8, which rounds no worse, and the accumulators are left alone at most steps
+      float top = fmaxf(m_run, top_of(s0));
+      if (__any(top > m_run + 8.f)) {
+        const float corr = __builtin_amdgcn_exp2f(m_run - (top == -INFINITY ? 0.f : top));
+        m_run = top;
+        l_run *= corr;
+#pragma unroll
+        for (int i = 0; i < ND; ++i) o[i] *= corr;
+      }
+      const float base0 = base_of();
+      rs = 0.f;
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int x = NS; x < NK; ++x) {
+        s1 = mfma32(f[x & 7], qf[x - NS], s1);
+        read(buf, x + 8);
+        expo(s0, buf, 0, (x - NS) * (16 / NS), 16 / NS, base0, p0);
+      }
+      l_run += rs;
+      if (masked) hide(s1, (uint32_t)(vis >> 32));
+      top = fmaxf(m_run, top_of(s1));
+      const bool move = __any(top > m_run + 8.f);
+      float corr = 1.f;
+      if (move) {                                                 // applied once the first half is added
+        corr = __builtin_amdgcn_exp2f(m_run - (top == -INFINITY ? 0.f : top));
+        m_run = top;
+        l_run *= corr;
+      }
+      const float base1 = base_of();
+      rs = 0.f;
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int x = 0; x < 2 * ND; ++x) {
+        o[x % ND] = mfma32(f[(NK + x) & 7], p0[x / ND], o[x % ND]);
+        read(buf, NK + x + 8);
+        expo(s1, buf, 2, x * (8 / ND), 8 / ND, base1, p1);
+      }
+      l_run += rs;
+      if (move) {
+#pragma unroll
+        for (int i = 0; i < ND; ++i) o[i] *= corr;
+      }
+      if (next_masked) clean(step + 1, keep);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int x = 2 * ND; x < 4 * ND; ++x) o[x % ND] = mfma32(f[(NK + x) & 7], p1[x / ND - 2], o[x % ND]);
+      store(buf ^ 1);                                             // after the last step: stale, and never read
+      __builtin_amdgcn_sched_barrier(0);
+    } else {
+      if (next_masked) clean(step + 1, keep);
+      store(buf ^ 1);
+    }
+    __syncthreads();
+  }
+  if (!active || row >= nrow) return;
+  float l = l_run;
+  l += __shfl_xor(l, 32, 64);
+  if (sm_odd) {
+    const int j0 = max(0, step0 * STEP - sr.ctx), j1 = min(sr.n, step1 * STEP - sr.ctx);
+#pragma unroll 1
+    for (int j = j0; j < j1; ++j) {
+      const int tok = sr.ctx + j, ph = page_of(p.r, p.c.num_blocks, b, tok / PAGE);
+      if (!((sees >> j) & 1) || ph < 0) continue;
+      const CT* vb = reinterpret_cast<const CT*>(p.c.v) + ((size_t)ph * n_kv + kvh) * D * PAGE + tok % PAGE;
+#pragma unroll
+      for (int i = 0; i < ND; ++i) {
+        __builtin_amdgcn_sched_barrier(0);                        // few loads at a time: rare, and it must not cost registers
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float v = odd_value<CT>(vb[(size_t)(32 * i + 8 * (r >> 2) + 4 * half + (r & 3)) * PAGE]);
+          if (!(fabsf(v) < INFINITY)) o[i][r] += v;
+        }
+      }
+    }
+  }
+  const int nsplit = gridDim.x;
+  const long rh = (sr.r0 + t) * (long)p.n_q + head;
+  if (nsplit == 1) {
+    bf16_t* out = reinterpret_cast<bf16_t*>(p.out) + (sr.r0 + t) * p.out_row + head * D + 4 * half;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int i = 0; i < ND; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        *reinterpret_cast<uint2*>(out + 32 * i + 2 * r) = make_uint2(pack2(o[i][r] * inv, o[i][r + 1] * inv), pack2(o[i][r + 2] * inv, o[i][r + 3] * inv));
+  } else {
+    float* part = p.partial + (rh * nsplit + split) * (D + 4);
+    if (half == 0) *reinterpret_cast<float2*>(part) = make_float2(m_run, l);
+#pragma unroll
+    for (int i = 0; i < ND; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        *reinterpret_cast<float4*>(part + 4 + 32 * i + 2 * r + 4 * half) = make_float4(o[i][r], o[i][r + 1], o[i][r + 2], o[i][r + 3]);
+  }
+}
+
+// Joins the splits of a row and head: a wave each, D / 64 dimensions per lane.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) tree_combine_kernel(TreeArgs p, int nsplit) {
+  const int lane = threadIdx.x & 63;
+  const SeqRows sr = seq_rows(p.r, blockIdx.y);
+  const int i = blockIdx.x * 4 + (threadIdx.x >> 6);     // row of the sequence and head
+  if (i >= sr.n * p.n_q) return;
+  const long t = sr.r0 + i / p.n_q;
+  const int head = i % p.n_q;
+  const float* part = p.partial + (t * p.n_q + head) * nsplit * (D + 4);
   const float m = lane < nsplit ? part[lane * (D + 4)] : -INFINITY;
   const float l = lane < nsplit ? part[lane * (D + 4) + 1] : 0.f;
   const float M = wave_max(m);
   const float f = M == -INFINITY ? 0.f : exp2f(m - M);
   const float L = wave_sum(f * l);
   float o[D / 64] = {};
+#pragma unroll 4
   for (int s = 0; s < nsplit; ++s) {
     const float w = __shfl(f, s, 64);
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) o[i] += w * part[s * (D + 4) + 4 + lane + 64 * i];
+    for (int d = 0; d < D / 64; ++d) o[d] += w * part[s * (D + 4) + 4 + lane + 64 * d];
   }
 #pragma unroll
-  for (int i = 0; i < D / 64; ++i)
-    reinterpret_cast<T*>(p.out)[t * p.out_row + head * D + lane + 64 * i] = from_f<T>(L == 0.f ? 0.f : o[i] / L);
+  for (int d = 0; d < D / 64; ++d)
+    reinterpret_cast<T*>(p.out)[t * p.out_row + head * D + lane + 64 * d] = from_f<T>(L == 0.f ? 0.f : o[d] / L);
 }
 
-// Row tiles (of 16) that a workgroup takes, and the splits of the context.
-struct TreePlan { int nq, tiles, nsplit, per; };
+// The kernel, the workgroups that a KV head's rows take, and the splits of the context.
+struct TreePlan { bool wide; int tiles, nsplit, per; };
 static TreePlan tree_plan(int type, int n_kv, int n_q, int batch, int max_rows, int max_ctx, int cus) {
   TreePlan t;
   const int rows = max_rows * (n_q / n_kv);
-  t.nq = type == CACHE_F32 ? 1 : rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-  t.tiles = (rows + 16 * t.nq - 1) / (16 * t.nq);
-  const int step = type == CACHE_E4M3 ? 64 : 32;
+  t.wide = type != CACHE_F32 && rows > 16;
+  t.tiles = (rows + (t.wide ? 127 : 15)) / (t.wide ? 128 : 16);
+  const int step = t.wide || type == CACHE_E4M3 ? 64 : 32;
   const int steps = (max_ctx + step - 1) / step;
   const int base = batch * n_kv * t.tiles;
   const int want = std::max(1, (2 * cus + base - 1) / base);
@@ -450,36 +780,32 @@ size_t tree_partial_floats(int type, int n_kv, int n_q, int D, int batch, int ro
   return t.nsplit > 1 ? (size_t)rows * n_q * t.nsplit * (D + 4) : 0;
 }
 
-template <typename CT, int D, int NQ>
+template <typename CT, int D>
 static hipError_t tree_launch(const TreeArgs& p, const TreePlan& t, hipStream_t s) {
   typedef typename TreeT<CT>::act T;
-  hipLaunchKernelGGL((tree_attn_kernel<CT, D, NQ>), dim3(t.nsplit, p.c.n_kv * t.tiles, p.r.batch), dim3(256), 0, s, p, t.per);
+  const dim3 grid(t.nsplit, p.c.n_kv * t.tiles, p.r.batch);
+  if constexpr (sizeof(CT) < 4) {
+    if (t.wide) hipLaunchKernelGGL((tree_wide_kernel<CT, D>), grid, dim3(256), 0, s, p, t.per);
+    else hipLaunchKernelGGL((tree_attn_kernel<CT, D, 1>), grid, dim3(256), 0, s, p, t.per);
+  } else {
+    hipLaunchKernelGGL((tree_attn_kernel<CT, D, 1>), grid, dim3(256), 0, s, p, t.per);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || t.nsplit == 1) return e;
-  const long rh = (long)p.r.rows * p.n_q;
-  hipLaunchKernelGGL((tree_combine_kernel<T, D>), dim3((unsigned)((rh + 3) / 4)), dim3(256), 0, s, p, t.nsplit, rh);
+  hipLaunchKernelGGL((tree_combine_kernel<T, D>), dim3((p.r.max_rows * p.n_q + 3) / 4, p.r.batch), dim3(256), 0, s, p, t.nsplit);
   return hipGetLastError();
-}
-template <typename CT, int D>
-static hipError_t tree_tiles(const TreeArgs& p, const TreePlan& t, hipStream_t s) {
-  if (t.nq == 1) return tree_launch<CT, D, 1>(p, t, s);
-  if constexpr (sizeof(CT) < 4) {
-    if (t.nq == 2) return tree_launch<CT, D, 2>(p, t, s);
-    return tree_launch<CT, D, 4>(p, t, s);
-  }
-  return hipErrorInvalidValue;
 }
 
 hipError_t tree_attention(const TreeArgs& p, int cus, hipStream_t s) {
   if (p.r.rows <= 0) return hipSuccess;
   const TreePlan t = tree_plan(p.c.type, p.c.n_kv, p.n_q, p.r.batch, p.r.max_rows, p.r.max_ctx, cus);
   if (t.nsplit > 1 && !p.partial) return hipErrorInvalidValue;
-  const bool wide = p.c.D == 128;
-  if (!wide && p.c.D != 64) return hipErrorInvalidValue;
+  const bool d128 = p.c.D == 128;
+  if (!d128 && p.c.D != 64) return hipErrorInvalidValue;
   switch (p.c.type) {
-    case CACHE_BF16: return wide ? tree_tiles<bf16_t, 128>(p, t, s) : tree_tiles<bf16_t, 64>(p, t, s);
-    case CACHE_F32: return wide ? tree_tiles<float, 128>(p, t, s) : tree_tiles<float, 64>(p, t, s);
-    case CACHE_E4M3: return wide ? tree_tiles<e4m3_t, 128>(p, t, s) : tree_tiles<e4m3_t, 64>(p, t, s);
+    case CACHE_BF16: return d128 ? tree_launch<bf16_t, 128>(p, t, s) : tree_launch<bf16_t, 64>(p, t, s);
+    case CACHE_F32: return d128 ? tree_launch<float, 128>(p, t, s) : tree_launch<float, 64>(p, t, s);
+    case CACHE_E4M3: return d128 ? tree_launch<e4m3_t, 128>(p, t, s) : tree_launch<e4m3_t, 64>(p, t, s);
   }
   return hipErrorInvalidValue;
 }

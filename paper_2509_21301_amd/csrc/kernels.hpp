@@ -250,10 +250,10 @@ struct LogprobArgs {
   const int* given; int n_given; float* given_lp;      // [rows][n_given]
   float* entropy;                                       // [rows] or null
   int n_top; float* top_lp; int* top_ids;               // [rows][n_top]
-  float* part_sum; unsigned long long* part_top;        // logprobs_part_sizes()
+  float* part_sum; float* part_max;                     // logprobs_part_sizes()
 };
 bool logprobs_fits(int vocab, int n_top);
-void logprobs_part_sizes(int rows, int vocab, int n_top, size_t* sum_floats, size_t* top_keys);
+void logprobs_part_sizes(int rows, int vocab, int n_top, size_t* sum_floats, size_t* max_floats);
 hipError_t logprobs(const LogprobArgs& p, hipStream_t s);
 
 }  // namespace nova

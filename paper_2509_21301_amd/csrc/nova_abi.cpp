@@ -862,10 +862,10 @@ extern "C" int nova_tree_attention(const nova_cache* cache, const nova_rows* row
 // ------------------------------------------------------------------ log probabilities
 namespace {
 size_t logprobs_bytes(int rows, int vocab, int n_top, size_t* sums) {
-  size_t f = 0, k = 0;
-  nova::logprobs_part_sizes(rows, vocab, n_top, &f, &k);
+  size_t f = 0, m = 0;
+  nova::logprobs_part_sizes(rows, vocab, n_top, &f, &m);
   *sums = align256(f * sizeof(float));
-  return *sums + align256(k * 8);
+  return *sums + align256(m * sizeof(float));
 }
 }  // namespace
 
@@ -886,14 +886,14 @@ extern "C" int nova_logprobs(const void* logits, int type, int64_t pitch, int ro
   if (n_given > 0 && (!given || !given_lp || !aligned4(given) || !aligned4(given_lp))) return fail(NOVA_EINVAL, "given and given_lp must be non-null and aligned");
   if (n_top > 0 && (!top_lp || !top_ids || !aligned4(top_lp) || !aligned4(top_ids))) return fail(NOVA_EINVAL, "top_lp and top_ids must be non-null and aligned");
   if (!aligned4(entropy)) return fail(NOVA_EINVAL, "entropy is misaligned");
-  if ((int64_t)rows * ((vocab + 2047) / 2048) > 0x7fffffffLL) return fail(NOVA_EUNSUPPORTED, "%d rows of %d logits are too many for one call", rows, vocab);
+  if ((int64_t)rows * ((vocab + 1023) / 1024 + 1) > 0x7fffffffLL) return fail(NOVA_EUNSUPPORTED, "%d rows of %d logits are too many for one call", rows, vocab);
   size_t sums;
   const size_t need = logprobs_bytes(rows, vocab, n_top, &sums);
   if (ws_bytes < need) return fail(NOVA_ENOSPACE, "workspace %zu < required %zu bytes", ws_bytes, need);
-  if (!ws || !aligned(ws)) return fail(NOVA_EINVAL, "null or misaligned workspace");
+  if (need > 0 && (!ws || !aligned(ws))) return fail(NOVA_EINVAL, "null or misaligned workspace");
   hipStream_t s = (hipStream_t)stream;
   const nova::LogprobArgs a{logits, type == NOVA_ACT_F32, pitch, rows, vocab, given, n_given, given_lp, entropy, n_top, top_lp, top_ids,
-                            (float*)ws, (unsigned long long*)((char*)ws + sums)};
+                            (float*)ws, (float*)((char*)ws + sums)};
   CALL(NOVA_KIND_MISC, s, nova::logprobs(a, s));
   return NOVA_OK;
 }

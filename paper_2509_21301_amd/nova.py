@@ -158,8 +158,8 @@ def _ptr(t) -> int | None:
 
 
 def _stream(stream) -> int | None:
-    if stream is None:
-        stream = torch.cuda.current_stream()
+    if stream is None:      # the handle itself: building a Stream object costs as much as a kernel launch
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream.cuda_stream
 
 
@@ -478,32 +478,27 @@ def _check_rows_of(what, t, rows, heads, d):
     act = _ACT.get(t.dtype)
     if act is None:
         raise ValueError(f"{what} must be bfloat16 or float32, got {t.dtype}")
-    if t.dim() != 3 or t.shape != (rows, heads, d) or t.stride(2) != 1 or (heads > 1 and t.stride(1) != d):
-        raise ValueError(f"{what} must be rows {(rows, heads, d)} with contiguous heads, got {tuple(t.shape)} strides {t.stride()}")
-    return act, t.stride(0) if rows > 1 else heads * d
+    st = t.stride()
+    if t.shape != (rows, heads, d) or st[2] != 1 or (st[1] != d and heads > 1):
+        raise ValueError(f"{what} must be rows {(rows, heads, d)} with contiguous heads, got {tuple(t.shape)} strides {st}")
+    return act, st[0] if rows > 1 else heads * d
 
 
-def _check_device(ref, *tensors):
-    """Every tensor lives on ``ref``'s device, which is the current one (the library launches there)."""
-    dev = ref.device
+def _check_device(dev, *tensors):
+    """Every tensor lives on the device of index ``dev``, the current one (the library launches there)."""
     for t in tensors:
-        if t is not None and t.device != dev:
-            raise ValueError(f"tensors on {t.device} and {dev}")
-    if not ref.is_cuda or dev.index != torch.cuda.current_device():
-        raise ValueError(f"tensors on {dev}, which is not the current device")
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"tensors on {t.device} and on device {dev}")
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise ValueError(f"tensors on device {dev}, which is not the current one")
 
 
-class _On:
-    """Allocate on the stream that a call runs on, so that memory freed after the call is reused behind it."""
-
-    def __init__(self, stream):
-        self.stream = stream
-
-    def empty(self, shape, dtype, device):
-        if self.stream is None:
-            return torch.empty(shape, dtype=dtype, device=device)
-        with torch.cuda.stream(self.stream):
-            return torch.empty(shape, dtype=dtype, device=device)
+def _empty(like, shape, dtype, stream):
+    """Memory on the stream that a call runs on, so that what is freed after the call is reused behind it."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(stream):
+        return like.new_empty(shape, dtype=dtype)
 
 
 class Cache:
@@ -546,6 +541,7 @@ class Cache:
             k_exp = v_exp = None
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
         self.num_blocks, self.n_kv, self.head_dim, self.layers = nb, n_kv, d, layers
+        self.device = k.get_device()
         self.dtype = torch.float32 if self.type == CACHE_F32 else torch.bfloat16      # of q and the attention's output
         e = [(None, None) if k_exp is None else (_ptr(k_exp[i]), _ptr(v_exp[i])) for i in range(layers)]
         self._c = [CacheC(_ptr(k[i]), _ptr(v[i]), *e[i], nb, n_kv, d, self.type) for i in range(layers)]
@@ -608,7 +604,7 @@ def kv_append(cache, rows, k, v, q=None, pos=None, rope=None, q_out=None, layer=
     behind their sequences' contexts in ``cache``, in its type.  k, v [rows, n_kv, head_dim], q [rows, n_q, head_dim],
     bf16 or fp32, may be views of one packed projection.  Returns the rotated q (``q_out``, which may be q itself)."""
     n, d = rows.rows, cache.head_dim
-    _check_device(cache.k, rows.tables, k, v, q, pos, q_out)
+    _check_device(cache.device, rows.tables, k, v, q, pos, q_out)
     act, k_pitch = _check_rows_of("k", k, n, cache.n_kv, d)
     act_v, v_pitch = _check_rows_of("v", v, n, cache.n_kv, d)
     _check_vector("pos", pos, torch.int32, n)
@@ -618,7 +614,7 @@ def kv_append(cache, rows, k, v, q=None, pos=None, rope=None, q_out=None, layer=
         n_q = q.shape[1] if q.dim() == 3 else 0
         act_q, q_pitch = _check_rows_of("q", q, n, n_q, d)
         if q_out is None:
-            q_out = _On(stream).empty((n, n_q, d), q.dtype, q.device)
+            q_out = _empty(q, (n, n_q, d), q.dtype, stream)
         act_out, out_pitch = _check_rows_of("q_out", q_out, n, n_q, d)
     elif q_out is not None:
         raise ValueError("q_out without q")
@@ -634,12 +630,11 @@ def kv_gather(cache, rows, slots=None, k_out=None, v_out=None, dtype=torch.bfloa
     (int32 [rows], token numbers in the row's sequence).  Rows behind the last sequence are left as they were."""
     n, d = rows.rows, cache.head_dim
     _check_vector("slots", slots, torch.int32, n)
-    on = _On(stream)
     if k_out is None:
-        k_out = on.empty((n, cache.n_kv, d), dtype, cache.k.device)
+        k_out = _empty(cache.k, (n, cache.n_kv, d), dtype, stream)
     if v_out is None:
-        v_out = on.empty((n, cache.n_kv, d), dtype, cache.k.device)
-    _check_device(cache.k, rows.tables, slots, k_out, v_out)
+        v_out = _empty(cache.k, (n, cache.n_kv, d), dtype, stream)
+    _check_device(cache.device, rows.tables, slots, k_out, v_out)
     act, k_pitch = _check_rows_of("k_out", k_out, n, cache.n_kv, d)
     act_v, v_pitch = _check_rows_of("v_out", v_out, n, cache.n_kv, d)
     if act != act_v:
@@ -654,18 +649,17 @@ def tree_attention(cache, rows, q, mask=None, out=None, scale=None, layer=0, str
     context and the drafted tokens i whose bit i is set in ``mask`` (int64 [rows]; None: those up to its own).
     q [rows, n_q, head_dim] in ``cache.dtype``; returns ``out`` of the same shape and type."""
     n, d = rows.rows, cache.head_dim
-    _check_device(cache.k, rows.tables, q, mask, out)
+    _check_device(cache.device, rows.tables, q, mask, out)
     _check_vector("mask", mask, torch.int64, n)
     n_q = q.shape[1] if q.dim() == 3 else 0
     act, q_pitch = _check_rows_of("q", q, n, n_q, d)
-    on = _On(stream)
     if out is None:
-        out = on.empty((n, n_q, d), q.dtype, q.device)
+        out = _empty(q, (n, n_q, d), q.dtype, stream)
     act_out, out_pitch = _check_rows_of("out", out, n, n_q, d)
     if q.dtype != cache.dtype or act_out != act:
         raise ValueError(f"q and out must be {cache.dtype}")
     nbytes = rows._tree_bytes(cache, n_q)
-    ws = on.empty(nbytes, torch.uint8, q.device) if nbytes else None
+    ws = _empty(q, nbytes, torch.uint8, stream) if nbytes else None
     _check(lib.nova_tree_attention(cache.layer(layer), rows.ref, _ptr(mask), q.data_ptr(), q_pitch, n_q,
                                    d ** -0.5 if scale is None else scale, out.data_ptr(), out_pitch, _ptr(ws), nbytes, _stream(stream)))
     return out
@@ -685,17 +679,22 @@ def logprobs(logits, given=None, n_top=0, stream=None):
         if given.dtype != torch.int32 or given.dim() != 2 or given.shape[0] != rows or not given.is_contiguous():
             raise ValueError(f"given must be contiguous int32 [{rows}, n], got {given.dtype} {tuple(given.shape)}")
         n_given = given.shape[1]
-    _check_device(logits, given)
-    on, dev = _On(stream), logits.device
+    _check_device(logits.get_device(), given)
     n_top = min(n_top, vocab)
-    lp = on.empty((rows, n_given), torch.float32, dev) if given is not None else None
-    entropy = on.empty((rows,), torch.float32, dev)
-    top_lp = on.empty((rows, n_top), torch.float32, dev) if n_top else None
-    top_ids = on.empty((rows, n_top), torch.int32, dev) if n_top else None
+    # one allocation for what is returned, cut into dense matrices
+    buf = _empty(logits, (rows * (n_given + 1 + 2 * n_top),), torch.float32, stream)
+    at = rows * n_given
+    lp = buf.as_strided((rows, n_given), (n_given, 1), 0) if given is not None else None
+    entropy = buf.as_strided((rows,), (1,), at)
+    at += rows
+    top_lp = top_ids = None
+    if n_top:
+        top_lp = buf.as_strided((rows, n_top), (n_top, 1), at)
+        top_ids = buf.as_strided((rows, n_top), (n_top, 1), at + rows * n_top).view(torch.int32)
     nbytes = lib.nova_logprobs_workspace_bytes(rows, vocab, n_top)
-    ws = on.empty(max(nbytes, 256), torch.uint8, dev)
+    ws = _empty(logits, nbytes, torch.uint8, stream) if nbytes else None
     _check(lib.nova_logprobs(logits.data_ptr(), act, logits.stride(0) if rows > 1 else vocab, rows, vocab, _ptr(given), n_given, _ptr(lp),
-                             entropy.data_ptr(), n_top, _ptr(top_lp), _ptr(top_ids), ws.data_ptr(), ws.numel(), _stream(stream)))
+                             entropy.data_ptr(), n_top, _ptr(top_lp), _ptr(top_ids), _ptr(ws), nbytes, _stream(stream)))
     return lp, entropy, top_lp, top_ids
 
 

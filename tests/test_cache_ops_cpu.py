@@ -97,17 +97,18 @@ def test_tree_refusals_and_workspace():
 
 
 def test_logprobs_refusals_and_workspace():
-    def call(x=FAKE, t=1, pitch=1000, rows=2, vocab=1000, given=FAKE, n=1, lp=FAKE, ent=FAKE, top=4, tl=FAKE, ti=FAKE, ws=FAKE, nb=1 << 30):
+    def call(x=FAKE, t=1, pitch=20000, rows=2, vocab=20000, given=FAKE, n=1, lp=FAKE, ent=FAKE, top=4, tl=FAKE, ti=FAKE, ws=FAKE, nb=1 << 30):
         return LIB.nova_logprobs(x, t, pitch, rows, vocab, given, n, lp, ent, top, tl, ti, ws, nb, None)
     assert call(rows=0) == nova.OK
-    for bad in [dict(t=4), dict(x=None), dict(x=FAKE + 2), dict(pitch=999), dict(vocab=0), dict(rows=-1), dict(n=-1), dict(given=None), dict(lp=None),
+    for bad in [dict(t=4), dict(x=None), dict(x=FAKE + 2), dict(pitch=19999), dict(vocab=0), dict(rows=-1), dict(n=-1), dict(given=None), dict(lp=None),
                 dict(top=-1), dict(top=5, vocab=4, pitch=4), dict(tl=None), dict(ti=None), dict(ent=FAKE + 1), dict(ws=None), dict(ws=FAKE + 8)]:
         assert call(**bad) == nova.EINVAL, bad
     assert call(top=33) == nova.EUNSUPPORTED
     assert call(vocab=(1 << 21) + 1, pitch=1 << 22) == nova.EUNSUPPORTED
-    need = LIB.nova_logprobs_workspace_bytes(2, 1000, 4)
+    need = LIB.nova_logprobs_workspace_bytes(2, 20000, 4)
     assert need > 0 and call(nb=need - 1) == nova.ENOSPACE
-    assert LIB.nova_logprobs_workspace_bytes(2, 1000, 33) == 0
+    assert LIB.nova_logprobs_workspace_bytes(2, 20000, 33) == 0
+    assert LIB.nova_logprobs_workspace_bytes(2, 4096, 4) == 0     # a short row is one workgroup
 
 
 def test_stage_refusals():
