@@ -49,6 +49,22 @@ template <typename T> NOVA_DEV void load8(const T* p, float* x) {
     }
   }
 }
+template <typename T> struct Raw8;
+template <> struct Raw8<bf16_t> { u32x4 a; };
+template <> struct Raw8<float> { f32x4 a, b; };
+NOVA_DEV Raw8<bf16_t> load_raw(const bf16_t* p) { return {*reinterpret_cast<const u32x4*>(p)}; }
+NOVA_DEV Raw8<float> load_raw(const float* p) { return {reinterpret_cast<const f32x4*>(p)[0], reinterpret_cast<const f32x4*>(p)[1]}; }
+NOVA_DEV void unpack8(const Raw8<bf16_t>& r, float* x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(r.a[i] << 16);
+    x[2 * i + 1] = __uint_as_float(r.a[i] & 0xFFFF0000u);
+  }
+}
+NOVA_DEV void unpack8(const Raw8<float>& r, float* x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = r.a[i], x[4 + i] = r.b[i];
+}
 template <typename T> NOVA_DEV void store8(T* p, const float* x) {
   if constexpr (sizeof(T) == 4) {
     *reinterpret_cast<float4*>(p) = *reinterpret_cast<const float4*>(x);
@@ -101,6 +117,22 @@ __global__ void __launch_bounds__(256) kv_append_kernel(AppendArgs p, int heads_
   const int n_kv = p.c.n_kv, heads = 2 * n_kv + (p.q ? p.n_q : 0);
   const int h0 = blockIdx.y * heads_per_wg, h1 = min(h0 + heads_per_wg, heads);
 
+  // The rows of a head, D / 8 lanes each, as loaded; rows that are not live read as zeros.
+  const int sub = lane % LPR, rr = lane / LPR;
+  Raw8<TI> raw[NI];
+  auto request = [&](int h) {
+    const bool is_k = h < n_kv, is_v = !is_k && h < 2 * n_kv;
+    const TI* src = reinterpret_cast<const TI*>(is_k ? p.k : is_v ? p.v : p.q);
+    const long row = is_k ? p.k_row : is_v ? p.v_row : p.q_row;
+    const int hh = is_k ? h : is_v ? h - n_kv : h - 2 * n_kv;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int slot = i * RPI + rr;
+      raw[i] = slot >= lo && slot < hi ? load_raw(src + (sr.r0 + t0 + slot) * row + hh * D + 8 * sub) : Raw8<TI>{};
+    }
+  };
+  if (h0 + wave < h1) request(h0 + wave);                // in flight while the angles are computed
+
   if (p.rot > 0 && !(h0 >= n_kv && h1 <= 2 * n_kv)) {    // heads in the order k, v, q: some head rotates
     const int half = p.rot >> 1;
     for (int i = threadIdx.x; i < PAGE * 64; i += 256) {
@@ -115,22 +147,13 @@ __global__ void __launch_bounds__(256) kv_append_kernel(AppendArgs p, int heads_
   }
   __syncthreads();
 
-  const int sub = lane % LPR, rr = lane / LPR;
   for (int h = h0 + wave; h < h1; h += 4) {
     const bool is_k = h < n_kv, is_v = !is_k && h < 2 * n_kv;
-    const TI* src = reinterpret_cast<const TI*>(is_k ? p.k : is_v ? p.v : p.q);
-    const long row = is_k ? p.k_row : is_v ? p.v_row : p.q_row;
     const int hh = is_k ? h : is_v ? h - n_kv : h - 2 * n_kv;
     float x[NI][8];
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int slot = i * RPI + rr;
-      if (slot >= lo && slot < hi) load8(src + (sr.r0 + t0 + slot) * row + hh * D + 8 * sub, x[i]);
-      else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
-      }
-    }
+    for (int i = 0; i < NI; ++i) unpack8(raw[i], x[i]);
+    if (h + 4 < h1) request(h + 4);                      // the next head's rows, during this one's work
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       const int slot = i * RPI + rr;
@@ -221,9 +244,11 @@ template <typename TI, typename TO, typename CT>
 static hipError_t append_launch(const AppendArgs& p, int cus, hipStream_t s) {
   const long tiles = std::min<long>(p.r.rows, p.r.rows / PAGE + 2L * p.r.batch);
   const int heads = 2 * p.c.n_kv + (p.q ? p.n_q : 0);
-  // 4 heads (one per wave) share the rows' sines and cosines; more where the blocks alone fill the GPU
-  int per = 4;
-  while (per < heads && tiles * ((heads + 2 * per - 1) / (2 * per)) >= 2L * cus) per *= 2;
+  // Heads are cut into groups that each compute the rows' sines and cosines: one head a wave while the blocks
+  // are few, fewer and larger groups once the workgroups are 2.5 for each compute unit (3579 tokens of
+  // 36 heads: 9 groups 18.7 us, 5 17.6, 3 16.1, 1 25.6; 32 single tokens: 6.9, 9.0, 10.4, 18.6).
+  const long most = (heads + 3) / 4, groups = std::min(most, std::max(1L, (5L * cus / 2 + tiles - 1) / tiles));
+  const int per = (int)(((heads + groups - 1) / groups + 3) / 4 * 4);
   const dim3 grid((unsigned)tiles, (heads + per - 1) / per);
   if (p.c.D == 64) hipLaunchKernelGGL((kv_append_kernel<TI, TO, CT, 64>), grid, dim3(256), 0, s, p, per);
   else hipLaunchKernelGGL((kv_append_kernel<TI, TO, CT, 128>), grid, dim3(256), 0, s, p, per);

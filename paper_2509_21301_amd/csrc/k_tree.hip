@@ -3,16 +3,14 @@
 // token below ctx and those drafted tokens whose bit is set in its mask:
 //   out = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale q.k_t - max).
 // One pass over the cache with a running maximum and sum (in fp32, base 2).
-//  * The rows (token, query head) that share a KV head are the MFMA columns, 16 to a tile, so K and V
-//    are read once for NQ tiles: S = K Q^T and O^T = V^T P^T.
-//  * A wave takes a step of 4 JN tokens per lane group (JN row blocks of S): which token is which MFMA
-//    row is free, so lane group g takes the step's tokens 4 JN g .. and finds its V of a dimension in
-//    one 16-byte load (e4m3: 16 tokens of a block, bf16: 8, f32: two loads of 4).
+//  * The rows (token, query head) that share a KV head are the MFMA columns, so K and V are read once
+//    for many: S = K Q^T and O^T = V^T P^T.
+//  * Which token is which MFMA row is free, so a lane (or lane group) is given consecutive tokens and
+//    finds its V of a dimension, [D][16 tokens] in the cache, in 16-byte loads.
 //  * e4m3 turns into bf16 exactly on the way to the MFMA: K with its token's scale, V without; V's
 //    scale goes onto p, a power of two.  p is rounded to bf16 once (the matrix cores take no other
 //    type beside bf16 V); the sum of p keeps fp32.  The f32 cache uses the fp32 matrix instructions.
-//  * grid (context splits, KV head x row tiles, sequence); the waves of a workgroup share a split and
-//    are merged through LDS, the splits by a second kernel.
+//  * grid (context splits, KV head x row tiles, sequence); a second kernel joins the splits.
 #include <algorithm>
 
 #include "paged.hpp"
@@ -33,7 +31,7 @@ template <typename CT, int D> struct TreeRaw {
   static constexpr int VW = 4 * JN * sizeof(CT) / 16;     // of a V row
   u32x4 k[JN][KW];
   u32x4 v[D / 16][VW];
-  float ks[JN];                                           // e4m3: scale of the lane's K rows
+  uint8_t ks[JN];                                         // e4m3: exponent bytes of the lane's K rows
   u32x4 ve;                                               // e4m3: exponent bytes of the lane group's 16 tokens
   bool ok;                                                // the lane group's own block (V) exists
 };
@@ -77,9 +75,15 @@ template <typename CT> NOVA_DEV u32x4 v_keep(u32x4 q, uint32_t keep) {
   return u32x4{w[0], w[1], w[2], w[3]};
 }
 
-template <typename CT, int D, int NQ>
+// Steps of a split: the plan's number of splits shares out the sequence's own steps, `least` at a time.
+NOVA_DEV int split_steps(int nsteps, int nsplit, int least) { return max(least, (nsteps + nsplit - 1) / nsplit); }
+
+// ------------------------------------------------------------------ few rows
+// One tile of 16 rows: bound by the cache's bytes.  The waves of a workgroup take steps in turn, each from
+// memory to its own registers (K of the next step is requested once S is formed, V once it is used).
+template <typename CT, int D>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
-tree_attn_kernel(TreeArgs p, int steps_per_split) {
+tree_attn_kernel(TreeArgs p, int least) {
   typedef typename TreeT<CT>::act T;
   typedef TreeRaw<CT, D> Raw;
   constexpr bool F32 = sizeof(CT) == 4, Q8 = sizeof(CT) == 1;
@@ -92,28 +96,18 @@ tree_attn_kernel(TreeArgs p, int steps_per_split) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n_kv = p.c.n_kv, G = p.n_q / n_kv;
-  const int split = blockIdx.x, kvh = blockIdx.y % n_kv, tile = blockIdx.y / n_kv, b = blockIdx.z;
+  const int split = blockIdx.x, kvh = blockIdx.y % n_kv, row0 = blockIdx.y / n_kv * 16, b = blockIdx.z;
   const int col = lane & 15, grp = lane >> 4;
   const SeqRows sr = seq_rows(p.r, b);
-  const int nrow = sr.n * G, row0 = tile * 16 * NQ;
+  const int nrow = sr.n * G;
   if (row0 >= nrow) return;
   const int total = sr.ctx + sr.n;
-  const int nsteps = (total + STEP - 1) / STEP, nblk = (total + PAGE - 1) / PAGE;
-  const int step0 = split * steps_per_split, step1 = min(step0 + steps_per_split, nsteps);
+  const int nsteps = (total + STEP - 1) / STEP, nblk = min((total + PAGE - 1) / PAGE, p.r.max_blocks);
+  const int per = split_steps(nsteps, gridDim.x, least);
+  const int step0 = split * per, step1 = min(step0 + per, nsteps);
   const int first = step0 + wave;
   const int n_it = first < step1 ? (step1 - first + 3) / 4 : 0;
   const int* table = p.r.tables + (size_t)b * p.r.max_blocks;
-
-  // this lane's row of each tile: its drafted token and what it sees of the drafted ones
-  const T* qrow[NQ];
-  unsigned long long sees[NQ];
-#pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    const int r = row0 + 16 * n + col, t = min(r, nrow - 1) / G;
-    const int head = kvh * G + min(r, nrow - 1) % G;
-    qrow[n] = reinterpret_cast<const T*>(p.q) + (sr.r0 + t) * p.q_row + head * D;
-    sees[n] = p.mask ? p.mask[sr.r0 + t] : (2ull << t) - 1;
-  }
 
   // block ids of 64 / BPS iterations at a time, one per lane
   int tl = -1, tl_chunk = -1;
@@ -122,14 +116,11 @@ tree_attn_kernel(TreeArgs p, int steps_per_split) {
     if (it / IPC != tl_chunk) {
       tl_chunk = it / IPC;
       const int blk = (first + 4 * (tl_chunk * IPC + lane / BPS)) * BPS + lane % BPS;
-      tl = blk < nblk && blk < p.r.max_blocks ? table[blk] : -1;
+      tl = blk < nblk ? table[blk] : -1;
       if ((unsigned)tl >= (unsigned)p.c.num_blocks) tl = -1;
     }
     return __shfl(tl, (it % IPC) * BPS + j, 64);
   };
-  if (tid == 0) sm_odd = 0;
-  __syncthreads();
-
   Raw raw;
   auto load_k = [&](int it) {
     // MFMA row col of block j is token TPG (col / 4) + 4 j + col % 4 of the step
@@ -141,7 +132,7 @@ tree_attn_kernel(TreeArgs p, int steps_per_split) {
       const u32x4* kr = reinterpret_cast<const u32x4*>(reinterpret_cast<const CT*>(p.c.k) + (tok + 4 * j) * D) + grp;
 #pragma unroll
       for (int w = 0; w < Raw::KW; ++w) raw.k[j][w] = kr[4 * w];
-      if constexpr (Q8) raw.ks[j] = exp_scale(p.c.k_exp[tok + 4 * j]);
+      if constexpr (Q8) raw.ks[j] = p.c.k_exp[tok + 4 * j];
     }
   };
   auto load_v = [&](int it) {
@@ -159,241 +150,185 @@ tree_attn_kernel(TreeArgs p, int steps_per_split) {
     load_k(0);
     load_v(0);
   }
+  if (tid == 0) sm_odd = 0;
+  __syncthreads();
 
+  // this lane's row: its drafted token, its q and what it sees of the drafted ones
+  const int rc = min(row0 + col, nrow - 1), mine_t = rc / G;
+  const T* qrow = reinterpret_cast<const T*>(p.q) + (sr.r0 + mine_t) * p.q_row + (kvh * G + rc % G) * D;
+  const unsigned long long sees = p.mask ? p.mask[sr.r0 + mine_t] : (2ull << mine_t) - 1;
   // Q^T fragments: the dimensions of each k-step in the order in which K's words hold them
-  Frag8 qf[NQ][F32 ? 1 : NS];
-  float4 qx[NQ][F32 ? D / 16 : 1];
+  Frag8 qf[F32 ? 1 : NS];
+  f32x4 qx[F32 ? D / 16 : 1];
+  if constexpr (F32) {
 #pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    if constexpr (F32) {
+    for (int w = 0; w < D / 16; ++w) qx[w] = *reinterpret_cast<const f32x4*>(qrow + 16 * w + 4 * grp) * (p.scale < 0.f ? -1.f : 1.f);
+  } else {
 #pragma unroll
-      for (int w = 0; w < D / 16; ++w) qx[n][w] = *reinterpret_cast<const float4*>(qrow[n] + 16 * w + 4 * grp);
-    } else {
+    for (int s = 0; s < NS; ++s) {
+      qf[s] = *reinterpret_cast<const Frag8*>(qrow + (Q8 ? 64 * (s >> 1) + 16 * grp + 8 * (s & 1) : 32 * s + 8 * grp));
+      if (p.scale < 0.f) {                                // |scale| is folded into the exponent below
 #pragma unroll
-      for (int s = 0; s < NS; ++s)
-        qf[n][s] = *reinterpret_cast<const Frag8*>(qrow[n] + (Q8 ? 64 * (s >> 1) + 16 * grp + 8 * (s & 1) : 32 * s + 8 * grp));
-    }
-  }
-
-  f32x4 o[NQ][ND];
-  float m_run[NQ], l_run[NQ];                             // l_run: of this lane group's tokens only
-#pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    m_run[n] = -INFINITY;
-    l_run[n] = 0.f;
-#pragma unroll
-    for (int i = 0; i < ND; ++i) o[n][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-  const float scale = p.scale * 1.4426950408889634f;
-
-  // V^T P^T of one dimension block added to its accumulators: `v` the lane's words, `pt` P^T
-  auto add_pv = [&](const u32x4 (&v)[Raw::VW], const auto& pt, f32x4 (&acc)[NQ]) {
-    if constexpr (F32) {
-      float f[TPG];
-      __builtin_memcpy(f, v, sizeof f);
-#pragma unroll
-      for (int e = 0; e < TPG; ++e)
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) acc[n] = mfma4(f[e], pt[n][e], acc[n]);
-    } else if constexpr (Q8) {
-      const u32x4 x = v[0];
-      const Frag8 a{{e4m3_pair<false>(x.x, 1.f), e4m3_pair<true>(x.x, 1.f), e4m3_pair<false>(x.y, 1.f), e4m3_pair<true>(x.y, 1.f)}};
-      const Frag8 c{{e4m3_pair<false>(x.z, 1.f), e4m3_pair<true>(x.z, 1.f), e4m3_pair<false>(x.w, 1.f), e4m3_pair<true>(x.w, 1.f)}};
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) {
-        acc[n] = mfma16(a, pt[n][0], acc[n]);
-        acc[n] = mfma16(c, pt[n][JN / 2 - 1], acc[n]);
+        for (int e = 0; e < 4; ++e) qf[s].w[e] ^= 0x80008000u;
       }
-    } else {
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) acc[n] = mfma16(__builtin_bit_cast(Frag8, v[0]), pt[n][0], acc[n]);
     }
-  };
+  }
 
-  // One step.  MASKED: it holds drafted tokens, the sequence's end or a missing block.
-  auto step = [&](int it, auto masked_) {
-    constexpr bool MASKED = decltype(masked_)::value;
-    const int mine = (first + 4 * it) * STEP + TPG * grp;        // the lane group's first token
-    const int valid = !MASKED ? TPG : raw.ok ? min(max(total - mine, 0), TPG) : 0;
+  f32x4 o[ND];
+#pragma unroll
+  for (int i = 0; i < ND; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m_run = -INFINITY, l_run = 0.f;                   // l_run: of this lane group's tokens only
+  const float scale = fmaxf(fabsf(p.scale) * 1.4426950408889634f, 1e-37f);   // not 0: -infinity stays what it is
+
+  for (int it = 0; it < n_it; ++it) {
+    const int mine = (first + 4 * it) * STEP + TPG * grp;         // the lane group's first token
+    const bool masked = (first + 4 * it) * STEP + STEP > sr.ctx || !__all(raw.ok);   // drafted tokens, the end, a missing block
+    const int valid = !masked ? TPG : raw.ok ? min(max(total - mine, 0), TPG) : 0;
     // S: lane holds scores of its lane group's tokens 4 j + q for row col
-    f32x4 sc[NQ][JN];
+    f32x4 sc[JN];
 #pragma unroll
     for (int j = 0; j < JN; ++j) {
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) sc[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      sc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < Raw::KW; ++w) {
         const u32x4 x = raw.k[j][w];
         if constexpr (F32) {
-          const float f[4] = {__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w)};
 #pragma unroll
-          for (int n = 0; n < NQ; ++n) {
-            sc[n][j] = mfma4(f[0], qx[n][w].x, sc[n][j]);
-            sc[n][j] = mfma4(f[1], qx[n][w].y, sc[n][j]);
-            sc[n][j] = mfma4(f[2], qx[n][w].z, sc[n][j]);
-            sc[n][j] = mfma4(f[3], qx[n][w].w, sc[n][j]);
-          }
+          for (int e = 0; e < 4; ++e) sc[j] = mfma4(__uint_as_float(x[e]), qx[w][e], sc[j]);
         } else if constexpr (Q8) {
-          const float s = raw.ks[j];
+          const float s = exp_scale(raw.ks[j]);
           const Frag8 a{{e4m3_pair<false>(x.x, s), e4m3_pair<true>(x.x, s), e4m3_pair<false>(x.y, s), e4m3_pair<true>(x.y, s)}};
           const Frag8 c{{e4m3_pair<false>(x.z, s), e4m3_pair<true>(x.z, s), e4m3_pair<false>(x.w, s), e4m3_pair<true>(x.w, s)}};
-#pragma unroll
-          for (int n = 0; n < NQ; ++n) {
-            sc[n][j] = mfma16(a, qf[n][2 * w], sc[n][j]);
-            sc[n][j] = mfma16(c, qf[n][2 * w + 1], sc[n][j]);
-          }
+          sc[j] = mfma16(a, qf[2 * w], sc[j]);
+          sc[j] = mfma16(c, qf[2 * w + 1], sc[j]);
         } else {
-          const Frag8 a = __builtin_bit_cast(Frag8, x);
-#pragma unroll
-          for (int n = 0; n < NQ; ++n) sc[n][j] = mfma16(a, qf[n][w], sc[n][j]);
+          sc[j] = mfma16(__builtin_bit_cast(Frag8, x), qf[w], sc[j]);
         }
       }
     }
     if (it + 1 < n_it) load_k(it + 1);
 
-    // what row n sees of the lane group's tokens, a bit each
-    uint32_t vis[NQ];
-    if constexpr (MASKED) {
+    if (masked) {
+      // what the lane's row sees of the lane group's tokens, a bit each
+      const int dr = mine - sr.ctx;                               // the first token as a drafted one
+      const unsigned long long m = dr >= 64 ? 0ull : dr >= 0 ? sees >> dr : dr <= -TPG ? ~0ull : (sees << -dr) | ((1ull << -dr) - 1);
+      const uint32_t held = (1u << valid) - 1u, vis = (uint32_t)m & held;
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) {
-        const int dr = mine - sr.ctx;                            // the first token as a drafted one
-        const unsigned long long m = dr >= 64 ? 0ull : dr >= 0 ? sees[n] >> dr : dr <= -TPG ? ~0ull : (sees[n] << -dr) | ((1ull << -dr) - 1);
-        vis[n] = (uint32_t)m & ((1u << valid) - 1u);
-      }
-      // slots past the last token may hold anything: their V is cleared
+      for (int e = 0; e < TPG; ++e) sc[e >> 2][e & 3] = (vis >> e) & 1 ? sc[e >> 2][e & 3] : -INFINITY;
+      // Slots past the last token may hold anything: their V is cleared.  A drafted token's V that is not
+      // finite concerns the rows that see it and no other, and 0 times infinity is not 0: such elements
+      // are cleared too and added when the rows are written.
+      const uint32_t drafted = mine >= sr.ctx ? ~0u : mine + TPG <= sr.ctx ? 0u : ~0u << (sr.ctx - mine);
+      uint32_t odd = 0;
 #pragma unroll
       for (int i = 0; i < ND; ++i)
 #pragma unroll
-        for (int w = 0; w < Raw::VW; ++w) raw.v[i][w] = v_keep<CT>(raw.v[i][w], ((1u << valid) - 1u) >> (w * 16 / sizeof(CT)));
-      // A drafted token's V that is not finite concerns the rows that see it and no other, and 0 times
-      // infinity is not 0: such elements are cleared here too and added when the rows are written.
-      if (mine + TPG > sr.ctx) {
-        const uint32_t drafted = mine >= sr.ctx ? ~0u : ~0u << (sr.ctx - mine);
-        uint32_t odd = 0;
-#pragma unroll
-        for (int i = 0; i < ND; ++i)
-#pragma unroll
-          for (int w = 0; w < Raw::VW; ++w) {
-            const uint32_t is = v_odd<CT>(raw.v[i][w]) & (drafted >> (w * 16 / sizeof(CT)));
-            if (is) raw.v[i][w] = v_keep<CT>(raw.v[i][w], ~is);
-            odd |= is;
-          }
-        if (odd) sm_odd = 1;
-      }
+        for (int w = 0; w < Raw::VW; ++w) {
+          constexpr int N = 16 / sizeof(CT);
+          u32x4 v = v_keep<CT>(raw.v[i][w], held >> (w * N));
+          const uint32_t is = v_odd<CT>(v) & (drafted >> (w * N));
+          if (is) v = v_keep<CT>(v, ~is);
+          odd |= is;
+          raw.v[i][w] = v;
+        }
+      if (odd) sm_odd = 1;
     }
 
-    // softmax of each row tile; p as the MFMA's P^T operand (tokens 8 h .. 8 h + 7 of the lane group)
-    Frag8 pf[NQ][F32 ? 1 : JN / 2];
-    float px[NQ][F32 ? TPG : 1];
+    // softmax; p as the MFMA's P^T operand (tokens 8 h .. 8 h + 7 of the lane group).  The sums move to a new
+    // maximum only when it exceeds theirs by 2^8: until then p is at most 2^8, which rounds no worse.
+    float s[TPG];
+    float tmax = -INFINITY;
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-      float s[TPG];
-      float tmax = -INFINITY;
+    for (int e = 0; e < TPG; ++e) tmax = fmaxf(tmax, sc[e >> 2][e & 3]);
+    tmax = fmaxf(tmax, __shfl_xor(tmax, 16, 64));
+    tmax = fmaxf(tmax, __shfl_xor(tmax, 32, 64));
+    const float m_new = fmaxf(m_run, tmax * scale);
+    if (__any(m_new > m_run + 8.f)) {
+      const float corr = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
+      m_run = m_new;
+      l_run *= corr;
 #pragma unroll
-      for (int e = 0; e < TPG; ++e) {
-        s[e] = sc[n][e >> 2][e & 3] * scale;
-        if constexpr (MASKED) s[e] = (vis[n] >> e) & 1 ? s[e] : -INFINITY;
-        tmax = fmaxf(tmax, s[e]);
-      }
-      tmax = fmaxf(tmax, __shfl_xor(tmax, 16, 64));
-      tmax = fmaxf(tmax, __shfl_xor(tmax, 32, 64));
-      const float m_new = fmaxf(m_run[n], tmax);
-      const float m_use = m_new == -INFINITY ? 0.f : m_new;      // nothing seen yet: every p is 0
-      const float corr = __builtin_amdgcn_exp2f(m_run[n] - m_use);
-      m_run[n] = m_new;
-      float rs = 0.f;
-#pragma unroll
-      for (int e = 0; e < TPG; ++e) {
-        s[e] = __builtin_amdgcn_exp2f(s[e] - m_use);
-        rs += s[e];
-      }
-      l_run[n] = l_run[n] * corr + rs;
-      if (__any(corr != 1.f)) {
-#pragma unroll
-        for (int i = 0; i < ND; ++i) o[n][i] *= corr;
-      }
-      if constexpr (F32) {
-#pragma unroll
-        for (int e = 0; e < TPG; ++e) px[n][e] = s[e];
-      } else {
-        if constexpr (Q8) {
-          const uint32_t w[4] = {raw.ve.x, raw.ve.y, raw.ve.z, raw.ve.w};
-#pragma unroll
-          for (int e = 0; e < TPG; ++e) {
-            const float vs = exp_scale((w[e >> 2] >> (8 * (e & 3))) & 255u);
-            s[e] = !MASKED || e < valid ? s[e] * vs : 0.f;
-          }
-        }
-#pragma unroll
-        for (int h = 0; h < JN / 2; ++h)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) pf[n][h].w[e] = pack2(s[8 * h + 2 * e], s[8 * h + 2 * e + 1]);
-      }
+      for (int i = 0; i < ND; ++i) o[i] *= corr;
     }
+    const float m_use = m_run == -INFINITY ? 0.f : m_run;         // nothing seen yet: every p is 0
+#pragma unroll
+    for (int e = 0; e < TPG; ++e) {
+      s[e] = __builtin_amdgcn_exp2f(fmaf(sc[e >> 2][e & 3], scale, -m_use));
+      l_run += s[e];
+    }
+    Frag8 pf[F32 ? 1 : JN / 2];
+    if constexpr (!F32) {
+      if constexpr (Q8) {
+#pragma unroll
+        for (int e = 0; e < TPG; ++e) {
+          const float vs = exp_scale((raw.ve[e >> 2] >> (8 * (e & 3))) & 255u);
+          s[e] = e < valid ? s[e] * vs : 0.f;
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < JN / 2; ++h)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) pf[h].w[e] = pack2(s[8 * h + 2 * e], s[8 * h + 2 * e + 1]);
+    }
+    // O^T += V^T P^T
 #pragma unroll
     for (int i = 0; i < ND; ++i) {
-      f32x4 acc[NQ];
+      if constexpr (F32) {
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) acc[n] = o[n][i];
-      if constexpr (F32) add_pv(raw.v[i], px, acc);
-      else add_pv(raw.v[i], pf, acc);
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) o[n][i] = acc[n];
+        for (int e = 0; e < TPG; ++e) o[i] = mfma4(__uint_as_float(raw.v[i][e >> 2][e & 3]), s[e], o[i]);
+      } else if constexpr (Q8) {
+        const u32x4 x = raw.v[i][0];
+        const Frag8 a{{e4m3_pair<false>(x.x, 1.f), e4m3_pair<true>(x.x, 1.f), e4m3_pair<false>(x.y, 1.f), e4m3_pair<true>(x.y, 1.f)}};
+        const Frag8 c{{e4m3_pair<false>(x.z, 1.f), e4m3_pair<true>(x.z, 1.f), e4m3_pair<false>(x.w, 1.f), e4m3_pair<true>(x.w, 1.f)}};
+        o[i] = mfma16(a, pf[0], o[i]);
+        o[i] = mfma16(c, pf[JN / 2 - 1], o[i]);
+      } else {
+        o[i] = mfma16(__builtin_bit_cast(Frag8, raw.v[i][0]), pf[0], o[i]);
+      }
     }
     if (it + 1 < n_it) load_v(it + 1);
-  };
-
-  for (int it = 0; it < n_it; ++it) {
-    if ((first + 4 * it) * STEP + STEP > sr.ctx || !__all(raw.ok)) step(it, std::true_type{});
-    else step(it, std::false_type{});
   }
 
-  // the lane groups' sums, then the four waves, one row tile at a time
+  // the lane groups' sums, then the four waves
   const int nsplit = gridDim.x;
+  l_run += __shfl_xor(l_run, 16, 64);
+  l_run += __shfl_xor(l_run, 32, 64);
+  if (grp == 0) { sm_m[wave][col] = m_run; sm_l[wave][col] = l_run; }
 #pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    if (row0 + 16 * n >= nrow) break;
-    float l = l_run[n];
-    l += __shfl_xor(l, 16, 64);
-    l += __shfl_xor(l, 32, 64);
-    if (n > 0) __syncthreads();
-    if (grp == 0) { sm_m[wave][col] = m_run[n]; sm_l[wave][col] = l; }
+  for (int i = 0; i < ND; ++i) *reinterpret_cast<f32x4*>(&sm_o[wave][col][16 * i + 4 * grp]) = o[i];
+  __syncthreads();
+  for (int idx = tid; idx < 16 * D; idx += 256) {
+    const int c = idx / D, d = idx % D, r = row0 + c;
+    if (r >= nrow) break;
+    float M = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < ND; ++i) *reinterpret_cast<f32x4*>(&sm_o[wave][col][16 * i + 4 * grp]) = o[n][i];
-    __syncthreads();
-    for (int idx = tid; idx < 16 * D; idx += 256) {
-      const int c = idx / D, d = idx % D, r = row0 + 16 * n + c;
-      if (r >= nrow) break;
-      float M = -INFINITY;
+    for (int w = 0; w < 4; ++w) M = fmaxf(M, sm_m[w][c]);
+    const float mu = M == -INFINITY ? 0.f : M;
+    float L = 0.f, O = 0.f;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) M = fmaxf(M, sm_m[w][c]);
-      const float mu = M == -INFINITY ? 0.f : M;
-      float L = 0.f, O = 0.f;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const float f = __builtin_amdgcn_exp2f(sm_m[w][c] - mu);
-        L += f * sm_l[w][c];
-        O += f * sm_o[w][c][d];
-      }
-      const long t = sr.r0 + r / G;
-      if (sm_odd) {
-        const unsigned long long see = p.mask ? p.mask[t] : (2ull << (r / G)) - 1;
+    for (int w = 0; w < 4; ++w) {
+      const float f = __builtin_amdgcn_exp2f(sm_m[w][c] - mu);
+      L += f * sm_l[w][c];
+      O += f * sm_o[w][c][d];
+    }
+    const long t = sr.r0 + r / G;
+    if (sm_odd) {
+      const unsigned long long see = p.mask ? p.mask[t] : (2ull << (r / G)) - 1;
 #pragma unroll 1
-        for (int j = max(0, step0 * STEP - sr.ctx); j < min(sr.n, step1 * STEP - sr.ctx); ++j) {
-          const int tok = sr.ctx + j, ph = page_of(p.r, p.c.num_blocks, b, tok / PAGE);
-          if (!((see >> j) & 1) || ph < 0) continue;
-          const float v = odd_value<CT>(reinterpret_cast<const CT*>(p.c.v)[(((size_t)ph * n_kv + kvh) * D + d) * PAGE + tok % PAGE]);
-          if (!(fabsf(v) < INFINITY)) O += v;
-        }
+      for (int j = max(0, step0 * STEP - sr.ctx); j < min(sr.n, step1 * STEP - sr.ctx); ++j) {
+        const int tok = sr.ctx + j, ph = page_of(p.r, p.c.num_blocks, b, tok / PAGE);
+        if (!((see >> j) & 1) || ph < 0) continue;
+        const float v = odd_value<CT>(reinterpret_cast<const CT*>(p.c.v)[(((size_t)ph * n_kv + kvh) * D + d) * PAGE + tok % PAGE]);
+        if (!(fabsf(v) < INFINITY)) O += v;
       }
-      const int head = kvh * G + r % G;
-      if (nsplit == 1) {
-        reinterpret_cast<T*>(p.out)[t * p.out_row + head * D + d] = from_f<T>(L == 0.f ? 0.f : O / L);
-      } else {
-        float* part = p.partial + ((t * p.n_q + head) * nsplit + split) * (D + 4);
-        part[4 + d] = O;
-        if (d == 0) { part[0] = M; part[1] = L; }
-      }
+    }
+    const int head = kvh * G + r % G;
+    if (nsplit == 1) {
+      reinterpret_cast<T*>(p.out)[t * p.out_row + head * D + d] = from_f<T>(L == 0.f ? 0.f : O / L);
+    } else {
+      float* part = p.partial + ((t * p.n_q + head) * nsplit + split) * (D + 4);
+      part[4 + d] = O;
+      if (d == 0) { part[0] = M; part[1] = L; }
     }
   }
 }
@@ -407,7 +342,7 @@ tree_attn_kernel(TreeArgs p, int steps_per_split) {
 // 16-byte pieces are swizzled by their row so that a read covers every bank once.
 template <typename CT, int D>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
-tree_wide_kernel(TreeArgs p, int steps_per_split) {
+tree_wide_kernel(TreeArgs p, int least) {
   constexpr bool Q8 = sizeof(CT) == 1;
   constexpr int STEP = 64, ND = D / 32, NS = D / 16;
   constexpr int LW = STEP * D * sizeof(CT) / 16 / 256;            // 16-byte loads of a thread, for K and for V
@@ -429,7 +364,8 @@ tree_wide_kernel(TreeArgs p, int steps_per_split) {
   if (row0 >= nrow) return;
   const int total = sr.ctx + sr.n;
   const int nsteps = (total + STEP - 1) / STEP;
-  const int step0 = split * steps_per_split, step1 = min(step0 + steps_per_split, nsteps);
+  const int per = split_steps(nsteps, gridDim.x, least);
+  const int step0 = split * per, step1 = min(step0 + per, nsteps);
   const bool active = row0 + 32 * wave < nrow;
   const int row = row0 + 32 * wave + col, rc = min(row, nrow - 1);
   const int t = rc / G, head = kvh * G + rc % G;
@@ -452,12 +388,14 @@ tree_wide_kernel(TreeArgs p, int steps_per_split) {
   u32x4 rk[LW], rv[LW];
   uint8_t rks[Q8 ? LW : 1], rvs[Q8 ? LW : 1];                     // exponent bytes: nothing waits for the loads here
   unsigned exists = 0;                                            // of the loaded step's 4 blocks, a bit each
-  auto load = [&](int step) {
-    const int at = 4 * ((step - step0) & 15);
-    if (at == 0 && step != step0) {
+  auto advance = [&](int step) {                                  // before the load of a step whose ids are the next 16's
+    if (((step - step0) & 15) == 0) {
       tl = tl_next;
       tl_next = entries(step + 16);
     }
+  };
+  auto load = [&](int step) {
+    const int at = 4 * ((step - step0) & 15);
     exists = (unsigned)(__ballot(tl >= 0) >> at) & 15u;
 #pragma unroll
     for (int u = 0; u < LW; ++u) {
@@ -545,20 +483,26 @@ tree_wide_kernel(TreeArgs p, int steps_per_split) {
   float m_run = -INFINITY, l_run = 0.f;                           // l_run: of this lane half's tokens
   const float scale = fmaxf(fabsf(p.scale) * 1.4426950408889634f, 1e-37f);   // not 0: -infinity stays what it is
   __syncthreads();                                                // sm_odd is cleared
-  unsigned long long keep = 0;
+  unsigned long long keep = 0, keep_next = 0;                     // of the step at hand and of the one in registers
   if (step0 < step1) {
     keep = keep_of(step0);
     if (masked_step(step0, keep)) clean(step0, keep);
     store(0);
+    if (step0 + 1 < step1) {
+      load(step0 + 1);
+      keep_next = keep_of(step0 + 1);
+    }
   }
   __syncthreads();
 
   // MFMA row m of S is token tau of its 32
   const int tau = 16 * (col >> 4) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3);
   // A step is two halves of 32 tokens, so that matrix and vector instructions of one wave run side by
-  // side: S of the second half beside the exponentials of the first, V^T P^T of the first beside those
-  // of the second, V^T P^T of the second beside the conversion of the next step.  The LDS reads of a
-  // product run 8 ahead of its MFMAs, 4 at a time.  The scheduler, left alone, does neither.
+  // side: S of the first half beside the conversion of the next step into the other buffer, S of the second
+  // beside the exponentials of the first, V^T P^T of the first beside those of the second; then the
+  // step's one barrier, and V^T P^T of the second beside the loads of the step after next.  The LDS
+  // reads of a product run L ahead of its MFMAs, over the steps' ends: V's last ones are read before
+  // the barrier, after which nothing reads the step's buffer.  Left alone, the scheduler does neither.
   const int kr = kat(tau, half), vr = 2 * KBUF + vat(col, half);
   auto k_read = [&](int buf, int x) {                             // x: 32-token half of the step and k-step
     return *reinterpret_cast<const Frag8*>(smem + ((kr + buf * KBUF) ^ (x % NS << 5)) + x / NS * 32 * 2 * D);
@@ -567,10 +511,9 @@ tree_wide_kernel(TreeArgs p, int steps_per_split) {
     return *reinterpret_cast<const Frag8*>(smem + ((vr + buf * VBUF) ^ (x / ND << 5)) + x % ND * 32 * 2 * STEP);
   };
   constexpr int NK = 2 * NS, NF = NK + 4 * ND;                    // operands of a step: K's, then V's (NS == 2 ND)
-  Frag8 f[8];
-  auto read = [&](int buf, int x) {
-    if (x < NF) f[x & 7] = x < NK ? k_read(buf, x) : v_read(buf, x - NK);
-  };
+  constexpr int L = 2 * ND;                                       // divides NK and NF
+  Frag8 f[L];
+  auto read = [&](int buf, int x) { f[x % L] = x < NK ? k_read(buf, x) : x < NF ? v_read(buf, x - NK) : k_read(buf ^ 1, x - NF); };
   // scores of one half: seen or not, and whether the running maximum has to move
   auto hide = [&](f32x16& sc, uint32_t seen) {
 #pragma unroll
@@ -580,7 +523,8 @@ tree_wide_kernel(TreeArgs p, int steps_per_split) {
     float m = sc[0];
 #pragma unroll
     for (int r = 1; r < 16; ++r) m = fmaxf(m, sc[r]);
-    return fmaxf(m, __shfl_xor(m, 32, 64)) * scale;
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])) * scale;   // both lane halves'
   };
   // p of elements e0 .. e0 + n - 1 of a half, packed as the second product's operand once 8 are there
   float px[8], rs = 0.f;
@@ -604,35 +548,35 @@ tree_wide_kernel(TreeArgs p, int steps_per_split) {
     __builtin_amdgcn_sched_barrier(0);
   };
   auto base_of = [&]() { return m_run == -INFINITY ? 0.f : m_run; };   // nothing seen yet: every p is 0
+  if (active) {
+#pragma unroll
+    for (int x = 0; x < L; ++x) read(0, x);
+  }
   for (int step = step0; step < step1; ++step) {
     const int buf = (step - step0) & 1;
-    const bool more = step + 1 < step1;
-    const unsigned long long now = keep;
-    if (more) {
-      load(step + 1);
-      keep = keep_of(step + 1);
-    }
-    const bool next_masked = more && masked_step(step + 1, keep);
+    if (step + 1 < step1 && masked_step(step + 1, keep_next)) clean(step + 1, keep_next);
+    const int then = min(step + 2, step1 - 1);                    // at the end the last step once more: the loads stay in line
+    if (step + 2 < step1) advance(step + 2);
     if (active) {
-      const bool masked = masked_step(step, now);
+      const bool masked = masked_step(step, keep);
       unsigned long long vis = ~0ull;
       if (masked) {                                               // drafted tokens, the end, or a missing block
         const int dr = step * STEP - sr.ctx;                      // the step's first token as a drafted one
         vis = dr >= 64 ? 0ull : dr >= 0 ? sees >> dr : dr <= -64 ? ~0ull : (sees << -dr) | ((1ull << -dr) - 1);
-        vis = (vis & now) >> (8 * half);
+        vis = (vis & keep) >> (8 * half);
       }
       f32x16 s0, s1;
       Frag8 p0[2], p1[2];
 #pragma unroll
       for (int r = 0; r < 16; ++r) s0[r] = s1[r] = 0.f;
-#pragma unroll
-      for (int x = 0; x < 8; ++x) read(buf, x);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int x = 0; x < NS; ++x) {
-        s0 = mfma32(f[x & 7], qf[x], s0);
-        read(buf, x + 8);
+        s0 = mfma32(f[x % L], qf[x], s0);
+        read(buf, x + L);
       }
+      store(buf ^ 1);                                             // after the last step: stale, and never used
+      __builtin_amdgcn_sched_barrier(0);
       if (masked) hide(s0, (uint32_t)vis);
       // the sums move to a new maximum only when it exceeds theirs by 2^8: until then p is at most
       // 2^8, which rounds no worse, and the accumulators are left alone at most steps
@@ -649,8 +593,8 @@ tree_wide_kernel(TreeArgs p, int steps_per_split) {
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int x = NS; x < NK; ++x) {
-        s1 = mfma32(f[x & 7], qf[x - NS], s1);
-        read(buf, x + 8);
+        s1 = mfma32(f[x % L], qf[x - NS], s1);
+        read(buf, x + L);
         expo(s0, buf, 0, (x - NS) * (16 / NS), 16 / NS, base0, p0);
       }
       l_run += rs;
@@ -668,8 +612,8 @@ tree_wide_kernel(TreeArgs p, int steps_per_split) {
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int x = 0; x < 2 * ND; ++x) {
-        o[x % ND] = mfma32(f[(NK + x) & 7], p0[x / ND], o[x % ND]);
-        read(buf, NK + x + 8);
+        o[x % ND] = mfma32(f[(NK + x) % L], p0[x / ND], o[x % ND]);
+        read(buf, NK + x + L);
         expo(s1, buf, 2, x * (8 / ND), 8 / ND, base1, p1);
       }
       l_run += rs;
@@ -677,17 +621,21 @@ tree_wide_kernel(TreeArgs p, int steps_per_split) {
 #pragma unroll
         for (int i = 0; i < ND; ++i) o[i] *= corr;
       }
-      if (next_masked) clean(step + 1, keep);
-      __builtin_amdgcn_sched_barrier(0);
+      __syncthreads();
 #pragma unroll
-      for (int x = 2 * ND; x < 4 * ND; ++x) o[x % ND] = mfma32(f[(NK + x) & 7], p1[x / ND - 2], o[x % ND]);
-      store(buf ^ 1);                                             // after the last step: stale, and never read
+      for (int x = 2 * ND; x < 4 * ND; ++x) {
+        o[x % ND] = mfma32(f[(NK + x) % L], p1[x / ND - 2], o[x % ND]);
+        read(buf, NK + x + L);
+      }
+      load(then);
       __builtin_amdgcn_sched_barrier(0);
     } else {
-      if (next_masked) clean(step + 1, keep);
       store(buf ^ 1);
+      __syncthreads();
+      load(then);
     }
-    __syncthreads();
+    keep = keep_next;
+    keep_next = keep_of(then);
   }
   if (!active || row >= nrow) return;
   float l = l_run;
@@ -747,19 +695,28 @@ __global__ void __launch_bounds__(256) tree_combine_kernel(TreeArgs p, int nspli
   const float f = M == -INFINITY ? 0.f : exp2f(m - M);
   const float L = wave_sum(f * l);
   float o[D / 64] = {};
-#pragma unroll 4
-  for (int s = 0; s < nsplit; ++s) {
-    const float w = __shfl(f, s, 64);
+  for (int s0 = 0; s0 < nsplit; s0 += 8) {                // 8 splits' loads at a time
+    float v[8][D / 64];
 #pragma unroll
-    for (int d = 0; d < D / 64; ++d) o[d] += w * part[s * (D + 4) + 4 + lane + 64 * d];
+    for (int s = 0; s < 8; ++s)
+#pragma unroll
+      for (int d = 0; d < D / 64; ++d) v[s][d] = s0 + s < nsplit ? part[(s0 + s) * (D + 4) + 4 + lane + 64 * d] : 0.f;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), min(s0 + s, 63)));
+#pragma unroll
+      for (int d = 0; d < D / 64; ++d) o[d] += w * v[s][d];
+    }
   }
 #pragma unroll
   for (int d = 0; d < D / 64; ++d)
     reinterpret_cast<T*>(p.out)[t * p.out_row + head * D + lane + 64 * d] = from_f<T>(L == 0.f ? 0.f : o[d] / L);
 }
 
-// The kernel, the workgroups that a KV head's rows take, and the splits of the context.
-struct TreePlan { bool wide; int tiles, nsplit, per; };
+// The kernel, the workgroups that a KV head's rows take, and the splits of the context, of 4 steps at least:
+// as many as give every compute unit two workgroups.
+constexpr int LEAST_STEPS = 4;
+struct TreePlan { bool wide; int tiles, nsplit; };
 static TreePlan tree_plan(int type, int n_kv, int n_q, int batch, int max_rows, int max_ctx, int cus) {
   TreePlan t;
   const int rows = max_rows * (n_q / n_kv);
@@ -767,11 +724,8 @@ static TreePlan tree_plan(int type, int n_kv, int n_q, int batch, int max_rows, 
   t.tiles = (rows + (t.wide ? 127 : 15)) / (t.wide ? 128 : 16);
   const int step = t.wide || type == CACHE_E4M3 ? 64 : 32;
   const int steps = (max_ctx + step - 1) / step;
-  const int base = batch * n_kv * t.tiles;
-  const int want = std::max(1, (2 * cus + base - 1) / base);
-  t.per = std::max(4, (steps + want - 1) / want);
-  t.nsplit = (steps + t.per - 1) / t.per;
-  while (t.nsplit > 64) t.nsplit = (steps + ++t.per - 1) / t.per;
+  const int want = (2 * cus + batch * n_kv * t.tiles - 1) / (batch * n_kv * t.tiles);
+  t.nsplit = std::max(1, std::min({want, 64, (steps + LEAST_STEPS - 1) / LEAST_STEPS}));
   return t;
 }
 
@@ -785,10 +739,10 @@ static hipError_t tree_launch(const TreeArgs& p, const TreePlan& t, hipStream_t 
   typedef typename TreeT<CT>::act T;
   const dim3 grid(t.nsplit, p.c.n_kv * t.tiles, p.r.batch);
   if constexpr (sizeof(CT) < 4) {
-    if (t.wide) hipLaunchKernelGGL((tree_wide_kernel<CT, D>), grid, dim3(256), 0, s, p, t.per);
-    else hipLaunchKernelGGL((tree_attn_kernel<CT, D, 1>), grid, dim3(256), 0, s, p, t.per);
+    if (t.wide) hipLaunchKernelGGL((tree_wide_kernel<CT, D>), grid, dim3(256), 0, s, p, LEAST_STEPS);
+    else hipLaunchKernelGGL((tree_attn_kernel<CT, D>), grid, dim3(256), 0, s, p, LEAST_STEPS);
   } else {
-    hipLaunchKernelGGL((tree_attn_kernel<CT, D, 1>), grid, dim3(256), 0, s, p, t.per);
+    hipLaunchKernelGGL((tree_attn_kernel<CT, D>), grid, dim3(256), 0, s, p, LEAST_STEPS);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || t.nsplit == 1) return e;

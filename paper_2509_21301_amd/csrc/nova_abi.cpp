@@ -755,12 +755,18 @@ void set_rope(nova::AppendArgs& a, const nova_rope& r) {
   a.rot = r.rot;
   a.interleaved = r.interleaved != 0;
   a.mscale = r.mscale;
+  // theta^(-2c/rot) as a product of the powers at c's binary digits: 6 roundings at most, and 6 calls
+  // of pow instead of 64 (3 us of a call)
+  double f[64] = {1.0};
+  for (int k = 1; k < r.rot / 2; k *= 2) {
+    const double step = std::pow((double)r.theta, -2.0 * k / r.rot);
+    for (int c = k; c < std::min(2 * k, r.rot / 2); ++c) f[c] = f[c - k] * step;
+  }
   for (int c = 0; c < r.rot / 2; ++c) {
-    const double f = std::pow((double)r.theta, -2.0 * c / r.rot);
-    double g = f / r.factor;
+    double g = f[c] / r.factor;
     if (r.orig_ctx > 0) {
-      const double keep = std::min(1.0, std::max(0.0, (r.orig_ctx * f / two_pi - r.alpha) / ((double)r.beta - r.alpha)));
-      g = keep * f + (1.0 - keep) * g;
+      const double keep = std::min(1.0, std::max(0.0, (r.orig_ctx * f[c] / two_pi - r.alpha) / ((double)r.beta - r.alpha)));
+      g = keep * f[c] + (1.0 - keep) * g;
     }
     a.turns[c] = g / two_pi;
   }
@@ -854,7 +860,7 @@ extern "C" int nova_tree_attention(const nova_cache* cache, const nova_rows* row
   if (need > 0 && (!ws || !aligned(ws))) return fail(NOVA_EINVAL, "null or misaligned workspace");
   hipStream_t s = (hipStream_t)stream;
   const nova::TreeArgs a{pool_layer(*cache, 0), batch_rows(*rows), (const unsigned long long*)mask, q, q_pitch, n_q, scale, out, out_pitch, (float*)ws};
-  const int cus = std::min(stream_cus(s) > 0 ? stream_cus(s) : device_cus(), device_cus());
+  const int on = stream_cus(s), cus = std::min(on > 0 ? on : device_cus(), device_cus());
   CALL(NOVA_KIND_DECODE_ATTN, s, nova::tree_attention(a, cus, s));
   return NOVA_OK;
 }

@@ -475,13 +475,12 @@ def _check_vector(what, t, dtype, n):
 
 def _check_rows_of(what, t, rows, heads, d):
     """Rows [rows, heads, d], heads and dimensions contiguous; returns (type, pitch)."""
-    act = _ACT.get(t.dtype)
+    act, st = _ACT.get(t.dtype), t.stride()
+    if act is not None and t.shape == (rows, heads, d) and st[2] == 1 and (st[1] == d or heads == 1):
+        return act, st[0] if rows > 1 else heads * d
     if act is None:
         raise ValueError(f"{what} must be bfloat16 or float32, got {t.dtype}")
-    st = t.stride()
-    if t.shape != (rows, heads, d) or st[2] != 1 or (st[1] != d and heads > 1):
-        raise ValueError(f"{what} must be rows {(rows, heads, d)} with contiguous heads, got {tuple(t.shape)} strides {st}")
-    return act, st[0] if rows > 1 else heads * d
+    raise ValueError(f"{what} must be rows {(rows, heads, d)} with contiguous heads, got {tuple(t.shape)} strides {st}")
 
 
 def _check_device(dev, *tensors):
@@ -614,8 +613,9 @@ def kv_append(cache, rows, k, v, q=None, pos=None, rope=None, q_out=None, layer=
         n_q = q.shape[1] if q.dim() == 3 else 0
         act_q, q_pitch = _check_rows_of("q", q, n, n_q, d)
         if q_out is None:
-            q_out = _empty(q, (n, n_q, d), q.dtype, stream)
-        act_out, out_pitch = _check_rows_of("q_out", q_out, n, n_q, d)
+            q_out, act_out, out_pitch = _empty(q, (n, n_q, d), q.dtype, stream), act_q, n_q * d
+        else:
+            act_out, out_pitch = _check_rows_of("q_out", q_out, n, n_q, d)
     elif q_out is not None:
         raise ValueError("q_out without q")
     if act_v != act or act_q != act:
@@ -630,15 +630,20 @@ def kv_gather(cache, rows, slots=None, k_out=None, v_out=None, dtype=torch.bfloa
     (int32 [rows], token numbers in the row's sequence).  Rows behind the last sequence are left as they were."""
     n, d = rows.rows, cache.head_dim
     _check_vector("slots", slots, torch.int32, n)
+    _check_device(cache.device, rows.tables, slots, k_out, v_out)
+    dtype = k_out.dtype if k_out is not None else v_out.dtype if v_out is not None else dtype
+    act = act_v = _ACT.get(dtype)
+    k_pitch = v_pitch = cache.n_kv * d
+    if k_out is not None:
+        act, k_pitch = _check_rows_of("k_out", k_out, n, cache.n_kv, d)
+    if v_out is not None:
+        act_v, v_pitch = _check_rows_of("v_out", v_out, n, cache.n_kv, d)
+    if act is None or act != act_v:
+        raise ValueError("k_out and v_out must have one type, bfloat16 or float32")
     if k_out is None:
         k_out = _empty(cache.k, (n, cache.n_kv, d), dtype, stream)
     if v_out is None:
         v_out = _empty(cache.k, (n, cache.n_kv, d), dtype, stream)
-    _check_device(cache.device, rows.tables, slots, k_out, v_out)
-    act, k_pitch = _check_rows_of("k_out", k_out, n, cache.n_kv, d)
-    act_v, v_pitch = _check_rows_of("v_out", v_out, n, cache.n_kv, d)
-    if act != act_v:
-        raise ValueError("k_out and v_out must have one type")
     _check(lib.nova_kv_gather(cache.layer(layer), rows.ref, _ptr(slots), act, k_out.data_ptr(), k_pitch, v_out.data_ptr(), v_pitch,
                               _stream(stream)))
     return k_out, v_out
@@ -653,9 +658,11 @@ def tree_attention(cache, rows, q, mask=None, out=None, scale=None, layer=0, str
     _check_vector("mask", mask, torch.int64, n)
     n_q = q.shape[1] if q.dim() == 3 else 0
     act, q_pitch = _check_rows_of("q", q, n, n_q, d)
+    act_out, out_pitch = act, n_q * d
     if out is None:
         out = _empty(q, (n, n_q, d), q.dtype, stream)
-    act_out, out_pitch = _check_rows_of("out", out, n, n_q, d)
+    else:
+        act_out, out_pitch = _check_rows_of("out", out, n, n_q, d)
     if q.dtype != cache.dtype or act_out != act:
         raise ValueError(f"q and out must be {cache.dtype}")
     nbytes = rows._tree_bytes(cache, n_q)
