@@ -227,7 +227,8 @@ int nova_llm_decode_noalloc(const nova_llm* llm, const int32_t* ids, const int32
  * A cache layer of one of three types.  BF16 and F32 are a layer of a nova_kv pool.  E4M3 stores
  * 8 bits per value: token t of a KV head is D OCP e4m3 numbers and one byte e + 127, the values
  * being number * 2^e with the smallest e >= -100 that keeps |number| <= 448 (NaN and infinite values
- * are stored as NaN).  Values read back are exact in bf16, and appending them again stores the same. */
+ * are stored as NaN).  Values read back are exact in bf16, and appending them again stores the same
+ * values (a largest one that rounded to 224 * 2^e becomes 448 * 2^(e-1)). */
 enum { NOVA_CACHE_BF16 = 0, NOVA_CACHE_F32 = 1, NOVA_CACHE_E4M3 = 2 };
 typedef struct {
   void* k;          /* [num_blocks][n_kv][16][head_dim], 256-byte aligned */
@@ -325,7 +326,8 @@ int nova_llm_prefill_cache(const nova_llm* llm, const void* vis, int n_vis, cons
  * mask, as nova_kv_append and nova_tree_attention do.  One row per sequence is a plain decode step.
  *  ids, pos: device int32 [rows], rows <= 32: tokens and their rotary positions
  *  mask:     device uint64 [rows] or NULL (chains)
- *  next_ids [rows], logits [rows][vocab] or NULL: as for nova_llm_decode, one per row
+ *  next_ids [rows], logits [rows][vocab] or NULL: as for nova_llm_decode, one per row; rows behind
+ *            the last sequence need valid ids too, and what they get means nothing
  * The sequences keep only the tokens that the caller accepts: the rest of the slots are overwritten
  * by the next step's rows. */
 size_t nova_llm_verify_workspace_bytes(const nova_llm* llm, const nova_cache* cache, const nova_rows* rows);

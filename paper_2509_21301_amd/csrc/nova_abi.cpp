@@ -835,7 +835,7 @@ int check_tree(const nova_cache* cache, const nova_rows* rows, int n_q) {
   if (int rc = check_rows(rows, true)) return rc;
   if (rows->max_rows > 64) return fail(NOVA_EUNSUPPORTED, "%d drafted tokens of one sequence (at most 64)", rows->max_rows);
   if (n_q <= 0 || n_q % cache->n_kv) return fail(NOVA_EINVAL, "n_q %d must be a positive multiple of n_kv %d", n_q, cache->n_kv);
-  if ((int64_t)rows->max_rows * n_q > (1 << 20)) return fail(NOVA_EUNSUPPORTED, "n_q %d is too large", n_q);
+  if ((int64_t)rows->max_rows * n_q > (1 << 19)) return fail(NOVA_EUNSUPPORTED, "n_q %d is too large", n_q);
   return NOVA_OK;
 }
 }  // namespace

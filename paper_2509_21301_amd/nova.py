@@ -433,15 +433,18 @@ class Llm:
 
     def verify(self, ids, pos, rows, cache, mask=None, next_ids=None, logits=None, stream=None):
         """A decode step over drafted tokens on a ``Cache``: ids, pos int32 [rows.rows] (at most 32 rows), ``mask``
-        int64 [rows] as for ``tree_attention``; the greedy id after every row.  One row per sequence decodes."""
+        int64 [rows] as for ``tree_attention``; the greedy id after every row.  One row per sequence decodes.  Rows
+        behind the last sequence need valid ids too; what comes back for them means nothing."""
         cache._check_layers(self.cfg.layers)
+        _check_device(cache.device, rows.tables, ids, pos, mask, next_ids, logits)
         for what, t, dt in (("ids", ids, torch.int32), ("pos", pos, torch.int32), ("mask", mask, torch.int64)):
             _check_vector(what, t, dt, rows.rows)
         if logits is not None and (logits.dtype != torch.float32 or not logits.is_contiguous() or
                                    logits.shape != (rows.rows, self.cfg.vocab)):
             raise ValueError(f"logits must be contiguous float32 {(rows.rows, self.cfg.vocab)}")
+        # memory of the call's own, so that a captured step keeps its workspace whatever runs later
         n = lib.nova_llm_verify_workspace_bytes(self.h, cache.layer(0), rows.ref)
-        ws = self._workspace("verify", max(n, 256), stream)
+        ws = _empty(cache.k, max(n, 256), torch.uint8, stream)
         if next_ids is None:
             next_ids = torch.empty(rows.rows, dtype=torch.int32, device=self.device)
         _check_vector("next_ids", next_ids, torch.int32, rows.rows)

@@ -208,6 +208,44 @@ def test_verify_in_a_graph(gpu_lib):
         assert torch.equal(n1, nxt) and torch.equal(l1, logits), t
 
 
+def test_two_graphs_and_a_larger_step_between(gpu_lib):
+    """Captured steps keep workspaces of their own: another capture and a larger eager step between the replays
+    change nothing."""
+    nova = gpu_lib
+    ref = _oracle("bf16")
+    llm, cache, tables, _ = _setup(nova, "bf16", ref)
+    ctx = torch.tensor(PROMPTS, dtype=torch.int32, device="cuda")
+
+    def step(n):
+        ids = torch.arange(2 * n, dtype=torch.int32, device="cuda") + 3
+        pos = (ctx[:, None] + torch.arange(n, dtype=torch.int32, device="cuda")).flatten().contiguous()
+        rows = nova.Rows(None, ctx, tables, max_rows=n, max_ctx=130)
+        out = torch.empty(2 * n, CFG.vocab, device="cuda")
+        return lambda: llm.verify(ids, pos, rows, cache, logits=out), out
+    steps = [step(1), step(4)]
+    want = []
+    for s, out in steps:
+        s()
+        want.append(out.clone())
+    torch.cuda.synchronize()
+    graphs = []
+    for s, _ in steps:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            s()
+        graphs.append(g)
+    big, _ = step(16)
+    for _ in range(3):
+        for g, (_, out), w in zip(graphs, steps, want):
+            big()
+            junk = torch.full((1 << 22,), float("nan"), device="cuda")
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, w)
+            del junk
+
+
 def test_model_checks(gpu_lib):
     nova = gpu_lib
     ref = _oracle("bf16")
