@@ -33,18 +33,37 @@ NOVA_DEV float key_value(uint32_t k) { return __uint_as_float((k >> 31) ? k & 0x
 // Larger first, equal values by the lower id; 0: none.
 NOVA_DEV unsigned long long rank_key(uint32_t key, int id) { return ((unsigned long long)key << 32) | (0xFFFFFFFFu - (uint32_t)id); }
 
-// N = 16 / sizeof(T) logits from i0 on, where row + i0 is 16-byte aligned; -infinity outside the row.
-template <typename T> NOVA_DEV void load_logits(const T* row, long i0, int vocab, float* x) {
+// A lane's logits of a chunk as loaded: 16 bytes at a time, N = 16 / sizeof(T) logits from first + 64 N j + N lane
+// on (an address that is a multiple of 16).  Those outside the row are -infinity.
+template <typename T> struct RawLogits { u32x4 w[LP_EPL * sizeof(T) / 16]; };
+template <typename T> NOVA_DEV void load_logits(const T* row, long first, int vocab, RawLogits<T>& x) {
   constexpr int N = 16 / sizeof(T);
-  if (i0 >= 0 && i0 + N <= vocab) {
-    const u32x4 w = *reinterpret_cast<const u32x4*>(row + i0);
+  const int lane = threadIdx.x & 63;
+  if (first >= 0 && first + LP_CHUNK <= vocab) {                  // the same for every lane
 #pragma unroll
-    for (int e = 0; e < N; ++e)
-      x[e] = sizeof(T) == 4 ? __uint_as_float(w[e & 3]) : __uint_as_float((e & 1) ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
-  } else {
-#pragma unroll
-    for (int e = 0; e < N; ++e) x[e] = i0 + e >= 0 && i0 + e < vocab ? to_f<T>(row[i0 + e]) : -INFINITY;
+    for (int j = 0; j < LP_EPL / N; ++j) x.w[j] = reinterpret_cast<const u32x4*>(row + first)[64 * j + lane];
+    return;
   }
+#pragma unroll
+  for (int j = 0; j < LP_EPL / N; ++j) {
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      uint32_t v = 0;
+#pragma unroll
+      for (int h = 0; h < (sizeof(T) == 2 ? 2 : 1); ++h) {
+        const long i = first + 64 * N * j + N * lane + (sizeof(T) == 2 ? 2 * d + h : d);
+        const bool in = i >= 0 && i < vocab;
+        if constexpr (sizeof(T) == 4) v = in ? __float_as_uint(row[i]) : 0xFF800000u;
+        else v |= (in ? (uint32_t)row[i] : 0xFF80u) << (16 * h);
+      }
+      x.w[j][d] = v;
+    }
+  }
+}
+template <typename T> NOVA_DEV float logit_of(const RawLogits<T>& x, int j) {
+  if constexpr (sizeof(T) == 4) return __uint_as_float(x.w[j / 4][j % 4]);
+  const uint32_t w = x.w[j / 8][j % 8 / 2];
+  return __uint_as_float(j & 1 ? w & 0xFFFF0000u : w << 16);
 }
 
 // m, S, T of a set of logits.
@@ -269,23 +288,21 @@ __global__ void __launch_bounds__(256) logprobs_part_kernel(LogprobArgs p, int p
   const int lead = (int)(((uintptr_t)row & 15) / sizeof(T));      // chunks start at the aligned address at or before the row
   const int total = (p.vocab + lead + LP_CHUNK - 1) / LP_CHUNK;
   const int c0 = part * chunks, c1 = min(c0 + chunks, total);
-  auto load = [&](int c, float (&x)[LP_EPL]) {
-#pragma unroll
-    for (int j = 0; j < LP_EPL; j += N) load_logits(row, (long)c * LP_CHUNK - lead + j * 64 + lane * N, p.vocab, x + j);
-  };
   const float gx = ONE ? given_logit<T>(p, r, tid) : 0.f;
-  LogSum a{-INFINITY, 0.f, 0.f};
-  float x[LP_EPL], next[LP_EPL];
-  if (c0 + wave < c1) load(c0 + wave, x);
-  for (int c = c0 + wave; c < c1; c += 4) {
-    if (c + 4 < c1) load(c + 4, next);
-    float top[LP_EPL / N], m = a.m;
+  // A lane's sums S and T relative to its maximum m, T in powers of 2.
+  constexpr float LOG2E = 1.44269504f;
+  float m = -INFINITY, s = 0.f, t = 0.f;
+  auto load = [&](int c, RawLogits<T>& x) { load_logits(row, (long)c * LP_CHUNK - lead, p.vocab, x); };
+  auto take = [&](int c, const RawLogits<T>& raw) {
+    float x[LP_EPL], top[LP_EPL / N], m_new = m;
+#pragma unroll
+    for (int j = 0; j < LP_EPL; ++j) x[j] = logit_of(raw, j);
 #pragma unroll
     for (int j = 0; j < LP_EPL / N; ++j) {
       top[j] = x[j * N];
 #pragma unroll
       for (int e = 1; e < N; ++e) top[j] = nan_max(top[j], x[j * N + e]);
-      m = fmaxf(m, top[j]);
+      m_new = fmaxf(m_new, top[j]);
     }
     if (p.n_top > 0) {                                            // lane LPG q + j writes group q of the j-th loads
       float mine = 0.f;
@@ -299,17 +316,45 @@ __global__ void __launch_bounds__(256) logprobs_part_kernel(LogprobArgs p, int p
       if constexpr (ONE) sm_max[g] = mine;
       else p.part_max[(long)r * groups + g] = mine;
     }
-    a = log_sum_at(a, m);
-    const float mu = m == -INFINITY ? 0.f : m;
-#pragma unroll
-    for (int j = 0; j < LP_EPL; ++j) {
-      const float d = x[j] - mu, e = __expf(d);
-      a.s += e;
-      a.t += e * fmaxf(d, -200.f);                                // e is 0 there: -infinity adds 0
+    if (m_new > m) {
+      const float d = (m - m_new) * LOG2E, f = s == 0.f ? 0.f : __builtin_amdgcn_exp2f(d);
+      t = f > 0.f ? f * (t + d * s) : 0.f * t;
+      s *= f;
+      m = m_new;
     }
+    if (__all(fabsf(m) < 65536.f)) {
+      // one fused multiply and an exponential each: relative to the rounded m log2e, and then to m itself
+      const float base = m * LOG2E, off = fmaf(m, LOG2E, -base), back = __builtin_amdgcn_exp2f(-off);
+      float sc = 0.f, tc = 0.f;
 #pragma unroll
-    for (int j = 0; j < LP_EPL; ++j) x[j] = next[j];
+      for (int j = 0; j < LP_EPL; ++j) {
+        const float d = fmaf(x[j], LOG2E, -base), e = __builtin_amdgcn_exp2f(d);
+        sc += e;
+        tc = fmaf(e, fmaxf(d, -200.f), tc);                       // e is 0 there: -infinity adds 0
+      }
+      s += sc * back;
+      t += (tc - off * sc) * back;
+    } else {                                                      // where m log2e is no longer exact enough, or infinite
+      const float mu = m == -INFINITY ? 0.f : m;
+#pragma unroll 4
+      for (int j = 0; j < LP_EPL; ++j) {
+        const float d = (x[j] - mu) * LOG2E, e = __builtin_amdgcn_exp2f(d);
+        s += e;
+        t = fmaf(e, fmaxf(d, -200.f), t);
+      }
+    }
+  };
+  RawLogits<T> x, y;
+  int c = c0 + wave;
+  if (c < c1) load(c, x);
+  for (; c < c1; c += 8) {                                        // two buffers in turn
+    if (c + 4 < c1) load(c + 4, y);
+    take(c, x);
+    if (c + 4 >= c1) break;
+    if (c + 8 < c1) load(c + 8, x);
+    take(c + 4, y);
   }
+  LogSum a{m, s, t * 0.693147181f};
   a = log_sum_wave(a);
   if (lane == 0) sm[wave] = a;
   __syncthreads();

@@ -7,6 +7,7 @@ PyTorch provides device memory, pinned host memory and streams.  The library mus
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -675,6 +676,11 @@ def tree_attention(cache, rows, q, mask=None, out=None, scale=None, layer=0, str
     return out
 
 
+@functools.lru_cache(maxsize=256)
+def _logprobs_bytes(rows, vocab, n_top):
+    return lib.nova_logprobs_workspace_bytes(rows, vocab, n_top)
+
+
 def logprobs(logits, given=None, n_top=0, stream=None):
     """Of logit rows [rows, vocab] (fp32 or bf16): (log probabilities of ``given`` int32 [rows, n] or None, entropies
     [rows], the ``n_top`` (at most 32) largest log probabilities [rows, n_top] and their ids, or None)."""
@@ -701,7 +707,7 @@ def logprobs(logits, given=None, n_top=0, stream=None):
     if n_top:
         top_lp = buf.as_strided((rows, n_top), (n_top, 1), at)
         top_ids = buf.as_strided((rows, n_top), (n_top, 1), at + rows * n_top).view(torch.int32)
-    nbytes = lib.nova_logprobs_workspace_bytes(rows, vocab, n_top)
+    nbytes = _logprobs_bytes(rows, vocab, n_top)
     ws = _empty(logits, nbytes, torch.uint8, stream) if nbytes else None
     _check(lib.nova_logprobs(logits.data_ptr(), act, logits.stride(0) if rows > 1 else vocab, rows, vocab, _ptr(given), n_given, _ptr(lp),
                              entropy.data_ptr(), n_top, _ptr(top_lp), _ptr(top_ids), _ptr(ws), nbytes, _stream(stream)))

@@ -528,6 +528,8 @@ def test_far_blocks(gpu_lib):
 def _check_logprobs(x, given, k, got):
     lp, ent, tl, ti = got
     w, h = oc.logprobs(_np(x))
+    # results are float32: what is beyond its range by half a step (2^128 - 2^103, as -6e38 is) rounds to -infinity
+    w = np.where(w <= -(2.0 ** 128 - 2.0 ** 103), -np.inf, w)
     # a lane adds at most 32 numbers a time and their sums are joined: under 400 roundings of S and T, and of
     # x - m and log S one each; exponents are off by |x - m| 2^-23, which S weighs with e^(x - m) |x - m| < 0.4 (T: < 0.6)
     tol = lambda v: 400 * 2.0 ** -24 + 2.0 ** -22 * (np.abs(v) + 12 + np.abs(_np(x)).max(initial=0.0, where=np.isfinite(_np(x))))  # noqa: E731
@@ -571,6 +573,30 @@ def test_logprobs_ties_and_masked_tokens(gpu_lib, act, vocab):
     given = _dev(np.stack([np.arange(6) % vocab, np.full(6, vocab - 1)], 1), torch.int32)
     with np.errstate(divide="ignore"):
         _check_logprobs(xt, given, 32, gpu_lib.logprobs(xt, given=given, n_top=32))
+
+
+@pytest.mark.parametrize("vocab", [700, 20001])
+def test_logprobs_of_masked_rows(gpu_lib, vocab):
+    """Logits masked with the type's lowest value, some of a row or all of it, and rows far from zero."""
+    r = _rng(vocab, 3)
+    for act in (F32, BF16):
+        low = torch.finfo(act).min
+        x = torch.from_numpy(r.normal(size=(6, vocab)) * 3).cuda()
+        x[0, 5:] = low
+        x[1] = low
+        x[2, ::3] = low
+        x[3] += 1e6
+        x[4] = torch.where(x[4] > 0, 3e38, -3e38)
+        x[5] -= 70000
+        x = x.to(act)
+        given = torch.tensor([[0, vocab - 1]] * 6, dtype=torch.int32, device="cuda")
+        got = gpu_lib.logprobs(x, given=given, n_top=8)
+        _check_logprobs(x, given, 8, got)
+        # x - m is exact to its own rounding: the size of the logits themselves costs nothing where the unmasked are near
+        w, h = oc.logprobs(_np(x[:4]))
+        want = np.take_along_axis(w, got[3][:4].cpu().numpy().astype(int), 1)
+        assert (np.abs(_np(got[2][:4]) - want) <= 400 * 2.0 ** -24 + 2.0 ** -22 * (np.abs(want) + 12))[[0, 2, 3]].all()
+        assert (np.abs(_np(got[1][:4]) - h) <= 400 * 2.0 ** -24 + 2.0 ** -22 * (h + 12) + h * 400 * 2.0 ** -23).all()
 
 
 def test_logprobs_odd_values_ids_and_pitch(gpu_lib):
