@@ -224,6 +224,8 @@ int nova_llm_decode_noalloc(const nova_llm* llm, const int32_t* ids, const int32
  * rows are [n_heads][head_dim] contiguous at a pitch of their own (a multiple of 16 bytes, so q, k
  * and v may be views of one packed projection).  head_dim is 64 or 128.
  *
+ * Of one call: at most 8192 heads, 2^25 rows and 2^30 tokens of a sequence.
+ *
  * A cache layer of one of three types.  BF16 and F32 are a layer of a nova_kv pool.  E4M3 stores
  * 8 bits per value: token t of a KV head is D OCP e4m3 numbers and one byte e + 127, the values
  * being number * 2^e with the smallest e >= -100 that keeps |number| <= 448 (NaN and infinite values
@@ -290,6 +292,7 @@ int nova_kv_gather(const nova_cache* cache, const nova_rows* rows, const int32_t
  * (device uint64 [rows]; NULL: i <= j, a chain; one row per sequence is a decode step).  A row that
  * sees nothing gets zeros; what a row does not see has no effect on it, whatever it holds.
  *  q, out: device, bf16 (F32 with an F32 cache), n_q heads (a multiple of n_kv); scale is applied to q.k
+ *          (scores and the sums of p v, where p is up to 2^8, are fp32: V up to 2^88 is safe)
  *  ws:     device, nova_tree_attention_workspace_bytes(), 256-byte aligned; contents need not be kept
  *          or cleared, but calls that may overlap in time need one each */
 size_t nova_tree_attention_workspace_bytes(const nova_cache* cache, const nova_rows* rows, int n_q);
@@ -306,7 +309,7 @@ int nova_tree_attention(const nova_cache* cache, const nova_rows* rows, const ui
  *  top_lp, top_ids[row][n_top]: the most likely tokens, descending, equal ones by the lower id (NaN
  *                     counts as the largest); n_top <= 32 and <= vocab, 0: none
  * A logit of -infinity has probability 0.  A row with a NaN or +infinity, or with nothing but
- * -infinity, has NaN for every log probability of a token and for its entropy.  vocab <= 2^21.
+ * -infinity, has NaN for every log probability of a token and for its entropy.  vocab <= 2^21, rows <= 2^23.
  *  ws: device, nova_logprobs_workspace_bytes(), 256-byte aligned, as for nova_tree_attention */
 size_t nova_logprobs_workspace_bytes(int rows, int vocab, int n_top);
 int nova_logprobs(const void* logits, int type, int64_t pitch, int rows, int vocab, const int32_t* given, int n_given,

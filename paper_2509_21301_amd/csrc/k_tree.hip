@@ -724,8 +724,8 @@ static TreePlan tree_plan(int type, int n_kv, int n_q, int batch, int max_rows, 
   t.tiles = (rows + (t.wide ? 127 : 15)) / (t.wide ? 128 : 16);
   const int step = t.wide || type == CACHE_E4M3 ? 64 : 32;
   const int steps = (max_ctx + step - 1) / step;
-  const int want = (2 * cus + batch * n_kv * t.tiles - 1) / (batch * n_kv * t.tiles);
-  t.nsplit = std::max(1, std::min({want, 64, (steps + LEAST_STEPS - 1) / LEAST_STEPS}));
+  const long wgs = (long)batch * n_kv * t.tiles, want = (2L * cus + wgs - 1) / wgs;
+  t.nsplit = (int)std::max(1L, std::min({want, 64L, (steps + LEAST_STEPS - 1L) / LEAST_STEPS}));
   return t;
 }
 

@@ -709,10 +709,14 @@ nova::BatchRows batch_rows(const nova_rows& r) {
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 inline bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
 
+// Within these every launch grid and every index of the kernels fits.
+constexpr int MAX_HEADS = 8192, MAX_ROWS = 1 << 25, MAX_TOKENS = 1 << 30, MAX_LOGIT_ROWS = 1 << 23;
+
 int check_cache(const nova_cache* c) {
   if (!c) return fail(NOVA_EINVAL, "null cache");
   if (cache_elem(c->type) == 0) return fail(NOVA_EINVAL, "unknown cache type %d", c->type);
   if (c->num_blocks <= 0 || c->n_kv <= 0) return fail(NOVA_EINVAL, "cache: non-positive sizes");
+  if (c->n_kv > MAX_HEADS) return fail(NOVA_EUNSUPPORTED, "cache of %d heads (at most %d)", c->n_kv, MAX_HEADS);
   if (c->head_dim != 64 && c->head_dim != 128) return fail(NOVA_EUNSUPPORTED, "cache head_dim %d (supported: 64, 128)", c->head_dim);
   if (!c->k || !c->v || !aligned(c->k) || !aligned(c->v)) return fail(NOVA_EINVAL, "cache k and v must be non-null and 256-byte aligned");
   if (c->type == NOVA_CACHE_E4M3 && (!c->k_exp || !c->v_exp || !aligned16(c->k_exp) || !aligned16(c->v_exp)))
@@ -725,6 +729,8 @@ int check_rows(const nova_rows* r, bool tokens) {
   if (!r) return fail(NOVA_EINVAL, "null rows");
   if (r->batch <= 0 || r->batch > 65535 || r->rows < 0 || r->max_rows <= 0 || r->max_blocks <= 0 || r->max_ctx <= 0)
     return fail(NOVA_EINVAL, "rows: batch must be 1..65535, rows >= 0, max_rows, max_blocks and max_ctx positive");
+  if (r->rows > MAX_ROWS || r->max_ctx > MAX_TOKENS)
+    return fail(NOVA_EUNSUPPORTED, "rows: %d rows and %d tokens of a sequence (at most %d and %d)", r->rows, r->max_ctx, MAX_ROWS, MAX_TOKENS);
   if (!r->tables || !aligned4(r->tables) || !aligned4(r->row_start) || !aligned4(r->ctx))
     return fail(NOVA_EINVAL, "rows: tables is null, or an array is misaligned");
   if (!r->row_start && (int64_t)r->batch * r->max_rows != r->rows)
@@ -797,6 +803,7 @@ extern "C" int nova_kv_append(const nova_cache* cache, const nova_rows* rows, co
   if (int rc = check_matrix("v", v, v_pitch, cache->n_kv, D, act_elem(in_type))) return rc;
   if (q) {
     if (n_q <= 0) return fail(NOVA_EINVAL, "q without heads");
+    if (n_q > MAX_HEADS) return fail(NOVA_EUNSUPPORTED, "%d query heads (at most %d)", n_q, MAX_HEADS);
     if (int rc = check_matrix("q", q, q_pitch, n_q, D, act_elem(in_type))) return rc;
     if (int rc = check_matrix("q_out", q_out, q_out_pitch, n_q, D, act_elem(q_out_type))) return rc;
     if (q_out == q && (q_out_type != in_type || q_out_pitch != q_pitch)) return fail(NOVA_EINVAL, "q_out over q needs the same type and pitch");
@@ -835,7 +842,7 @@ int check_tree(const nova_cache* cache, const nova_rows* rows, int n_q) {
   if (int rc = check_rows(rows, true)) return rc;
   if (rows->max_rows > 64) return fail(NOVA_EUNSUPPORTED, "%d drafted tokens of one sequence (at most 64)", rows->max_rows);
   if (n_q <= 0 || n_q % cache->n_kv) return fail(NOVA_EINVAL, "n_q %d must be a positive multiple of n_kv %d", n_q, cache->n_kv);
-  if ((int64_t)rows->max_rows * n_q > (1 << 19)) return fail(NOVA_EUNSUPPORTED, "n_q %d is too large", n_q);
+  if (n_q > MAX_HEADS) return fail(NOVA_EUNSUPPORTED, "%d query heads (at most %d)", n_q, MAX_HEADS);
   return NOVA_OK;
 }
 }  // namespace
@@ -892,7 +899,7 @@ extern "C" int nova_logprobs(const void* logits, int type, int64_t pitch, int ro
   if (n_given > 0 && (!given || !given_lp || !aligned4(given) || !aligned4(given_lp))) return fail(NOVA_EINVAL, "given and given_lp must be non-null and aligned");
   if (n_top > 0 && (!top_lp || !top_ids || !aligned4(top_lp) || !aligned4(top_ids))) return fail(NOVA_EINVAL, "top_lp and top_ids must be non-null and aligned");
   if (!aligned4(entropy)) return fail(NOVA_EINVAL, "entropy is misaligned");
-  if ((int64_t)rows * ((vocab + 1023) / 1024 + 1) > 0x7fffffffLL) return fail(NOVA_EUNSUPPORTED, "%d rows of %d logits are too many for one call", rows, vocab);
+  if (rows > MAX_LOGIT_ROWS) return fail(NOVA_EUNSUPPORTED, "%d rows (at most %d)", rows, MAX_LOGIT_ROWS);
   size_t sums;
   const size_t need = logprobs_bytes(rows, vocab, n_top, &sums);
   if (ws_bytes < need) return fail(NOVA_ENOSPACE, "workspace %zu < required %zu bytes", ws_bytes, need);

@@ -414,6 +414,8 @@ class Llm:
             next_id = torch.empty(1, dtype=torch.int32, device=self.device)
         if isinstance(kv, Cache):
             kv._check_layers(self.cfg.layers)
+            _check_device(kv.device, vis, ids, table, next_id, logits)
+            _check_vector("table", table, torch.int32, (n_vis + n_text + 15) // 16)
             _check(lib.nova_llm_prefill_cache(self.h, _ptr(vis), n_vis, _ptr(ids), n_text, _ptr(table), kv.layer(0),
                                               _ptr(next_id), _ptr(logits), _ptr(ws), ws.numel(), _stream(stream)))
             return next_id
@@ -535,6 +537,8 @@ class Cache:
         layers, nb, n_kv, _, d = k.shape
         if v.shape != (layers, nb, n_kv, d, 16) or not k.is_contiguous() or not v.is_contiguous():
             raise ValueError(f"k and v must be contiguous, v {(layers, nb, n_kv, d, 16)}: got {tuple(v.shape)}")
+        if any(t is not None and t.device != k.device for t in (v, k_exp, v_exp)):
+            raise ValueError("k, v and their exponents must be on one device")
         self.type = types[k.dtype]
         if self.type == CACHE_E4M3:
             for t in (k_exp, v_exp):
@@ -578,6 +582,8 @@ class Rows:
             _check_vector(what, t, torch.int32, n)
             if t is not None and t.device != tables.device:
                 raise ValueError(f"{what} on {t.device}, tables on {tables.device}")
+        if any(not 0 <= n < 1 << 31 for n in (rows, max_rows, max_ctx)):
+            raise ValueError(f"rows {rows}, max_rows {max_rows} and max_ctx {max_ctx} must be 32-bit sizes")
         self.row_start, self.ctx, self.tables = row_start, ctx, tables
         self.batch, self.rows, self.max_rows, self.max_ctx = batch, rows, max_rows, max_ctx
         self._c = RowsC(_ptr(row_start), _ptr(ctx), _ptr(tables), max_blocks, batch, rows, max_rows, max_ctx)

@@ -174,6 +174,31 @@ def test_binding_checks():
         nova.logprobs(x)
 
 
+def test_sizes_beyond_a_launch():
+    """More heads, rows or tokens than a grid or an index holds are refused by each entry."""
+    big = dict(rows=1 << 26, max_rows=1 << 26, max_ctx=1 << 26, max_blocks=1 << 23, batch=1)
+    long = dict(max_ctx=(1 << 30) + 1, max_blocks=1 << 27)
+    for kw in (dict(c=_cache(n_kv=8193)), dict(n_q=8193, qp=8193 * 64, op=8193 * 64), dict(r=_rows(**big)), dict(r=_rows(**long))):
+        assert _append(**kw) == nova.EUNSUPPORTED, kw
+    for c, r in ((_cache(n_kv=8193), _rows()), (_cache(), _rows(**big)), (_cache(), _rows(**long))):
+        assert LIB.nova_kv_gather(C.byref(c), C.byref(r), FAKE, 0, FAKE, 1 << 20, FAKE, 1 << 20, None) == nova.EUNSUPPORTED
+    for n_q, r in ((8194, _rows()), (4, _rows(**long))):
+        assert LIB.nova_tree_attention(C.byref(_cache()), C.byref(r), None, FAKE, 1 << 20, n_q, 0.1, FAKE, 1 << 20, FAKE, 1 << 40,
+                                       None) == nova.EUNSUPPORTED
+    assert LIB.nova_logprobs(FAKE, 1, 64, (1 << 23) + 1, 64, None, 0, None, FAKE, 0, None, None, None, 0, None) == nova.EUNSUPPORTED
+    t = torch.zeros(2, 4, dtype=torch.int32)
+    for kw in (dict(max_ctx=(1 << 32) + 16), dict(max_rows=1 << 31), dict(rows=-1)):
+        with pytest.raises(ValueError):
+            nova.Rows(None, None, t, **kw)
+
+
+def test_cache_of_tensors_on_two_devices():
+    c = nova.Cache(4, 2, 64, device="cpu")
+    for kw in (dict(v=c.v.to("meta")), dict(k_exp=c.k_exp.to("meta")), dict(v_exp=c.v_exp.to("meta"))):
+        with pytest.raises(ValueError):
+            nova.Cache.of(**{**dict(k=c.k, v=c.v, k_exp=c.k_exp, v_exp=c.v_exp), **kw})
+
+
 def test_oracle_quantiser_against_torch():
     """The oracle's e4m3 rounding is torch's, and writing back what was read changes nothing."""
     g = np.random.default_rng(3)
