@@ -713,10 +713,15 @@ __global__ void __launch_bounds__(256) tree_combine_kernel(TreeArgs p, int nspli
     reinterpret_cast<T*>(p.out)[t * p.out_row + head * D + lane + 64 * d] = from_f<T>(L == 0.f ? 0.f : o[d] / L);
 }
 
-// The kernel, the workgroups that a KV head's rows take, and the splits of the context, of 4 steps at least:
-// as many as give every compute unit two workgroups.
+// The kernel, the workgroups that a KV head's rows take, and the splits of the context: as many as give every
+// compute unit two workgroups, of `least` steps at least.
+//  * few rows: 4, one for each wave (1530 tokens, 32 sequences: 2 and 3 steps cost up to 1.5 us more).
+//  * many rows: a split's steps follow one another (1.7 us each), but every split is one more to join.  While there are
+//    few workgroups short splits win (5 tokens behind 1000, one sequence: 10.9 us with 1, 14.2 with 4; 64 behind
+//    600: 16.5 with 1, 14.3 with 2, 16.0 with 4), with many of them 4 do (5 behind 8000: 18.0 with 2, 16.6 with 4): as
+//    many steps as keep the workgroups at half the compute units, 4 at most.
 constexpr int LEAST_STEPS = 4;
-struct TreePlan { bool wide; int tiles, nsplit; };
+struct TreePlan { bool wide; int tiles, nsplit, least; };
 static TreePlan tree_plan(int type, int n_kv, int n_q, int batch, int max_rows, int max_ctx, int cus) {
   TreePlan t;
   const int rows = max_rows * (n_q / n_kv);
@@ -725,7 +730,8 @@ static TreePlan tree_plan(int type, int n_kv, int n_q, int batch, int max_rows, 
   const int step = t.wide || type == CACHE_E4M3 ? 64 : 32;
   const int steps = (max_ctx + step - 1) / step;
   const long wgs = (long)batch * n_kv * t.tiles, want = (2L * cus + wgs - 1) / wgs;
-  t.nsplit = (int)std::max(1L, std::min({want, 64L, (steps + LEAST_STEPS - 1L) / LEAST_STEPS}));
+  t.least = t.wide ? (int)std::min<long>(LEAST_STEPS, std::max(1L, (2 * wgs * steps + cus - 1) / cus)) : LEAST_STEPS;
+  t.nsplit = (int)std::max(1L, std::min({want, 64L, (steps + t.least - 1L) / t.least}));
   return t;
 }
 
@@ -739,10 +745,10 @@ static hipError_t tree_launch(const TreeArgs& p, const TreePlan& t, hipStream_t 
   typedef typename TreeT<CT>::act T;
   const dim3 grid(t.nsplit, p.c.n_kv * t.tiles, p.r.batch);
   if constexpr (sizeof(CT) < 4) {
-    if (t.wide) hipLaunchKernelGGL((tree_wide_kernel<CT, D>), grid, dim3(256), 0, s, p, LEAST_STEPS);
-    else hipLaunchKernelGGL((tree_attn_kernel<CT, D>), grid, dim3(256), 0, s, p, LEAST_STEPS);
+    if (t.wide) hipLaunchKernelGGL((tree_wide_kernel<CT, D>), grid, dim3(256), 0, s, p, t.least);
+    else hipLaunchKernelGGL((tree_attn_kernel<CT, D>), grid, dim3(256), 0, s, p, t.least);
   } else {
-    hipLaunchKernelGGL((tree_attn_kernel<CT, D>), grid, dim3(256), 0, s, p, LEAST_STEPS);
+    hipLaunchKernelGGL((tree_attn_kernel<CT, D>), grid, dim3(256), 0, s, p, t.least);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || t.nsplit == 1) return e;
