@@ -120,9 +120,11 @@ template <int W> struct TopShared {
 //  1. The groups are dealt to 64 sets (one per lane number).  The k-th largest of the sets' maxima bounds
 //     the k-th logit of the row from below, and few groups reach it: some 64 ln(64 / (64 - k)).
 //  2. Their logits that reach it are ranked by counting the larger ones.
-//  3. Where too many reach it (equal values, or the best ones side by side), and where the row holds a NaN,
-//     the k-th group is bisected exactly, on its maximum and its number, and the logits of the best k
-//     groups that are not below its maximum are ranked: at most 16 k.
+//  3. Where more reach it (a row that is masked but for a few tokens), those above it are taken, and if they are
+//     fewer than k, the first ones that equal it.
+//  4. Where even those above it are too many (the best ones side by side), and where the row holds a NaN, the k-th
+//     group is bisected exactly, on its maximum and its number, and the logits of the best k groups that are not
+//     below its maximum are ranked: at most 16 k.
 // A thread takes V groups at a time; the first AHEAD times V are requested before anything waits.
 template <typename T, int W, int V, int AHEAD>
 struct RowTop {
@@ -189,6 +191,40 @@ struct RowTop {
     return sm.m;
   }
 
+  // The first groups with the maximum `value` (k - have of them at least), into sm.group from `have` up to k.
+  NOVA_DEV void first_equal(float value, int have, int k, TopShared<W>& sm) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+#pragma unroll 1
+    for (int g0 = 0; g0 < groups && have < k; g0 += STRIDE) {
+      float m[V];
+      take(g0 + V * tid, m);
+      int mine = 0, upto;
+#pragma unroll
+      for (int q = 0; q < V; ++q) mine += g0 + V * tid + q < groups && m[q] == value;
+      upto = mine;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int up = __shfl_up(upto, o, 64);
+        if (lane >= o) upto += up;
+      }
+      if (lane == 63) sm.count[wave] = upto;
+      __syncthreads();
+      int at = have + upto - mine;
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        at += w < wave ? sm.count[w] : 0;
+        have += sm.count[w];
+      }
+#pragma unroll
+      for (int q = 0; q < V; ++q) {
+        if (!(g0 + V * tid + q < groups && m[q] == value)) continue;
+        if (at < k) sm.group[at] = g0 + V * tid + q;
+        ++at;
+      }
+      __syncthreads();
+    }
+  }
+
   NOVA_DEV void operator()(const LogSum& a, float log_s, TopShared<W>& sm) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, k = p.n_top;
     float best = -INFINITY;
@@ -209,12 +245,12 @@ struct RowTop {
     for (int l = 0; l < 64; ++l) above += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(best), l)) > best;
     const float tau = -wave_max(above < k ? -best : -INFINITY);
     int n = LP_CAND + 1;
-    if (!nan) {
+    // the groups whose maximum is above `least`, or with `equal` not below it: how many
+    auto reach = [&](float least, bool equal) {
       auto put = [&](float m, int g) {
-        if (m >= tau) {
-          const int to = atomicAdd(&sm.n, 1);
-          if (to < LP_CAND) sm.group[to] = g;
-        }
+        if (!(m > least || (equal && m == least))) return;
+        const int to = atomicAdd(&sm.n, 1);
+        if (to < LP_CAND) sm.group[to] = g;
       };
 #pragma unroll
       for (int e = 0; e < AHEAD; ++e)
@@ -226,8 +262,24 @@ struct RowTop {
           if (g >= AHEAD * STRIDE) put(m, g);
         });
       __syncthreads();
-      n = sm.n;
-      if (n <= LP_CAND) n = logits_of(n, order_key(tau), sm);
+      return sm.n;
+    };
+    if (!nan) {
+      n = reach(tau, true);
+      if (n <= 64 + k) {
+        n = logits_of(n, order_key(tau), sm);
+      } else {
+        __syncthreads();
+        if (tid == 0) sm.n = 0;
+        __syncthreads();
+        n = reach(tau, false);
+        if (n < k) {
+          first_equal(tau, n, k, sm);
+          n = logits_of(k, order_key(tau), sm);
+        } else if (n <= LP_CAND) {
+          n = logits_of(n, order_key(tau) + 1, sm);
+        }
+      }
     }
     if (n > LP_CAND) {
       // the largest bound that k groups reach (there are 64 at least): exactly k, since keys differ
@@ -324,9 +376,10 @@ __global__ void __launch_bounds__(256) logprobs_part_kernel(LogprobArgs p, int p
       s *= f;
       m = m_new;
     }
-    if (__all(fabsf(m) < 65536.f)) {
+    const float mu = m == -INFINITY ? 0.f : m;                    // nothing but -infinity yet: every e is 0
+    if (__all(fabsf(mu) < 65536.f)) {
       // one fused multiply and an exponential each: relative to the rounded m log2e, and then to m itself
-      const float base = m * LOG2E, off = fmaf(m, LOG2E, -base), back = __builtin_amdgcn_exp2f(-off);
+      const float base = mu * LOG2E, off = fmaf(mu, LOG2E, -base), back = __builtin_amdgcn_exp2f(-off);
       float sc = 0.f, tc = 0.f;
 #pragma unroll
       for (int j = 0; j < LP_EPL; ++j) {
@@ -337,7 +390,6 @@ __global__ void __launch_bounds__(256) logprobs_part_kernel(LogprobArgs p, int p
       s += sc * back;
       t += (tc - off * sc) * back;
     } else {                                                      // where m log2e is no longer exact enough, or infinite
-      const float mu = m == -INFINITY ? 0.f : m;
 #pragma unroll 4
       for (int j = 0; j < LP_EPL; ++j) {
         const float d = (x[j] - mu) * LOG2E, e = __builtin_amdgcn_exp2f(d);

@@ -599,6 +599,31 @@ def test_logprobs_of_masked_rows(gpu_lib, vocab):
         assert (np.abs(_np(got[1][:4]) - h) <= 400 * 2.0 ** -24 + 2.0 ** -22 * (h + 12) + h * 400 * 2.0 ** -23).all()
 
 
+@pytest.mark.parametrize("vocab", [700, 9001, 152064])
+def test_logprobs_of_few_tokens_left(gpu_lib, vocab):
+    """Rows masked but for 0 to 300 tokens side by side, which may be fewer than the alternatives asked for; and rows
+    whose largest logits are all in groups that a few lanes of a wave look at."""
+    r = _rng(vocab, 5)
+    for act in (F32, BF16):
+        for low in (-np.inf, torch.finfo(act).min, -1e4):
+            x = np.full((8, vocab), low)
+            for i, n in enumerate((1, 5, 19, 31, 32, 40, 300)):
+                at = (0, vocab - n, 77)[i % 3]
+                x[i, at:at + n] = r.normal(size=n)
+            if low == -np.inf:
+                x[7, 0] = 1.0                                     # a row of nothing else has no distribution
+            xt = _dev(x, act)
+            given = torch.tensor([[0, vocab - 1]] * 8, dtype=torch.int32, device="cuda")
+            with np.errstate(divide="ignore"):
+                for k in (32, 7):
+                    _check_logprobs(xt, given, k, gpu_lib.logprobs(xt, given=given, n_top=k))
+        x = r.normal(size=(3, vocab))
+        x[:, (np.arange(vocab) // 64) % 64 < 19] += 10
+        x[2] = np.round(x[2])
+        xt = _dev(x, act)
+        _check_logprobs(xt, None, 20, gpu_lib.logprobs(xt, n_top=20))
+
+
 def test_logprobs_odd_values_ids_and_pitch(gpu_lib):
     nova = gpu_lib
     x = torch.randn(5, 3001, device="cuda")
