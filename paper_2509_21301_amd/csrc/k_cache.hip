@@ -291,6 +291,9 @@ template <typename CT> NOVA_DEV void cached8(const CT* p, float scale, float* x)
   }
 }
 
+NOVA_DEV float cached1(e4m3_t x, float scale) { return __uint_as_float(e4m3_pair<false>(x.v, scale) << 16); }
+template <typename T> NOVA_DEV float cached1(T x, float) { return to_f<T>(x); }
+
 // Consecutive rows: workgroup (block of 16 slots, group of K and V heads), a wave per head.  K rows are
 // copied with 8 elements per lane; a V block [D][16] is read whole, 16 tokens per lane, and turned
 // through wave-private LDS.  Rows whose block is missing read as zeros.  Bound by HBM: 32 sequences of 1846
@@ -343,17 +346,21 @@ __global__ void __launch_bounds__(256) kv_gather_kernel(GatherArgs p) {
   }
 }
 
-// Rows by token number: workgroup (group of rows, group of heads), D / 8 lanes per row and head; the 8 V
-// elements of a lane lie 16 elements apart.  For a handful of accepted tokens: bound by latency (eight
-// sequences' accepted tokens, 36 at most, of 4 KV heads: 4.3 us).
+// Rows by token number: workgroup (group of rows, group of heads), D / 8 lanes per row and head.  A V row lies 16
+// elements apart, so its lanes take one element each, neighbours side by side: a load touches 16 (e4m3) or 32
+// (bf16) lines of 64 bytes, not 64 as with 8 elements a lane.  For a handful of accepted tokens bound by latency (eight
+// sequences' accepted tokens, 36 of 4 KV heads: 4.3 us), for many by V's lines, of which a token uses a sixteenth
+// (32 sequences' 750 to 1500 tokens anywhere among 2000, e4m3: 49.8 us, 64.5 with 8 elements a lane; bf16 67.5 and 73).
 template <typename CT, typename TO, int D>
 __global__ void __launch_bounds__(256) kv_pick_kernel(GatherArgs p) {
   constexpr int LPR = D / 8, ROWS = 64 / LPR;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int sub = lane % LPR, n_kv = p.c.n_kv;
-  const int r = blockIdx.x * ROWS + lane / LPR, h = blockIdx.y * 4 + wave;
-  if (r >= p.r.rows || h >= 2 * n_kv) return;
-  int b;
+  const int r0 = blockIdx.x * ROWS, r = r0 + lane / LPR, h = blockIdx.y * 4 + wave;
+  if (h >= 2 * n_kv) return;
+  const bool is_k = h < n_kv;
+  const int hh = is_k ? h : h - n_kv;
+  int b = 0;
   if (p.r.row_start) {                                   // sequences that end at or before row r
     int lo = 0, hi = p.r.batch;
     while (lo < hi) {
@@ -365,29 +372,43 @@ __global__ void __launch_bounds__(256) kv_pick_kernel(GatherArgs p) {
   } else {
     b = r / p.r.max_rows;
   }
-  if (b >= p.r.batch) return;
-  const SeqRows sr = seq_rows(p.r, b);
-  if (r < sr.r0 || r >= sr.r0 + sr.n) return;
-  const bool is_k = h < n_kv;
-  const int hh = is_k ? h : h - n_kv;
-  const int t = p.slots[r];
-  const int ph = t < 0 ? -1 : page_of(p.r, p.c.num_blocks, b, t / PAGE);
-  float x[8] = {};
-  if (ph >= 0) {
-    const int slot = t % PAGE;
-    const size_t tok0 = ((size_t)ph * n_kv + hh) * PAGE;
-    float scale = 1.f;
-    if constexpr (sizeof(CT) == 1) scale = exp_scale((is_k ? p.c.k_exp : p.c.v_exp)[tok0 + slot]);
-    if (is_k) {
-      cached8(reinterpret_cast<const CT*>(p.c.k) + (tok0 + slot) * D + 8 * sub, scale, x);
-    } else {
-      __align__(16) CT v[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = reinterpret_cast<const CT*>(p.c.v)[tok0 * D + (size_t)(8 * sub + e) * PAGE + slot];
-      cached8(v, scale, x);
-    }
+  bool live = r < p.r.rows && b < p.r.batch;
+  int ph = -1, slot = 0;
+  if (live) {
+    const SeqRows sr = seq_rows(p.r, b);
+    live = r >= sr.r0 && r < sr.r0 + sr.n;
+    const int t = live ? p.slots[r] : -1;
+    ph = t < 0 ? -1 : page_of(p.r, p.c.num_blocks, b, t / PAGE);
+    slot = t < 0 ? 0 : t % PAGE;
   }
-  store8(reinterpret_cast<TO*>(is_k ? p.k : p.v) + r * (is_k ? p.k_row : p.v_row) + hh * D + 8 * sub, x);
+  const size_t tok = ((size_t)max(ph, 0) * n_kv + hh) * PAGE + slot;
+  float scale = 1.f;
+  if constexpr (sizeof(CT) == 1)
+    if (ph >= 0) scale = exp_scale((is_k ? p.c.k_exp : p.c.v_exp)[tok]);
+  if (is_k) {
+    if (!live) return;
+    float x[8] = {};
+    if (ph >= 0) cached8(reinterpret_cast<const CT*>(p.c.k) + tok * D + 8 * sub, scale, x);
+    store8(reinterpret_cast<TO*>(p.k) + r * p.k_row + hh * D + 8 * sub, x);
+    return;
+  }
+  CT v[ROWS][D / 64];
+  float x[ROWS];
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {                       // the rows' loads together
+    const int phi = __shfl(ph, i * LPR, 64), si = __shfl(slot, i * LPR, 64);
+    x[i] = phi >= 0 ? __shfl(scale, i * LPR, 64) : 0.f;
+    const CT* vb = reinterpret_cast<const CT*>(p.c.v) + ((size_t)max(phi, 0) * n_kv + hh) * PAGE * D + si;
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) v[i][j] = vb[(size_t)(lane + 64 * j) * PAGE];
+  }
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    if (!__shfl((int)live, i * LPR, 64)) continue;
+    TO* out = reinterpret_cast<TO*>(p.v) + (long)(r0 + i) * p.v_row + hh * D + lane;
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) out[64 * j] = from_f<TO>(x[i] != 0.f ? cached1(v[i][j], x[i]) : 0.f);
+  }
 }
 
 template <typename CT, typename TO, int D>
