@@ -494,7 +494,7 @@ def _check_device(dev, *tensors):
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise ValueError(f"tensors on {t.device} and on device {dev}")
-    if dev < 0 or dev != torch.cuda.current_device():
+    if dev < 0 or dev != torch._C._cuda_getDevice():
         raise ValueError(f"tensors on device {dev}, which is not the current one")
 
 
@@ -504,6 +504,19 @@ def _empty(like, shape, dtype, stream):
         return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
         return like.new_empty(shape, dtype=dtype)
+
+
+def _dense_like(t, stream):
+    """Contiguous memory of t's shape and type, as ``_empty`` (a third faster)."""
+    if stream is None:
+        return torch.empty_like(t, memory_format=torch.contiguous_format)
+    with torch.cuda.stream(stream):
+        return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
+def _stream_on(dev, stream):
+    """``_stream`` for a call whose tensors are known to be on the current device."""
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
 class Cache:
@@ -623,7 +636,7 @@ def kv_append(cache, rows, k, v, q=None, pos=None, rope=None, q_out=None, layer=
         n_q = q.shape[1] if q.dim() == 3 else 0
         act_q, q_pitch = _check_rows_of("q", q, n, n_q, d)
         if q_out is None:
-            q_out, act_out, out_pitch = _empty(q, (n, n_q, d), q.dtype, stream), act_q, n_q * d
+            q_out, act_out, out_pitch = _dense_like(q, stream), act_q, n_q * d
         else:
             act_out, out_pitch = _check_rows_of("q_out", q_out, n, n_q, d)
     elif q_out is not None:
@@ -631,7 +644,8 @@ def kv_append(cache, rows, k, v, q=None, pos=None, rope=None, q_out=None, layer=
     if act_v != act or act_q != act:
         raise ValueError("q, k and v must have one type")
     _check(lib.nova_kv_append(cache.layer(layer), rows.ref, rope.ref if rope is not None else None, _ptr(pos), act, _ptr(q), q_pitch,
-                              n_q, k.data_ptr(), k_pitch, v.data_ptr(), v_pitch, _ptr(q_out), act_out, out_pitch, _stream(stream)))
+                              n_q, k.data_ptr(), k_pitch, v.data_ptr(), v_pitch, _ptr(q_out), act_out, out_pitch,
+                              _stream_on(cache.device, stream)))
     return q_out
 
 
@@ -655,7 +669,7 @@ def kv_gather(cache, rows, slots=None, k_out=None, v_out=None, dtype=torch.bfloa
     if v_out is None:
         v_out = _empty(cache.k, (n, cache.n_kv, d), dtype, stream)
     _check(lib.nova_kv_gather(cache.layer(layer), rows.ref, _ptr(slots), act, k_out.data_ptr(), k_pitch, v_out.data_ptr(), v_pitch,
-                              _stream(stream)))
+                              _stream_on(cache.device, stream)))
     return k_out, v_out
 
 
@@ -670,7 +684,7 @@ def tree_attention(cache, rows, q, mask=None, out=None, scale=None, layer=0, str
     act, q_pitch = _check_rows_of("q", q, n, n_q, d)
     act_out, out_pitch = act, n_q * d
     if out is None:
-        out = _empty(q, (n, n_q, d), q.dtype, stream)
+        out = _dense_like(q, stream)
     else:
         act_out, out_pitch = _check_rows_of("out", out, n, n_q, d)
     if q.dtype != cache.dtype or act_out != act:
@@ -678,7 +692,8 @@ def tree_attention(cache, rows, q, mask=None, out=None, scale=None, layer=0, str
     nbytes = rows._tree_bytes(cache, n_q)
     ws = _empty(q, nbytes, torch.uint8, stream) if nbytes else None
     _check(lib.nova_tree_attention(cache.layer(layer), rows.ref, _ptr(mask), q.data_ptr(), q_pitch, n_q,
-                                   d ** -0.5 if scale is None else scale, out.data_ptr(), out_pitch, _ptr(ws), nbytes, _stream(stream)))
+                                   d ** -0.5 if scale is None else scale, out.data_ptr(), out_pitch, _ptr(ws), nbytes,
+                                   _stream_on(cache.device, stream)))
     return out
 
 
@@ -701,10 +716,11 @@ def logprobs(logits, given=None, n_top=0, stream=None):
         if given.dtype != torch.int32 or given.dim() != 2 or given.shape[0] != rows or not given.is_contiguous():
             raise ValueError(f"given must be contiguous int32 [{rows}, n], got {given.dtype} {tuple(given.shape)}")
         n_given = given.shape[1]
-    _check_device(logits.get_device(), given)
+    dev = logits.get_device()
+    _check_device(dev, given)
     n_top = min(n_top, vocab)
     # one allocation for what is returned, cut into dense matrices
-    buf = _empty(logits, (rows * (n_given + 1 + 2 * n_top),), torch.float32, stream)
+    buf = _empty(logits, rows * (n_given + 1 + 2 * n_top), torch.float32, stream)
     at = rows * n_given
     lp = buf.as_strided((rows, n_given), (n_given, 1), 0) if given is not None else None
     entropy = buf.as_strided((rows,), (1,), at)
@@ -716,7 +732,7 @@ def logprobs(logits, given=None, n_top=0, stream=None):
     nbytes = _logprobs_bytes(rows, vocab, n_top)
     ws = _empty(logits, nbytes, torch.uint8, stream) if nbytes else None
     _check(lib.nova_logprobs(logits.data_ptr(), act, logits.stride(0) if rows > 1 else vocab, rows, vocab, _ptr(given), n_given, _ptr(lp),
-                             entropy.data_ptr(), n_top, _ptr(top_lp), _ptr(top_ids), _ptr(ws), nbytes, _stream(stream)))
+                             entropy.data_ptr(), n_top, _ptr(top_lp), _ptr(top_ids), _ptr(ws), nbytes, _stream_on(dev, stream)))
     return lp, entropy, top_lp, top_ids
 
 
