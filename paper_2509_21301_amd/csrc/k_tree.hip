@@ -724,7 +724,10 @@ __global__ void __launch_bounds__(256) tree_combine_kernel(TreeArgs p, int nspli
 
 // The kernel, the workgroups that a KV head's rows take, and the splits of the context: as many as give every
 // compute unit two workgroups, of `least` steps at least.
-//  * few rows: 4, one for each wave (1530 tokens, 32 sequences: 2 and 3 steps cost up to 1.5 us more).
+//  * few rows: 4, one for each wave (1530 tokens, 32 sequences: 2 and 3 steps cost up to 1.5 us more).  A context of two
+//    steps a wave is not split, nor one of four where the workgroups fill half the compute units (one token behind
+//    400 in e4m3: 8.9 us, and 10.1 with two splits and their join; 32 sequences of one behind 1000: 13.0 and 14.6; but
+//    one behind 1000: 11.8 and 10.7).
 //  * many rows: a split's steps follow one another (1.7 us each), but every split is one more to join.  While there are
 //    few workgroups short splits win (5 tokens behind 1000, one sequence: 10.9 us with 1, 14.2 with 4; 64 behind
 //    600: 16.5 with 1, 14.3 with 2, 16.0 with 4), with many of them 4 do (5 behind 8000: 18.0 with 2, 16.6 with 4): as
@@ -739,7 +742,8 @@ static TreePlan tree_plan(int type, int n_kv, int n_q, int batch, int max_rows, 
   const int step = t.wide || type == CACHE_E4M3 ? 64 : 32;
   const int steps = (max_ctx + step - 1) / step;
   const long wgs = (long)batch * n_kv * t.tiles, want = (2L * cus + wgs - 1) / wgs;
-  t.least = t.wide ? (int)std::min<long>(LEAST_STEPS, std::max(1L, (2 * wgs * steps + cus - 1) / cus)) : LEAST_STEPS;
+  if (t.wide) t.least = (int)std::min<long>(LEAST_STEPS, std::max(1L, (2 * wgs * steps + cus - 1) / cus));
+  else t.least = steps <= 8 || (steps <= 16 && 2 * wgs >= cus) ? std::max(steps, LEAST_STEPS) : LEAST_STEPS;
   t.nsplit = (int)std::max(1L, std::min({want, 64L, (steps + t.least - 1L) / t.least}));
   return t;
 }
