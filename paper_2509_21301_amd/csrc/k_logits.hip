@@ -330,7 +330,7 @@ struct RowTop {
 // Workgroup (part of a row), its waves taking chunks of 1024 logits in turn, the next one's loads in
 // flight.  ONE: the part is the whole row, and the workgroup finishes it (4096 logits: 5.7 us, a chain of loads,
 // reductions and barriers).  Bound by HBM for many rows: 601 of 152064 in bf16 38.5 us, 4.8 TB/s; 32 of 152064
-// in fp32 7.2 us, of which 3.9 are their bytes at a large copy's rate and the rest launch, ramp and drain.
+// in fp32 7.1 us, of which 3.9 are their bytes at a large copy's rate and the rest launch, ramp and drain.
 template <typename T, bool ONE>
 __global__ void __launch_bounds__(256) logprobs_part_kernel(LogprobArgs p, int parts, int chunks, int groups) {
   constexpr int N = 16 / sizeof(T), LPG = LP_GROUP / N;           // a load's logits, lanes that share a group
@@ -429,7 +429,7 @@ __global__ void __launch_bounds__(256) logprobs_part_kernel(LogprobArgs p, int p
 }
 
 // Workgroup (row): the parts' sums joined, the most likely tokens from the groups' maxima.  Bound by latency:
-// 32 rows of 152064 with 20 tokens 7.4 us (9504 maxima, a bound, 20 groups, a rank), 601 rows without tokens 4.8 us.
+// 32 rows of 152064 with 20 tokens 6.7 us (9504 maxima, a bound, 20 groups, a rank), 601 rows without tokens 4.8 us.
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(TOP ? 512 : 64) logprobs_join_kernel(LogprobArgs p, int parts, int groups) {
   const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63;

@@ -81,8 +81,8 @@ NOVA_DEV int split_steps(int nsteps, int nsplit, int least) { return max(least, 
 // ------------------------------------------------------------------ few rows
 // One tile of 16 rows: bound by the cache's bytes.  The waves of a workgroup take steps in turn, each from
 // memory to its own registers (K of the next step is requested once S is formed, V once it is used).  32 single
-// tokens of 28/4 heads of 128 behind 2700 to 3627 e4m3 tokens: 106 MB in 24.5 us, 4.3 TB/s where a large copy
-// reaches 5.0.  The fp32 cache's calls are small: 5 tokens behind 96, 6.9 us of latency.
+// tokens of 28/4 heads of 128 behind 2700 to 3627 e4m3 tokens: 106 MB in 23.4 to 24.6 us, 4.4 TB/s where a large copy
+// reaches 5.0.  The fp32 cache's calls are small: 5 tokens behind 96, 6.8 us of latency.
 template <typename CT, int D>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
 tree_attn_kernel(TreeArgs p, int least) {
