@@ -375,6 +375,24 @@ def test_tree_long_context_splits(gpu_lib, kind, n_q, n_kv, d):
 
 
 @pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("n", [1, 5, 40])
+def test_tree_where_splits_begin(gpu_lib, kind, n):
+    """Contexts about the lengths from which they are cut, in one, two or more steps a split, alone, beside a shorter
+    sequence, and with a bound on the length that is larger than any."""
+    nova = gpu_lib
+    n_q, n_kv, d = 8, 2, 64
+    for ctx in (60, 127, 190, 256, 300, 511, 512, 700, 1100):
+        for other in (None, 17):
+            ctxs = [ctx] if other is None else [ctx, other]
+            bt = Batch(nova, ctxs, [n] * len(ctxs), n_kv, d, kind, seed=ctx).fill(ctx, stale=float("nan"))
+            q = _dev(_rng(ctx, n).normal(size=(bt.total, n_q, d)), bt.cache.dtype)
+            _check_tree(bt, q, None, nova.tree_attention(bt.cache, bt.desc, q), d ** -0.5)
+            most = 16 * bt.desc.tables.shape[1]
+            loose = nova.Rows(bt.desc.row_start, bt.desc.ctx, bt.desc.tables, rows=bt.total, max_rows=64, max_ctx=max(most, 64))
+            _check_tree(bt, q, None, nova.tree_attention(bt.cache, loose, q), d ** -0.5)
+
+
+@pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("ctx", [0, 30, 2000])
 @pytest.mark.parametrize("n_q,n", [(4, 20), (2, 14)])
 def test_tree_unseen_tokens_have_no_effect(gpu_lib, kind, ctx, n_q, n):
