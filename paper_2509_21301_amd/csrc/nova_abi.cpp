@@ -1070,19 +1070,21 @@ int llm_decode_t(const nova_llm* m, const int* ids, const int* pos, const int* t
   const bf16_t* final_gain = (const bf16_t*)(hw + m->head.off[0]);
   // the QKV projection's output: split-K slabs for the fused attention, finished rows for a verify step
   float* qkv_out = sp_qkv > 1 && !vf ? nullptr : d.qkv;
+  nova::AppendArgs app{};                // of a verify step: the same in every layer but for the cache
+  if (vf) {
+    app.r = batch_rows(*vf->rows);
+    app.pos = pos;
+    app.q = d.qkv, app.k = d.qkv + qd, app.v = d.qkv + qd + c.n_kv * D;
+    app.q_row = app.k_row = app.v_row = m->qkvw, app.n_q = c.n_q;
+    app.q_out = vb.q, app.q_out_row = qd;
+    app.in_f32 = true, app.q_out_f32 = f32;
+    set_rope(app, nova_rope{D, 0, c.rope_theta, 1.f, 0, 1.f, 32.f, 1.f});
+  }
   auto attention_block = [&](int l) -> int {
     if (vf) {
-      nova::AppendArgs a{};
-      a.c = pool_layer(*vf->pool, l);
-      a.r = batch_rows(*vf->rows);
-      a.pos = pos;
-      a.q = d.qkv, a.k = d.qkv + qd, a.v = d.qkv + qd + c.n_kv * D;
-      a.q_row = a.k_row = a.v_row = m->qkvw, a.n_q = c.n_q;
-      a.q_out = vb.q, a.q_out_row = qd;
-      a.in_f32 = true, a.q_out_f32 = f32;
-      set_rope(a, nova_rope{D, 0, c.rope_theta, 1.f, 0, 1.f, 32.f, 1.f});
-      CALL(NOVA_KIND_MISC, s, nova::kv_append(a, cus, s));
-      nova::TreeArgs t{a.c, a.r, (const unsigned long long*)vf->mask, vb.q, qd, c.n_q, 1.0f / sqrtf((float)D), d.att, qd, vb.part};
+      app.c = pool_layer(*vf->pool, l);
+      CALL(NOVA_KIND_MISC, s, nova::kv_append(app, cus, s));
+      nova::TreeArgs t{app.c, app.r, (const unsigned long long*)vf->mask, vb.q, qd, c.n_q, 1.0f / sqrtf((float)D), d.att, qd, vb.part};
       CALL(NOVA_KIND_DECODE_ATTN, s, nova::tree_attention(t, cus, s));
       return (int)NOVA_OK;
     }
