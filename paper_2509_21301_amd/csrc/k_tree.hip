@@ -344,11 +344,16 @@ tree_attn_kernel(TreeArgs p, int least) {
 // 16-byte pieces are swizzled by their row so that a read covers every bank once.
 // Two sequences of 64 and 48 tokens behind 32700 and 28613 (28/4 heads of 128, e4m3): 5.0e10 operations in
 // 87 us, 0.57 PFLOP/s; a step of the two workgroups of a compute unit takes 2.8 us, its MFMAs 1.0 and its
-// LDS accesses 1.7 of them, the exponentials, conversions and sums of a wave about as much as its MFMAs.  64 rows a wave halve the LDS reads, but
-// leave one wave a SIMD, whose vector instructions issue every 5 clocks instead of 4 and wait alone: 116 us.
+// LDS accesses 1.7 of them, the exponentials, conversions and sums of a wave about as much as its MFMAs.
+// 64 rows a wave halve the LDS reads, but leave one wave a SIMD, whose vector instructions issue every 5 clocks
+// instead of 4 and wait alone: 116 us.
 // Eight sequences of 9 to 16 tokens behind 1222 to 1564 (bf16): 17 us, four steps of 1.7 us, the rest
 // launch and first loads.
-template <typename CT, int D>
+// HALF (up to 64 rows): waves 0 and 1 take the first 32 tokens of every step, waves 2 and 3 the others for the same
+// rows, and the pairs join at the end.  Five tokens of 28/4 heads (35 rows), 32 sequences behind 1800 e4m3 tokens:
+// 24.9 us, with two waves idle 27.9; one sequence behind 30000 25.8 and 28.1; but where a workgroup has a step or
+// two the join costs 0.4 us more than it gains.
+template <typename CT, int D, bool HALF>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
 tree_wide_kernel(TreeArgs p, int least) {
   constexpr bool Q8 = sizeof(CT) == 1;
@@ -368,14 +373,14 @@ tree_wide_kernel(TreeArgs p, int least) {
   const int split = blockIdx.x, kvh = blockIdx.y % n_kv, tile = blockIdx.y / n_kv, b = blockIdx.z;
   const int col = lane & 31, half = lane >> 5;
   const SeqRows sr = seq_rows(p.r, b);
-  const int nrow = sr.n * G, row0 = tile * 128;
+  const int nrow = sr.n * G, row0 = tile * 128, rows_of = HALF ? wave & 1 : wave, second = HALF ? wave >> 1 : 0;
   if (row0 >= nrow) return;
   const int total = sr.ctx + sr.n;
   const int nsteps = (total + STEP - 1) / STEP;
   const int per = split_steps(nsteps, gridDim.x, least);
   const int step0 = split * per, step1 = min(step0 + per, nsteps);
-  const bool active = row0 + 32 * wave < nrow;
-  const int row = row0 + 32 * wave + col, rc = min(row, nrow - 1);
+  const bool active = row0 + 32 * rows_of < nrow;
+  const int row = row0 + 32 * rows_of + col, rc = min(row, nrow - 1);
   const int t = rc / G, head = kvh * G + rc % G;
   const unsigned long long sees = p.mask ? p.mask[sr.r0 + t] : (2ull << t) - 1;
   if (tid == 0) sm_odd = 0;
@@ -511,14 +516,14 @@ tree_wide_kernel(TreeArgs p, int least) {
   // step's one barrier, and V^T P^T of the second beside the loads of the step after next.  The LDS
   // reads of a product run L ahead of its MFMAs, over the steps' ends: V's last ones are read before
   // the barrier, after which nothing reads the step's buffer.  Left alone, the scheduler does neither.
-  const int kr = kat(tau, half), vr = 2 * KBUF + vat(col, half);
+  const int kr = kat(tau, half) + second * 32 * 2 * D, vr = (2 * KBUF + vat(col, half)) ^ (second * 2 << 5);
   auto k_read = [&](int buf, int x) {                             // x: 32-token half of the step and k-step
     return *reinterpret_cast<const Frag8*>(smem + ((kr + buf * KBUF) ^ (x % NS << 5)) + x / NS * 32 * 2 * D);
   };
   auto v_read = [&](int buf, int x) {                             // x: 16 tokens and 32 dimensions
     return *reinterpret_cast<const Frag8*>(smem + ((vr + buf * VBUF) ^ (x / ND << 5)) + x % ND * 32 * 2 * STEP);
   };
-  constexpr int NK = 2 * NS, NF = NK + 4 * ND;                    // operands of a step: K's, then V's (NS == 2 ND)
+  constexpr int NK = HALF ? NS : 2 * NS, NF = NK + (HALF ? 2 : 4) * ND;   // operands of a step: K's, then V's (NS == 2 ND)
   constexpr int L = 2 * ND;                                       // divides NK and NF
   Frag8 f[L];
   auto read = [&](int buf, int x) { f[x % L] = x < NK ? k_read(buf, x) : x < NF ? v_read(buf, x - NK) : k_read(buf ^ 1, x - NF); };
@@ -571,7 +576,7 @@ tree_wide_kernel(TreeArgs p, int least) {
       if (masked) {                                               // drafted tokens, the end, or a missing block
         const int dr = step * STEP - sr.ctx;                      // the step's first token as a drafted one
         vis = dr >= 64 ? 0ull : dr >= 0 ? sees >> dr : dr <= -64 ? ~0ull : (sees << -dr) | ((1ull << -dr) - 1);
-        vis = (vis & keep) >> (8 * half);
+        vis = (vis & keep) >> (8 * half + 32 * second);
       }
       f32x16 s0, s1;
       Frag8 p0[2], p1[2];
@@ -596,44 +601,58 @@ tree_wide_kernel(TreeArgs p, int least) {
 #pragma unroll
         for (int i = 0; i < ND; ++i) o[i] *= corr;
       }
-      const float base0 = base_of();
-      rs = 0.f;
-      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (HALF) {
+        const float base = base_of();
+        rs = 0.f;
+        __builtin_amdgcn_sched_barrier(0);
+        expo(s0, buf, 2 * second, 0, 16, base, p0);
+        l_run += rs;
+        __syncthreads();
 #pragma unroll
-      for (int x = NS; x < NK; ++x) {
-        s1 = mfma32(f[x % L], qf[x - NS], s1);
-        read(buf, x + L);
-        expo(s0, buf, 0, (x - NS) * (16 / NS), 16 / NS, base0, p0);
-      }
-      l_run += rs;
-      if (masked) hide(s1, (uint32_t)(vis >> 32));
-      top = fmaxf(m_run, top_of(s1));
-      const bool move = __any(top > m_run + 8.f);
-      float corr = 1.f;
-      if (move) {                                                 // applied once the first half is added
-        corr = __builtin_amdgcn_exp2f(m_run - (top == -INFINITY ? 0.f : top));
-        m_run = top;
-        l_run *= corr;
-      }
-      const float base1 = base_of();
-      rs = 0.f;
-      __builtin_amdgcn_sched_barrier(0);
+        for (int x = 0; x < 2 * ND; ++x) {
+          o[x % ND] = mfma32(f[(NK + x) % L], p0[x / ND], o[x % ND]);
+          read(buf, NK + x + L);
+        }
+      } else {
+        const float base0 = base_of();
+        rs = 0.f;
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int x = 0; x < 2 * ND; ++x) {
-        o[x % ND] = mfma32(f[(NK + x) % L], p0[x / ND], o[x % ND]);
-        read(buf, NK + x + L);
-        expo(s1, buf, 2, x * (8 / ND), 8 / ND, base1, p1);
-      }
-      l_run += rs;
-      if (move) {
+        for (int x = NS; x < NK; ++x) {
+          s1 = mfma32(f[x % L], qf[x - NS], s1);
+          read(buf, x + L);
+          expo(s0, buf, 0, (x - NS) * (16 / NS), 16 / NS, base0, p0);
+        }
+        l_run += rs;
+        if (masked) hide(s1, (uint32_t)(vis >> 32));
+        top = fmaxf(m_run, top_of(s1));
+        const bool move = __any(top > m_run + 8.f);
+        float corr = 1.f;
+        if (move) {                                               // applied once the first half is added
+          corr = __builtin_amdgcn_exp2f(m_run - (top == -INFINITY ? 0.f : top));
+          m_run = top;
+          l_run *= corr;
+        }
+        const float base1 = base_of();
+        rs = 0.f;
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < ND; ++i) o[i] *= corr;
-      }
-      __syncthreads();
+        for (int x = 0; x < 2 * ND; ++x) {
+          o[x % ND] = mfma32(f[(NK + x) % L], p0[x / ND], o[x % ND]);
+          read(buf, NK + x + L);
+          expo(s1, buf, 2, x * (8 / ND), 8 / ND, base1, p1);
+        }
+        l_run += rs;
+        if (move) {
 #pragma unroll
-      for (int x = 2 * ND; x < 4 * ND; ++x) {
-        o[x % ND] = mfma32(f[(NK + x) % L], p1[x / ND - 2], o[x % ND]);
-        read(buf, NK + x + L);
+          for (int i = 0; i < ND; ++i) o[i] *= corr;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int x = 2 * ND; x < 4 * ND; ++x) {
+          o[x % ND] = mfma32(f[(NK + x) % L], p1[x / ND - 2], o[x % ND]);
+          read(buf, NK + x + L);
+        }
       }
       load(then);
       __builtin_amdgcn_sched_barrier(0);
@@ -644,6 +663,27 @@ tree_wide_kernel(TreeArgs p, int least) {
     }
     keep = keep_next;
     keep_next = keep_of(then);
+  }
+  if constexpr (HALF) {                                           // nothing reads the steps' buffers any more after the barrier
+    float* other = reinterpret_cast<float*>(smem) + rows_of * (16 * ND + 2) * 64 + lane;
+    __syncthreads();
+    if (second) {
+      other[0] = m_run, other[64] = l_run;
+#pragma unroll
+      for (int i = 0; i < ND; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) other[64 * (2 + 16 * i + r)] = o[i][r];
+    }
+    __syncthreads();
+    if (second) return;
+    const float m = other[0], top = fmaxf(m, m_run), mu = top == -INFINITY ? 0.f : top;
+    const float mine = __builtin_amdgcn_exp2f(m_run - mu), its = __builtin_amdgcn_exp2f(m - mu);
+    l_run = l_run * mine + other[64] * its;
+    m_run = top;
+#pragma unroll
+    for (int i = 0; i < ND; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[i][r] = o[i][r] * mine + other[64 * (2 + 16 * i + r)] * its;
   }
   if (!active || row >= nrow) return;
   float l = l_run;
@@ -724,8 +764,8 @@ __global__ void __launch_bounds__(256) tree_combine_kernel(TreeArgs p, int nspli
 
 // The kernel, the workgroups that a KV head's rows take, and the splits of the context: as many as give every
 // compute unit two workgroups, of `least` steps at least.
-//  * few rows: 4, one for each wave (1530 tokens, 32 sequences: 2 and 3 steps cost up to 1.5 us more).  A context of two
-//    steps a wave is not split, nor one of four where the workgroups fill half the compute units (one token behind
+//  * few rows: 4, one for each wave (1530 tokens, 32 sequences: 2 and 3 steps cost up to 1.5 us more).  A context of
+//    two steps a wave is not split, nor one of four where the workgroups fill half the compute units (one token behind
 //    400 in e4m3: 8.9 us, and 10.1 with two splits and their join; 32 sequences of one behind 1000: 13.0 and 14.6; but
 //    one behind 1000: 11.8 and 10.7).
 //  * many rows: a split's steps follow one another (1.7 us each), but every split is one more to join.  While there are
@@ -733,7 +773,7 @@ __global__ void __launch_bounds__(256) tree_combine_kernel(TreeArgs p, int nspli
 //    600: 16.5 with 1, 14.3 with 2, 16.0 with 4), with many of them 4 do (5 behind 8000: 18.0 with 2, 16.6 with 4): as
 //    many steps as keep the workgroups at half the compute units, 4 at most.
 constexpr int LEAST_STEPS = 4;
-struct TreePlan { bool wide; int tiles, nsplit, least; };
+struct TreePlan { bool wide, half; int tiles, nsplit, least; };
 static TreePlan tree_plan(int type, int n_kv, int n_q, int batch, int max_rows, int max_ctx, int cus) {
   TreePlan t;
   const int rows = max_rows * (n_q / n_kv);
@@ -744,6 +784,7 @@ static TreePlan tree_plan(int type, int n_kv, int n_q, int batch, int max_rows, 
   const long wgs = (long)batch * n_kv * t.tiles, want = (2L * cus + wgs - 1) / wgs;
   if (t.wide) t.least = (int)std::min<long>(LEAST_STEPS, std::max(1L, (2 * wgs * steps + cus - 1) / cus));
   else t.least = steps <= 8 || (steps <= 16 && 2 * wgs >= cus) ? std::max(steps, LEAST_STEPS) : LEAST_STEPS;
+  t.half = t.wide && rows <= 64 && t.least == LEAST_STEPS;
   t.nsplit = (int)std::max(1L, std::min({want, 64L, (steps + t.least - 1L) / t.least}));
   return t;
 }
@@ -758,7 +799,8 @@ static hipError_t tree_launch(const TreeArgs& p, const TreePlan& t, hipStream_t 
   typedef typename TreeT<CT>::act T;
   const dim3 grid(t.nsplit, p.c.n_kv * t.tiles, p.r.batch);
   if constexpr (sizeof(CT) < 4) {
-    if (t.wide) hipLaunchKernelGGL((tree_wide_kernel<CT, D>), grid, dim3(256), 0, s, p, t.least);
+    if (t.half) hipLaunchKernelGGL((tree_wide_kernel<CT, D, true>), grid, dim3(256), 0, s, p, t.least);
+    else if (t.wide) hipLaunchKernelGGL((tree_wide_kernel<CT, D, false>), grid, dim3(256), 0, s, p, t.least);
     else hipLaunchKernelGGL((tree_attn_kernel<CT, D>), grid, dim3(256), 0, s, p, t.least);
   } else {
     hipLaunchKernelGGL((tree_attn_kernel<CT, D>), grid, dim3(256), 0, s, p, t.least);

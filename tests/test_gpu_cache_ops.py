@@ -393,6 +393,29 @@ def test_tree_where_splits_begin(gpu_lib, kind, n):
 
 
 @pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n_q,n", [(14, 3), (14, 5), (14, 9)])
+def test_tree_waves_that_share_a_step(gpu_lib, kind, d, n_q, n):
+    """21 to 63 rows of a KV head over steps enough that two waves each take half of a step's tokens: random masks, a
+    sequence that ends inside the first half of a step, a drafted value that is not finite."""
+    nova = gpu_lib
+    n_kv, ctx = 2, [4100, 1033, 70, 0, 2047]
+    r = _rng(d, n)
+    bt = Batch(nova, ctx, [n] * 5, n_kv, d, kind, seed=61).fill(61, stale=float("nan"))
+    bad = bt.v[1][1033 + 1].copy()
+    bad[0, 3], bad[1, d - 1] = np.nan, np.nan
+    bt.put(1, 1033 + 1, bt.k[1][1033 + 1], bad)
+    masks = [m for _ in ctx for m in _tree_mask(n, r)]
+    masks[0] = 0
+    q = _dev(r.normal(size=(bt.total, n_q, d)) * 2, bt.cache.dtype)
+    mask = torch.tensor(_signed(masks), dtype=torch.int64, device="cuda")
+    for desc in (bt.desc, nova.Rows(None, bt.desc.ctx, bt.desc.tables, max_rows=n, max_ctx=bt.max_ctx)):
+        out = nova.tree_attention(bt.cache, desc, q, mask=mask)
+        _check_tree(bt, q, masks, out, d ** -0.5)
+        assert torch.equal(torch.nan_to_num(out), torch.nan_to_num(nova.tree_attention(bt.cache, desc, q, mask=mask)))
+
+
+@pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("ctx", [0, 30, 2000])
 @pytest.mark.parametrize("n_q,n", [(4, 20), (2, 14)])
 def test_tree_unseen_tokens_have_no_effect(gpu_lib, kind, ctx, n_q, n):
