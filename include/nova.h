@@ -230,7 +230,8 @@ int nova_llm_decode_noalloc(const nova_llm* llm, const int32_t* ids, const int32
  * 8 bits per value: token t of a KV head is D OCP e4m3 numbers and one byte e + 127, the values
  * being number * 2^e with the smallest e >= -100 that keeps |number| <= 448 (NaN and infinite values
  * are stored as NaN).  Values read back are exact in bf16, and appending them again stores the same
- * values (a largest one that rounded to 224 * 2^e becomes 448 * 2^(e-1)). */
+ * values (a largest one that rounded to 224 * 2^e becomes 448 * 2^(e-1)).  With the largest e, 120, a
+ * number is at most 240, so that every finite value reads back finite. */
 enum { NOVA_CACHE_BF16 = 0, NOVA_CACHE_F32 = 1, NOVA_CACHE_E4M3 = 2 };
 typedef struct {
   void* k;          /* [num_blocks][n_kv][16][head_dim], 256-byte aligned */

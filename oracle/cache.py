@@ -45,7 +45,8 @@ def e4m3_round(x):
 
 
 def quantise(x):
-    """(values an 8-bit cache stands for, exponents) of rows [..., D]; NaN and infinities become NaN."""
+    """(values an 8-bit cache stands for, exponents) of rows [..., D]; NaN and infinities become NaN.  Values are
+    float32, so with the largest exponent, 120, a number is at most 240 (256 2^120 is beyond their range)."""
     x = np.asarray(x, F64)
     fine = np.isfinite(x)
     amax = np.where(fine, np.abs(x), 0.0).max(-1)
@@ -53,7 +54,8 @@ def quantise(x):
     e = np.where(m > 0.875, e - 8, e - 9)
     e = np.where(amax > 0, np.maximum(e, MIN_EXP), MIN_EXP)
     scale = np.ldexp(1.0, e)[..., None]
-    return np.where(fine, e4m3_round(np.where(fine, x, 0.0) / scale) * scale, np.nan), e
+    most = np.where(e >= 120, 240.0, E4M3_MAX)[..., None]
+    return np.where(fine, np.clip(e4m3_round(np.where(fine, x, 0.0) / scale), -most, most) * scale, np.nan), e
 
 
 def tree_attention(q, k, v, ctx, mask, scale):

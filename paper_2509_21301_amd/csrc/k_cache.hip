@@ -13,6 +13,9 @@
 namespace nova {
 
 constexpr int MIN_SCALE_EXP = -100;      // so that every value read back is a normal bf16
+// The largest float below 248 2^120.  With the largest scale, 2^120, a value from there on would round to 256 2^120,
+// which no float holds; taken back to it, it rounds to 240 2^120, within half a step (2^-4) like any other.
+constexpr float MAX_QUANT = 0x1.effffep127f;
 
 // sin and cos of 2 pi t.  t is reduced in double to a quarter turn, the rest is at most pi/4, where
 // the Taylor series to x^9 and x^10 are within 2e-9 and 2e-10 of the functions: what remains is
@@ -80,7 +83,7 @@ template <typename T> NOVA_DEV void store8(T* p, const float* x) {
 NOVA_DEV uint2 quant8(const float* x, float inv) {
   float y[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] = fabsf(x[i]) < INFINITY ? x[i] * inv : __uint_as_float(0x7FC00000u);
+  for (int i = 0; i < 8; ++i) y[i] = fabsf(x[i]) < INFINITY ? __builtin_amdgcn_fmed3f(x[i], -MAX_QUANT, MAX_QUANT) * inv : __uint_as_float(0x7FC00000u);
   int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
   lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
   int hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[4], y[5], 0, false);
