@@ -315,10 +315,10 @@ class Vit:
         self.h = h
         self._ws = {}
 
-    def workspace(self, batch):
+    def workspace(self, batch, stream=None):
         if batch not in self._ws:
             n = lib.nova_vit_workspace_bytes(self.h, batch)
-            self._ws[batch] = torch.empty(n, dtype=torch.uint8, device=self.device)
+            self._ws[batch] = _empty(self.embed, n, torch.uint8, stream)
         return self._ws[batch]
 
     def out_shape(self, batch):
@@ -329,8 +329,8 @@ class Vit:
         assert pixels.dtype == torch.bfloat16 and pixels.is_cuda and pixels.is_contiguous()
         b = pixels.shape[0]
         if out is None:
-            out = torch.empty(self.out_shape(b), dtype=act_dtype(self.act), device=self.device)
-        ws = self.workspace(b)
+            out = _empty(self.embed, self.out_shape(b), act_dtype(self.act), stream)
+        ws = self.workspace(b, stream)
         _check(lib.nova_vit_encode(self.h, _ptr(pixels), b, _ptr(out), _ptr(ws), ws.numel(), _stream(stream)))
         return out
 
@@ -389,7 +389,7 @@ class Llm:
                 ev = torch.cuda.Event()
                 ev.record(stream if stream is not None else torch.cuda.current_stream())
                 self._retired.append((t, ev))
-            t = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            t = _empty(self.embed, nbytes, torch.uint8, stream)
             self._ws[key] = t
         if self._retired:
             self._retired = [(b, e) for b, e in self._retired if not e.query()]
@@ -411,7 +411,7 @@ class Llm:
         n_text = ids.shape[0]
         ws = self._workspace("prefill", lib.nova_llm_prefill_workspace_bytes(self.h, n_vis + n_text), stream)
         if next_id is None:
-            next_id = torch.empty(1, dtype=torch.int32, device=self.device)
+            next_id = _empty(self.embed, 1, torch.int32, stream)
         if isinstance(kv, Cache):
             kv._check_layers(self.cfg.layers)
             _check_device(kv.device, vis, ids, table, next_id, logits)
@@ -428,7 +428,7 @@ class Llm:
         # one decode workspace for every batch size: a larger one serves a smaller step as well
         ws = self._workspace("decode", lib.nova_llm_decode_workspace_bytes(self.h, b, max_ctx), stream)
         if next_ids is None:
-            next_ids = torch.empty(b, dtype=torch.int32, device=self.device)
+            next_ids = _empty(self.embed, b, torch.int32, stream)
         _check(lib.nova_llm_decode(self.h, _ptr(ids), _ptr(pos), _ptr(tables), tables.shape[1], b, max_ctx,
                                    C.byref(kv.c), _ptr(next_ids), _ptr(logits), _ptr(ws), ws.numel(),
                                    _stream(stream)))
@@ -449,7 +449,7 @@ class Llm:
         n = lib.nova_llm_verify_workspace_bytes(self.h, cache.layer(0), rows.ref)
         ws = _empty(cache.k, max(n, 256), torch.uint8, stream)
         if next_ids is None:
-            next_ids = torch.empty(rows.rows, dtype=torch.int32, device=self.device)
+            next_ids = _empty(self.embed, rows.rows, torch.int32, stream)
         _check_vector("next_ids", next_ids, torch.int32, rows.rows)
         _check(lib.nova_llm_verify(self.h, _ptr(ids), _ptr(pos), _ptr(mask), rows.ref, cache.layer(0), _ptr(next_ids),
                                    _ptr(logits), _ptr(ws), ws.numel(), _stream(stream)))
@@ -499,7 +499,8 @@ def _check_device(dev, *tensors):
 
 
 def _empty(like, shape, dtype, stream):
-    """Memory on the stream that a call runs on, so that what is freed after the call is reused behind it."""
+    """Memory on the stream that a call runs on: what the allocator hands out may still be in use by work queued on its
+    own stream, and what is freed after the call is reused behind it."""
     if stream is None:
         return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
