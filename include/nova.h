@@ -246,7 +246,9 @@ size_t nova_cache_bytes(int type, int num_blocks, int n_kv, int head_dim, size_t
 
 /* A batch of sequences over a cache and the rows (tokens) that each brings.  Row j of sequence b is
  * row row_start[b] + j of the arrays and token ctx[b] + j of the sequence.  The arrays are read on
- * the device when the kernels run; contents outside the stated bounds are clamped into them. */
+ * the device when the kernels run.  Row starts outside the rows are clamped into them; tokens outside
+ * 0 .. max_ctx - 1 do not exist: such a row is not written to the cache, reads as zeros and is not seen
+ * (its q is still rotated, and it still attends to what exists). */
 typedef struct {
   const int32_t* row_start;  /* device int32 [batch + 1], ascending; NULL: max_rows rows each (rows == batch * max_rows) */
   const int32_t* ctx;        /* device int32 [batch]: tokens in the cache before these rows; NULL: 0 */
@@ -255,7 +257,7 @@ typedef struct {
   int max_blocks, batch;
   int rows;                  /* rows of the arrays; those behind row_start[batch] are left as they were */
   int max_rows;              /* upper bound of one sequence's rows; rows beyond it are left out */
-  int max_ctx;               /* upper bound of ctx[b] plus its rows, at most 16 * max_blocks */
+  int max_ctx;               /* upper bound of ctx[b] plus its rows, at most 16 * max_blocks: see above */
 } nova_rows;
 
 /* Rotary embedding of the first `rot` dimensions (a multiple of 16, at most head_dim) of a head:

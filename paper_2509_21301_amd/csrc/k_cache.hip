@@ -117,7 +117,8 @@ __global__ void __launch_bounds__(256) kv_append_kernel(AppendArgs p, int heads_
   const SeqRows sr = find_tile(p.r, blockIdx.x, &b, &blk);
   if (b < 0) return;
   const int t0 = blk * PAGE - sr.ctx;                    // row of the sequence at slot 0 of the block
-  const int lo = max(-t0, 0), hi = min(sr.n - t0, PAGE); // slots lo .. hi - 1 get rows
+  const int lo = max(-t0, 0), hi = min(sr.n - t0, PAGE); // slots lo .. hi - 1 get rows,
+  const int kept = min(hi, p.r.max_ctx - blk * PAGE);    // of which the cache keeps those below `kept`
   const int ph = page_of(p.r, p.c.num_blocks, b, blk);
   const int n_kv = p.c.n_kv, heads = 2 * n_kv + (p.q ? p.n_q : 0);
   const int h0 = blockIdx.y * heads_per_wg, h1 = min(h0 + heads_per_wg, heads);
@@ -196,6 +197,7 @@ __global__ void __launch_bounds__(256) kv_append_kernel(AppendArgs p, int heads_
         continue;
       }
       if (ph < 0) continue;                              // no such block: the row is not kept
+      const bool keep = slot >= lo && slot < kept;
       const size_t tok = ((size_t)ph * n_kv + hh) * PAGE + slot;
       if constexpr (Q8) {
         float amax = 0.f;
@@ -208,15 +210,15 @@ __global__ void __launch_bounds__(256) kv_append_kernel(AppendArgs p, int heads_
         for (int o = 1; o < LPR; o <<= 1) amax = fmaxf(amax, __shfl_xor(amax, o, 64));
         const int e = scale_exp(amax);
         const uint2 w = quant8(x[i], exp_scale(127 - e));
-        if (live && sub == 0) (is_k ? p.c.k_exp : p.c.v_exp)[tok] = (uint8_t)(e + 127);
+        if (keep && sub == 0) (is_k ? p.c.k_exp : p.c.v_exp)[tok] = (uint8_t)(e + 127);
         if (is_k) {
-          if (live) *reinterpret_cast<uint2*>((uint8_t*)p.c.k + tok * D + 8 * sub) = w;
+          if (keep) *reinterpret_cast<uint2*>((uint8_t*)p.c.k + tok * D + 8 * sub) = w;
         } else {
           *reinterpret_cast<uint2*>(&sm_v[wave][slot][8 * sub]) = w;
         }
       } else {
         if (is_k) {
-          if (live) store8(reinterpret_cast<CT*>(p.c.k) + tok * D + 8 * sub, x[i]);
+          if (keep) store8(reinterpret_cast<CT*>(p.c.k) + tok * D + 8 * sub, x[i]);
         } else {
           store8(&sm_v[wave][slot][8 * sub], x[i]);
         }
@@ -227,7 +229,7 @@ __global__ void __launch_bounds__(256) kv_append_kernel(AppendArgs p, int heads_
       CT* vb = reinterpret_cast<CT*>(p.c.v) + ((size_t)ph * n_kv + hh) * PAGE * D;
 #pragma unroll
       for (int d = lane; d < D; d += 64) {
-        if (hi - lo == PAGE) {
+        if (kept - lo == PAGE) {
           CT t[PAGE];
 #pragma unroll
           for (int j = 0; j < PAGE; ++j) t[j] = sm_v[wave][j][d];
@@ -237,7 +239,7 @@ __global__ void __launch_bounds__(256) kv_append_kernel(AppendArgs p, int heads_
 #pragma unroll
           for (int j = 0; j < N16; ++j) reinterpret_cast<uint4*>(vb + (size_t)d * PAGE)[j] = w[j];
         } else {
-          for (int j = lo; j < hi; ++j) vb[(size_t)d * PAGE + j] = sm_v[wave][j][d];
+          for (int j = lo; j < kept; ++j) vb[(size_t)d * PAGE + j] = sm_v[wave][j][d];
         }
       }
       wave_lds_fence();
@@ -299,7 +301,7 @@ template <typename T> NOVA_DEV float cached1(T x, float) { return to_f<T>(x); }
 
 // Consecutive rows: workgroup (block of 16 slots, group of K and V heads), a wave per head.  K rows are
 // copied with 8 elements per lane; a V block [D][16] is read whole, 16 tokens per lane, and turned
-// through wave-private LDS.  Rows whose block is missing read as zeros.  Bound by HBM: 32 sequences of 1846
+// through wave-private LDS.  Rows whose token does not exist read as zeros.  Bound by HBM: 32 sequences of 1846
 // to 3579 tokens from e4m3 to bf16, 261 MB in 51 us, 5.1 TB/s, a large copy's rate.
 template <typename CT, typename TO, int D>
 __global__ void __launch_bounds__(256) kv_gather_kernel(GatherArgs p) {
@@ -311,7 +313,7 @@ __global__ void __launch_bounds__(256) kv_gather_kernel(GatherArgs p) {
   if (b < 0) return;
   const int t0 = blk * PAGE - sr.ctx;
   const int lo = max(-t0, 0), hi = min(sr.n - t0, PAGE);
-  const int ph = page_of(p.r, p.c.num_blocks, b, blk);
+  const int ph = page_of(p.r, p.c.num_blocks, b, blk), held = p.r.max_ctx - blk * PAGE;
   const int sub = lane % LPR, rr = lane / LPR, n_kv = p.c.n_kv;
   const int h = blockIdx.y * 4 + wave;
   if (h >= 2 * n_kv) return;
@@ -338,7 +340,7 @@ __global__ void __launch_bounds__(256) kv_gather_kernel(GatherArgs p) {
     const int slot = i * RPI + rr;
     if (slot < lo || slot >= hi) continue;
     float x[8] = {};
-    if (ph >= 0) {
+    if (ph >= 0 && slot < held) {
       float scale = 1.f;
       if constexpr (sizeof(CT) == 1) scale = exp_scale((is_k ? p.c.k_exp : p.c.v_exp)[tok0 + slot]);
       if (is_k) cached8(reinterpret_cast<const CT*>(p.c.k) + (tok0 + slot) * D + 8 * sub, scale, x);

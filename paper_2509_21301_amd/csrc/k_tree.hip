@@ -103,7 +103,7 @@ tree_attn_kernel(TreeArgs p, int least) {
   const SeqRows sr = seq_rows(p.r, b);
   const int nrow = sr.n * G;
   if (row0 >= nrow) return;
-  const int total = sr.ctx + sr.n;
+  const int total = min(sr.ctx + sr.n, p.r.max_ctx);      // the sequence's tokens that exist
   const int nsteps = (total + STEP - 1) / STEP, nblk = min((total + PAGE - 1) / PAGE, p.r.max_blocks);
   const int per = split_steps(nsteps, gridDim.x, least);
   const int step0 = split * per, step1 = min(step0 + per, nsteps);
@@ -317,7 +317,7 @@ tree_attn_kernel(TreeArgs p, int least) {
     if (sm_odd) {
       const unsigned long long see = p.mask ? p.mask[t] : (2ull << (r / G)) - 1;
 #pragma unroll 1
-      for (int j = max(0, step0 * STEP - sr.ctx); j < min(sr.n, step1 * STEP - sr.ctx); ++j) {
+      for (int j = max(0, step0 * STEP - sr.ctx); j < min(total, step1 * STEP) - sr.ctx; ++j) {
         const int tok = sr.ctx + j, ph = page_of(p.r, p.c.num_blocks, b, tok / PAGE);
         if (!((see >> j) & 1) || ph < 0) continue;
         const float v = odd_value<CT>(reinterpret_cast<const CT*>(p.c.v)[(((size_t)ph * n_kv + kvh) * D + d) * PAGE + tok % PAGE]);
@@ -375,7 +375,7 @@ tree_wide_kernel(TreeArgs p, int least) {
   const SeqRows sr = seq_rows(p.r, b);
   const int nrow = sr.n * G, row0 = tile * 128, rows_of = HALF ? wave & 1 : wave, second = HALF ? wave >> 1 : 0;
   if (row0 >= nrow) return;
-  const int total = sr.ctx + sr.n;
+  const int total = min(sr.ctx + sr.n, p.r.max_ctx);      // the sequence's tokens that exist
   const int nsteps = (total + STEP - 1) / STEP;
   const int per = split_steps(nsteps, gridDim.x, least);
   const int step0 = split * per, step1 = min(step0 + per, nsteps);
@@ -689,7 +689,7 @@ tree_wide_kernel(TreeArgs p, int least) {
   float l = l_run;
   l += __shfl_xor(l, 32, 64);
   if (sm_odd) {
-    const int j0 = max(0, step0 * STEP - sr.ctx), j1 = min(sr.n, step1 * STEP - sr.ctx);
+    const int j0 = max(0, step0 * STEP - sr.ctx), j1 = min(total, step1 * STEP) - sr.ctx;
 #pragma unroll 1
     for (int j = j0; j < j1; ++j) {
       const int tok = sr.ctx + j, ph = page_of(p.r, p.c.num_blocks, b, tok / PAGE);

@@ -12,7 +12,8 @@ struct e4m3_t { uint8_t v; };            // one OCP e4m3 number; its token's sca
 
 template <typename CT> struct PageElem { static constexpr int bytes = sizeof(CT); };
 
-// One sequence's rows: global rows r0 .. r0 + n - 1 are its tokens ctx .. ctx + n - 1.
+// One sequence's rows: global rows r0 .. r0 + n - 1 are its tokens ctx .. ctx + n - 1.  Tokens outside 0 .. max_ctx - 1
+// do not exist: ctx is between -n and max_ctx, so that what lies outside is neither kept nor seen.
 struct SeqRows { int r0, n, ctx; };
 
 NOVA_DEV SeqRows seq_rows(const BatchRows& p, int b) {
@@ -25,10 +26,13 @@ NOVA_DEV SeqRows seq_rows(const BatchRows& p, int b) {
     s.n = p.max_rows;
   }
   s.n = min(s.n, p.max_rows);
-  s.ctx = p.ctx ? min(max(p.ctx[b], 0), p.max_ctx - s.n) : 0;
-  s.ctx = max(s.ctx, 0);
+  s.ctx = p.ctx ? min(max(p.ctx[b], -s.n), p.max_ctx) : 0;
   return s;
 }
+
+// Block of a token, rounded down (a token before the sequence is in block -1 or below).
+NOVA_DEV int block_of(int t) { return t >> 4; }
+static_assert(PAGE == 16);
 
 // The tile-th of all 16-token cache blocks that the batch's rows touch, counted over the sequences:
 // its sequence in *b (-1: the batch has fewer tiles) and the block's number in the sequence in *blk.
@@ -42,7 +46,7 @@ NOVA_DEV SeqRows find_tile(const BatchRows& p, int tile, int* b, int* blk) {
     int tiles = 0;
     if (i < p.batch) {
       s = seq_rows(p, i);
-      tiles = s.n > 0 ? (s.ctx + s.n - 1) / PAGE - s.ctx / PAGE + 1 : 0;
+      tiles = s.n > 0 ? block_of(s.ctx + s.n - 1) - block_of(s.ctx) + 1 : 0;
     }
     int sum = tiles;                     // inclusive prefix sum over the lanes
 #pragma unroll
@@ -58,7 +62,7 @@ NOVA_DEV SeqRows find_tile(const BatchRows& p, int tile, int* b, int* blk) {
       f.n = __builtin_amdgcn_readlane(s.n, l);
       f.ctx = __builtin_amdgcn_readlane(s.ctx, l);
       *b = base + l;
-      *blk = f.ctx / PAGE + tile - (before + __builtin_amdgcn_readlane(sum - tiles, l));
+      *blk = block_of(f.ctx) + tile - (before + __builtin_amdgcn_readlane(sum - tiles, l));
       return f;
     }
     before += __builtin_amdgcn_readlane(sum, 63);

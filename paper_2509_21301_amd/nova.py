@@ -580,7 +580,8 @@ class Rows:
     """Which rows of a call belong to which sequence: ``row_start`` int32 [batch + 1] (None: max_rows rows each), ``ctx``
     int32 [batch] tokens cached before them (None: 0), ``tables`` int32 [batch, max_blocks].  Row j of sequence b is
     its token ctx[b] + j.  ``rows``, ``max_rows`` (of one sequence) and ``max_ctx`` (cached and new tokens of one
-    sequence) bound what the device arrays may hold when a call runs; the arrays may change between calls."""
+    sequence) bound what the device arrays may hold when a call runs; the arrays may change between calls.  Tokens
+    outside 0 .. max_ctx - 1 do not exist: a row there is neither kept nor seen."""
 
     def __init__(self, row_start, ctx, tables, rows=None, max_rows=1, max_ctx=None):
         if tables.dtype != torch.int32 or tables.dim() != 2 or not tables.is_contiguous():
