@@ -293,7 +293,8 @@ int nova_kv_gather(const nova_cache* cache, const nova_rows* rows, const int32_t
 /* Attention of each sequence's rows (drafted tokens, at most 64, already appended) over its cache:
  * row j sees every token below ctx[b], and token ctx[b] + i where bit i of mask[row] is set
  * (device uint64 [rows]; NULL: i <= j, a chain; one row per sequence is a decode step).  A row that
- * sees nothing gets zeros; what a row does not see has no effect on it, whatever it holds.
+ * sees nothing gets zeros (one that sees scores of -infinity only has no softmax: NaN); what a row does
+ * not see has no effect on it, whatever it holds.
  *  q, out: device, bf16 (F32 with an F32 cache), n_q heads (a multiple of n_kv); scale is applied to q.k
  *          (scores and the sums of p v, where p is up to 2^8, are fp32: V up to 2^88 is safe)
  *  ws:     device, nova_tree_attention_workspace_bytes(), 256-byte aligned; contents need not be kept

@@ -75,6 +75,23 @@ template <typename CT> NOVA_DEV u32x4 v_keep(u32x4 q, uint32_t keep) {
   return u32x4{w[0], w[1], w[2], w[3]};
 }
 
+// A row whose sum of p is 0: zeros where it sees no token, and NaN where it sees some, all with scores of -infinity,
+// whose softmax is 0 / 0.  Found out here, at the end and rarely, so that the passes over the cache pay nothing for it.
+NOVA_DEV float empty_row(const TreeArgs& p, int b, unsigned long long sees) {
+  const SeqRows sr = seq_rows(p.r, b);
+  const int total = min(sr.ctx + sr.n, p.r.max_ctx);
+  bool any = false;
+#pragma unroll 1
+  for (int j = max(0, -sr.ctx); j < total - sr.ctx && !any; ++j)
+    any = ((sees >> j) & 1) && page_of(p.r, p.c.num_blocks, b, (sr.ctx + j) / PAGE) >= 0;
+#pragma unroll 1
+  for (int t = 0; t < sr.ctx && !any; t += PAGE) any = page_of(p.r, p.c.num_blocks, b, t / PAGE) >= 0;
+  return any ? __uint_as_float(0x7FC00000u) : 0.f;
+}
+NOVA_DEV unsigned long long seen_by(const TreeArgs& p, const SeqRows& sr, int t) {
+  return p.mask ? p.mask[sr.r0 + t] : (2ull << t) - 1;    // of its sequence's drafted tokens, a bit each
+}
+
 // Steps of a split: the plan's number of splits shares out the sequence's own steps, `least` at a time.
 NOVA_DEV int split_steps(int nsteps, int nsplit, int least) { return max(least, (nsteps + nsplit - 1) / nsplit); }
 
@@ -158,7 +175,7 @@ tree_attn_kernel(TreeArgs p, int least) {
   // this lane's row: its drafted token, its q and what it sees of the drafted ones
   const int rc = min(row0 + col, nrow - 1), mine_t = rc / G;
   const T* qrow = reinterpret_cast<const T*>(p.q) + (sr.r0 + mine_t) * p.q_row + (kvh * G + rc % G) * D;
-  const unsigned long long sees = p.mask ? p.mask[sr.r0 + mine_t] : (2ull << mine_t) - 1;
+  const unsigned long long sees = seen_by(p, sr, mine_t);
   // Q^T fragments: the dimensions of each k-step in the order in which K's words hold them
   Frag8 qf[F32 ? 1 : NS];
   f32x4 qx[F32 ? D / 16 : 1];
@@ -315,7 +332,7 @@ tree_attn_kernel(TreeArgs p, int least) {
     }
     const long t = sr.r0 + r / G;
     if (sm_odd) {
-      const unsigned long long see = p.mask ? p.mask[t] : (2ull << (r / G)) - 1;
+      const unsigned long long see = seen_by(p, sr, r / G);
 #pragma unroll 1
       for (int j = max(0, step0 * STEP - sr.ctx); j < min(total, step1 * STEP) - sr.ctx; ++j) {
         const int tok = sr.ctx + j, ph = page_of(p.r, p.c.num_blocks, b, tok / PAGE);
@@ -326,7 +343,7 @@ tree_attn_kernel(TreeArgs p, int least) {
     }
     const int head = kvh * G + r % G;
     if (nsplit == 1) {
-      reinterpret_cast<T*>(p.out)[t * p.out_row + head * D + d] = from_f<T>(L == 0.f ? 0.f : O / L);
+      reinterpret_cast<T*>(p.out)[t * p.out_row + head * D + d] = from_f<T>(L == 0.f ? empty_row(p, b, seen_by(p, sr, r / G)) : O / L);
     } else {
       float* part = p.partial + ((t * p.n_q + head) * nsplit + split) * (D + 4);
       part[4 + d] = O;
@@ -382,7 +399,7 @@ tree_wide_kernel(TreeArgs p, int least) {
   const bool active = row0 + 32 * rows_of < nrow;
   const int row = row0 + 32 * rows_of + col, rc = min(row, nrow - 1);
   const int t = rc / G, head = kvh * G + rc % G;
-  const unsigned long long sees = p.mask ? p.mask[sr.r0 + t] : (2ull << t) - 1;
+  const unsigned long long sees = seen_by(p, sr, t);
   if (tid == 0) sm_odd = 0;
 
   // Block ids of 16 steps at a time, one per lane (those that exist), the next 16 requested ahead: a
@@ -710,7 +727,7 @@ tree_wide_kernel(TreeArgs p, int least) {
   const long rh = (sr.r0 + t) * (long)p.n_q + head;
   if (nsplit == 1) {
     bf16_t* out = reinterpret_cast<bf16_t*>(p.out) + (sr.r0 + t) * p.out_row + head * D + 4 * half;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float inv = l == 0.f ? empty_row(p, b, sees) : 1.f / l;
 #pragma unroll
     for (int i = 0; i < ND; ++i)
 #pragma unroll
@@ -757,9 +774,10 @@ __global__ void __launch_bounds__(256) tree_combine_kernel(TreeArgs p, int nspli
       for (int d = 0; d < D / 64; ++d) o[d] += w * v[s][d];
     }
   }
+  const float empty = L == 0.f ? empty_row(p, blockIdx.y, seen_by(p, sr, i / p.n_q)) : 0.f;
 #pragma unroll
   for (int d = 0; d < D / 64; ++d)
-    reinterpret_cast<T*>(p.out)[t * p.out_row + head * D + lane + 64 * d] = from_f<T>(L == 0.f ? 0.f : o[d] / L);
+    reinterpret_cast<T*>(p.out)[t * p.out_row + head * D + lane + 64 * d] = from_f<T>(L == 0.f ? empty : o[d] / L);
 }
 
 // The kernel, the workgroups that a KV head's rows take, and the splits of the context: as many as give every
