@@ -313,7 +313,7 @@ int nova_tree_attention(const nova_cache* cache, const nova_rows* rows, const ui
  *  top_lp, top_ids[row][n_top]: the most likely tokens, descending, equal ones by the lower id (NaN
  *                     counts as the largest); n_top <= 32 and <= vocab, 0: none
  * A logit of -infinity has probability 0.  A row with a NaN or +infinity, or with nothing but
- * -infinity, has NaN for every log probability of a token and for its entropy.  vocab <= 2^21, rows <= 2^23.
+ * -infinity, has NaN for every log probability of a token and for its entropy.  vocab <= 2^21, rows < 2^23.
  *  ws: device, nova_logprobs_workspace_bytes(), 256-byte aligned, as for nova_tree_attention */
 size_t nova_logprobs_workspace_bytes(int rows, int vocab, int n_top);
 int nova_logprobs(const void* logits, int type, int64_t pitch, int rows, int vocab, const int32_t* given, int n_given,

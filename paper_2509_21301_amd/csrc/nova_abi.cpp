@@ -710,7 +710,7 @@ inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 inline bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
 
 // Within these every launch grid and every index of the kernels fits.
-constexpr int MAX_HEADS = 8192, MAX_ROWS = 1 << 25, MAX_TOKENS = 1 << 30, MAX_LOGIT_ROWS = 1 << 23;
+constexpr int MAX_HEADS = 8192, MAX_ROWS = 1 << 25, MAX_TOKENS = 1 << 30, MAX_LOGIT_ROWS = (1 << 23) - 1;
 
 int check_cache(const nova_cache* c) {
   if (!c) return fail(NOVA_EINVAL, "null cache");
