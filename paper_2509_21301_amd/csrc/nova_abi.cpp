@@ -1196,11 +1196,21 @@ int llm_decode_t(const nova_llm* m, const int* ids, const int* pos, const int* t
 }
 }  // namespace
 
+namespace {
+// The kernels count a prompt in 32 bits, rounded up to their tiles.
+int check_prompt(int n_vis, int n_text) {
+  const int64_t n = (int64_t)n_vis + n_text;
+  if (n_vis < 0 || n_text < 0 || n == 0) return fail(NOVA_EINVAL, "empty prompt");
+  if (n > MAX_TOKENS) return fail(NOVA_EUNSUPPORTED, "prompt of %lld tokens (at most %d)", (long long)n, MAX_TOKENS);
+  return NOVA_OK;
+}
+}  // namespace
+
 extern "C" int nova_llm_prefill(const nova_llm* m, const void* vis, int n_vis, const int32_t* ids, int n_text,
                                 const int32_t* table, const nova_kv* kv, int32_t* next_id, float* logits, void* ws,
                                 size_t ws_bytes, nova_stream_t stream) {
   if (!m || !kv) return fail(NOVA_EINVAL, "null model or kv");
-  if (n_vis < 0 || n_text < 0 || n_vis + n_text <= 0) return fail(NOVA_EINVAL, "empty prompt");
+  if (int rc = check_prompt(n_vis, n_text)) return rc;
   if ((n_vis > 0 && (!vis || !aligned(vis))) || (n_text > 0 && !ids) || !table || !next_id || !ws || !aligned(ws))
     return fail(NOVA_EINVAL, "null or misaligned pointer");
   if (!kv->k || !kv->v || kv->num_blocks <= 0) return fail(NOVA_EINVAL, "invalid kv pool");
@@ -1263,7 +1273,7 @@ extern "C" int nova_llm_prefill_cache(const nova_llm* m, const void* vis, int n_
                                       const int32_t* table, const nova_cache* cache, int32_t* next_id, float* logits, void* ws,
                                       size_t ws_bytes, nova_stream_t stream) {
   if (int rc = check_model_cache(m, cache)) return rc;
-  if (n_vis < 0 || n_text < 0 || (int64_t)n_vis + n_text <= 0) return fail(NOVA_EINVAL, "empty prompt");
+  if (int rc = check_prompt(n_vis, n_text)) return rc;
   if ((n_vis > 0 && (!vis || !aligned(vis))) || (n_text > 0 && !ids) || !table || !next_id || !ws || !aligned(ws))
     return fail(NOVA_EINVAL, "null or misaligned pointer");
   const int S = n_vis + n_text;
