@@ -10,8 +10,6 @@ namespace nova {
 constexpr int PAGE = 16;                 // tokens per block
 struct e4m3_t { uint8_t v; };            // one OCP e4m3 number; its token's scale is kept beside the pool
 
-template <typename CT> struct PageElem { static constexpr int bytes = sizeof(CT); };
-
 // One sequence's rows: global rows r0 .. r0 + n - 1 are its tokens ctx .. ctx + n - 1.  Tokens outside 0 .. max_ctx - 1
 // do not exist: ctx is between -n and max_ctx, so that what lies outside is neither kept nor seen.
 struct SeqRows { int r0, n, ctx; };
