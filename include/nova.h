@@ -323,14 +323,16 @@ int nova_logprobs(const void* logits, int type, int64_t pitch, int rows, int voc
 /* ------------------------------------------------------------------ LLM on a cache of any type
  * nova_llm_prefill into a pool of nova_cache layers (cache describes layer 0; layer l's arrays follow
  * at l times their size): the prompt's attention reads K and V as computed, the cache keeps them in
- * its type.  The cache type is BF16 or E4M3 for a bf16 model, F32 for an fp32 one. */
+ * its type.  The cache type is BF16 or E4M3 for a bf16 model, F32 for an fp32 one.  An E4M3 cache holds
+ * what a BF16 one would, quantised: K is rounded to bf16 after its rotation and then to 8 bits. */
 int nova_llm_prefill_cache(const nova_llm* llm, const void* vis, int n_vis, const int32_t* ids, int n_text,
                            const int32_t* block_table, const nova_cache* cache, int32_t* next_id, float* logits,
                            void* ws, size_t ws_bytes, nova_stream_t stream);
 
 /* One decode step over drafted tokens (speculative decoding): the rows' tokens ids run through the
- * model together, each layer appending their K and V behind its sequence's context and attending by
- * mask, as nova_kv_append and nova_tree_attention do.  One row per sequence is a plain decode step.
+ * model together, each layer appending their K and V (in fp32 from the projection, rounded once) behind
+ * its sequence's context and attending by mask, as nova_kv_append and nova_tree_attention do.  One row per
+ * sequence is a plain decode step.
  *  ids, pos: device int32 [rows], rows <= 32: tokens and their rotary positions
  *  mask:     device uint64 [rows] or NULL (chains)
  *  next_ids [rows], logits [rows][vocab] or NULL: as for nova_llm_decode, one per row; rows behind

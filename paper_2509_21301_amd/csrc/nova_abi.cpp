@@ -987,6 +987,8 @@ int llm_prefill_t(const nova_llm* m, const T* vis, int n_vis, const int* ids, in
     CALL(NOVA_KIND_MISC, s, nova::qkv_prefill<T>(qkv, S, 1, c.n_q, c.n_kv, D, c.rope_theta, 0, vt, skp, kp, vp, kv ? table : nullptr,
                                                   c.block, s, att_cnt, n_cnt));
     if (pool) {
+      // K as the attention below reads it, rotated and rounded to bf16: so an 8-bit cache holds the 16-bit one's values,
+      // quantised, at 0.6% more error than quantised from the fp32 rotation (rms 0.02664 of K's, and 0.02649)
       nova::AppendArgs p{};
       p.c = pool_layer(*pool, l);
       p.r = nova::BatchRows{nullptr, nullptr, table, (S + c.block - 1) / c.block, 1, S, S, S};
