@@ -379,6 +379,10 @@ class Llm:
         self._retired = []
 
     def _workspace(self, key, nbytes, stream=None):
+        if torch.cuda.is_current_stream_capturing():
+            # memory of the graph's own: a later, larger call would free the one that is kept here, and two graphs
+            # would share it
+            return _empty(self.embed, nbytes, torch.uint8, stream)
         t = self._ws.get(key)
         if t is None or t.numel() < nbytes:
             if t is not None:
@@ -445,7 +449,7 @@ class Llm:
         if logits is not None and (logits.dtype != torch.float32 or not logits.is_contiguous() or
                                    logits.shape != (rows.rows, self.cfg.vocab)):
             raise ValueError(f"logits must be contiguous float32 {(rows.rows, self.cfg.vocab)}")
-        # memory of the call's own, so that a captured step keeps its workspace whatever runs later
+        # memory of the call's own, as the operators take it
         n = lib.nova_llm_verify_workspace_bytes(self.h, cache.layer(0), rows.ref)
         ws = _empty(cache.k, max(n, 256), torch.uint8, stream)
         if next_ids is None:
