@@ -296,7 +296,8 @@ int nova_kv_gather(const nova_cache* cache, const nova_rows* rows, const int32_t
  * sees nothing gets zeros (one that sees scores of -infinity only has no softmax: NaN); what a row does
  * not see has no effect on it, whatever it holds.
  *  q, out: device, bf16 (F32 with an F32 cache), n_q heads (a multiple of n_kv); scale is applied to q.k
- *          (scores and the sums of p v, where p is up to 2^8, are fp32: V up to 2^88 is safe)
+ *          (scores and the sums of p v, where p is up to 2^8, are fp32: scores up to 2^24 in magnitude and
+ *          V up to 2^88 are safe)
  *  ws:     device, nova_tree_attention_workspace_bytes(), 256-byte aligned; contents need not be kept
  *          or cleared, but calls that may overlap in time need one each */
 size_t nova_tree_attention_workspace_bytes(const nova_cache* cache, const nova_rows* rows, int n_q);

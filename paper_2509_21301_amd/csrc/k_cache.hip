@@ -355,7 +355,7 @@ __global__ void __launch_bounds__(256) kv_gather_kernel(GatherArgs p) {
 // elements apart, so its lanes take one element each, neighbours side by side: a load touches 16 (e4m3) or 32
 // (bf16) lines of 64 bytes, not 64 as with 8 elements a lane.  For a handful of accepted tokens bound by latency (eight
 // sequences' accepted tokens, 36 of 4 KV heads: 4.1 us), for many by V's lines, of which a token uses a sixteenth
-// (32 sequences' 750 to 1500 tokens anywhere among 2000, e4m3: 49.8 us, 64.5 with 8 elements a lane; bf16 67.5 and 73).
+// (32 sequences' 750 to 1500 tokens anywhere among 2000, e4m3: 49.7 us, 64.1 with 8 elements a lane; bf16 74.4 and 81.9).
 template <typename CT, typename TO, int D>
 __global__ void __launch_bounds__(256) kv_pick_kernel(GatherArgs p) {
   constexpr int LPR = D / 8, ROWS = 64 / LPR;

@@ -98,8 +98,8 @@ NOVA_DEV int split_steps(int nsteps, int nsplit, int least) { return max(least, 
 // ------------------------------------------------------------------ few rows
 // One tile of 16 rows: bound by the cache's bytes.  The waves of a workgroup take steps in turn, each from
 // memory to its own registers (K of the next step is requested once S is formed, V once it is used).  32 single
-// tokens of 28/4 heads of 128 behind 2700 to 3627 e4m3 tokens: 106 MB in 23.4 to 24.6 us, 4.4 TB/s where a large copy
-// reaches 5.0.  The fp32 cache's calls are small: 5 tokens behind 96, 6.8 us of latency.
+// tokens of 28/4 heads of 128 behind 2700 to 3627 e4m3 tokens: 106 MB in 23.4 to 25 us, 4.2 to 4.5 TB/s where a large
+// copy reaches 5.0; bf16 209 MB in 42.4 us, 4.9 TB/s.  The fp32 cache's calls are small: 5 tokens behind 96, 6.8 us of latency.
 template <typename CT, int D>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
 tree_attn_kernel(TreeArgs p, int least) {
@@ -360,8 +360,9 @@ tree_attn_kernel(TreeArgs p, int least) {
 // lane half h then holds tokens 16 u + 8 h + e of each 32, the ones that it hands to the second product.
 // 16-byte pieces are swizzled by their row so that a read covers every bank once.
 // Two sequences of 64 and 48 tokens behind 32700 and 28613 (28/4 heads of 128, e4m3): 5.0e10 operations in
-// 87 us, 0.57 PFLOP/s; a step of the two workgroups of a compute unit takes 2.8 us, its MFMAs 1.0 and its
-// LDS accesses 1.7 of them, the exponentials, conversions and sums of a wave about as much as its MFMAs.
+// 86 us, 0.58 PFLOP/s.  Of its cycles the MFMAs are busy for 24% and LDS for 30% (and 7% of bank conflicts), and vector
+// instructions issue in 32%: none of them bounds it, the two waves of a SIMD do, whose chains (scores, exponentials,
+// conversion, product, barrier) cover each other's waits in part; 31% of their time is waiting.
 // 64 rows a wave halve the LDS reads, but leave one wave a SIMD, whose vector instructions issue every 5 clocks
 // instead of 4 and wait alone: 116 us.
 // Eight sequences of 9 to 16 tokens behind 1222 to 1564 (bf16): 17 us, four steps of 1.7 us, the rest
