@@ -284,6 +284,32 @@ int nova_kv_append(const nova_cache* cache, const nova_rows* rows, const nova_ro
                    int in_type, const void* q, int64_t q_pitch, int n_q, const void* k, int64_t k_pitch, const void* v,
                    int64_t v_pitch, void* q_out, int q_out_type, int64_t q_out_pitch, nova_stream_t stream);
 
+/* Positions with several axes (time, row and column of an image's or video's tokens): pair c turns by the
+ * position of one of n_axes axes (1 to 4), of which axis a gets pairs[a] pairs (their sum is rot / 2; 0: none):
+ * runs of them in order, or when cyclic dealt one by one to the axes in turn, leaving out those that have theirs.
+ * Pair c keeps the frequency theta^(-2c/rot) whatever its axis; with own_freqs the i-th of an axis' m pairs has
+ * theta^(-i/m) (the axes' frequencies are alike).  Scaling for longer contexts applies to either. */
+typedef struct {
+  int n_axes;
+  int pairs[4];
+  int cyclic, own_freqs;
+} nova_rope_axes;
+
+/* nova_kv_append with positions of several axes: pos is device int32 [n_axes][rows] (NULL: the token's number on
+ * every axis).  axes NULL: nova_kv_append; else rope is needed. */
+int nova_kv_append_axes(const nova_cache* cache, const nova_rows* rows, const nova_rope* rope, const nova_rope_axes* axes,
+                        const int32_t* pos, int in_type, const void* q, int64_t q_pitch, int n_q, const void* k,
+                        int64_t k_pitch, const void* v, int64_t v_pitch, void* q_out, int q_out_type, int64_t q_out_pitch,
+                        nova_stream_t stream);
+
+/* Rotary embedding of dense rows [n_heads][head_dim] (a vision encoder's q and k, say): head_dim is a multiple of 8
+ * up to 256, rot as in nova_rope up to head_dim; what is not turned is copied.
+ *  pos:    device int32 [n_axes][rows], or [rows] with axes NULL
+ *  x, out: device, in_type and out_type, pitches in elements; out may be x itself (same type and pitch) */
+int nova_rotate(const nova_rope* rope, const nova_rope_axes* axes, const int32_t* pos, int rows, int n_heads, int head_dim,
+                int in_type, const void* x, int64_t x_pitch, int out_type, void* out, int64_t out_pitch,
+                nova_stream_t stream);
+
 /* Read cached rows back as dense rows of out_type: row j of sequence b is token slots[row] (device
  * int32 [rows]; NULL: ctx[b] + j) of it.  Tokens of missing blocks read as zeros.  With the accepted
  * tokens of a tree as slots, a following nova_kv_append (no rope) moves them behind the context. */
@@ -320,6 +346,105 @@ size_t nova_logprobs_workspace_bytes(int rows, int vocab, int n_top);
 int nova_logprobs(const void* logits, int type, int64_t pitch, int rows, int vocab, const int32_t* given, int n_given,
                   float* given_lp, float* entropy, int n_top, float* top_lp, int32_t* top_ids, void* ws,
                   size_t ws_bytes, nova_stream_t stream);
+
+/* ------------------------------------------------------------------ between two model calls
+ * What a program does with a verify step's logits and rows before the next one, on the device throughout, so that a
+ * captured graph can hold the whole step.  Of `rows` the acceptance and the adapters read row_start, batch, rows and
+ * max_rows only.
+ *
+ * Which drafted tokens are kept.  Row j of a sequence (at most 64) feeds token ids[row] and logits[row] are what the
+ * target says after it; row 0 is the last token that is certain, the others are drafted.  With p a row's
+ * probabilities at the sequence's temperature:
+ *  - draft NULL: every row draws a token from p with its number u[row]; from row 0 the walk goes on in the first row
+ *    that hangs under the present one and feeds the token drawn there, and ends where there is none.  mask (as for
+ *    nova_tree_attention: a row hangs under the highest row below it that it sees) NULL: a chain.
+ *  - draft (logits of the distributions that the drafted tokens were drawn from, row j's token from draft[row j]; row
+ *    0's are not read; a chain, mask must be NULL): row j >= 1 is kept while u[row j] q(x) < p(x), p of the row before
+ *    it.  Behind the last kept row the token is drawn with u[row 0]: from max(p - q, 0) where a row was not kept, else
+ *    from p.  (Speculative sampling: the tokens are distributed as the target's own.)  A draft row without a
+ *    distribution keeps nothing, and p is drawn from.
+ * A draw is the first token whose running sum of probabilities exceeds u times their total (64-bit sums; u outside [0, 1)
+ * is taken into it, NaN as 0).  Temperature 0 is greedy (the largest logit, of equal ones the lowest id; a drafted token
+ * is kept if it is that).  A row with a NaN or +infinity, with nothing but -infinity, or of a sequence whose temperature
+ * is negative, infinite or NaN has no distribution: its token is -1, its log probability NaN, and the walk ends there.
+ *  logits, draft: device, NOVA_ACT_BF16 / NOVA_ACT_F32, pitch in elements, any alignment of their element
+ *  temperature:   device fp32 [batch], or NULL: 1
+ *  n_keep: device int32 [batch]: rows kept, row 0 among them (0: the sequence has no rows)
+ *  path:   device int32 [batch][max_rows]: the kept rows' numbers in their sequence, ascending; -1 behind
+ *  tokens: device int32 [batch][max_rows]: the token after each kept row (the last of them is new); -1 behind
+ *  lp:     device fp32 [batch][max_rows]: their log probabilities under p (0 at temperature 0 and behind)
+ * vocab <= 2^21, and rows (twice with draft) and batch times ceil(vocab / 4096) are below 2^24.
+ *  ws: device, nova_accept_workspace_bytes(), 256-byte aligned, as for nova_tree_attention */
+size_t nova_accept_workspace_bytes(const nova_rows* rows, int vocab, int with_draft);
+int nova_accept(const nova_rows* rows, const int32_t* ids, const uint64_t* mask, const void* logits, int type, int64_t pitch,
+                const void* draft, int draft_type, int64_t draft_pitch, int vocab, const float* temperature, const float* u,
+                int32_t* n_keep, int32_t* path, int32_t* tokens, float* lp, void* ws, size_t ws_bytes, nova_stream_t stream);
+
+/* Keep the accepted rows in `layers` layers of a cache (cache describes layer 0; layer l's arrays follow at l times
+ * their size): token ctx[b] + path[b][i] of sequence b becomes its token ctx[b] + i, for i < n_keep[b] (as nova_accept
+ * gives them; path NULL: the rows are in their places).  Everything is read before anything is written.  A path entry
+ * outside the sequence's rows, or a token that does not exist, leaves its place as it was.
+ *  ctx_out: device int32 [batch]: ctx[b] + n_keep[b] (n_keep taken into 0 .. the sequence's rows); not ctx itself; or NULL
+ * At most 64 rows of a sequence; batch * layers * n_kv is at most 2^24. */
+int nova_kv_keep(const nova_cache* cache, int layers, const nova_rows* rows, const int32_t* path, const int32_t* n_keep,
+                 int32_t* ctx_out, nova_stream_t stream);
+
+/* Blocks from[i] of one cache to blocks to[i] of another of the same type and heads, or of itself, in `layers` layers
+ * (from, to: device int32 [n]).  Entries outside the pools copy nothing.  No block may be named twice in `to`, nor in both. */
+int nova_kv_copy(const nova_cache* src, const nova_cache* dst, int layers, const int32_t* from, const int32_t* to, int n,
+                 nova_stream_t stream);
+
+/* The blocks of a pool: refs[block] is how many table entries name it; a block with 0 is free.  tables are device int32
+ * [batch][max_blocks], an entry outside the pool names no block.  What is taken are always the lowest free blocks, in the
+ * order of the requests; a request is served (done 1) if it and the requests before it find enough, and else left as it
+ * was (done 0).  Calls on one pool are made one after the other (on one stream, say).  At most 65535 requests.
+ *  ws: device, nova_pages_workspace_bytes(), 256-byte aligned, as for nova_tree_attention */
+typedef struct {
+  int32_t* refs;    /* device [num_blocks], all 0 at first */
+  int num_blocks;
+} nova_pages;
+size_t nova_pages_workspace_bytes(const nova_pages* pages, int batch, int n);
+/* Give every sequence the blocks of its first tokens[b] tokens (device int32 [batch]; those that it lacks are taken);
+ * done: device int32 [batch] (0 also where the table is too short). */
+int nova_pages_extend(const nova_pages* pages, int32_t* tables, int max_blocks, int batch, const int32_t* tokens,
+                      int32_t* done, void* ws, size_t ws_bytes, nova_stream_t stream);
+/* Row dst[i] of the tables becomes the first tokens[i] tokens of row src[i] (device int32 [n] each): whole blocks are
+ * shared, the last one, if tokens[i] fills it only in part, is copied in `layers` layers to a block that is taken.  What
+ * row dst[i] named before is overwritten (give it up first).  Refused (done[i] 0): rows outside the tables, a target
+ * that is another request's source, or of an earlier request, tokens beyond the source's blocks. */
+int nova_pages_fork(const nova_pages* pages, const nova_cache* cache, int layers, int32_t* tables, int max_blocks, int batch,
+                    const int32_t* src, const int32_t* dst, const int32_t* tokens, int n, int32_t* done, void* ws,
+                    size_t ws_bytes, nova_stream_t stream);
+/* Rows seqs[i] give up what lies behind their first tokens[i] tokens (device int32 [n] each; tokens NULL: everything);
+ * the entries become -1. */
+int nova_pages_free(const nova_pages* pages, int32_t* tables, int max_blocks, int batch, const int32_t* seqs,
+                    const int32_t* tokens, int n, nova_stream_t stream);
+/* Move the pool's used blocks to its front: of `live` of them those at live and above go to the free ones below, in order,
+ * in `layers` layers, and tables and refs follow (refs_out, tables_out: of their shapes, or refs and tables themselves;
+ * entries that name no used block become -1).  live_out: device int32 [1], or NULL.  Every table that names blocks of the
+ * pool has to be among the tables. */
+int nova_pages_compact(const nova_pages* pages, const nova_cache* cache, int layers, const int32_t* tables, int max_blocks,
+                       int batch, int32_t* refs_out, int32_t* tables_out, int32_t* live_out, void* ws, size_t ws_bytes,
+                       nova_stream_t stream);
+
+/* ------------------------------------------------------------------ adapters
+ * Low-rank adapters of many requests beside a projection that they share:
+ *   out[row] = base[row] + scale[i] b[i] (a[i] x[row]),  i = which[sequence of the row]
+ * (fp32 sums, rounded once; which outside 0 .. n - 1: no adapter, out is base).  Rows outside the sequences are left as
+ * they were.
+ *  which: device int32 [batch];  x: device, x_type;  base: device, out_type, NULL: 0;  out: device, out_type, may be
+ *         base itself (same pitch); pitches in elements, a multiple of 16 bytes
+ * rank is a multiple of 8 up to 128; k and n_out are multiples of 8 up to 2^24. */
+typedef struct {
+  const void* a;       /* device bf16 [n][rank][k] */
+  const void* b;       /* device bf16 [n][n_out][rank] */
+  const float* scale;  /* device fp32 [n], or NULL: 1 */
+  int n, rank, k, n_out;
+} nova_adapters;
+size_t nova_lora_workspace_bytes(const nova_adapters* adapters, const nova_rows* rows);
+int nova_lora(const nova_adapters* adapters, const nova_rows* rows, const int32_t* which, int x_type, const void* x,
+              int64_t x_pitch, int out_type, const void* base, int64_t base_pitch, void* out, int64_t out_pitch, void* ws,
+              size_t ws_bytes, nova_stream_t stream);
 
 /* ------------------------------------------------------------------ LLM on a cache of any type
  * nova_llm_prefill into a pool of nova_cache layers (cache describes layer 0; layer l's arrays follow

@@ -1,0 +1,461 @@
+// Which drafted tokens the target's probabilities keep, and the token that is drawn behind them, from given numbers.
+// With z = l / T, p = e^(z - max z) / sum: a row's probabilities at its sequence's temperature T.
+//  * With the draft's probabilities q (a chain): row j's token x is kept while u_j q_j(x) < p_(j-1)(x); behind the
+//    first that is not, the token is drawn from max(p - q, 0), behind the last row from p (speculative sampling: what
+//    comes out is distributed as the target's own tokens).
+//  * Without (a tree or a chain of tokens): every row draws its token from p, and the walk goes on in the row that
+//    brought it.
+// A draw is the first token whose running sum exceeds u times the total.  The running sums reach over the whole
+// vocabulary and are compared with a number that may lie next to any of them, so weights and sums are in 64 bits (an
+// fp32 sum would move about one draw in a thousand at 152064 logits).
+// Two launches: the first reads every logit once (maximum, sum and largest id of chunks of 4096), the second
+// decides and draws, reading again only chunks of the rows where something is drawn.
+#include <algorithm>
+
+#include "paged.hpp"
+
+namespace nova {
+
+constexpr int AC_CHUNK = 4096;             // logits of a workgroup
+constexpr int AC_PER = AC_CHUNK / 256;     // of a thread
+
+// A wave's or a workgroup's sums in a fixed order (so that every call gives the same draws).
+NOVA_DEV double wave_sum64(double v) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+NOVA_DEV double wave_scan64(double v) {    // inclusive
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const double up = __shfl_up(v, o, 64);
+    if (lane >= o) v += up;
+  }
+  return v;
+}
+
+// The sequence of a row (batch: none).
+NOVA_DEV int seq_of_row(const BatchRows& p, int r) {
+  if (!p.row_start) return r / p.max_rows;
+  int lo = 0, hi = p.batch;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (p.row_start[mid + 1] <= r) lo = mid + 1;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// 1 / T, 0 for T = 0 (the largest logit takes all), negative where T gives no distribution.
+NOVA_DEV double inv_temperature(const AcceptArgs& p, int b) {
+  const float t = p.temperature ? p.temperature[b] : 1.f;
+  if (t == 0.f) return 0.0;
+  return t > 0.f && t < INFINITY ? 1.0 / (double)t : -1.0;
+}
+
+// e^x for x <= 0 in 64 bits: 2^k e^r with |r| <= ln 2 / 2, and the Taylor series of e^r to r^13 (its rest is below 5e-18).
+NOVA_DEV double exp_neg(double x) {
+  if (!(x > -745.0)) return x != x ? x : 0.0;
+  const double k = rint(x * 1.4426950408889634);
+  double r = fma(k, -0x1.62e42fefa39efp-1, x);
+  r = fma(k, -0x1.abc9e3b39803fp-56, r);
+  double y = 1.0 / 6227020800.0;
+  y = fma(y, r, 1.0 / 479001600.0);
+  y = fma(y, r, 1.0 / 39916800.0);
+  y = fma(y, r, 1.0 / 3628800.0);
+  y = fma(y, r, 1.0 / 362880.0);
+  y = fma(y, r, 1.0 / 40320.0);
+  y = fma(y, r, 1.0 / 5040.0);
+  y = fma(y, r, 1.0 / 720.0);
+  y = fma(y, r, 1.0 / 120.0);
+  y = fma(y, r, 1.0 / 24.0);
+  y = fma(y, r, 1.0 / 6.0);
+  y = fma(y, r, 0.5);
+  y = fma(y, r, 1.0);
+  y = fma(y, r, 1.0);
+  return ldexp(y, (int)k);
+}
+
+// A logit of a row, from memory in its type.
+template <typename T> NOVA_DEV float logit(const T* row, int i) { return to_f<T>(row[i]); }
+
+// ------------------------------------------------------------------ first pass
+// Workgroup: a chunk of one row.  Rows 0 .. rows - 1 are the target's, the next `rows` the draft's.
+template <typename TL, typename TD>
+__global__ void __launch_bounds__(256) accept_stats_kernel(AcceptArgs p) {
+  // what the second kernel counts, and the outputs of sequences without rows
+  for (long b = (long)blockIdx.x * 256 + threadIdx.x; b < p.r.batch; b += (long)gridDim.x * 256) {
+    p.counters[b] = 0u;
+    if (seq_rows(p.r, (int)b).n > 0) continue;
+    p.n_keep[b] = 0;
+    for (int i = 0; i < p.r.max_rows; ++i) {
+      p.path[b * p.r.max_rows + i] = p.tokens[b * p.r.max_rows + i] = -1;
+      p.lp[b * p.r.max_rows + i] = 0.f;
+    }
+  }
+  const int item = blockIdx.x / p.chunks, chunk = blockIdx.x % p.chunks;
+  if (item >= p.items) return;
+  const bool draft = item >= p.r.rows;
+  const int r = draft ? item - p.r.rows : item, b = seq_of_row(p.r, r);
+  if (b >= p.r.batch) return;
+  const SeqRows sr = seq_rows(p.r, b);
+  if (r < sr.r0 + (draft ? 1 : 0) || r >= sr.r0 + sr.n) return;   // a sequence's first row was drawn by nobody
+  const double inv = inv_temperature(p, b);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c0 = chunk * AC_CHUNK;
+  float x[AC_PER];
+#pragma unroll
+  for (int i = 0; i < AC_PER; ++i) {
+    const int at = c0 + i * 256 + threadIdx.x;
+    x[i] = at >= p.vocab ? -INFINITY : draft ? logit((const TD*)p.draft + (long)r * p.draft_row, at) : logit((const TL*)p.logits + (long)r * p.row, at);
+  }
+  float m = -INFINITY;
+  int arg = 0x7FFFFFFF;
+  bool bad = false;                        // NaN or +infinity: no distribution
+#pragma unroll
+  for (int i = 0; i < AC_PER; ++i) {
+    bad |= !(x[i] < INFINITY);
+    if (x[i] > m) m = x[i], arg = c0 + i * 256 + threadIdx.x;
+  }
+  __shared__ float sm_m[4];
+  __shared__ int sm_arg[4], sm_bad[4];
+  __shared__ double sm_s[4];
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) {
+    const float om = __shfl_xor(m, o, 64);
+    const int oa = __shfl_xor(arg, o, 64);
+    if (om > m || (om == m && oa < arg)) m = om, arg = oa;
+  }
+  const bool any_bad = __ballot(bad) != 0;
+  if (lane == 0) sm_m[wave] = m, sm_arg[wave] = arg, sm_bad[wave] = any_bad;
+  __syncthreads();
+  m = sm_m[0], arg = sm_arg[0], bad = sm_bad[0];
+#pragma unroll
+  for (int w = 1; w < 4; ++w) {
+    if (sm_m[w] > m || (sm_m[w] == m && sm_arg[w] < arg)) m = sm_m[w], arg = sm_arg[w];
+    bad |= sm_bad[w];
+  }
+  double sum = 0.0;
+  if (inv > 0.0 && m > -INFINITY && !bad) {
+#pragma unroll
+    for (int i = 0; i < AC_PER; ++i) sum += exp_neg(((double)x[i] - (double)m) * inv);
+  }
+  sum = wave_sum64(sum);
+  if (lane == 0) sm_s[wave] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const long at = (long)item * p.chunks + chunk;
+    p.part_max[at] = bad ? __uint_as_float(0x7FC00000u) : m;
+    p.part_arg[at] = arg;
+    p.part_sum[at] = ((sm_s[0] + sm_s[1]) + sm_s[2]) + sm_s[3];
+  }
+}
+
+// ------------------------------------------------------------------ a row's chunks joined
+// m: the row's maximum (NaN: no distribution), s: its sum relative to it, arg: the first of the largest logits.
+struct RowStats { float m; int arg; double s; };
+NOVA_DEV bool has_dist(const RowStats& a, double inv) { return a.m > -INFINITY && inv >= 0.0; }   // NaN compares false
+
+// By one wave; every lane returns the same.
+NOVA_DEV RowStats join_row(const AcceptArgs& p, int item, double inv) {
+  const int lane = threadIdx.x & 63;
+  const long at = (long)item * p.chunks;
+  RowStats a{-INFINITY, 0x7FFFFFFF, 0.0};
+  bool bad = false;
+  for (int c = lane; c < p.chunks; c += 64) {
+    const float m = p.part_max[at + c];
+    bad |= m != m;
+    if (m > a.m) a.m = m, a.arg = p.part_arg[at + c];
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) {
+    const float om = __shfl_xor(a.m, o, 64);
+    const int oa = __shfl_xor(a.arg, o, 64);
+    if (om > a.m || (om == a.m && oa < a.arg)) a.m = om, a.arg = oa;
+  }
+  if (__ballot(bad)) {
+    a.m = __uint_as_float(0x7FC00000u);
+    return a;
+  }
+  if (a.m == -INFINITY || !(inv > 0.0)) return a;
+  for (int c = lane; c < p.chunks; c += 64) {
+    const float m = p.part_max[at + c];
+    if (m > -INFINITY) a.s += p.part_sum[at + c] * exp_neg(((double)m - (double)a.m) * inv);
+  }
+  a.s = wave_sum64(a.s);
+  return a;
+}
+
+// A number in [0, 1) (1 and above: the largest below; NaN and below 0: 0).
+NOVA_DEV double uniform(float u) { return u > 0.f ? (double)fminf(u, 0x1.fffffep-1f) : 0.0; }
+
+// The first place of 0 .. n - 1 whose running sum exceeds `target` (none, by rounding: the last with a positive value),
+// and the running sum before it.  value(i) is asked for in order; by one wave, every lane returns the same.
+template <typename F> NOVA_DEV int first_above(int n, double target, double* before, F&& value) {
+  const int lane = threadIdx.x & 63;
+  double run = 0.0, run_last = 0.0;
+  int last = 0;
+  for (int i0 = 0; i0 < n; i0 += 64) {
+    const double v = i0 + lane < n ? value(i0 + lane) : 0.0;
+    const double incl = run + wave_scan64(v);
+    const unsigned long long over = __ballot(incl > target && v > 0.0), some = __ballot(v > 0.0);
+    if (over) {
+      const int l = __ffsll(over) - 1;
+      *before = __shfl(incl - v, l, 64);
+      return i0 + l;
+    }
+    if (some) {
+      const int l = 63 - __clzll(some);
+      last = i0 + l;
+      run_last = __shfl(incl - v, l, 64);
+    }
+    run = __shfl(incl, 63, 64);
+  }
+  *before = run_last;
+  return last;
+}
+
+// The token of a chunk whose running sum of weight(i) exceeds `target`; by the whole workgroup of 256.
+template <typename F> NOVA_DEV int draw_in_chunk(int c0, int vocab, double target, F&& weight) {
+  __shared__ double sm_sum[256];
+  __shared__ int sm_pick;
+  const int first = c0 + threadIdx.x * AC_PER;
+  double w[AC_PER], sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < AC_PER; ++i) {
+    w[i] = first + i < vocab ? weight(first + i) : 0.0;
+    sum += w[i];
+  }
+  __syncthreads();
+  sm_sum[threadIdx.x] = sum;
+  __syncthreads();
+  double before = 0.0;
+  const int t = first_above(256, target, &before, [&](int i) { return sm_sum[i]; });
+  if ((int)threadIdx.x == t) {
+    double run = before;
+    int pick = first;
+    bool found = false;
+#pragma unroll
+    for (int i = 0; i < AC_PER; ++i) {
+      run += w[i];
+      if (!found && w[i] > 0.0) pick = first + i;          // the last with a weight, unless the sum is exceeded before
+      found |= w[i] > 0.0 && run > target;
+    }
+    sm_pick = pick;
+  }
+  __syncthreads();
+  return sm_pick;
+}
+
+// A token drawn from a target row by its number u; by the whole workgroup.  -1: the row has no distribution.
+template <typename TL> NOVA_DEV int draw_row(const AcceptArgs& p, int r, const RowStats& a, double inv, float u) {
+  if (!has_dist(a, inv)) return -1;
+  if (inv == 0.0) return a.arg;
+  const TL* row = (const TL*)p.logits + (long)r * p.row;
+  const long at = (long)r * p.chunks;
+  double before = 0.0;
+  const double target = uniform(u) * a.s;
+  auto scale = [&](float m) { return m > -INFINITY ? exp_neg(((double)m - (double)a.m) * inv) : 0.0; };
+  const int c = first_above(p.chunks, target, &before, [&](int i) { return p.part_sum[at + i] * scale(p.part_max[at + i]); });
+  return draw_in_chunk(c * AC_CHUNK, p.vocab, target - before, [&](int i) { return exp_neg(((double)logit(row, i) - (double)a.m) * inv); });
+}
+
+// log p of a token of a row.
+template <typename TL> NOVA_DEV float log_p(const AcceptArgs& p, int r, const RowStats& a, double inv, int token) {
+  if (token < 0) return __uint_as_float(0x7FC00000u);
+  if (inv == 0.0) return 0.f;
+  return (float)(((double)logit((const TL*)p.logits + (long)r * p.row, token) - (double)a.m) * inv - log(a.s));
+}
+
+// The workgroups of a sequence that have come this far, this one included; what each stored before (with
+// device-scope stores) is at the coherent level then.
+NOVA_DEV unsigned arrive(unsigned* counter) {
+  __shared__ unsigned sm_n;
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+  if (threadIdx.x == 0) sm_n = 1u + __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  return sm_n;
+}
+template <typename T> NOVA_DEV void put(T* at, T v) { __hip_atomic_store(at, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+template <typename T> NOVA_DEV T get(const T* at) { return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// ------------------------------------------------------------------ second pass without the draft's probabilities
+// Workgroup: a row, which draws its token; the last of a sequence walks from its first row on.
+template <typename TL>
+__global__ void __launch_bounds__(256) accept_follow_kernel(AcceptArgs p) {
+  const int r = blockIdx.x, b = seq_of_row(p.r, r);
+  if (b >= p.r.batch) return;
+  const SeqRows sr = seq_rows(p.r, b);
+  if (r < sr.r0 || r >= sr.r0 + sr.n) return;
+  const double inv = inv_temperature(p, b);
+  const RowStats a = join_row(p, r, inv);
+  const int token = draw_row<TL>(p, r, a, inv, p.u[r]);
+  if (threadIdx.x == 0) {
+    put(p.row_token + r, token);
+    put(p.row_lp + r, log_p<TL>(p, r, a, inv, token));
+  }
+  if (arrive(p.counters + b) != (unsigned)sr.n) return;
+  if (threadIdx.x >= 64) return;
+  // lane j: row j of the sequence (at most 64), the row that it hangs under (-1: none) and its token
+  const int j = threadIdx.x;
+  const bool live = j < sr.n;
+  int parent = j - 1;
+  if (p.mask) {
+    const unsigned long long up = live ? p.mask[sr.r0 + j] & ((1ull << j) - 1) : 0;
+    parent = up ? 63 - __clzll(up) : -1;
+  }
+  const int id = live ? p.ids[sr.r0 + j] : -1;
+  const int drawn = live ? get(p.row_token + sr.r0 + j) : -1;
+  const float lp = live ? get(p.row_lp + sr.r0 + j) : 0.f;
+  int path = -1, n = 0, at = 0;            // lane i: the i-th kept row
+  while (true) {
+    if (j == n) path = at;
+    ++n;
+    const int t = __shfl(drawn, at, 64);
+    const unsigned long long kids = __ballot(live && j > at && parent == at && id == t && t >= 0);
+    if (!kids) break;
+    at = __ffsll(kids) - 1;
+  }
+  const int from = path < 0 ? 0 : path;
+  const int tok = __shfl(drawn, from, 64);
+  const float tlp = __shfl(lp, from, 64);
+  if (j == 0) p.n_keep[b] = n;
+  if (j < p.r.max_rows) {
+    const long o = (long)b * p.r.max_rows + j;
+    p.path[o] = path;
+    p.tokens[o] = path < 0 ? -1 : tok;
+    p.lp[o] = path < 0 ? 0.f : tlp;
+  }
+}
+
+// ------------------------------------------------------------------ second pass with the draft's probabilities
+// Workgroup: a chunk of a sequence.  Each finds the first row that is not kept (a wave tests a row); where the token is
+// drawn from what the target has more than the draft, it sums that over its chunk, and the last to arrive draws.  Else
+// the first chunk's workgroup draws from the target's row.
+template <typename TL, typename TD>
+__global__ void __launch_bounds__(256) accept_draft_kernel(AcceptArgs p) {
+  const int b = blockIdx.x / p.chunks, chunk = blockIdx.x % p.chunks;
+  const SeqRows sr = seq_rows(p.r, b);
+  if (sr.n <= 0) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const double inv = inv_temperature(p, b);
+  __shared__ float sm_lp[64];
+  __shared__ int sm_kept[4], sm_rest[4];   // of a wave's row: its token is kept; else what remains of p is drawn from
+  __shared__ RowStats sm_p[4], sm_q[4];
+  int at = 0;                              // the last kept row
+  bool rest = false;
+  RowStats tp{}, tq{};                     // of it, and of the draft's row behind it
+  for (int j0 = 1;; j0 += 4) {
+    // wave w: row j0 + w against its draft, the target's row before it
+    const int j = j0 + wave;
+    if (j <= sr.n) {
+      const int r = sr.r0 + j - 1;
+      const RowStats a = join_row(p, r, inv);
+      RowStats q{__uint_as_float(0x7FC00000u), 0, 0.0};
+      bool kept = false, some = false;
+      float lp = 0.f;
+      if (j < sr.n && has_dist(a, inv)) {
+        const int x = p.ids[r + 1];
+        const bool in = (unsigned)x < (unsigned)p.vocab;
+        if (inv == 0.0) {
+          kept = x == a.arg;
+        } else {
+          q = join_row(p, p.r.rows + r + 1, inv);
+          some = has_dist(q, inv);
+          if (in && some) {
+            const double zp = ((double)logit((const TL*)p.logits + (long)r * p.row, x) - (double)a.m) * inv;
+            const double zq = ((double)logit((const TD*)p.draft + (long)(r + 1) * p.draft_row, x) - (double)q.m) * inv;
+            kept = uniform(p.u[r + 1]) * (exp_neg(zq) / q.s) < exp_neg(zp) / a.s;
+            lp = (float)(zp - log(a.s));
+          }
+        }
+      }
+      if (lane == 0) {
+        sm_kept[wave] = kept, sm_rest[wave] = some && !kept;
+        sm_p[wave] = a, sm_q[wave] = q;
+        if (kept) sm_lp[j - 1] = lp;
+      }
+    } else if (lane == 0) {
+      sm_kept[wave] = 0;
+    }
+    __syncthreads();
+    int w = 0;
+    while (w < 4 && sm_kept[w]) ++w;
+    if (w < 4) {
+      at = j0 + w - 1;
+      rest = sm_rest[w];
+      tp = sm_p[w], tq = sm_q[w];
+      break;
+    }
+    __syncthreads();
+  }
+  const int r = sr.r0 + at;
+  const float u = p.u[sr.r0];
+  int token;
+  if (rest) {
+    const TL* rp = (const TL*)p.logits + (long)r * p.row;
+    const TD* rq = (const TD*)p.draft + (long)(r + 1) * p.draft_row;
+    const double ip = 1.0 / tp.s, iq = 1.0 / tq.s;
+    auto more = [&](int i) {
+      const double d = exp_neg(((double)logit(rp, i) - (double)tp.m) * inv) * ip - exp_neg(((double)logit(rq, i) - (double)tq.m) * inv) * iq;
+      return d > 0.0 ? d : 0.0;
+    };
+    __shared__ double sm_s[4];
+    double sum = 0.0;
+    const int first = chunk * AC_CHUNK + threadIdx.x;
+#pragma unroll 4
+    for (int i = 0; i < AC_PER; ++i)
+      if (first + 256 * i < p.vocab) sum += more(first + 256 * i);
+    sum = wave_sum64(sum);
+    if (lane == 0) sm_s[wave] = sum;
+    __syncthreads();
+    double* parts = p.rest_sum + (long)b * p.chunks;
+    if (threadIdx.x == 0) put(parts + chunk, ((sm_s[0] + sm_s[1]) + sm_s[2]) + sm_s[3]);
+    if (arrive(p.counters + b) != (unsigned)p.chunks) return;
+    double total = 0.0;
+    for (int c = lane; c < p.chunks; c += 64) total += get(parts + c);
+    total = wave_sum64(total);
+    if (total > 0.0) {
+      const double target = uniform(u) * total;
+      double before = 0.0;
+      const int c = first_above(p.chunks, target, &before, [&](int i) { return get(parts + i); });
+      token = draw_in_chunk(c * AC_CHUNK, p.vocab, target - before, more);
+    } else {                               // nothing is left by rounding: p and q are alike
+      token = draw_row<TL>(p, r, tp, inv, u);
+    }
+  } else {
+    if (chunk != 0) return;
+    token = draw_row<TL>(p, r, tp, inv, u);
+  }
+  const int i = threadIdx.x;
+  if (i == 0) p.n_keep[b] = at + 1;
+  if (i < p.r.max_rows) {
+    const long o = (long)b * p.r.max_rows + i;
+    p.path[o] = i <= at ? i : -1;
+    p.tokens[o] = i < at ? p.ids[sr.r0 + i + 1] : i == at ? token : -1;
+    p.lp[o] = i < at ? sm_lp[i] : i == at ? log_p<TL>(p, r, tp, inv, token) : 0.f;
+  }
+}
+
+// ------------------------------------------------------------------ launch
+int accept_chunks(int vocab) { return (vocab + AC_CHUNK - 1) / AC_CHUNK; }
+
+template <typename TL, typename TD>
+static hipError_t accept_types(const AcceptArgs& p, hipStream_t s) {
+  const long blocks = std::max<long>(1, (long)p.items * p.chunks);
+  hipLaunchKernelGGL((accept_stats_kernel<TL, TD>), dim3((unsigned)blocks), dim3(256), 0, s, p);
+  if (hipError_t e = hipGetLastError()) return e;
+  if (p.r.rows == 0) return hipSuccess;
+  if (p.draft) hipLaunchKernelGGL((accept_draft_kernel<TL, TD>), dim3((unsigned)((long)p.r.batch * p.chunks)), dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((accept_follow_kernel<TL>), dim3((unsigned)p.r.rows), dim3(256), 0, s, p);
+  return hipGetLastError();
+}
+
+hipError_t accept(const AcceptArgs& p, hipStream_t s) {
+  if (p.r.max_rows <= 0 || p.r.max_rows > 64 || p.vocab <= 0) return hipErrorInvalidValue;
+  if (p.f32) return p.draft_f32 ? accept_types<float, float>(p, s) : accept_types<float, bf16_t>(p, s);
+  return p.draft_f32 ? accept_types<bf16_t, float>(p, s) : accept_types<bf16_t, bf16_t>(p, s);
+}
+
+}  // namespace nova

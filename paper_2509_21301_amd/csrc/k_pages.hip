@@ -1,0 +1,383 @@
+// Pages of a paged cache on the device: blocks taken for tokens to come, sequences forked (whole pages shared, the
+// last one copied), given up, the pool's used blocks moved to its front, blocks copied by number, and the accepted
+// rows of drafted trees moved next to their context.  refs[block] counts the table entries that name a block; a block
+// with none is free.  What is taken is always the lowest free blocks in the order of the requests, so results do not
+// depend on scheduling.
+//
+// A plan (who gets which block) is one workgroup of 1024 threads: prefix sums over the requests and over the pool,
+// bound by the latency of their few steps.  Moving the pages themselves, in every layer, is the second launch, bound
+// by HBM.
+#include <algorithm>
+
+#include "paged.hpp"
+
+namespace nova {
+
+constexpr int PLAN = 1024;
+
+// Exclusive prefix sum over the workgroup's threads, and the total.
+template <typename T> NOVA_DEV T block_scan(T v, T* total) {
+  __shared__ T sm[PLAN / 64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  T s = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const T up = __shfl_up(s, o, 64);
+    if (lane >= o) s += up;
+  }
+  __syncthreads();
+  if (lane == 63) sm[wave] = s;
+  __syncthreads();
+  T before = 0, sum = 0;
+#pragma unroll
+  for (int w = 0; w < PLAN / 64; ++w) {
+    if (w < wave) before += sm[w];
+    sum += sm[w];
+  }
+  *total = sum;
+  return before + s - v;
+}
+
+// The lowest `want` free blocks of the pool into list[]; returns how many there are (at most `want`).
+NOVA_DEV int free_blocks(const int* refs, int num_blocks, int want, int* list) {
+  int got = 0;
+  for (int b0 = 0; b0 < num_blocks && got < want; b0 += 4 * PLAN) {
+    const int first = b0 + 4 * threadIdx.x;
+    bool is[4];
+    int n = 0, total;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      is[i] = first + i < num_blocks && refs[first + i] <= 0;
+      n += is[i];
+    }
+    int at = got + block_scan(n, &total);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (is[i]) {
+        if (at < want) list[at] = first + i;
+        ++at;
+      }
+    got += total;
+  }
+  __syncthreads();                          // list[] is read by other threads
+  return min(got, want);
+}
+
+NOVA_DEV bool in_pool(int block, int num_blocks) { return (unsigned)block < (unsigned)num_blocks; }
+
+// ------------------------------------------------------------------ blocks for tokens to come
+// A wave per sequence counts the entries below need / 16 that name no block; a sequence is served if it and those
+// before it find enough free blocks.
+__global__ void __launch_bounds__(PLAN) pages_extend_kernel(PagesArgs p) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int b = wave; b < p.n; b += PLAN / 64) {
+    const int need = p.lens[b];
+    const long blocks = need <= 0 ? 0 : ((long)need + PAGE - 1) / PAGE;
+    int miss = 0;
+    if (blocks <= p.max_blocks)
+      for (int e = lane; e < blocks; e += 64) miss += !in_pool(p.tables[(long)b * p.max_blocks + e], p.num_blocks);
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) miss += __shfl_xor(miss, o, 64);
+    if (lane == 0) p.want[b] = blocks > p.max_blocks ? -1 : miss;       // -1: the table is too short
+  }
+  __syncthreads();
+  long asked = 0;
+  for (int b0 = 0; b0 < p.n; b0 += PLAN) {
+    const int b = b0 + threadIdx.x;
+    long total;
+    const long before = block_scan<long>(b < p.n ? max(p.want[b], 0) : 0, &total);
+    if (b < p.n) p.rank[b] = (int)min(asked + before, 0x7FFFFFFFL);
+    asked += total;
+  }
+  const int found = free_blocks(p.refs, p.num_blocks, (int)min(asked, (long)p.num_blocks), p.list);
+  for (int b = wave; b < p.n; b += PLAN / 64) {
+    const int want = p.want[b], rank = p.rank[b];
+    const bool ok = want == 0 || (want > 0 && (long)rank + want <= found);
+    if (lane == 0) p.done[b] = ok;
+    if (!ok || want == 0) continue;
+    const int blocks = (int)(((long)p.lens[b] + PAGE - 1) / PAGE);
+    int at = rank;
+    for (int e0 = 0; e0 < blocks; e0 += 64) {
+      const int e = e0 + lane;
+      int* entry = p.tables + (long)b * p.max_blocks + e;
+      const bool miss = e < blocks && !in_pool(*entry, p.num_blocks);
+      const unsigned long long m = __ballot(miss);
+      if (miss) {
+        const int block = p.list[at + __popcll(m & ((1ull << lane) - 1))];
+        *entry = block;
+        p.refs[block] = 1;
+      }
+      at += __popcll(m);
+    }
+  }
+}
+
+// ------------------------------------------------------------------ forks
+// Fork i: row dst[i] of the tables becomes the first lens[i] tokens of row src[i].  Refused (done 0, nothing changed):
+// rows outside the tables, a row that is another fork's target too (the first of them counts) or a target that is a
+// source, lengths that the source's pages do not cover, and forks behind the pool's last free block.
+__global__ void __launch_bounds__(PLAN) pages_fork_kernel(PagesArgs p) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int b = threadIdx.x; b < p.batch; b += PLAN) __hip_atomic_store(p.claim + b, 0x7FFFFFFF, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  for (int i = threadIdx.x; i < p.n; i += PLAN)
+    if ((unsigned)p.dst[i] < (unsigned)p.batch) __hip_atomic_fetch_min(p.claim + p.dst[i], i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  for (int i = wave; i < p.n; i += PLAN / 64) {
+    const int src = p.src[i], dst = p.dst[i], len = p.lens[i];
+    const long blocks = ((long)len + PAGE - 1) / PAGE;
+    bool ok = (unsigned)src < (unsigned)p.batch && (unsigned)dst < (unsigned)p.batch && len >= 0 && blocks <= p.max_blocks;
+    if (ok) ok = __hip_atomic_load(p.claim + dst, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == i &&
+                 __hip_atomic_load(p.claim + src, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 0x7FFFFFFF;
+    bool miss = false;
+    if (ok)
+      for (int e = lane; e < blocks; e += 64) miss |= !in_pool(p.tables[(long)src * p.max_blocks + e], p.num_blocks);
+    if (__ballot(miss)) ok = false;
+    if (lane == 0) p.want[i] = ok ? len % PAGE > 0 : -1;
+  }
+  __syncthreads();
+  int asked = 0;
+  for (int i0 = 0; i0 < p.n; i0 += PLAN) {
+    const int i = i0 + threadIdx.x;
+    int total;
+    const int before = block_scan(i < p.n ? max(p.want[i], 0) : 0, &total);
+    if (i < p.n) p.rank[i] = asked + before;
+    asked += total;
+  }
+  const int found = free_blocks(p.refs, p.num_blocks, min(asked, p.num_blocks), p.list);
+  for (int i = wave; i < p.n; i += PLAN / 64) {
+    const int want = p.want[i], rank = p.rank[i];
+    const bool ok = want == 0 || (want == 1 && rank < found);
+    int from = -1, to = -1;
+    if (ok) {
+      const int full = p.lens[i] / PAGE;
+      const int* theirs = p.tables + (long)p.src[i] * p.max_blocks;
+      int* mine = p.tables + (long)p.dst[i] * p.max_blocks;
+      if (want) from = theirs[full], to = p.list[rank];
+      for (int e = lane; e < p.max_blocks; e += 64) {
+        const int block = e < full ? theirs[e] : e == full ? to : -1;
+        mine[e] = block;
+        if (e < full) atomicAdd(p.refs + block, 1);
+      }
+      if (lane == 0 && want) atomicAdd(p.refs + to, 1 - p.refs[to]);
+    }
+    if (lane == 0) p.done[i] = ok, p.from[i] = from, p.to[i] = to;
+  }
+}
+
+// ------------------------------------------------------------------ pages given up
+// Row seqs[i] of the tables keeps the pages of its first lens[i] tokens (lens null: none).  An entry is taken out of
+// the table by one thread, whoever else is at it.
+__global__ void __launch_bounds__(256) pages_free_kernel(PagesArgs p) {
+  const int row = p.src[blockIdx.y];
+  if ((unsigned)row >= (unsigned)p.batch) return;
+  const int len = p.lens ? max(p.lens[blockIdx.y], 0) : 0;
+  const int keep = (int)(((long)len + PAGE - 1) / PAGE);
+  for (int e = keep + blockIdx.x * 256 + threadIdx.x; e < p.max_blocks; e += gridDim.x * 256) {
+    int* entry = p.tables + (long)row * p.max_blocks + e;
+    if (*entry == -1) continue;
+    const int block = atomicExch(entry, -1);
+    if (in_pool(block, p.num_blocks)) atomicSub(p.refs + block, 1);
+  }
+}
+
+// ------------------------------------------------------------------ the pool's used blocks to its front
+// Of `live` used blocks those at live and above move to the free ones below it, in order.  place[b]: where block b
+// goes (-1: it is free).
+__global__ void __launch_bounds__(PLAN) pages_compact_kernel(PagesArgs p) {
+  const int per = (p.num_blocks + PLAN - 1) / PLAN;
+  const int lo = min((long)p.num_blocks, (long)per * threadIdx.x), hi = min(p.num_blocks, lo + per);
+  int used = 0, live, total;
+  for (int b = lo; b < hi; ++b) used += p.refs[b] > 0;
+  block_scan(used, &live);
+  int holes = 0, movers = 0;
+  for (int b = lo; b < hi; ++b) {
+    const bool is = p.refs[b] > 0;
+    holes += !is && b < live;
+    movers += is && b >= live;
+  }
+  int hole = block_scan(holes, &total), mover = block_scan(movers, &total);
+  for (int b = lo; b < hi; ++b)
+    if (p.refs[b] <= 0 && b < live) p.to[hole++] = b;
+  __syncthreads();
+  for (int b = lo; b < hi; ++b) {
+    const bool is = p.refs[b] > 0;
+    int to = is ? b : -1;
+    if (is && b >= live) {
+      to = p.to[mover];
+      p.from[mover++] = b;
+    }
+    p.place[b] = to;
+  }
+  if (threadIdx.x == 0) {
+    *p.moves = total;
+    *p.live = live;
+  }
+}
+
+// ------------------------------------------------------------------ blocks moved, in every layer
+// Units (move, layer, K or V) are dealt to the workgroups; a lane has four 16-byte loads in flight.  Moves: from[i] to
+// to[i]; either outside its pool: none.
+NOVA_DEV void copy_bytes(const char* from, char* to, long bytes) {
+  const u32x4* f = reinterpret_cast<const u32x4*>(from);
+  u32x4* t = reinterpret_cast<u32x4*>(to);
+  const long n = bytes / 16;
+  long i = threadIdx.x;
+  for (; i + 3 * 256 < n; i += 4 * 256) {
+    const u32x4 a = f[i], b = f[i + 256], c = f[i + 512], d = f[i + 768];
+    t[i] = a, t[i + 256] = b, t[i + 512] = c, t[i + 768] = d;
+  }
+  for (; i < n; i += 256) t[i] = f[i];
+}
+NOVA_DEV void copy_unit(const CopyArgs& p, long unit) {
+  const int side = unit & 1, layer = (unit >> 1) % p.layers;
+  const long i = (unit >> 1) / p.layers;
+  const int from = p.from[i], to = p.to[i];
+  if (!in_pool(from, p.src.num_blocks) || !in_pool(to, p.dst.num_blocks)) return;
+  const char* s = (const char*)(side ? p.src.v : p.src.k) + ((size_t)layer * p.src.num_blocks + from) * p.page;
+  char* d = (char*)(side ? p.dst.v : p.dst.k) + ((size_t)layer * p.dst.num_blocks + to) * p.page;
+  if (s == d) return;
+  copy_bytes(s, d, p.page);
+  if (!p.src.k_exp) return;
+  const int n = p.src.n_kv * PAGE;
+  copy_bytes((const char*)(side ? p.src.v_exp : p.src.k_exp) + ((size_t)layer * p.src.num_blocks + from) * n,
+             (char*)(side ? p.dst.v_exp : p.dst.k_exp) + ((size_t)layer * p.dst.num_blocks + to) * n, n);
+}
+__global__ void __launch_bounds__(256) copy_pages_kernel(CopyArgs p) {
+  const long units = 2l * p.layers * (p.moves ? *p.moves : p.n);
+  for (long u = blockIdx.x; u < units; u += gridDim.x) copy_unit(p, u);
+}
+
+// A compaction's pages, with its tables and counts: the first workgroups take those.
+__global__ void __launch_bounds__(256) compact_move_kernel(CopyArgs p, PagesArgs g) {
+  const int moves = *p.moves;
+  const long entries = (long)g.batch * g.max_blocks, stride = (long)gridDim.x * 256, t0 = (long)blockIdx.x * 256 + threadIdx.x;
+  for (long i = t0; i < entries; i += stride) {
+    const int block = g.tables[i];
+    g.tables_out[i] = in_pool(block, g.num_blocks) ? g.place[block] : -1;
+  }
+  for (long i = t0; i < moves; i += stride) {
+    const int from = p.from[i], to = p.to[i], n = g.refs[from];
+    g.refs_out[to] = n;
+    g.refs_out[from] = 0;
+  }
+  const int live = *g.live;
+  for (long b = t0; b < g.num_blocks; b += stride) {
+    const int at = g.place[b];
+    if (at == b) g.refs_out[b] = g.refs[b];
+    else if (at < 0 && b >= live) g.refs_out[b] = 0;        // free before and after; the others are above
+  }
+  const long units = 2l * p.layers * moves;
+  for (long u = blockIdx.x; u < units; u += gridDim.x) copy_unit(p, u);
+}
+
+// ------------------------------------------------------------------ accepted rows
+// Workgroup: a KV head of a layer of a sequence.  Row path[i] of the sequence's rows becomes row i, for i below n_keep:
+// what is read is held in LDS until every read is done, so a path may have any order.
+template <typename CT, int D>
+__global__ void __launch_bounds__(128) kv_keep_kernel(KeepArgs p) {
+  extern __shared__ __align__(16) char sm_raw[];
+  CT* sm = reinterpret_cast<CT*>(sm_raw);                   // [rows][D]
+  __shared__ int sm_from[64];
+  __shared__ uint8_t sm_exp[64];
+  const int n_kv = p.c.n_kv, h = blockIdx.x % n_kv, layer = blockIdx.x / n_kv % p.layers, b = blockIdx.x / n_kv / p.layers;
+  const SeqRows sr = seq_rows(p.r, b);
+  const int kept = min(max(p.n_keep[b], 0), sr.n);
+  if (p.ctx_out && h == 0 && layer == 0 && threadIdx.x == 0) p.ctx_out[b] = (p.r.ctx ? p.r.ctx[b] : 0) + kept;
+  if (!p.path) return;
+  bool moves = false;
+  if (threadIdx.x < 64) {
+    const int i = threadIdx.x, j = i < kept ? p.path[(long)b * p.r.max_rows + i] : -1;
+    moves = (unsigned)j < (unsigned)sr.n && j != i;
+    sm_from[i] = moves ? j : -1;
+  }
+  if (!__syncthreads_or(moves)) return;
+  const size_t base = (size_t)layer * p.c.num_blocks;
+  // places of tokens: block * 16 + slot within the layer, -1 where there is none
+  auto place = [&](int t) -> long {
+    if (t < 0 || t >= p.r.max_ctx) return -1;
+    const int ph = page_of(p.r, p.c.num_blocks, b, t / PAGE);
+    return ph < 0 ? -1 : (long)ph * PAGE + t % PAGE;
+  };
+  constexpr int WORDS = D * sizeof(CT) / 16;                // 16-byte words of a K row
+  const int words = kept * WORDS;
+  CT* kc = reinterpret_cast<CT*>(p.c.k);
+  CT* vc = reinterpret_cast<CT*>(p.c.v);
+  auto k_at = [&](long at) { return kc + (((base + at / PAGE) * n_kv + h) * PAGE + at % PAGE) * D; };
+  auto v_at = [&](long at, int d) { return vc + (((base + at / PAGE) * n_kv + h) * D + d) * PAGE + at % PAGE; };
+  auto exp_at = [&](uint8_t* e, long at) { return e + ((base + at / PAGE) * n_kv + h) * PAGE + at % PAGE; };
+  for (int side = 0; side < 2; ++side) {
+    uint8_t* exps = side ? p.c.v_exp : p.c.k_exp;
+    for (int w = threadIdx.x; w < (side ? kept * D : words); w += 128) {
+      const int i = side ? w / D : w / WORDS, c = side ? w % D : w % WORDS;
+      const long at = sm_from[i] < 0 ? -1 : place(sr.ctx + sm_from[i]);
+      if (at < 0) continue;
+      if (side) sm[i * D + c] = *v_at(at, c);
+      else reinterpret_cast<u32x4*>(sm)[w] = reinterpret_cast<const u32x4*>(k_at(at))[c];
+      if (sizeof(CT) == 1 && c == 0) sm_exp[i] = *exp_at(exps, at);
+    }
+    __syncthreads();
+    for (int w = threadIdx.x; w < (side ? kept * D : words); w += 128) {
+      const int i = side ? w / D : w / WORDS, c = side ? w % D : w % WORDS;
+      if (sm_from[i] < 0 || place(sr.ctx + sm_from[i]) < 0) continue;
+      const long at = place(sr.ctx + i);
+      if (at < 0) continue;
+      if (side) *v_at(at, c) = sm[i * D + c];
+      else reinterpret_cast<u32x4*>(k_at(at))[c] = reinterpret_cast<const u32x4*>(sm)[w];
+      if (sizeof(CT) == 1 && c == 0) *exp_at(exps, at) = sm_exp[i];
+    }
+    __syncthreads();
+  }
+}
+
+// ------------------------------------------------------------------ launch
+hipError_t pages_extend(const PagesArgs& p, hipStream_t s) {
+  hipLaunchKernelGGL(pages_extend_kernel, dim3(1), dim3(PLAN), 0, s, p);
+  return hipGetLastError();
+}
+hipError_t pages_fork(const PagesArgs& p, hipStream_t s) {
+  hipLaunchKernelGGL(pages_fork_kernel, dim3(1), dim3(PLAN), 0, s, p);
+  return hipGetLastError();
+}
+hipError_t pages_free(const PagesArgs& p, hipStream_t s) {
+  const int x = std::min(64, (p.max_blocks + 255) / 256);
+  hipLaunchKernelGGL(pages_free_kernel, dim3(x, p.n), dim3(256), 0, s, p);
+  return hipGetLastError();
+}
+hipError_t pages_compact(const PagesArgs& p, hipStream_t s) {
+  hipLaunchKernelGGL(pages_compact_kernel, dim3(1), dim3(PLAN), 0, s, p);
+  return hipGetLastError();
+}
+
+// Eight workgroups for each compute unit take the units in turn.
+static unsigned copy_grid(long units, int cus) { return (unsigned)std::max(1l, std::min(units, 8l * cus)); }
+
+hipError_t copy_pages(const CopyArgs& p, int cus, hipStream_t s) {
+  if (p.n <= 0) return hipSuccess;
+  hipLaunchKernelGGL(copy_pages_kernel, dim3(copy_grid(2l * p.layers * p.n, cus)), dim3(256), 0, s, p);
+  return hipGetLastError();
+}
+hipError_t compact_move(const CopyArgs& p, const PagesArgs& g, int cus, hipStream_t s) {
+  const long units = std::max(2l * p.layers * (g.num_blocks / 2), ((long)g.batch * g.max_blocks + 255) / 256);
+  hipLaunchKernelGGL(compact_move_kernel, dim3(copy_grid(units, cus)), dim3(256), 0, s, p, g);
+  return hipGetLastError();
+}
+
+template <typename CT> static hipError_t keep_launch(const KeepArgs& p, hipStream_t s) {
+  const dim3 grid((unsigned)((long)p.r.batch * p.layers * p.c.n_kv));
+  const size_t lds = (size_t)p.r.max_rows * p.c.D * sizeof(CT);
+  if (p.c.D == 64) hipLaunchKernelGGL((kv_keep_kernel<CT, 64>), grid, dim3(128), lds, s, p);
+  else hipLaunchKernelGGL((kv_keep_kernel<CT, 128>), grid, dim3(128), lds, s, p);
+  return hipGetLastError();
+}
+hipError_t kv_keep(const KeepArgs& p, hipStream_t s) {
+  if ((p.c.D != 64 && p.c.D != 128) || p.r.max_rows > 64) return hipErrorInvalidValue;
+  switch (p.c.type) {
+    case CACHE_BF16: return keep_launch<bf16_t>(p, s);
+    case CACHE_F32: return keep_launch<float>(p, s);
+    case CACHE_E4M3: return keep_launch<e4m3_t>(p, s);
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace nova

@@ -217,14 +217,28 @@ struct AppendArgs {
   CachePool c;
   BatchRows r;
   const int* pos;                       // rotary position of each row (null: its token number)
+  long pos_axis;                        // 0: one position a row; else pair c turns by pos[axis[c] * pos_axis + row]
   const void* q; const void* k; const void* v; long q_row, k_row, v_row; int n_q;   // q null: none
   void* q_out; long q_out_row;
   bool in_f32, q_out_f32;
   int rot; bool interleaved;            // rotated dimensions (0: none)
   float mscale;                         // factor of the sines and cosines
   double turns[64];                     // turns of a pair per position: inverse frequency / 2 pi
+  uint8_t axis[64];
 };
 hipError_t kv_append(const AppendArgs& p, int cus, hipStream_t s);
+// Rotary embedding of dense rows of `heads` heads of D (a multiple of 8, at most 256).
+struct RotateArgs {
+  const void* x; long x_row; bool in_f32;
+  void* out; long out_row; bool out_f32;   // may be x (same type and pitch)
+  int rows, heads, D;
+  const int* pos; long pos_axis;        // as for AppendArgs
+  int rot; bool interleaved;
+  float mscale;
+  double turns[128];
+  uint8_t axis[128];
+};
+hipError_t rotate(const RotateArgs& p, int cus, hipStream_t s);
 struct GatherArgs {
   CachePool c;
   BatchRows r;
@@ -252,6 +266,67 @@ struct LogprobArgs {
   int n_top; float* top_lp; int* top_ids;               // [rows][n_top]
   float* part_sum; float* part_max;                     // logprobs_part_sizes()
 };
+// Which drafted tokens are kept.  draft null: every row draws and the walk follows.
+struct AcceptArgs {
+  const void* logits; long row; bool f32;               // [rows][vocab] at a pitch
+  const void* draft; long draft_row; bool draft_f32;
+  int vocab;
+  BatchRows r;                                          // row starts only; max_rows <= 64
+  const int* ids; const unsigned long long* mask; const float* temperature; const float* u;
+  int* n_keep; int* path; int* tokens; float* lp;       // [batch], [batch][max_rows]
+  // workspace: of each item (row of logits, then of the draft) and chunk
+  int items, chunks;
+  float* part_max; int* part_arg; double* part_sum;
+  int* row_token; float* row_lp;                        // [rows]
+  double* rest_sum;                                     // [batch][chunks]
+  unsigned* counters;                                   // [batch]
+};
+int accept_chunks(int vocab);
+hipError_t accept(const AcceptArgs& p, hipStream_t s);
+// Plans over the pages of a pool: refs [num_blocks], tables [batch][max_blocks], n requests.
+struct PagesArgs {
+  int* refs; int num_blocks;
+  int* tables; int batch, max_blocks;
+  const int* src; const int* dst; const int* lens; int n;
+  int* done;
+  int* want; int* rank; int* list; int* claim;          // workspace: [n], [n], [num_blocks], [batch]
+  int* from; int* to;                                   // block moves: [n] of a fork, [num_blocks / 2] of a compaction
+  int* place; int* moves; int* live;                    // of a compaction: [num_blocks], [1], [1]
+  int* refs_out; int* tables_out;
+};
+hipError_t pages_extend(const PagesArgs& p, hipStream_t s);
+hipError_t pages_fork(const PagesArgs& p, hipStream_t s);
+hipError_t pages_free(const PagesArgs& p, hipStream_t s);
+hipError_t pages_compact(const PagesArgs& p, hipStream_t s);
+// Blocks from[i] of one pool to blocks to[i] of another (or the same) in `layers` layers.
+struct CopyArgs {
+  CachePool src, dst;                                   // layer 0; the others follow at their size
+  int layers;
+  size_t page;                                          // bytes of K (and of V) of a block
+  const int* from; const int* to;
+  int n; const int* moves;                              // moves: how many, on the device (null: n)
+};
+hipError_t copy_pages(const CopyArgs& p, int cus, hipStream_t s);
+hipError_t compact_move(const CopyArgs& p, const PagesArgs& g, int cus, hipStream_t s);
+struct KeepArgs {
+  CachePool c; int layers;
+  BatchRows r;                                          // max_rows <= 64
+  const int* path; const int* n_keep; int* ctx_out;
+};
+hipError_t kv_keep(const KeepArgs& p, hipStream_t s);
+// out = base + scale B (A x) with each sequence's adapter.
+struct LoraArgs {
+  const bf16_t* a; const bf16_t* b; const float* scale; int n, rank, k, nout;   // [n][rank][k], [n][nout][rank], [n]
+  BatchRows r;                                          // row starts only
+  const int* which;                                     // [batch]
+  const void* x; long x_row; bool x_f32;
+  const void* base; long base_row;
+  void* out; long out_row; bool out_f32;
+  float* part;                                          // [slices][rows][rank]
+  int slices, kslice, cols;                             // set by the launcher
+};
+int lora_slices(const LoraArgs& p, int cus);
+hipError_t lora(const LoraArgs& p, int cus, hipStream_t s);
 bool logprobs_fits(int vocab, int n_top);
 void logprobs_part_sizes(int rows, int vocab, int n_top, size_t* sum_floats, size_t* max_floats);
 hipError_t logprobs(const LogprobArgs& p, hipStream_t s);

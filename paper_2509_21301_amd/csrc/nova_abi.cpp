@@ -756,19 +756,51 @@ int check_rope(const nova_rope* r, int D) {
   if (r->orig_ctx < 0 || (r->orig_ctx > 0 && !(r->beta > r->alpha))) return fail(NOVA_EINVAL, "rope: orig_ctx must be >= 0 and beta above alpha");
   return NOVA_OK;
 }
-void set_rope(nova::AppendArgs& a, const nova_rope& r) {
+// Rotary pairs' axes (the axis that each pair of `half` gets) and what is wrong with them, or NOVA_OK.
+int check_axes(const nova_rope_axes* x, int half) {
+  if (x->n_axes < 1 || x->n_axes > 4) return fail(NOVA_EINVAL, "rope: %d axes outside 1..4", x->n_axes);
+  int64_t sum = 0;
+  for (int a = 0; a < x->n_axes; ++a) {
+    if (x->pairs[a] < 0) return fail(NOVA_EINVAL, "rope: axis %d has %d pairs", a, x->pairs[a]);
+    sum += x->pairs[a];
+  }
+  if (sum != half) return fail(NOVA_EINVAL, "rope: the axes have %lld pairs, rot / 2 is %d", (long long)sum, half);
+  return NOVA_OK;
+}
+// f[i] = theta^(-i/m), i < m, as a product of the powers at i's binary digits: 7 roundings at most, and 7 calls of pow
+// instead of m (3 us of a call at 64)
+void rope_ladder(double theta, int m, double* f) {
+  f[0] = 1.0;
+  for (int k = 1; k < m; k *= 2) {
+    const double step = std::pow(theta, -(double)k / m);
+    for (int i = k; i < std::min(2 * k, m); ++i) f[i] = f[i - k] * step;
+  }
+}
+// `A`: AppendArgs or RotateArgs.
+template <typename A>
+void set_rope(A& a, const nova_rope& r, const nova_rope_axes* x = nullptr, int rows = 0) {
   const double two_pi = 6.283185307179586;
+  const int half = r.rot / 2;
   a.rot = r.rot;
   a.interleaved = r.interleaved != 0;
   a.mscale = r.mscale;
-  // theta^(-2c/rot) as a product of the powers at c's binary digits: 6 roundings at most, and 6 calls
-  // of pow instead of 64 (3 us of a call)
-  double f[64] = {1.0};
-  for (int k = 1; k < r.rot / 2; k *= 2) {
-    const double step = std::pow((double)r.theta, -2.0 * k / r.rot);
-    for (int c = k; c < std::min(2 * k, r.rot / 2); ++c) f[c] = f[c - k] * step;
+  double f[128], of_axis[128];
+  rope_ladder(r.theta, half, f);
+  if (x) {
+    a.pos_axis = rows;
+    int left[4] = {}, n = 0;
+    for (int i = 0; i < x->n_axes; ++i) left[i] = x->pairs[i];
+    while (n < half)
+      for (int i = 0; i < x->n_axes; ++i)
+        for (int m = x->cyclic ? std::min(left[i], 1) : left[i]; m > 0; --m, --left[i]) a.axis[n++] = (uint8_t)i;
+    for (int i = 0; x->own_freqs && i < x->n_axes; ++i) {
+      if (x->pairs[i] == 0) continue;
+      rope_ladder(r.theta, x->pairs[i], of_axis);
+      for (int c = 0, at = 0; c < half; ++c)
+        if (a.axis[c] == i) f[c] = of_axis[at++];
+    }
   }
-  for (int c = 0; c < r.rot / 2; ++c) {
+  for (int c = 0; c < half; ++c) {
     double g = f[c] / r.factor;
     if (r.orig_ctx > 0) {
       const double keep = std::min(1.0, std::max(0.0, (r.orig_ctx * f[c] / two_pi - r.alpha) / ((double)r.beta - r.alpha)));
@@ -787,14 +819,18 @@ extern "C" size_t nova_cache_bytes(int type, int num_blocks, int n_kv, int head_
   return tokens * head_dim * cache_elem(type);
 }
 
-extern "C" int nova_kv_append(const nova_cache* cache, const nova_rows* rows, const nova_rope* rope, const int32_t* pos,
-                              int in_type, const void* q, int64_t q_pitch, int n_q, const void* k, int64_t k_pitch,
+extern "C" int nova_kv_append_axes(const nova_cache* cache, const nova_rows* rows, const nova_rope* rope, const nova_rope_axes* axes,
+                                   const int32_t* pos, int in_type, const void* q, int64_t q_pitch, int n_q, const void* k, int64_t k_pitch,
                               const void* v, int64_t v_pitch, void* q_out, int q_out_type, int64_t q_out_pitch,
                               nova_stream_t stream) {
   if (int rc = check_cache(cache)) return rc;
   if (int rc = check_rows(rows, true)) return rc;
   if (rope)
     if (int rc = check_rope(rope, cache->head_dim)) return rc;
+  if (axes) {
+    if (!rope) return fail(NOVA_EINVAL, "axes without a rope");
+    if (int rc = check_axes(axes, rope->rot / 2)) return rc;
+  }
   if (!act_ok(in_type) || (q && !act_ok(q_out_type))) return fail(NOVA_EINVAL, "types must be NOVA_ACT_BF16 or NOVA_ACT_F32");
   if (!aligned4(pos)) return fail(NOVA_EINVAL, "pos is misaligned");
   if (rows->rows == 0) return NOVA_OK;
@@ -816,8 +852,43 @@ extern "C" int nova_kv_append(const nova_cache* cache, const nova_rows* rows, co
   a.q = q, a.k = k, a.v = v, a.q_row = q_pitch, a.k_row = k_pitch, a.v_row = v_pitch, a.n_q = q ? n_q : 0;
   a.q_out = q_out, a.q_out_row = q_out_pitch;
   a.in_f32 = in_type == NOVA_ACT_F32, a.q_out_f32 = q && q_out_type == NOVA_ACT_F32;
-  if (rope) set_rope(a, *rope);
+  if (rope) set_rope(a, *rope, axes, rows->rows);
   CALL(NOVA_KIND_MISC, s, nova::kv_append(a, device_cus(), s));
+  return NOVA_OK;
+}
+
+extern "C" int nova_kv_append(const nova_cache* cache, const nova_rows* rows, const nova_rope* rope, const int32_t* pos,
+                              int in_type, const void* q, int64_t q_pitch, int n_q, const void* k, int64_t k_pitch,
+                              const void* v, int64_t v_pitch, void* q_out, int q_out_type, int64_t q_out_pitch,
+                              nova_stream_t stream) {
+  return nova_kv_append_axes(cache, rows, rope, nullptr, pos, in_type, q, q_pitch, n_q, k, k_pitch, v, v_pitch, q_out, q_out_type,
+                             q_out_pitch, stream);
+}
+
+extern "C" int nova_rotate(const nova_rope* rope, const nova_rope_axes* axes, const int32_t* pos, int rows, int n_heads, int head_dim,
+                           int in_type, const void* x, int64_t x_pitch, int out_type, void* out, int64_t out_pitch,
+                           nova_stream_t stream) {
+  if (!rope) return fail(NOVA_EINVAL, "null rope");
+  if (rows < 0 || n_heads <= 0) return fail(NOVA_EINVAL, "rotate: %d rows of %d heads", rows, n_heads);
+  if (head_dim <= 0 || head_dim > 256 || head_dim % 8) return fail(NOVA_EUNSUPPORTED, "rotate: head_dim %d must be a multiple of 8 up to 256", head_dim);
+  if (n_heads > MAX_HEADS || rows > MAX_ROWS) return fail(NOVA_EUNSUPPORTED, "rotate: %d rows of %d heads (at most %d and %d)", rows, n_heads, MAX_ROWS, MAX_HEADS);
+  if (int rc = check_rope(rope, head_dim)) return rc;
+  if (axes)
+    if (int rc = check_axes(axes, rope->rot / 2)) return rc;
+  if (!act_ok(in_type) || !act_ok(out_type)) return fail(NOVA_EINVAL, "types must be NOVA_ACT_BF16 or NOVA_ACT_F32");
+  if (rows == 0) return NOVA_OK;
+  if (!pos || !aligned4(pos)) return fail(NOVA_EINVAL, "pos null or misaligned");
+  if (int rc = check_matrix("x", x, x_pitch, n_heads, head_dim, act_elem(in_type))) return rc;
+  if (int rc = check_matrix("out", out, out_pitch, n_heads, head_dim, act_elem(out_type))) return rc;
+  if (out == x && (out_type != in_type || out_pitch != x_pitch)) return fail(NOVA_EINVAL, "out over x needs the same type and pitch");
+  hipStream_t s = (hipStream_t)stream;
+  nova::RotateArgs a{};
+  a.x = x, a.x_row = x_pitch, a.in_f32 = in_type == NOVA_ACT_F32;
+  a.out = out, a.out_row = out_pitch, a.out_f32 = out_type == NOVA_ACT_F32;
+  a.rows = rows, a.heads = n_heads, a.D = head_dim;
+  a.pos = pos;
+  set_rope(a, *rope, axes, rows);
+  CALL(NOVA_KIND_MISC, s, nova::rotate(a, device_cus(), s));
   return NOVA_OK;
 }
 
@@ -908,6 +979,303 @@ extern "C" int nova_logprobs(const void* logits, int type, int64_t pitch, int ro
   const nova::LogprobArgs a{logits, type == NOVA_ACT_F32, pitch, rows, vocab, given, n_given, given_lp, entropy, n_top, top_lp, top_ids,
                             (float*)ws, (float*)((char*)ws + sums)};
   CALL(NOVA_KIND_MISC, s, nova::logprobs(a, s));
+  return NOVA_OK;
+}
+
+// ------------------------------------------------------------------ between two model calls
+namespace {
+// Of rows what says which of them belong to which sequence.
+int check_row_starts(const nova_rows* r, int most) {
+  if (!r) return fail(NOVA_EINVAL, "null rows");
+  if (r->batch <= 0 || r->batch > 65535 || r->rows < 0 || r->max_rows <= 0)
+    return fail(NOVA_EINVAL, "rows: batch must be 1..65535, rows >= 0 and max_rows positive");
+  if (r->rows > MAX_ROWS) return fail(NOVA_EUNSUPPORTED, "%d rows (at most %d)", r->rows, MAX_ROWS);
+  if (most > 0 && r->max_rows > most) return fail(NOVA_EUNSUPPORTED, "%d rows of one sequence (at most %d)", r->max_rows, most);
+  if (!aligned4(r->row_start)) return fail(NOVA_EINVAL, "row_start is misaligned");
+  if (!r->row_start && (int64_t)r->batch * r->max_rows != r->rows)
+    return fail(NOVA_EINVAL, "rows: without row_start, rows must be batch * max_rows");
+  return NOVA_OK;
+}
+// The same for the kernels, which then read nothing else.
+nova::BatchRows row_starts(const nova_rows& r) { return nova::BatchRows{r.row_start, nullptr, nullptr, 0, r.batch, r.rows, r.max_rows, 0}; }
+
+int check_ws(const void* ws, size_t have, size_t need) {
+  if (have < need) return fail(NOVA_ENOSPACE, "workspace %zu < required %zu bytes", have, need);
+  if (need > 0 && (!ws || !aligned(ws))) return fail(NOVA_EINVAL, "null or misaligned workspace");
+  return NOVA_OK;
+}
+// [a, a + na) and [b, b + nb) (bytes) share a byte.
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
+
+constexpr int64_t MAX_ACCEPT_BLOCKS = 1 << 24;    // workgroups of 256 threads: a grid dimension has fewer than 2^32
+
+int check_accept(const nova_rows* rows, int vocab, bool draft) {
+  if (int rc = check_row_starts(rows, 64)) return rc;
+  if (vocab <= 0) return fail(NOVA_EINVAL, "accept: vocab %d", vocab);
+  if (vocab > 1 << 21) return fail(NOVA_EUNSUPPORTED, "accept: vocab %d (at most 2^21)", vocab);
+  const int64_t chunks = nova::accept_chunks(vocab), items = (int64_t)rows->rows * (draft ? 2 : 1);
+  if (std::max<int64_t>(items, rows->batch) * chunks >= MAX_ACCEPT_BLOCKS)
+    return fail(NOVA_EUNSUPPORTED, "accept: %d rows of %d sequences with %d logits", rows->rows, rows->batch, vocab);
+  return NOVA_OK;
+}
+size_t accept_ws(nova::AcceptArgs* a, void* base) {
+  Carve w(base);
+  const size_t parts = (size_t)a->items * a->chunks;
+  a->part_sum = w.take<double>(parts);
+  a->part_max = w.take<float>(parts);
+  a->part_arg = w.take<int>(parts);
+  a->row_token = w.take<int>(a->r.rows);
+  a->row_lp = w.take<float>(a->r.rows);
+  a->rest_sum = w.take<double>(a->items > a->r.rows ? (size_t)a->r.batch * a->chunks : 0);
+  a->counters = w.take<unsigned>(a->r.batch);
+  return w.used;
+}
+void accept_sizes(nova::AcceptArgs* a, const nova_rows* rows, int vocab, bool draft) {
+  a->r = row_starts(*rows);
+  a->vocab = vocab;
+  a->items = rows->rows * (draft ? 2 : 1);
+  a->chunks = nova::accept_chunks(vocab);
+}
+}  // namespace
+
+extern "C" size_t nova_accept_workspace_bytes(const nova_rows* rows, int vocab, int with_draft) {
+  if (check_accept(rows, vocab, with_draft != 0)) return 0;
+  nova::AcceptArgs a{};
+  accept_sizes(&a, rows, vocab, with_draft != 0);
+  return accept_ws(&a, nullptr);
+}
+
+extern "C" int nova_accept(const nova_rows* rows, const int32_t* ids, const uint64_t* mask, const void* logits, int type, int64_t pitch,
+                           const void* draft, int draft_type, int64_t draft_pitch, int vocab, const float* temperature, const float* u,
+                           int32_t* n_keep, int32_t* path, int32_t* tokens, float* lp, void* ws, size_t ws_bytes, nova_stream_t stream) {
+  if (int rc = check_accept(rows, vocab, draft != nullptr)) return rc;
+  if (!act_ok(type) || (draft && !act_ok(draft_type))) return fail(NOVA_EINVAL, "types must be NOVA_ACT_BF16 or NOVA_ACT_F32");
+  if (draft && mask) return fail(NOVA_EUNSUPPORTED, "accept: the draft's logits go with a chain (mask NULL)");
+  if (rows->rows > 0) {
+    if (!logits || (uintptr_t)logits % act_elem(type) || pitch < vocab) return fail(NOVA_EINVAL, "logits null or misaligned, or pitch below vocab");
+    if (draft && ((uintptr_t)draft % act_elem(draft_type) || draft_pitch < vocab)) return fail(NOVA_EINVAL, "draft misaligned, or its pitch below vocab");
+    if (!ids || !aligned4(ids) || !u || !aligned4(u)) return fail(NOVA_EINVAL, "ids or u null or misaligned");
+  }
+  if ((uintptr_t)mask & 7) return fail(NOVA_EINVAL, "mask must be 8-byte aligned");
+  if (!aligned4(temperature)) return fail(NOVA_EINVAL, "temperature is misaligned");
+  for (const void* o : {(const void*)n_keep, (const void*)path, (const void*)tokens, (const void*)lp})
+    if (!o || !aligned4(o)) return fail(NOVA_EINVAL, "n_keep, path, tokens and lp must be non-null and aligned");
+  nova::AcceptArgs a{};
+  accept_sizes(&a, rows, vocab, draft != nullptr);
+  if (int rc = check_ws(ws, ws_bytes, accept_ws(&a, nullptr))) return rc;
+  accept_ws(&a, ws);
+  a.logits = logits, a.row = pitch, a.f32 = type == NOVA_ACT_F32;
+  a.draft = draft, a.draft_row = draft_pitch, a.draft_f32 = draft && draft_type == NOVA_ACT_F32;
+  a.ids = ids, a.mask = (const unsigned long long*)mask, a.temperature = temperature, a.u = u;
+  a.n_keep = n_keep, a.path = path, a.tokens = tokens, a.lp = lp;
+  hipStream_t s = (hipStream_t)stream;
+  CALL(NOVA_KIND_MISC, s, nova::accept(a, s));
+  return NOVA_OK;
+}
+
+extern "C" int nova_kv_keep(const nova_cache* cache, int layers, const nova_rows* rows, const int32_t* path, const int32_t* n_keep,
+                            int32_t* ctx_out, nova_stream_t stream) {
+  if (int rc = check_cache(cache)) return rc;
+  if (int rc = check_rows(rows, true)) return rc;
+  if (rows->max_rows > 64) return fail(NOVA_EUNSUPPORTED, "%d drafted tokens of one sequence (at most 64)", rows->max_rows);
+  if (layers <= 0) return fail(NOVA_EINVAL, "%d layers", layers);
+  if ((int64_t)rows->batch * layers > (1 << 24) / cache->n_kv) return fail(NOVA_EUNSUPPORTED, "keep: %d sequences, %d layers and %d heads", rows->batch, layers, cache->n_kv);
+  if (!n_keep || !aligned4(n_keep) || !aligned4(path) || !aligned4(ctx_out)) return fail(NOVA_EINVAL, "n_keep null, or an array misaligned");
+  const size_t bytes = (size_t)rows->batch * sizeof(int32_t);
+  if (ctx_out && ((rows->ctx && overlap(ctx_out, bytes, rows->ctx, bytes)) || overlap(ctx_out, bytes, n_keep, bytes)))
+    return fail(NOVA_EINVAL, "ctx_out may not lie over ctx or n_keep");
+  hipStream_t s = (hipStream_t)stream;
+  const nova::KeepArgs a{pool_layer(*cache, 0), layers, batch_rows(*rows), path, n_keep, ctx_out};
+  CALL(NOVA_KIND_MISC, s, nova::kv_keep(a, s));
+  return NOVA_OK;
+}
+
+namespace {
+nova::CopyArgs copy_args(const nova_cache& src, const nova_cache& dst, int layers) {
+  nova::CopyArgs c{};
+  c.src = pool_layer(src, 0), c.dst = pool_layer(dst, 0), c.layers = layers;
+  c.page = (size_t)src.n_kv * 16 * src.head_dim * cache_elem(src.type);
+  return c;
+}
+int check_pages(const nova_pages* p, const void* tables, int max_blocks, int batch, int n) {
+  if (!p) return fail(NOVA_EINVAL, "null pages");
+  if (!p->refs || !aligned4(p->refs) || p->num_blocks <= 0) return fail(NOVA_EINVAL, "pages: refs null or misaligned, or no blocks");
+  if (!tables || !aligned4(tables) || max_blocks <= 0) return fail(NOVA_EINVAL, "tables null or misaligned, or max_blocks not positive");
+  if (batch <= 0 || batch > 65535 || n < 0 || n > 65535) return fail(NOVA_EINVAL, "batch must be 1..65535 and at most 65535 requests");
+  if (max_blocks > MAX_TOKENS / 16 || p->num_blocks > 1 << 30) return fail(NOVA_EUNSUPPORTED, "pages: %d blocks, tables of %d", p->num_blocks, max_blocks);
+  return NOVA_OK;
+}
+int check_pages_cache(const nova_pages* p, const nova_cache* c, int layers) {
+  if (int rc = check_cache(c)) return rc;
+  if (layers <= 0) return fail(NOVA_EINVAL, "%d layers", layers);
+  if (c->num_blocks != p->num_blocks) return fail(NOVA_EINVAL, "a cache of %d blocks, pages of %d", c->num_blocks, p->num_blocks);
+  return NOVA_OK;
+}
+// The workspace of any of the calls.
+size_t pages_ws(nova::PagesArgs* a, int batch, int n, void* base) {
+  Carve w(base);
+  const size_t req = std::max(batch, n), moves = std::max<size_t>(req, a->num_blocks / 2 + 1);
+  a->want = w.take<int>(req);
+  a->rank = w.take<int>(req);
+  a->claim = w.take<int>(batch);
+  a->list = w.take<int>(a->num_blocks);
+  a->from = w.take<int>(moves);
+  a->to = w.take<int>(moves);
+  a->place = a->list;                  // of a compaction
+  a->moves = w.take<int>(1);
+  a->live = w.take<int>(1);
+  return w.used;
+}
+nova::PagesArgs pages_args(const nova_pages* p, const int32_t* tables, int max_blocks, int batch) {
+  nova::PagesArgs a{};
+  a.refs = p->refs, a.num_blocks = p->num_blocks;
+  a.tables = (int32_t*)tables, a.batch = batch, a.max_blocks = max_blocks;
+  return a;
+}
+}  // namespace
+
+extern "C" int nova_kv_copy(const nova_cache* src, const nova_cache* dst, int layers, const int32_t* from, const int32_t* to, int n,
+                            nova_stream_t stream) {
+  if (int rc = check_cache(src)) return rc;
+  if (int rc = check_cache(dst)) return rc;
+  if (src->type != dst->type || src->n_kv != dst->n_kv || src->head_dim != dst->head_dim)
+    return fail(NOVA_EINVAL, "copy between caches of different type or heads");
+  if (layers <= 0 || n < 0) return fail(NOVA_EINVAL, "copy: %d blocks of %d layers", n, layers);
+  if (n == 0) return NOVA_OK;
+  if (!from || !to || !aligned4(from) || !aligned4(to)) return fail(NOVA_EINVAL, "from or to null or misaligned");
+  hipStream_t s = (hipStream_t)stream;
+  nova::CopyArgs c = copy_args(*src, *dst, layers);
+  c.from = from, c.to = to, c.n = n;
+  CALL(NOVA_KIND_MISC, s, nova::copy_pages(c, device_cus(), s));
+  return NOVA_OK;
+}
+
+extern "C" size_t nova_pages_workspace_bytes(const nova_pages* pages, int batch, int n) {
+  if (!pages || pages->num_blocks <= 0 || batch <= 0 || n < 0) return 0;
+  nova::PagesArgs a{};
+  a.num_blocks = pages->num_blocks;
+  return pages_ws(&a, batch, n, nullptr);
+}
+
+extern "C" int nova_pages_extend(const nova_pages* pages, int32_t* tables, int max_blocks, int batch, const int32_t* tokens,
+                                 int32_t* done, void* ws, size_t ws_bytes, nova_stream_t stream) {
+  if (int rc = check_pages(pages, tables, max_blocks, batch, batch)) return rc;
+  if (!tokens || !done || !aligned4(tokens) || !aligned4(done)) return fail(NOVA_EINVAL, "tokens or done null or misaligned");
+  nova::PagesArgs a = pages_args(pages, tables, max_blocks, batch);
+  if (int rc = check_ws(ws, ws_bytes, pages_ws(&a, batch, batch, nullptr))) return rc;
+  pages_ws(&a, batch, batch, ws);
+  a.lens = tokens, a.n = batch, a.done = done;
+  hipStream_t s = (hipStream_t)stream;
+  CALL(NOVA_KIND_MISC, s, nova::pages_extend(a, s));
+  return NOVA_OK;
+}
+
+extern "C" int nova_pages_fork(const nova_pages* pages, const nova_cache* cache, int layers, int32_t* tables, int max_blocks, int batch,
+                               const int32_t* src, const int32_t* dst, const int32_t* tokens, int n, int32_t* done, void* ws,
+                               size_t ws_bytes, nova_stream_t stream) {
+  if (int rc = check_pages(pages, tables, max_blocks, batch, n)) return rc;
+  if (int rc = check_pages_cache(pages, cache, layers)) return rc;
+  if (n == 0) return NOVA_OK;
+  for (const void* o : {(const void*)src, (const void*)dst, (const void*)tokens, (const void*)done})
+    if (!o || !aligned4(o)) return fail(NOVA_EINVAL, "src, dst, tokens and done must be non-null and aligned");
+  nova::PagesArgs a = pages_args(pages, tables, max_blocks, batch);
+  if (int rc = check_ws(ws, ws_bytes, pages_ws(&a, batch, n, nullptr))) return rc;
+  pages_ws(&a, batch, n, ws);
+  a.src = src, a.dst = dst, a.lens = tokens, a.n = n, a.done = done;
+  nova::CopyArgs c = copy_args(*cache, *cache, layers);
+  c.from = a.from, c.to = a.to, c.n = n;
+  hipStream_t s = (hipStream_t)stream;
+  CALL(NOVA_KIND_MISC, s, nova::pages_fork(a, s));
+  CALL(NOVA_KIND_MISC, s, nova::copy_pages(c, device_cus(), s));
+  return NOVA_OK;
+}
+
+extern "C" int nova_pages_free(const nova_pages* pages, int32_t* tables, int max_blocks, int batch, const int32_t* seqs,
+                               const int32_t* tokens, int n, nova_stream_t stream) {
+  if (int rc = check_pages(pages, tables, max_blocks, batch, n)) return rc;
+  if (n == 0) return NOVA_OK;
+  if (!seqs || !aligned4(seqs) || !aligned4(tokens)) return fail(NOVA_EINVAL, "seqs null, or an array misaligned");
+  nova::PagesArgs a = pages_args(pages, tables, max_blocks, batch);
+  a.src = seqs, a.lens = tokens, a.n = n;
+  hipStream_t s = (hipStream_t)stream;
+  CALL(NOVA_KIND_MISC, s, nova::pages_free(a, s));
+  return NOVA_OK;
+}
+
+extern "C" int nova_pages_compact(const nova_pages* pages, const nova_cache* cache, int layers, const int32_t* tables, int max_blocks,
+                                  int batch, int32_t* refs_out, int32_t* tables_out, int32_t* live_out, void* ws, size_t ws_bytes,
+                                  nova_stream_t stream) {
+  if (int rc = check_pages(pages, tables, max_blocks, batch, 0)) return rc;
+  if (int rc = check_pages_cache(pages, cache, layers)) return rc;
+  if (!refs_out || !tables_out || !aligned4(refs_out) || !aligned4(tables_out) || !aligned4(live_out))
+    return fail(NOVA_EINVAL, "refs_out or tables_out null, or an array misaligned");
+  const size_t nr = (size_t)pages->num_blocks * 4, nt = (size_t)batch * max_blocks * 4;
+  if ((refs_out != pages->refs && overlap(refs_out, nr, pages->refs, nr)) || (tables_out != tables && overlap(tables_out, nt, tables, nt)) ||
+      overlap(refs_out, nr, tables, nt) || overlap(tables_out, nt, pages->refs, nr) || overlap(refs_out, nr, tables_out, nt))
+    return fail(NOVA_EINVAL, "refs_out and tables_out must be refs and tables themselves or lie apart from them");
+  nova::PagesArgs a = pages_args(pages, tables, max_blocks, batch);
+  if (int rc = check_ws(ws, ws_bytes, pages_ws(&a, batch, 0, nullptr))) return rc;
+  pages_ws(&a, batch, 0, ws);
+  a.refs_out = refs_out, a.tables_out = tables_out;
+  if (live_out) a.live = live_out;
+  nova::CopyArgs c = copy_args(*cache, *cache, layers);
+  c.from = a.from, c.to = a.to, c.moves = a.moves;
+  hipStream_t s = (hipStream_t)stream;
+  CALL(NOVA_KIND_MISC, s, nova::pages_compact(a, s));
+  CALL(NOVA_KIND_MISC, s, nova::compact_move(c, a, device_cus(), s));
+  return NOVA_OK;
+}
+
+// ------------------------------------------------------------------ adapters
+namespace {
+int check_adapters(const nova_adapters* d) {
+  if (!d) return fail(NOVA_EINVAL, "null adapters");
+  if (d->n <= 0 || d->rank <= 0 || d->k <= 0 || d->n_out <= 0) return fail(NOVA_EINVAL, "adapters: non-positive sizes");
+  if (d->rank > 128 || d->rank % 8 || d->k % 8 || d->n_out % 8 || d->k > 1 << 24 || d->n_out > 1 << 24)
+    return fail(NOVA_EUNSUPPORTED, "adapters of rank %d, %d to %d: multiples of 8, rank at most 128, the others 2^24", d->rank, d->k, d->n_out);
+  return NOVA_OK;
+}
+nova::LoraArgs lora_args(const nova_adapters& d, const nova_rows& r) {
+  nova::LoraArgs a{};
+  a.a = (const bf16_t*)d.a, a.b = (const bf16_t*)d.b, a.scale = d.scale, a.n = d.n, a.rank = d.rank, a.k = d.k, a.nout = d.n_out;
+  a.r = row_starts(r);
+  return a;
+}
+}  // namespace
+
+extern "C" size_t nova_lora_workspace_bytes(const nova_adapters* adapters, const nova_rows* rows) {
+  if (check_adapters(adapters) || check_row_starts(rows, 0)) return 0;
+  const nova::LoraArgs a = lora_args(*adapters, *rows);
+  return align256((size_t)nova::lora_slices(a, device_cus()) * rows->rows * adapters->rank * sizeof(float));
+}
+
+extern "C" int nova_lora(const nova_adapters* adapters, const nova_rows* rows, const int32_t* which, int x_type, const void* x,
+                         int64_t x_pitch, int out_type, const void* base, int64_t base_pitch, void* out, int64_t out_pitch, void* ws,
+                         size_t ws_bytes, nova_stream_t stream) {
+  if (int rc = check_adapters(adapters)) return rc;
+  if (int rc = check_row_starts(rows, 0)) return rc;
+  if (!act_ok(x_type) || !act_ok(out_type)) return fail(NOVA_EINVAL, "types must be NOVA_ACT_BF16 or NOVA_ACT_F32");
+  if (rows->rows == 0) return NOVA_OK;
+  if (!adapters->a || !adapters->b || !aligned16(adapters->a) || !aligned16(adapters->b) || !aligned4(adapters->scale))
+    return fail(NOVA_EINVAL, "a and b must be non-null and 16-byte aligned, scale aligned");
+  if (!which || !aligned4(which)) return fail(NOVA_EINVAL, "which null or misaligned");
+  if (int rc = check_matrix("x", x, x_pitch, 1, adapters->k, act_elem(x_type))) return rc;
+  if (int rc = check_matrix("out", out, out_pitch, 1, adapters->n_out, act_elem(out_type))) return rc;
+  if (base) {
+    if (int rc = check_matrix("base", base, base_pitch, 1, adapters->n_out, act_elem(out_type))) return rc;
+    if (base == out && base_pitch != out_pitch) return fail(NOVA_EINVAL, "out over base needs the same pitch");
+  }
+  if (int rc = check_ws(ws, ws_bytes, nova_lora_workspace_bytes(adapters, rows))) return rc;
+  nova::LoraArgs a = lora_args(*adapters, *rows);
+  a.which = which;
+  a.x = x, a.x_row = x_pitch, a.x_f32 = x_type == NOVA_ACT_F32;
+  a.base = base, a.base_row = base_pitch;
+  a.out = out, a.out_row = out_pitch, a.out_f32 = out_type == NOVA_ACT_F32;
+  a.part = (float*)ws;
+  hipStream_t s = (hipStream_t)stream;
+  CALL(NOVA_KIND_GEMM, s, nova::lora(a, device_cus(), s));
   return NOVA_OK;
 }
 

@@ -71,6 +71,19 @@ class RopeC(C.Structure):
                 ("orig_ctx", C.c_int), ("alpha", C.c_float), ("beta", C.c_float), ("mscale", C.c_float)]
 
 
+class RopeAxesC(C.Structure):
+    _fields_ = [("n_axes", C.c_int), ("pairs", C.c_int * 4), ("cyclic", C.c_int), ("own_freqs", C.c_int)]
+
+
+class PagesC(C.Structure):
+    _fields_ = [("refs", C.c_void_p), ("num_blocks", C.c_int)]
+
+
+class AdaptersC(C.Structure):
+    _fields_ = [("a", C.c_void_p), ("b", C.c_void_p), ("scale", C.c_void_p), ("n", C.c_int), ("rank", C.c_int), ("k", C.c_int),
+                ("n_out", C.c_int)]
+
+
 # symbol -> (restype, argtypes); mirrors include/nova.h
 _SIG = {
     "nova_last_error": (C.c_char_p, []),
@@ -102,6 +115,11 @@ _SIG = {
     "nova_cache_bytes": (C.c_size_t, [C.c_int, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_size_t)]),
     "nova_kv_append": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int64, C.c_int,
                                  C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int, C.c_int64, C.c_void_p]),
+    "nova_kv_append_axes": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int64,
+                                      C.c_int, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int, C.c_int64,
+                                      C.c_void_p]),
+    "nova_rotate": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int64, C.c_int,
+                              C.c_void_p, C.c_int64, C.c_void_p]),
     "nova_kv_gather": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
                                  C.c_void_p]),
     "nova_tree_attention_workspace_bytes": (C.c_size_t, [C.c_void_p, C.c_void_p, C.c_int]),
@@ -110,6 +128,21 @@ _SIG = {
     "nova_logprobs_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int, C.c_int]),
     "nova_logprobs": (C.c_int, [C.c_void_p, C.c_int, C.c_int64, C.c_int, C.c_int, C.c_void_p, C.c_int, C.c_void_p,
                                 C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "nova_accept_workspace_bytes": (C.c_size_t, [C.c_void_p, C.c_int, C.c_int]),
+    "nova_accept": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_int, C.c_int64, C.c_int,
+                              C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "nova_kv_keep": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "nova_kv_copy": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p]),
+    "nova_pages_workspace_bytes": (C.c_size_t, [C.c_void_p, C.c_int, C.c_int]),
+    "nova_pages_extend": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "nova_pages_fork": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p,
+                                  C.c_int, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "nova_pages_free": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p]),
+    "nova_pages_compact": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p,
+                                     C.c_void_p, C.c_size_t, C.c_void_p]),
+    "nova_lora_workspace_bytes": (C.c_size_t, [C.c_void_p, C.c_void_p]),
+    "nova_lora": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int64, C.c_int, C.c_void_p, C.c_int64, C.c_void_p,
+                            C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]),
     "nova_llm_prefill_cache": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p,
                                          C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "nova_llm_verify_workspace_bytes": (C.c_size_t, [C.c_void_p, C.c_void_p, C.c_void_p]),
@@ -620,22 +653,44 @@ class Rows:
 
 class Rope:
     """Rotary embedding of the first ``rot`` dimensions, half-split or ``interleaved`` pairs; ``factor`` and
-    ``orig_ctx`` (with ``alpha``, ``beta``) scale it for longer contexts, ``mscale`` multiplies sines and cosines."""
+    ``orig_ctx`` (with ``alpha``, ``beta``) scale it for longer contexts, ``mscale`` multiplies sines and cosines.
+    ``axes``: how many of the rot / 2 pairs turn by the position on each of 1 to 4 axes (time, row, column), in runs or
+    dealt in turn (``cyclic``); positions are then int32 [len(axes), rows].  ``own_freqs``: the i-th of an axis' m
+    pairs has frequency theta^(-i/m), else pair c has theta^(-2c/rot) whatever its axis."""
 
-    def __init__(self, rot, theta=10000.0, interleaved=False, factor=1.0, orig_ctx=0, alpha=1.0, beta=32.0, mscale=1.0):
+    def __init__(self, rot, theta=10000.0, interleaved=False, factor=1.0, orig_ctx=0, alpha=1.0, beta=32.0, mscale=1.0, axes=None,
+                 cyclic=False, own_freqs=False):
         self._c = RopeC(rot, int(interleaved), theta, factor, orig_ctx, alpha, beta, mscale)
         self.ref = C.addressof(self._c)
+        self.n_axes, self.axes_ref = 0, None
+        if axes is not None:
+            if not 1 <= len(axes) <= 4:
+                raise ValueError(f"{len(axes)} axes outside 1..4")
+            self._axes = RopeAxesC(len(axes), (C.c_int * 4)(*axes), int(cyclic), int(own_freqs))
+            self.n_axes, self.axes_ref = len(axes), C.addressof(self._axes)
+        elif cyclic or own_freqs:
+            raise ValueError("cyclic and own_freqs are of axes")
+
+    def _check_pos(self, pos, rows):
+        """One position a row, or one on every axis."""
+        if self.n_axes == 0:
+            _check_vector("pos", pos, torch.int32, rows)
+        elif pos is not None and (pos.dtype != torch.int32 or pos.shape != (self.n_axes, rows) or not pos.is_contiguous()):
+            raise ValueError(f"pos must be contiguous int32 {(self.n_axes, rows)}, got {pos.dtype} {tuple(pos.shape)}")
 
 
 def kv_append(cache, rows, k, v, q=None, pos=None, rope=None, q_out=None, layer=0, stream=None):
-    """Rotate q and k (``rope`` None: not) at ``pos`` (int32 [rows]; None: the rows' token numbers) and write k and v
+    """Rotate q and k (``rope`` None: not) at ``pos`` (int32 [rows], with axes [axes, rows]; None: the rows' token numbers) and write k and v
     behind their sequences' contexts in ``cache``, in its type.  k, v [rows, n_kv, head_dim], q [rows, n_q, head_dim],
     bf16 or fp32, may be views of one packed projection.  Returns the rotated q (``q_out``, which may be q itself)."""
     n, d = rows.rows, cache.head_dim
     _check_device(cache.device, rows.tables, k, v, q, pos, q_out)
     act, k_pitch = _check_rows_of("k", k, n, cache.n_kv, d)
     act_v, v_pitch = _check_rows_of("v", v, n, cache.n_kv, d)
-    _check_vector("pos", pos, torch.int32, n)
+    if rope is None:
+        _check_vector("pos", pos, torch.int32, n)
+    else:
+        rope._check_pos(pos, n)
     n_q = q_pitch = out_pitch = act_out = 0
     act_q = act
     if q is not None:
@@ -649,10 +704,35 @@ def kv_append(cache, rows, k, v, q=None, pos=None, rope=None, q_out=None, layer=
         raise ValueError("q_out without q")
     if act_v != act or act_q != act:
         raise ValueError("q, k and v must have one type")
-    _check(lib.nova_kv_append(cache.layer(layer), rows.ref, rope.ref if rope is not None else None, _ptr(pos), act, _ptr(q), q_pitch,
-                              n_q, k.data_ptr(), k_pitch, v.data_ptr(), v_pitch, _ptr(q_out), act_out, out_pitch,
-                              _stream_on(cache.device, stream)))
+    axes = None
+    if rope is not None:
+        rope, axes = rope.ref, rope.axes_ref
+    _check(lib.nova_kv_append_axes(cache.layer(layer), rows.ref, rope, axes, _ptr(pos), act, _ptr(q), q_pitch, n_q, k.data_ptr(), k_pitch,
+                                   v.data_ptr(), v_pitch, _ptr(q_out), act_out, out_pitch, _stream_on(cache.device, stream)))
     return q_out
+
+
+def rotate(x, pos, rope, out=None, stream=None):
+    """Rotary embedding of dense rows x [rows, heads, head_dim] (bf16 or fp32, heads contiguous: a view of a packed
+    projection, say) at ``pos`` (int32 [rows], with axes [axes, rows]); head_dim a multiple of 8 up to 256.  ``out`` of
+    the same shape, either type, may be x itself."""
+    if x.dim() != 3:
+        raise ValueError(f"x must be rows [rows, heads, head_dim], got {tuple(x.shape)}")
+    n, heads, d = x.shape
+    dev = x.get_device()
+    _check_device(dev, pos, out)
+    act, x_pitch = _check_rows_of("x", x, n, heads, d)
+    if pos is None:
+        raise ValueError("pos is needed")
+    rope._check_pos(pos, n)
+    act_out, out_pitch = act, heads * d
+    if out is None:
+        out = _dense_like(x, stream)
+    else:
+        act_out, out_pitch = _check_rows_of("out", out, n, heads, d)
+    _check(lib.nova_rotate(rope.ref, rope.axes_ref, pos.data_ptr(), n, heads, d, act, x.data_ptr(), x_pitch, act_out, out.data_ptr(),
+                           out_pitch, _stream_on(dev, stream)))
+    return out
 
 
 def kv_gather(cache, rows, slots=None, k_out=None, v_out=None, dtype=torch.bfloat16, layer=0, stream=None):
@@ -740,6 +820,206 @@ def logprobs(logits, given=None, n_top=0, stream=None):
     _check(lib.nova_logprobs(logits.data_ptr(), act, logits.stride(0) if rows > 1 else vocab, rows, vocab, _ptr(given), n_given, _ptr(lp),
                              entropy.data_ptr(), n_top, _ptr(top_lp), _ptr(top_ids), _ptr(ws), nbytes, _stream_on(dev, stream)))
     return lp, entropy, top_lp, top_ids
+
+
+# ----------------------------------------------------------------------------- between two model calls
+def accept(rows, ids, logits, u, mask=None, draft=None, temperature=None, stream=None):
+    """Which of the drafted tokens that a verify step ran (``rows``, ``ids`` int32 [rows], ``mask``) its ``logits`` [rows,
+    vocab] keep, decided by the numbers ``u`` (fp32 [rows] in [0, 1)) at each sequence's ``temperature`` (fp32 [batch];
+    None: 1; 0: greedy).  ``draft``: logits of the distributions that a chain's tokens were drawn from (row 0's are not
+    read): rejection sampling; else every row draws and the walk goes on in the row that feeds what was drawn.  Returns
+    (rows kept int32 [batch], their numbers int32 [batch, max_rows], the token after each, its log probability)."""
+    act = _ACT.get(logits.dtype)
+    n, batch, width = rows.rows, rows.batch, rows.max_rows
+    dev = logits.get_device()
+    _check_device(dev, rows.tables, ids, logits, u, mask, draft, temperature)
+    for what, t in (("logits", logits), ("draft", draft)):
+        if t is not None and (t.dtype not in _ACT or t.dim() != 2 or t.shape[0] != n or t.shape != logits.shape or t.stride(1) != 1):
+            raise ValueError(f"{what} must be float32 or bfloat16 [{n}, vocab] with contiguous rows, got {t.dtype} {tuple(t.shape)}")
+    _check_vector("ids", ids, torch.int32, n)
+    _check_vector("u", u, torch.float32, n)
+    _check_vector("mask", mask, torch.int64, n)
+    _check_vector("temperature", temperature, torch.float32, batch)
+    vocab = logits.shape[1]
+    key = (vocab, draft is not None)
+    nbytes = rows._ws.get(key)
+    if nbytes is None:
+        nbytes = rows._ws[key] = lib.nova_accept_workspace_bytes(rows.ref, vocab, int(draft is not None))
+    ws = _empty(logits, max(nbytes, 256), torch.uint8, stream)
+    # one allocation for what is returned
+    buf = _empty(logits, batch * (1 + 3 * width), torch.int32, stream)
+    n_keep = buf.as_strided((batch,), (1,), 0)
+    path, tokens, lp = (buf.as_strided((batch, width), (width, 1), batch * (1 + i * width)) for i in range(3))
+    lp = lp.view(torch.float32)
+    _check(lib.nova_accept(rows.ref, ids.data_ptr(), _ptr(mask), logits.data_ptr(), act, logits.stride(0) if n > 1 else vocab, _ptr(draft),
+                           _ACT[draft.dtype] if draft is not None else 0, 0 if draft is None else draft.stride(0) if n > 1 else vocab,
+                           vocab, _ptr(temperature), u.data_ptr(), n_keep.data_ptr(), path.data_ptr(), tokens.data_ptr(), lp.data_ptr(),
+                           ws.data_ptr(), nbytes, _stream_on(dev, stream)))
+    return n_keep, path, tokens, lp
+
+
+def kv_keep(cache, rows, path, n_keep, ctx_out=None, stream=None):
+    """The accepted rows (``path`` int32 [batch, max_rows] and ``n_keep`` int32 [batch] as ``accept`` returns them; path
+    None: a chain) moved next to their context in every layer of ``cache``.  Returns the new contexts ``ctx_out`` int32
+    [batch] (not the tensor that ``rows`` holds)."""
+    _check_device(cache.device, rows.tables, path, n_keep, ctx_out)
+    if path is not None and (path.dtype != torch.int32 or path.shape != (rows.batch, rows.max_rows) or not path.is_contiguous()):
+        raise ValueError(f"path must be contiguous int32 {(rows.batch, rows.max_rows)}, got {path.dtype} {tuple(path.shape)}")
+    _check_vector("n_keep", n_keep, torch.int32, rows.batch)
+    if ctx_out is None:
+        ctx_out = _empty(n_keep, rows.batch, torch.int32, stream)
+    _check_vector("ctx_out", ctx_out, torch.int32, rows.batch)
+    _check(lib.nova_kv_keep(cache.layer(0), cache.layers, rows.ref, _ptr(path), n_keep.data_ptr(), ctx_out.data_ptr(),
+                            _stream_on(cache.device, stream)))
+    return ctx_out
+
+
+def kv_copy(cache, src, dst, to=None, stream=None):
+    """Blocks ``src`` of ``cache`` to blocks ``dst`` (int32 [n] each) of ``to`` (another cache of its type, heads and
+    layers, or None: itself), in every layer.  A block may be written once, and not be read too."""
+    to = cache if to is None else to
+    if to.layers != cache.layers:
+        raise ValueError(f"caches of {cache.layers} and {to.layers} layers")
+    _check_device(cache.device, to.k, src, dst)
+    n = src.shape[0] if src.dim() == 1 else -1
+    for what, t in (("src", src), ("dst", dst)):
+        if t.dtype != torch.int32 or t.shape != (n,) or not t.is_contiguous():
+            raise ValueError(f"{what} must be a contiguous int32 vector, src and dst of one length, got {t.dtype} {tuple(t.shape)}")
+    _check(lib.nova_kv_copy(cache.layer(0), to.layer(0), cache.layers, src.data_ptr(), dst.data_ptr(), n, _stream_on(cache.device, stream)))
+
+
+class Pages:
+    """Which blocks of a pool are in use: ``refs`` int32 [num_blocks], how many table entries name each.  Tables are int32
+    [batch, max_blocks], -1 where there is no block.  The lowest free blocks are taken, in the order of the requests; a
+    request that finds too few is left as it was and says 0 in what the call returns (int32, 1: served)."""
+
+    def __init__(self, num_blocks, device="cuda"):
+        self._own(torch.zeros(num_blocks, dtype=torch.int32, device=device))
+
+    @classmethod
+    def of(cls, refs):
+        self = cls.__new__(cls)
+        self._own(refs)
+        return self
+
+    def _own(self, refs):
+        if refs.dtype != torch.int32 or refs.dim() != 1 or refs.shape[0] < 1 or not refs.is_contiguous():
+            raise ValueError(f"refs must be a contiguous int32 vector, got {refs.dtype} {tuple(refs.shape)}")
+        self.refs, self.num_blocks, self.device = refs, refs.shape[0], refs.get_device()
+        self._c = PagesC(_ptr(refs), self.num_blocks)
+        self.ref = C.addressof(self._c)
+
+    def _tables(self, tables, what="tables"):
+        if tables.dtype != torch.int32 or tables.dim() != 2 or not tables.is_contiguous():
+            raise ValueError(f"{what} must be contiguous int32 [batch, max_blocks], got {tables.dtype} {tuple(tables.shape)}")
+        return tables.shape
+
+    def _workspace(self, batch, n, stream):
+        return _empty(self.refs, max(256, lib.nova_pages_workspace_bytes(self.ref, batch, n)), torch.uint8, stream)
+
+    def extend(self, tables, tokens, stream=None):
+        """Blocks for the first ``tokens`` (int32 [batch]) tokens of every sequence, those that it lacks."""
+        batch, width = self._tables(tables)
+        _check_device(self.device, tables, tokens)
+        _check_vector("tokens", tokens, torch.int32, batch)
+        done = _empty(tokens, batch, torch.int32, stream)
+        ws = self._workspace(batch, batch, stream)
+        _check(lib.nova_pages_extend(self.ref, tables.data_ptr(), width, batch, tokens.data_ptr(), done.data_ptr(), ws.data_ptr(), ws.numel(),
+                                     _stream_on(self.device, stream)))
+        return done
+
+    def fork(self, cache, tables, src, dst, tokens, stream=None):
+        """Rows ``dst`` of the tables become the first ``tokens`` tokens of rows ``src`` (int32 [n] each): whole blocks are
+        shared, a last one in part is copied in every layer of ``cache``.  What the rows named before is overwritten."""
+        batch, width = self._tables(tables)
+        _check_device(self.device, cache.k, tables, src, dst, tokens)
+        n = dst.shape[0] if dst.dim() == 1 else 0
+        for what, t in (("src", src), ("dst", dst), ("tokens", tokens)):
+            _check_vector(what, t, torch.int32, n)
+        done = _empty(tables, n, torch.int32, stream)
+        ws = self._workspace(batch, n, stream)
+        _check(lib.nova_pages_fork(self.ref, cache.layer(0), cache.layers, tables.data_ptr(), width, batch, src.data_ptr(), dst.data_ptr(),
+                                   tokens.data_ptr(), n, done.data_ptr(), ws.data_ptr(), ws.numel(), _stream_on(self.device, stream)))
+        return done
+
+    def free(self, tables, seqs, tokens=None, stream=None):
+        """Rows ``seqs`` (int32 [n]) give up what lies behind their first ``tokens`` (int32 [n]; None: 0) tokens."""
+        batch, width = self._tables(tables)
+        _check_device(self.device, tables, seqs, tokens)
+        n = seqs.shape[0] if seqs.dim() == 1 else 0
+        _check_vector("seqs", seqs, torch.int32, n)
+        _check_vector("tokens", tokens, torch.int32, n)
+        _check(lib.nova_pages_free(self.ref, tables.data_ptr(), width, batch, seqs.data_ptr(), _ptr(tokens), n, _stream_on(self.device, stream)))
+
+    def compact(self, cache, tables, refs_out=None, tables_out=None, stream=None):
+        """The pool's used blocks moved to its front in every layer of ``cache``; the tables (all that name its blocks)
+        and refs follow, in place or in ``tables_out`` and ``refs_out``.  Returns the number of used blocks, int32 [1]."""
+        batch, width = self._tables(tables)
+        refs_out, tables_out = self.refs if refs_out is None else refs_out, tables if tables_out is None else tables_out
+        _check_device(self.device, cache.k, tables, refs_out, tables_out)
+        if self._tables(tables_out, "tables_out") != tables.shape:
+            raise ValueError(f"tables {tuple(tables.shape)} and tables_out {tuple(tables_out.shape)}")
+        _check_vector("refs_out", refs_out, torch.int32, self.num_blocks)
+        live = _empty(tables, 1, torch.int32, stream)
+        ws = self._workspace(batch, 0, stream)
+        _check(lib.nova_pages_compact(self.ref, cache.layer(0), cache.layers, tables.data_ptr(), width, batch, refs_out.data_ptr(),
+                                      tables_out.data_ptr(), live.data_ptr(), ws.data_ptr(), ws.numel(), _stream_on(self.device, stream)))
+        return live
+
+
+# ----------------------------------------------------------------------------- adapters
+class Adapters:
+    """Low-rank adapters ``a`` bf16 [n, rank, k] and ``b`` bf16 [n, n_out, rank] with factors ``scale`` fp32 [n] (None: 1);
+    rank a multiple of 8 up to 128, k and n_out multiples of 8."""
+
+    def __init__(self, a, b, scale=None):
+        for what, t in (("a", a), ("b", b)):
+            if t.dtype != torch.bfloat16 or t.dim() != 3 or not t.is_contiguous():
+                raise ValueError(f"{what} must be contiguous bfloat16 of three dimensions, got {t.dtype} {tuple(t.shape)}")
+        n, rank, k = a.shape
+        if b.shape[0] != n or b.shape[2] != rank:
+            raise ValueError(f"a {tuple(a.shape)} and b {tuple(b.shape)} do not belong together")
+        _check_vector("scale", scale, torch.float32, n)
+        if any(t is not None and t.device != a.device for t in (b, scale)):
+            raise ValueError("a, b and scale must be on one device")
+        self.a, self.b, self.scale, self.device = a, b, scale, a.get_device()
+        self.n, self.rank, self.k, self.n_out = n, rank, k, b.shape[1]
+        self._c = AdaptersC(_ptr(a), _ptr(b), _ptr(scale), n, rank, k, self.n_out)
+        self.ref = C.addressof(self._c)
+
+
+def _check_matrix(what, t, rows, cols):
+    """Rows [rows, cols] with contiguous elements; returns (type, pitch)."""
+    act = _ACT.get(t.dtype)
+    if act is None or t.shape != (rows, cols) or t.stride(1) != 1:
+        raise ValueError(f"{what} must be bfloat16 or float32 rows {(rows, cols)}, got {t.dtype} {tuple(t.shape)} strides {t.stride()}")
+    return act, t.stride(0) if rows > 1 else cols
+
+
+def lora(adapters, rows, which, x, base=None, out=None, dtype=None, stream=None):
+    """``base`` + scale b (a x) for the rows x [rows, k] (bf16 or fp32) of ``rows``' sequences, each with its adapter
+    ``which`` (int32 [batch]; outside 0 .. n - 1: none), as ``out`` [rows, n_out] of base's type (None given: ``dtype``, or
+    x's).  out may be base itself; base None: 0.  Rows outside the sequences are left as they were."""
+    n = rows.rows
+    _check_device(adapters.device, rows.tables, which, x, base, out)
+    _check_vector("which", which, torch.int32, rows.batch)
+    act, x_pitch = _check_matrix("x", x, n, adapters.k)
+    if out is None:
+        out = _empty(x, (n, adapters.n_out), base.dtype if base is not None else dtype or x.dtype, stream)
+    act_out, out_pitch = _check_matrix("out", out, n, adapters.n_out)
+    base_pitch = 0
+    if base is not None:
+        act_base, base_pitch = _check_matrix("base", base, n, adapters.n_out)
+        if act_base != act_out:
+            raise ValueError("base and out must have one type")
+    key = ("lora", adapters.rank, adapters.k, adapters.n_out)
+    nbytes = rows._ws.get(key)
+    if nbytes is None:
+        nbytes = rows._ws[key] = lib.nova_lora_workspace_bytes(adapters.ref, rows.ref)
+    ws = _empty(x, nbytes, torch.uint8, stream) if nbytes else None
+    _check(lib.nova_lora(adapters.ref, rows.ref, which.data_ptr(), act, x.data_ptr(), x_pitch, act_out, _ptr(base), base_pitch, out.data_ptr(),
+                         out_pitch, _ptr(ws), nbytes, _stream_on(adapters.device, stream)))
+    return out
 
 
 # ----------------------------------------------------------------------------- linear co-run study
