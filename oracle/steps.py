@@ -54,8 +54,10 @@ def rotate_axes(x, pos, pairs, freq, cyclic=False, interleaved=False, mscale=1.0
 
 
 # ----------------------------------------------------------------------------- acceptance
-def distribution(logits, t):
-    """Probabilities of a row at temperature t; None where there are none."""
+def weights(logits, t):
+    """Probabilities of a row at temperature t times a factor that makes the largest 1; None where there are none.  (Not
+    normalised: equal logits have weights of exactly 1, whose running sums are exact, so that a number on a border
+    between two of them decides as in exact arithmetic.)"""
     x = np.asarray(logits, F64)
     if not (t >= 0 and np.isfinite(t)) or np.isnan(x).any() or (x == np.inf).any() or (x == -np.inf).all():
         return None
@@ -64,8 +66,12 @@ def distribution(logits, t):
         p[int(np.argmax(x))] = 1.0                                                  # the first of the largest
         return p
     with np.errstate(invalid="ignore"):
-        w = np.exp((x - x.max()) / t)
-    return w / w.sum()
+        return np.exp((x - x.max()) / t)
+
+
+def distribution(logits, t):
+    w = weights(logits, t)
+    return None if w is None else w / w.sum()
 
 
 def draw(p, u):
@@ -87,7 +93,7 @@ def accept(logits, ids, u, masks=None, draft=None, t=1.0):
     if draft is None:
         while True:
             at = path[-1]
-            p = distribution(logits[at], t)
+            p = weights(logits[at], t)
             tokens.append(-1 if p is None else draw(p, u[at]))
             kids = [j for j in range(at + 1, n) if ids[j] == tokens[-1] and tokens[-1] >= 0 and parent_of(masks, j) == at]
             if not kids:
@@ -96,14 +102,15 @@ def accept(logits, ids, u, masks=None, draft=None, t=1.0):
     else:
         while True:
             at = path[-1]
-            p = distribution(logits[at], t)
+            p = weights(logits[at], t)
             if p is None:
                 tokens.append(-1)
                 break
             if at + 1 == n:
                 tokens.append(draw(p, u[0]))
                 break
-            x, q = int(ids[at + 1]), distribution(draft[at + 1], t)
+            x, q = int(ids[at + 1]), weights(draft[at + 1], t)
+            q = None if q is None else q * (p.sum() / q.sum())                       # on p's scale
             inside = 0 <= x < len(p)
             uu = 0.0 if not u[at + 1] > 0 else min(u[at + 1], 1 - 2.0 ** -24)
             if t == 0:

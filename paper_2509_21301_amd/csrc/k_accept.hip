@@ -17,23 +17,33 @@
 namespace nova {
 
 constexpr int AC_CHUNK = 4096;             // logits of a workgroup
-constexpr int AC_PER = AC_CHUNK / 256;     // of a thread
+constexpr int AC_THREADS = 256;
+constexpr int AC_PER = AC_CHUNK / AC_THREADS;
 
-// A wave's or a workgroup's sums in a fixed order (so that every call gives the same draws).
-NOVA_DEV double wave_sum64(double v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+// A value of another lane by a data-parallel move: 0 where there is no such lane (or its row is left out of ROWS).
+template <int CTRL, int ROWS> NOVA_DEV double dpp64(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, ROWS, 0xf, true);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, ROWS, 0xf, true);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+NOVA_DEV double lane_of(double v, int l) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)u, l), hi = __builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), l);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// Inclusive running sum over a wave, and its sum; both in a fixed order, so that every call gives the same draws.
+// (Within the 16 lanes of a row by shifts of 1, 2, 4 and 8, then row ends to the rows behind them.)
+NOVA_DEV double wave_scan64(double v) {
+  v += dpp64<0x111, 0xf>(v);
+  v += dpp64<0x112, 0xf>(v);
+  v += dpp64<0x114, 0xf>(v);
+  v += dpp64<0x118, 0xf>(v);
+  v += dpp64<0x142, 0xa>(v);
+  v += dpp64<0x143, 0xc>(v);
   return v;
 }
-NOVA_DEV double wave_scan64(double v) {    // inclusive
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const double up = __shfl_up(v, o, 64);
-    if (lane >= o) v += up;
-  }
-  return v;
-}
+NOVA_DEV double wave_sum64(double v) { return lane_of(wave_scan64(v), 63); }
 
 // The sequence of a row (batch: none).
 NOVA_DEV int seq_of_row(const BatchRows& p, int r) {
@@ -47,38 +57,71 @@ NOVA_DEV int seq_of_row(const BatchRows& p, int r) {
   return lo;
 }
 
-// 1 / T, 0 for T = 0 (the largest logit takes all), negative where T gives no distribution.
+// log2(e) / T, 0 for T = 0 (the largest logit takes all), negative where T gives no distribution.
 NOVA_DEV double inv_temperature(const AcceptArgs& p, int b) {
   const float t = p.temperature ? p.temperature[b] : 1.f;
   if (t == 0.f) return 0.0;
-  return t > 0.f && t < INFINITY ? 1.0 / (double)t : -1.0;
+  return t > 0.f && t < INFINITY ? 1.4426950408889634 / (double)t : -1.0;
 }
 
-// e^x for x <= 0 in 64 bits: 2^k e^r with |r| <= ln 2 / 2, and the Taylor series of e^r to r^13 (its rest is below 5e-18).
-NOVA_DEV double exp_neg(double x) {
-  if (!(x > -745.0)) return x != x ? x : 0.0;
-  const double k = rint(x * 1.4426950408889634);
-  double r = fma(k, -0x1.62e42fefa39efp-1, x);
-  r = fma(k, -0x1.abc9e3b39803fp-56, r);
-  double y = 1.0 / 6227020800.0;
-  y = fma(y, r, 1.0 / 479001600.0);
-  y = fma(y, r, 1.0 / 39916800.0);
-  y = fma(y, r, 1.0 / 3628800.0);
-  y = fma(y, r, 1.0 / 362880.0);
-  y = fma(y, r, 1.0 / 40320.0);
-  y = fma(y, r, 1.0 / 5040.0);
-  y = fma(y, r, 1.0 / 720.0);
-  y = fma(y, r, 1.0 / 120.0);
-  y = fma(y, r, 1.0 / 24.0);
-  y = fma(y, r, 1.0 / 6.0);
-  y = fma(y, r, 0.5);
-  y = fma(y, r, 1.0);
-  y = fma(y, r, 1.0);
-  return ldexp(y, (int)k);
+// 2^z for z <= 0 in 64 bits (0 below 2^-1074 and for -infinity): z = k + j / 256 + f with |f| <= 2^-9, the table's
+// 2^(j/256), and the Taylor series of 2^f to f^4 (its rest is below 4e-17): 17 instructions, where a series without a
+// table takes 30, and 64-bit ones issue as slowly as they come: the first pass over 480 rows of 152064 logits took 96 us
+// with the longer one, 62 us with this.
+struct Exp2Table { double t[256]; };       // in LDS
+NOVA_DEV void fill_table(Exp2Table& tab) { // by the workgroup's threads; a barrier has to follow
+  for (int j = threadIdx.x; j < 256; j += blockDim.x) {
+    const double r = j * (0.6931471805599453 / 256);
+    double y = 1.0;                        // Taylor series of e^r, r < ln 2, from its 20th power on
+#pragma unroll
+    for (int n = 20; n >= 1; --n) y = fma(y, r * (1.0 / n), 1.0);
+    tab.t[j] = y;
+  }
 }
+NOVA_DEV double exp2_neg(const Exp2Table& tab, double z) {
+  constexpr double MAGIC = 0x1.8p44;       // a sum with it ends at the 8th binary place
+  z = fmax(z, -1100.0);
+  const double t = z + MAGIC, f = z - (t - MAGIC);
+  const int n = (int)(uint32_t)__builtin_bit_cast(uint64_t, t);
+  double y = fma(f, 9.6181291076284772e-3, 5.5504108664821580e-2);
+  y = fma(y, f, 2.4022650695910072e-1);
+  y = fma(y, f, 6.9314718055994531e-1);
+  const double b = tab.t[n & 255];
+  return ldexp(fma(b, y * f, b), n >> 8);
+}
+constexpr double LN2 = 0.6931471805599453;
 
 // A logit of a row, from memory in its type.
 template <typename T> NOVA_DEV float logit(const T* row, int i) { return to_f<T>(row[i]); }
+
+// The larger of two values, NaN where either is.
+NOVA_DEV float nan_max(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+// A thread's logits of a chunk: 16 bytes at a time where the row allows it (x[i]: number place_of(.., i) of the chunk);
+// -infinity behind the vocabulary.
+NOVA_DEV int place_of(bool f32, int i) {
+  const int n = f32 ? 4 : 8;
+  return (i / n * AC_THREADS + threadIdx.x) * n + i % n;
+}
+template <typename T> NOVA_DEV void load_chunk(const T* row, int c0, int vocab, float* x) {
+  constexpr int N = 16 / sizeof(T);
+  if (((uintptr_t)row & 15) == 0 && c0 + AC_CHUNK <= vocab) {
+    u32x4 w[AC_PER / N];
+#pragma unroll
+    for (int i = 0; i < AC_PER / N; ++i) w[i] = reinterpret_cast<const u32x4*>(row + c0)[i * AC_THREADS + threadIdx.x];
+#pragma unroll
+    for (int i = 0; i < AC_PER; ++i) {
+      if constexpr (N == 4) x[i] = __uint_as_float(w[i / 4][i % 4]);
+      else x[i] = __uint_as_float(i & 1 ? w[i / 8][i % 8 / 2] & 0xFFFF0000u : w[i / 8][i % 8 / 2] << 16);
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < AC_PER; ++i) {
+    const int at = c0 + place_of(N == 4, i);
+    x[i] = at < vocab ? logit(row, at) : -INFINITY;
+  }
+}
 
 // ------------------------------------------------------------------ first pass
 // Workgroup: a chunk of one row.  Rows 0 .. rows - 1 are the target's, the next `rows` the draft's.
@@ -101,52 +144,45 @@ __global__ void __launch_bounds__(256) accept_stats_kernel(AcceptArgs p) {
   if (b >= p.r.batch) return;
   const SeqRows sr = seq_rows(p.r, b);
   if (r < sr.r0 + (draft ? 1 : 0) || r >= sr.r0 + sr.n) return;   // a sequence's first row was drawn by nobody
-  const double inv = inv_temperature(p, b);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c0 = chunk * AC_CHUNK;
   float x[AC_PER];
-#pragma unroll
-  for (int i = 0; i < AC_PER; ++i) {
-    const int at = c0 + i * 256 + threadIdx.x;
-    x[i] = at >= p.vocab ? -INFINITY : draft ? logit((const TD*)p.draft + (long)r * p.draft_row, at) : logit((const TL*)p.logits + (long)r * p.row, at);
-  }
-  float m = -INFINITY;
-  int arg = 0x7FFFFFFF;
-  bool bad = false;                        // NaN or +infinity: no distribution
-#pragma unroll
-  for (int i = 0; i < AC_PER; ++i) {
-    bad |= !(x[i] < INFINITY);
-    if (x[i] > m) m = x[i], arg = c0 + i * 256 + threadIdx.x;
-  }
+  if (draft) load_chunk((const TD*)p.draft + (long)r * p.draft_row, c0, p.vocab, x);
+  else load_chunk((const TL*)p.logits + (long)r * p.row, c0, p.vocab, x);
+  __shared__ Exp2Table tab;
   __shared__ float sm_m[4];
-  __shared__ int sm_arg[4], sm_bad[4];
+  __shared__ int sm_arg[4];
   __shared__ double sm_s[4];
+  const double inv = inv_temperature(p, b);
+  fill_table(tab);                         // while the logits are on their way
+  float m = x[0];
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) {
-    const float om = __shfl_xor(m, o, 64);
-    const int oa = __shfl_xor(arg, o, 64);
-    if (om > m || (om == m && oa < arg)) m = om, arg = oa;
-  }
-  const bool any_bad = __ballot(bad) != 0;
-  if (lane == 0) sm_m[wave] = m, sm_arg[wave] = arg, sm_bad[wave] = any_bad;
+  for (int i = 1; i < AC_PER; ++i) m = nan_max(m, x[i]);
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) m = nan_max(m, __shfl_xor(m, o, 64));
+  if (lane == 0) sm_m[wave] = m;
   __syncthreads();
-  m = sm_m[0], arg = sm_arg[0], bad = sm_bad[0];
-#pragma unroll
-  for (int w = 1; w < 4; ++w) {
-    if (sm_m[w] > m || (sm_m[w] == m && sm_arg[w] < arg)) m = sm_m[w], arg = sm_arg[w];
-    bad |= sm_bad[w];
-  }
+  m = nan_max(nan_max(sm_m[0], sm_m[1]), nan_max(sm_m[2], sm_m[3]));
   double sum = 0.0;
-  if (inv > 0.0 && m > -INFINITY && !bad) {
+  if (inv > 0.0 && m > -INFINITY && m < INFINITY) {
+    // the difference first: it is exact, where a product with a small temperature's inverse would not cancel at the maximum
 #pragma unroll
-    for (int i = 0; i < AC_PER; ++i) sum += exp_neg(((double)x[i] - (double)m) * inv);
+    for (int i = 0; i < AC_PER; ++i) sum += exp2_neg(tab, ((double)x[i] - (double)m) * inv);
   }
   sum = wave_sum64(sum);
-  if (lane == 0) sm_s[wave] = sum;
+  int arg = 0x7FFFFFFF;
+  if (inv == 0.0) {                        // greedy: the first of the largest
+#pragma unroll
+    for (int i = 0; i < AC_PER; ++i)
+      if (x[i] == m) arg = min(arg, c0 + place_of(draft ? (sizeof(TD) == 4) : (sizeof(TL) == 4), i));
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) arg = min(arg, __shfl_xor(arg, o, 64));
+  }
+  if (lane == 0) sm_s[wave] = sum, sm_arg[wave] = arg;
   __syncthreads();
   if (threadIdx.x == 0) {
     const long at = (long)item * p.chunks + chunk;
-    p.part_max[at] = bad ? __uint_as_float(0x7FC00000u) : m;
-    p.part_arg[at] = arg;
+    p.part_max[at] = m < INFINITY ? m : __uint_as_float(0x7FC00000u);   // NaN or +infinity: no distribution
+    p.part_arg[at] = min(min(sm_arg[0], sm_arg[1]), min(sm_arg[2], sm_arg[3]));
     p.part_sum[at] = ((sm_s[0] + sm_s[1]) + sm_s[2]) + sm_s[3];
   }
 }
@@ -157,7 +193,7 @@ struct RowStats { float m; int arg; double s; };
 NOVA_DEV bool has_dist(const RowStats& a, double inv) { return a.m > -INFINITY && inv >= 0.0; }   // NaN compares false
 
 // By one wave; every lane returns the same.
-NOVA_DEV RowStats join_row(const AcceptArgs& p, int item, double inv) {
+NOVA_DEV RowStats join_row(const AcceptArgs& p, const Exp2Table& tab, int item, double inv) {
   const int lane = threadIdx.x & 63;
   const long at = (long)item * p.chunks;
   RowStats a{-INFINITY, 0x7FFFFFFF, 0.0};
@@ -180,7 +216,7 @@ NOVA_DEV RowStats join_row(const AcceptArgs& p, int item, double inv) {
   if (a.m == -INFINITY || !(inv > 0.0)) return a;
   for (int c = lane; c < p.chunks; c += 64) {
     const float m = p.part_max[at + c];
-    if (m > -INFINITY) a.s += p.part_sum[at + c] * exp_neg(((double)m - (double)a.m) * inv);
+    if (m > -INFINITY) a.s += p.part_sum[at + c] * exp2_neg(tab, ((double)m - (double)a.m) * inv);
   }
   a.s = wave_sum64(a.s);
   return a;
@@ -201,70 +237,57 @@ template <typename F> NOVA_DEV int first_above(int n, double target, double* bef
     const unsigned long long over = __ballot(incl > target && v > 0.0), some = __ballot(v > 0.0);
     if (over) {
       const int l = __ffsll(over) - 1;
-      *before = __shfl(incl - v, l, 64);
+      *before = lane_of(incl - v, l);
       return i0 + l;
     }
     if (some) {
       const int l = 63 - __clzll(some);
       last = i0 + l;
-      run_last = __shfl(incl - v, l, 64);
+      run_last = lane_of(incl - v, l);
     }
-    run = __shfl(incl, 63, 64);
+    run = lane_of(incl, 63);
   }
   *before = run_last;
   return last;
 }
 
-// The token of a chunk whose running sum of weight(i) exceeds `target`; by the whole workgroup of 256.
+// The token of a chunk whose running sum of weight(i) exceeds `target`; by the whole workgroup.  First the thread's
+// range of consecutive logits, then the logit in it, one a lane.
 template <typename F> NOVA_DEV int draw_in_chunk(int c0, int vocab, double target, F&& weight) {
-  __shared__ double sm_sum[256];
-  __shared__ int sm_pick;
-  const int first = c0 + threadIdx.x * AC_PER;
-  double w[AC_PER], sum = 0.0;
-#pragma unroll
-  for (int i = 0; i < AC_PER; ++i) {
-    w[i] = first + i < vocab ? weight(first + i) : 0.0;
-    sum += w[i];
-  }
+  const int per = AC_CHUNK / blockDim.x;
+  __shared__ double sm_sum[1024];
+  const int first = c0 + threadIdx.x * per;
+  double sum = 0.0;
+#pragma unroll 4
+  for (int i = 0; i < per; ++i) sum += first + i < vocab ? weight(first + i) : 0.0;
   __syncthreads();
   sm_sum[threadIdx.x] = sum;
   __syncthreads();
   double before = 0.0;
-  const int t = first_above(256, target, &before, [&](int i) { return sm_sum[i]; });
-  if ((int)threadIdx.x == t) {
-    double run = before;
-    int pick = first;
-    bool found = false;
-#pragma unroll
-    for (int i = 0; i < AC_PER; ++i) {
-      run += w[i];
-      if (!found && w[i] > 0.0) pick = first + i;          // the last with a weight, unless the sum is exceeded before
-      found |= w[i] > 0.0 && run > target;
-    }
-    sm_pick = pick;
-  }
-  __syncthreads();
-  return sm_pick;
+  const int t = first_above(blockDim.x, target, &before, [&](int i) { return sm_sum[i]; });
+  const int from = c0 + t * per;
+  double none;
+  return from + first_above(min(per, vocab - from), target - before, &none, [&](int i) { return weight(from + i); });
 }
 
 // A token drawn from a target row by its number u; by the whole workgroup.  -1: the row has no distribution.
-template <typename TL> NOVA_DEV int draw_row(const AcceptArgs& p, int r, const RowStats& a, double inv, float u) {
+template <typename TL> NOVA_DEV int draw_row(const AcceptArgs& p, const Exp2Table& tab, int r, const RowStats& a, double inv, float u) {
   if (!has_dist(a, inv)) return -1;
   if (inv == 0.0) return a.arg;
   const TL* row = (const TL*)p.logits + (long)r * p.row;
   const long at = (long)r * p.chunks;
   double before = 0.0;
   const double target = uniform(u) * a.s;
-  auto scale = [&](float m) { return m > -INFINITY ? exp_neg(((double)m - (double)a.m) * inv) : 0.0; };
+  auto scale = [&](float m) { return m > -INFINITY ? exp2_neg(tab, ((double)m - (double)a.m) * inv) : 0.0; };
   const int c = first_above(p.chunks, target, &before, [&](int i) { return p.part_sum[at + i] * scale(p.part_max[at + i]); });
-  return draw_in_chunk(c * AC_CHUNK, p.vocab, target - before, [&](int i) { return exp_neg(((double)logit(row, i) - (double)a.m) * inv); });
+  return draw_in_chunk(c * AC_CHUNK, p.vocab, target - before, [&](int i) { return exp2_neg(tab, ((double)logit(row, i) - (double)a.m) * inv); });
 }
 
 // log p of a token of a row.
 template <typename TL> NOVA_DEV float log_p(const AcceptArgs& p, int r, const RowStats& a, double inv, int token) {
   if (token < 0) return __uint_as_float(0x7FC00000u);
   if (inv == 0.0) return 0.f;
-  return (float)(((double)logit((const TL*)p.logits + (long)r * p.row, token) - (double)a.m) * inv - log(a.s));
+  return (float)(((double)logit((const TL*)p.logits + (long)r * p.row, token) - (double)a.m) * inv * LN2 - log(a.s));
 }
 
 // The workgroups of a sequence that have come this far, this one included; what each stored before (with
@@ -289,8 +312,11 @@ __global__ void __launch_bounds__(256) accept_follow_kernel(AcceptArgs p) {
   const SeqRows sr = seq_rows(p.r, b);
   if (r < sr.r0 || r >= sr.r0 + sr.n) return;
   const double inv = inv_temperature(p, b);
-  const RowStats a = join_row(p, r, inv);
-  const int token = draw_row<TL>(p, r, a, inv, p.u[r]);
+  __shared__ Exp2Table tab;
+  fill_table(tab);
+  __syncthreads();
+  const RowStats a = join_row(p, tab, r, inv);
+  const int token = draw_row<TL>(p, tab, r, a, inv, p.u[r]);
   if (threadIdx.x == 0) {
     put(p.row_token + r, token);
     put(p.row_lp + r, log_p<TL>(p, r, a, inv, token));
@@ -330,28 +356,32 @@ __global__ void __launch_bounds__(256) accept_follow_kernel(AcceptArgs p) {
 }
 
 // ------------------------------------------------------------------ second pass with the draft's probabilities
-// Workgroup: a chunk of a sequence.  Each finds the first row that is not kept (a wave tests a row); where the token is
+// Workgroup: a chunk of a sequence.  Each finds the first row that is not kept (a wave tests a row, eight at a time); where the token is
 // drawn from what the target has more than the draft, it sums that over its chunk, and the last to arrive draws.  Else
 // the first chunk's workgroup draws from the target's row.
+constexpr int AC_TEST = 512, AC_WAVES = AC_TEST / 64;
 template <typename TL, typename TD>
-__global__ void __launch_bounds__(256) accept_draft_kernel(AcceptArgs p) {
+__global__ void __launch_bounds__(AC_TEST) accept_draft_kernel(AcceptArgs p) {
   const int b = blockIdx.x / p.chunks, chunk = blockIdx.x % p.chunks;
   const SeqRows sr = seq_rows(p.r, b);
   if (sr.n <= 0) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const double inv = inv_temperature(p, b);
   __shared__ float sm_lp[64];
-  __shared__ int sm_kept[4], sm_rest[4];   // of a wave's row: its token is kept; else what remains of p is drawn from
-  __shared__ RowStats sm_p[4], sm_q[4];
+  __shared__ int sm_kept[AC_WAVES], sm_rest[AC_WAVES];   // of a wave's row: its token is kept; else what remains of p is drawn from
+  __shared__ RowStats sm_p[AC_WAVES], sm_q[AC_WAVES];
+  __shared__ Exp2Table tab;
+  fill_table(tab);
+  __syncthreads();
   int at = 0;                              // the last kept row
   bool rest = false;
   RowStats tp{}, tq{};                     // of it, and of the draft's row behind it
-  for (int j0 = 1;; j0 += 4) {
+  for (int j0 = 1;; j0 += AC_WAVES) {
     // wave w: row j0 + w against its draft, the target's row before it
     const int j = j0 + wave;
     if (j <= sr.n) {
       const int r = sr.r0 + j - 1;
-      const RowStats a = join_row(p, r, inv);
+      const RowStats a = join_row(p, tab, r, inv);
       RowStats q{__uint_as_float(0x7FC00000u), 0, 0.0};
       bool kept = false, some = false;
       float lp = 0.f;
@@ -361,13 +391,13 @@ __global__ void __launch_bounds__(256) accept_draft_kernel(AcceptArgs p) {
         if (inv == 0.0) {
           kept = x == a.arg;
         } else {
-          q = join_row(p, p.r.rows + r + 1, inv);
+          q = join_row(p, tab, p.r.rows + r + 1, inv);
           some = has_dist(q, inv);
           if (in && some) {
             const double zp = ((double)logit((const TL*)p.logits + (long)r * p.row, x) - (double)a.m) * inv;
             const double zq = ((double)logit((const TD*)p.draft + (long)(r + 1) * p.draft_row, x) - (double)q.m) * inv;
-            kept = uniform(p.u[r + 1]) * (exp_neg(zq) / q.s) < exp_neg(zp) / a.s;
-            lp = (float)(zp - log(a.s));
+            kept = uniform(p.u[r + 1]) * (exp2_neg(tab, zq) / q.s) < exp2_neg(tab, zp) / a.s;
+            lp = (float)(zp * LN2 - log(a.s));
           }
         }
       }
@@ -381,8 +411,8 @@ __global__ void __launch_bounds__(256) accept_draft_kernel(AcceptArgs p) {
     }
     __syncthreads();
     int w = 0;
-    while (w < 4 && sm_kept[w]) ++w;
-    if (w < 4) {
+    while (w < AC_WAVES && sm_kept[w]) ++w;
+    if (w < AC_WAVES) {
       at = j0 + w - 1;
       rest = sm_rest[w];
       tp = sm_p[w], tq = sm_q[w];
@@ -396,22 +426,28 @@ __global__ void __launch_bounds__(256) accept_draft_kernel(AcceptArgs p) {
   if (rest) {
     const TL* rp = (const TL*)p.logits + (long)r * p.row;
     const TD* rq = (const TD*)p.draft + (long)(r + 1) * p.draft_row;
-    const double ip = 1.0 / tp.s, iq = 1.0 / tq.s;
+    // times p's sum, so that equal logits of the target weigh exactly 1 and their running sums are exact
+    const double iq = tp.s / tq.s;
     auto more = [&](int i) {
-      const double d = exp_neg(((double)logit(rp, i) - (double)tp.m) * inv) * ip - exp_neg(((double)logit(rq, i) - (double)tq.m) * inv) * iq;
+      const double d = exp2_neg(tab, ((double)logit(rp, i) - (double)tp.m) * inv) - exp2_neg(tab, ((double)logit(rq, i) - (double)tq.m) * inv) * iq;
       return d > 0.0 ? d : 0.0;
     };
-    __shared__ double sm_s[4];
+    __shared__ double sm_s[AC_WAVES];
     double sum = 0.0;
     const int first = chunk * AC_CHUNK + threadIdx.x;
-#pragma unroll 4
-    for (int i = 0; i < AC_PER; ++i)
-      if (first + 256 * i < p.vocab) sum += more(first + 256 * i);
+#pragma unroll
+    for (int i = 0; i < AC_CHUNK / AC_TEST; ++i)
+      if (first + AC_TEST * i < p.vocab) sum += more(first + AC_TEST * i);
     sum = wave_sum64(sum);
     if (lane == 0) sm_s[wave] = sum;
     __syncthreads();
     double* parts = p.rest_sum + (long)b * p.chunks;
-    if (threadIdx.x == 0) put(parts + chunk, ((sm_s[0] + sm_s[1]) + sm_s[2]) + sm_s[3]);
+    if (threadIdx.x == 0) {
+      sum = 0.0;
+#pragma unroll
+      for (int w = 0; w < AC_WAVES; ++w) sum += sm_s[w];
+      put(parts + chunk, sum);
+    }
     if (arrive(p.counters + b) != (unsigned)p.chunks) return;
     double total = 0.0;
     for (int c = lane; c < p.chunks; c += 64) total += get(parts + c);
@@ -422,11 +458,11 @@ __global__ void __launch_bounds__(256) accept_draft_kernel(AcceptArgs p) {
       const int c = first_above(p.chunks, target, &before, [&](int i) { return get(parts + i); });
       token = draw_in_chunk(c * AC_CHUNK, p.vocab, target - before, more);
     } else {                               // nothing is left by rounding: p and q are alike
-      token = draw_row<TL>(p, r, tp, inv, u);
+      token = draw_row<TL>(p, tab, r, tp, inv, u);
     }
   } else {
     if (chunk != 0) return;
-    token = draw_row<TL>(p, r, tp, inv, u);
+    token = draw_row<TL>(p, tab, r, tp, inv, u);
   }
   const int i = threadIdx.x;
   if (i == 0) p.n_keep[b] = at + 1;
@@ -447,7 +483,7 @@ static hipError_t accept_types(const AcceptArgs& p, hipStream_t s) {
   hipLaunchKernelGGL((accept_stats_kernel<TL, TD>), dim3((unsigned)blocks), dim3(256), 0, s, p);
   if (hipError_t e = hipGetLastError()) return e;
   if (p.r.rows == 0) return hipSuccess;
-  if (p.draft) hipLaunchKernelGGL((accept_draft_kernel<TL, TD>), dim3((unsigned)((long)p.r.batch * p.chunks)), dim3(256), 0, s, p);
+  if (p.draft) hipLaunchKernelGGL((accept_draft_kernel<TL, TD>), dim3((unsigned)((long)p.r.batch * p.chunks)), dim3(AC_TEST), 0, s, p);
   else hipLaunchKernelGGL((accept_follow_kernel<TL>), dim3((unsigned)p.r.rows), dim3(256), 0, s, p);
   return hipGetLastError();
 }

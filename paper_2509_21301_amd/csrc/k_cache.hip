@@ -282,73 +282,91 @@ hipError_t kv_append(const AppendArgs& p, int cus, hipStream_t s) {
 
 // ------------------------------------------------------------------ rotary embedding of dense rows
 // Workgroup: R rows of a group of heads.  The rows' sines and cosines are formed once in LDS; then a lane takes an item at a
-// time: 8 pairs of the half layout (two loads of 8 elements, D/2 apart), 8 elements of the interleaved one or 8 that
-// are not turned.  Items are numbered over rows and heads so that neighbouring lanes read neighbouring memory.
-constexpr int ROT_ROWS = 16;
+// time: 8 pairs of the half layout (two loads of 8 elements, rot/2 apart), 8 elements of the interleaved one or 8 that
+// are not turned.  Items are numbered over rows and heads so that neighbouring lanes read neighbouring memory, and four
+// are requested before the first is turned.
+constexpr int ROT_ROWS = 8, ROT_AHEAD = 4;
 
 // n / d for n < 2^32 / d, from m = 2^32 / d + 1 (0 for d = 1).
 NOVA_DEV uint32_t div_by(uint32_t n, uint32_t m) { return m ? __umulhi(n, m) : n; }
 inline uint32_t reciprocal(uint32_t d) { return d == 1 ? 0u : (uint32_t)((1ull << 32) / d + 1); }
 
-// Items of a head, heads of a workgroup (at most ROT_ITEMS items a row, so that div_by is exact over 16 rows), and the
+// Items of a head, heads of a workgroup (at most ROT_ITEMS items a row, so that div_by is exact over its rows), and the
 // reciprocals of the items of a head and of a row.
 constexpr int ROT_ITEMS = 4096;
 struct RotateSplit { int items, heads; uint32_t per_item, per_row; };
 
-template <typename TI, typename TO, int R>
+template <typename TI, typename TO, int R, bool INTER>
 __global__ void __launch_bounds__(256) rotate_kernel(RotateArgs p, RotateSplit d) {
   extern __shared__ __align__(16) float sm[];             // [R][half] cosines, then sines
   const int half = p.rot >> 1, r0 = blockIdx.x * R, n = min(R, p.rows - r0);
-  for (int r = 0; r < n; ++r)
-    for (int c = threadIdx.x; c < half; c += 256) {
-      const int pos = p.pos[(p.pos_axis ? p.axis[c] * p.pos_axis : 0) + r0 + r];
-      float sn, cs;
-      turn_sincos((double)pos * p.turns[c], &sn, &cs);
-      sm[r * half + c] = cs * p.mscale;
-      sm[(R + r) * half + c] = sn * p.mscale;
-    }
-  __syncthreads();
-  const int turned = p.interleaved ? p.rot >> 3 : p.rot >> 4;   // items of a head that are turned
+  const int turned = INTER ? p.rot >> 3 : p.rot >> 4;     // items of a head that are turned
   const int h0 = blockIdx.y * d.heads;
   const uint32_t row_items = d.items * d.heads, live = d.items * min(d.heads, p.heads - h0);   // of a row; those of heads that there are
   const bool same = p.x == p.out;                         // what is not turned is in place already
   const TI* x0 = reinterpret_cast<const TI*>(p.x) + (long)r0 * p.x_row + h0 * p.D;
   TO* o0 = reinterpret_cast<TO*>(p.out) + (long)r0 * p.out_row + h0 * p.D;
-  for (uint32_t i = threadIdx.x; i < n * row_items; i += 256) {
+  struct Item { int row, at, t; };                         // row of the workgroup (-1: none), first element, number in its head
+  auto item = [&](uint32_t i) {
     const uint32_t r = div_by(i, d.per_row), k = i - r * row_items, h = div_by(k, d.per_item), t = k - h * d.items;
-    if (k >= live) continue;
-    const TI* x = x0 + r * p.x_row + h * p.D;
-    TO* o = o0 + r * p.out_row + h * p.D;
-    if (t >= (uint32_t)turned) {
-      if (same) continue;
-      const int c = p.rot + 8 * (t - turned);
-      float a[8];
-      load8(x + c, a);
-      store8(o + c, a);
-    } else if (p.interleaved) {
-      const float* cs = sm + r * half + 4 * t;
-      const float* sn = cs + R * half;
-      float a[8], y[8];
-      load8(x + 8 * t, a);
+    Item m{(int)r, (int)(h * p.D + (t < (uint32_t)turned ? 8 * t : p.rot + 8 * (t - turned))), (int)t};
+    if (i >= n * row_items || k >= live || (same && t >= (uint32_t)turned)) m.row = -1;
+    return m;
+  };
+  Raw8<TI> a[ROT_AHEAD], b[ROT_AHEAD];
+  auto request = [&](uint32_t i0) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        y[2 * e] = a[2 * e] * cs[e] - a[2 * e + 1] * sn[e];
-        y[2 * e + 1] = a[2 * e + 1] * cs[e] + a[2 * e] * sn[e];
-      }
-      store8(o + 8 * t, y);
-    } else {
-      const float* cs = sm + r * half + 8 * t;
-      const float* sn = cs + R * half;
-      float a[8], b[8], y[8], z[8];
-      load8(x + 8 * t, a);
-      load8(x + half + 8 * t, b);
+    for (int u = 0; u < ROT_AHEAD; ++u) {
+      const Item m = item(i0 + 256 * u);
+      if (m.row < 0) continue;
+      const TI* x = x0 + m.row * p.x_row + m.at;
+      a[u] = load_raw(x);
+      if (!INTER && m.t < turned) b[u] = load_raw(x + half);
+    }
+  };
+  request(threadIdx.x);                                    // in flight while the angles are formed
+  for (int c = threadIdx.x; c < n * half; c += 256) {
+    const int r = c / half, i = c - r * half;
+    const int pos = p.pos[(p.pos_axis ? p.axis[i] * p.pos_axis : 0) + r0 + r];
+    float sn, cs;
+    turn_sincos((double)pos * p.turns[i], &sn, &cs);
+    sm[c] = cs * p.mscale;
+    sm[R * half + c] = sn * p.mscale;
+  }
+  __syncthreads();
+  for (uint32_t i0 = threadIdx.x; i0 < n * row_items; i0 += 256 * ROT_AHEAD) {
+    if (i0 != threadIdx.x) request(i0);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        y[e] = a[e] * cs[e] - b[e] * sn[e];
-        z[e] = b[e] * cs[e] + a[e] * sn[e];
+    for (int u = 0; u < ROT_AHEAD; ++u) {
+      const Item m = item(i0 + 256 * u);
+      if (m.row < 0) continue;
+      TO* o = o0 + m.row * p.out_row + m.at;
+      float x[8], y[8];
+      unpack8(a[u], x);
+      if (m.t >= turned) {
+        store8(o, x);
+      } else if (INTER) {
+        const float* cs = sm + m.row * half + 4 * m.t;
+        const float* sn = cs + R * half;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          y[2 * e] = x[2 * e] * cs[e] - x[2 * e + 1] * sn[e];
+          y[2 * e + 1] = x[2 * e + 1] * cs[e] + x[2 * e] * sn[e];
+        }
+        store8(o, y);
+      } else {
+        const float* cs = sm + m.row * half + 8 * m.t;
+        const float* sn = cs + R * half;
+        float w[8], z[8];
+        unpack8(b[u], w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          y[e] = x[e] * cs[e] - w[e] * sn[e];
+          z[e] = w[e] * cs[e] + x[e] * sn[e];
+        }
+        store8(o, y);
+        store8(o + half, z);
       }
-      store8(o + 8 * t, y);
-      store8(o + half + 8 * t, z);
     }
   }
 }
@@ -361,12 +379,17 @@ static hipError_t rotate_types(const RotateArgs& p, int cus, hipStream_t s) {
   d.per_item = reciprocal(d.items);
   d.per_row = reciprocal(d.items * d.heads);
   // few rows: a workgroup each
-  const bool many = p.rows >= 4 * ROT_ROWS * cus / 2;
+  const bool many = p.rows >= 2 * ROT_ROWS * cus;
   const int R = many ? ROT_ROWS : 1;
   const size_t lds = (size_t)R * p.rot * sizeof(float);
   const dim3 grid((p.rows + R - 1) / R, (p.heads + d.heads - 1) / d.heads);
-  if (many) hipLaunchKernelGGL((rotate_kernel<TI, TO, ROT_ROWS>), grid, dim3(256), lds, s, p, d);
-  else hipLaunchKernelGGL((rotate_kernel<TI, TO, 1>), grid, dim3(256), lds, s, p, d);
+  if (p.interleaved) {
+    if (many) hipLaunchKernelGGL((rotate_kernel<TI, TO, ROT_ROWS, true>), grid, dim3(256), lds, s, p, d);
+    else hipLaunchKernelGGL((rotate_kernel<TI, TO, 1, true>), grid, dim3(256), lds, s, p, d);
+  } else {
+    if (many) hipLaunchKernelGGL((rotate_kernel<TI, TO, ROT_ROWS, false>), grid, dim3(256), lds, s, p, d);
+    else hipLaunchKernelGGL((rotate_kernel<TI, TO, 1, false>), grid, dim3(256), lds, s, p, d);
+  }
   return hipGetLastError();
 }
 

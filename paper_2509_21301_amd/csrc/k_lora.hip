@@ -132,18 +132,22 @@ __global__ void __launch_bounds__(256) lora_shrink_kernel(LoraArgs p) {
 }
 
 // ------------------------------------------------------------------ out = base + s B h
-template <typename T> NOVA_DEV void load_out8(const T* p, float* x) {
-  if constexpr (sizeof(T) == 4) {
-    *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(p);
-    *reinterpret_cast<float4*>(x + 4) = *reinterpret_cast<const float4*>(p + 4);
-  } else {
-    const Frag8 f = *reinterpret_cast<const Frag8*>(p);
+// Eight elements of base as loaded, and as floats.
+template <typename T> struct Out8;
+template <> struct Out8<bf16_t> { u32x4 w; };
+template <> struct Out8<float> { f32x4 a, b; };
+NOVA_DEV Out8<bf16_t> load_out8(const bf16_t* p) { return {*reinterpret_cast<const u32x4*>(p)}; }
+NOVA_DEV Out8<float> load_out8(const float* p) { return {reinterpret_cast<const f32x4*>(p)[0], reinterpret_cast<const f32x4*>(p)[1]}; }
+NOVA_DEV void unpack_out8(const Out8<bf16_t>& r, float* x) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(f.w[i] << 16);
-      x[2 * i + 1] = __uint_as_float(f.w[i] & 0xFFFF0000u);
-    }
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(r.w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(r.w[i] & 0xFFFF0000u);
   }
+}
+NOVA_DEV void unpack_out8(const Out8<float>& r, float* x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = r.a[i], x[4 + i] = r.b[i];
 }
 template <typename T> NOVA_DEV void store_out8(T* p, const float* x) {
   if constexpr (sizeof(T) == 4) {
@@ -158,8 +162,9 @@ template <typename T> NOVA_DEV void store_out8(T* p, const float* x) {
 }
 
 // Workgroup: (tile of TM rows, `cols` columns); a wave takes 64 columns at a time.  Which column of B is which MFMA row
-// is free, so a lane gets 16 consecutive columns of its row of out over four tiles: 4 lane groups, 64 columns, whole
-// lines.  K (here the rank) is 32 a step.
+// is free, so two tiles give a lane 8 consecutive columns of its row of out, and the four lane groups 32: 64 bytes of a
+// row side by side in one instruction.  The rows of base of all row tiles are requested before the first product.  K (here the rank) is 32 a
+// step.
 template <typename TO, int RT, int TM>
 __global__ void __launch_bounds__(256) lora_expand_kernel(LoraArgs p) {
   constexpr int KS = (RT + 1) / 2;                           // steps of 32 of the rank
@@ -196,34 +201,31 @@ __global__ void __launch_bounds__(256) lora_expand_kernel(LoraArgs p) {
   const bf16_t* B = p.b + (has ? (size_t)i * p.nout * p.rank : 0);
   const int n_end = min(p.nout, (int)(blockIdx.y + 1) * p.cols);
   for (int n0 = blockIdx.y * p.cols + 64 * wave; n0 < n_end; n0 += 256) {
-    // tile t, MFMA row m: column n0 + 16 (m / 4) + 4 t + m % 4, so that lane group g holds columns n0 + 16 g ..
+    Out8<TO> old[TM / 16][2];
+#pragma unroll
+    for (int rt = 0; rt < TM / 16; ++rt)
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const int rr = 16 * rt + col, n = n0 + 32 * q + 8 * grp;
+        old[rt][q] = base && rr < rows && n < p.nout ? load_out8(base + (r0 + rr) * p.base_row + n) : Out8<TO>{};
+      }
+    // tile t = 2 q + h, MFMA row m: column n0 + 32 q + 8 (m / 4) + 4 h + m % 4, so that lane group g holds 32 q + 8 g ..
     Frag8 bf[KS][4];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        const int n = n0 + 16 * (col >> 2) + 4 * t + (col & 3), k = 32 * ks + 8 * grp;
+        const int n = n0 + 32 * (t >> 1) + 8 * (col >> 2) + 4 * (t & 1) + (col & 3), k = 32 * ks + 8 * grp;
         bf[ks][t] = has && n < p.nout && k < p.rank ? *reinterpret_cast<const Frag8*>(B + (size_t)n * p.rank + k) : zero_frag();
       }
 #pragma unroll
     for (int rt = 0; rt < TM / 16; ++rt) {
       if (16 * rt >= rows) break;
       const int rr = 16 * rt + col;
-      const long at = (r0 + rr);
-      const int n = n0 + 16 * grp;
-      float y[16];
-      if (rr < rows && base) {
+      f32x4 acc[4];
 #pragma unroll
-        for (int q = 0; q < 2; ++q)
-          if (n + 8 * q < p.nout) load_out8(base + at * p.base_row + n + 8 * q, y + 8 * q);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) y[e] = 0.f;
-      }
+      for (int t = 0; t < 4; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
       if (has) {
-        f32x4 acc[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
           Frag8 h[NH];
@@ -234,15 +236,18 @@ __global__ void __launch_bounds__(256) lora_expand_kernel(LoraArgs p) {
 #pragma unroll
             for (int q = 0; q < NH; ++q) acc[t] = mfma16(bf[ks][t], h[q], acc[t]);
         }
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) y[4 * t + e] += acc[t][e];
       }
-      if (rr < rows) {
+      if (rr >= rows) continue;
 #pragma unroll
-        for (int q = 0; q < 2; ++q)
-          if (n + 8 * q < p.nout) store_out8(out + at * p.out_row + n + 8 * q, y + 8 * q);
+      for (int q = 0; q < 2; ++q) {
+        const int n = n0 + 32 * q + 8 * grp;
+        if (n >= p.nout) continue;
+        float y[8];
+        unpack_out8(old[rt][q], y);
+        if (has)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] += acc[2 * q + (e >> 2)][e & 3];
+        store_out8(out + (r0 + rr) * p.out_row + n, y);
       }
     }
   }

@@ -145,23 +145,12 @@ __global__ void __launch_bounds__(PLAN) pages_fork_kernel(PagesArgs p) {
     asked += total;
   }
   const int found = free_blocks(p.refs, p.num_blocks, min(asked, p.num_blocks), p.list);
-  for (int i = wave; i < p.n; i += PLAN / 64) {
+  for (int i = threadIdx.x; i < p.n; i += PLAN) {
     const int want = p.want[i], rank = p.rank[i];
     const bool ok = want == 0 || (want == 1 && rank < found);
     int from = -1, to = -1;
-    if (ok) {
-      const int full = p.lens[i] / PAGE;
-      const int* theirs = p.tables + (long)p.src[i] * p.max_blocks;
-      int* mine = p.tables + (long)p.dst[i] * p.max_blocks;
-      if (want) from = theirs[full], to = p.list[rank];
-      for (int e = lane; e < p.max_blocks; e += 64) {
-        const int block = e < full ? theirs[e] : e == full ? to : -1;
-        mine[e] = block;
-        if (e < full) atomicAdd(p.refs + block, 1);
-      }
-      if (lane == 0 && want) atomicAdd(p.refs + to, 1 - p.refs[to]);
-    }
-    if (lane == 0) p.done[i] = ok, p.from[i] = from, p.to[i] = to;
+    if (ok && want) from = p.tables[(long)p.src[i] * p.max_blocks + p.lens[i] / PAGE], to = p.list[rank];
+    p.done[i] = ok, p.from[i] = from, p.to[i] = to;
   }
 }
 
@@ -216,7 +205,7 @@ __global__ void __launch_bounds__(PLAN) pages_compact_kernel(PagesArgs p) {
 }
 
 // ------------------------------------------------------------------ blocks moved, in every layer
-// Units (move, layer, K or V) are dealt to the workgroups; a lane has four 16-byte loads in flight.  Moves: from[i] to
+// Units (move, layer, K or V) are dealt to the workgroups; a lane has up to four 16-byte loads in flight.  Moves: from[i] to
 // to[i]; either outside its pool: none.
 NOVA_DEV void copy_bytes(const char* from, char* to, long bytes) {
   const u32x4* f = reinterpret_cast<const u32x4*>(from);
@@ -243,8 +232,29 @@ NOVA_DEV void copy_unit(const CopyArgs& p, long unit) {
   copy_bytes((const char*)(side ? p.src.v_exp : p.src.k_exp) + ((size_t)layer * p.src.num_blocks + from) * n,
              (char*)(side ? p.dst.v_exp : p.dst.k_exp) + ((size_t)layer * p.dst.num_blocks + to) * n, n);
 }
+// A fork's pages, with its tables and counts: behind the workgroups that copy there is one for each request's row.  (One
+// workgroup of the plan would add to 7000 counts of 32 branches of 3579 tokens in 12 us.)
+__global__ void __launch_bounds__(256) fork_move_kernel(CopyArgs p, PagesArgs g, int copiers) {
+  if (blockIdx.x >= (unsigned)copiers) {
+    const int i = blockIdx.x - copiers;
+    if (!g.done[i]) return;
+    const int full = g.lens[i] / PAGE, to = g.to[i];
+    const int* theirs = g.tables + (long)g.src[i] * g.max_blocks;
+    int* mine = g.tables + (long)g.dst[i] * g.max_blocks;
+    for (int e = threadIdx.x; e < g.max_blocks; e += 256) {
+      const int block = e < full ? theirs[e] : e == full ? to : -1;
+      mine[e] = block;
+      if (e < full) atomicAdd(g.refs + block, 1);
+    }
+    if (threadIdx.x == 0 && to >= 0) atomicExch(g.refs + to, 1);
+    return;
+  }
+  const long units = 2l * p.layers * p.n;
+  for (long u = blockIdx.x; u < units; u += copiers) copy_unit(p, u);
+}
+
 __global__ void __launch_bounds__(256) copy_pages_kernel(CopyArgs p) {
-  const long units = 2l * p.layers * (p.moves ? *p.moves : p.n);
+  const long units = 2l * p.layers * p.n;
   for (long u = blockIdx.x; u < units; u += gridDim.x) copy_unit(p, u);
 }
 
@@ -355,6 +365,11 @@ static unsigned copy_grid(long units, int cus) { return (unsigned)std::max(1l, s
 hipError_t copy_pages(const CopyArgs& p, int cus, hipStream_t s) {
   if (p.n <= 0) return hipSuccess;
   hipLaunchKernelGGL(copy_pages_kernel, dim3(copy_grid(2l * p.layers * p.n, cus)), dim3(256), 0, s, p);
+  return hipGetLastError();
+}
+hipError_t fork_move(const CopyArgs& p, const PagesArgs& g, int cus, hipStream_t s) {
+  const int copiers = (int)copy_grid(2l * p.layers * p.n, cus);
+  hipLaunchKernelGGL(fork_move_kernel, dim3(copiers + g.n), dim3(256), 0, s, p, g, copiers);
   return hipGetLastError();
 }
 hipError_t compact_move(const CopyArgs& p, const PagesArgs& g, int cus, hipStream_t s) {

@@ -307,6 +307,7 @@ struct CopyArgs {
   int n; const int* moves;                              // moves: how many, on the device (null: n)
 };
 hipError_t copy_pages(const CopyArgs& p, int cus, hipStream_t s);
+hipError_t fork_move(const CopyArgs& p, const PagesArgs& g, int cus, hipStream_t s);
 hipError_t compact_move(const CopyArgs& p, const PagesArgs& g, int cus, hipStream_t s);
 struct KeepArgs {
   CachePool c; int layers;

@@ -1188,7 +1188,7 @@ extern "C" int nova_pages_fork(const nova_pages* pages, const nova_cache* cache,
   c.from = a.from, c.to = a.to, c.n = n;
   hipStream_t s = (hipStream_t)stream;
   CALL(NOVA_KIND_MISC, s, nova::pages_fork(a, s));
-  CALL(NOVA_KIND_MISC, s, nova::copy_pages(c, device_cus(), s));
+  CALL(NOVA_KIND_MISC, s, nova::fork_move(c, a, device_cus(), s));
   return NOVA_OK;
 }
 
