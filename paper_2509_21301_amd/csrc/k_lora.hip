@@ -1,7 +1,8 @@
 // Low-rank adapters of many requests beside a projection that they share: with i the adapter of a row's sequence,
 //   out = base + s_i B_i (A_i x),   A_i [rank][K], B_i [N][rank].
 //  * shrink: h = A_i x per row, tiles of a sequence's rows times a slice of K, fp32 partials [slice][row][rank];
-//  * expand: the slices summed in order, times s_i, then B_i h onto base, rounded once.
+//  * join (long sequences): the slices summed in order, as the operands that expand takes;
+//  * expand: B_i h, times s_i, onto base, rounded once.  Short tiles sum the slices themselves (a launch less).
 // The ranks are far below what would make this compute-bound: it is bound by reading x, base and the adapters and by
 // writing out.  The matrix cores take bf16, so h goes to them as a sum of bf16 parts, an MFMA each: two (a relative error
 // of 2^-16 instead of a bf16 rounding's 2^-8) where out is bf16, three (all 24 bits) where it is fp32.  x in fp32 likewise.
@@ -11,8 +12,13 @@
 
 namespace nova {
 
-constexpr int LO_ROWS = 64;                // rows of a tile of long sequences
-constexpr int LO_STEP = 16;                // of a tile of short ones
+constexpr int LO_STEP = 16;                // rows of a tile of short sequences; long ones have 64 or 128
+
+// Orders a wave's own LDS writes before its own LDS reads.
+NOVA_DEV void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
 
 // The tile-th tile of `rows` rows of the batch's sequences, counted over them: its sequence (-1: none) and first row.
 template <int TM> NOVA_DEV SeqRows find_row_tile(const BatchRows& p, int tile, int* b, int* row) {
@@ -60,74 +66,186 @@ template <int N> NOVA_DEV void split_parts(float* x, Frag8* f) {
       x[2 * i + 1] = rest_of(x[2 * i + 1], __uint_as_float(f[n].w[i] & 0xFFFF0000u));
     }
 }
-// Eight elements of x as N operands (of bf16 there is one).
-template <int N> NOVA_DEV void load_x(const bf16_t* p, Frag8* f) { f[0] = *reinterpret_cast<const Frag8*>(p); }
-template <int N> NOVA_DEV void load_x(const float* p, Frag8* f) {
+// Eight elements of x as loaded, and as N operands.
+template <typename T> struct Raw;
+template <> struct Raw<bf16_t> { Frag8 f; };
+template <> struct Raw<float> { f32x4 a, b; };
+NOVA_DEV Raw<bf16_t> load_raw_x(const bf16_t* p) { return {*reinterpret_cast<const Frag8*>(p)}; }
+NOVA_DEV Raw<float> load_raw_x(const float* p) { return {reinterpret_cast<const f32x4*>(p)[0], reinterpret_cast<const f32x4*>(p)[1]}; }
+template <int N> NOVA_DEV void split_raw(const Raw<bf16_t>& r, Frag8* f) { f[0] = r.f; }
+template <int N> NOVA_DEV void split_raw(const Raw<float>& r, Frag8* f) {
   float x[8];
-  *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(p);
-  *reinterpret_cast<float4*>(x + 4) = *reinterpret_cast<const float4*>(p + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = r.a[i], x[4 + i] = r.b[i];
   split_parts<N>(x, f);
 }
 
-// ------------------------------------------------------------------ h = A x
-// Workgroup: (tile of TM rows, slice of K).  Lane (row or rank column = lane % 16, k group = lane / 16) loads 16 bytes
-// of its row of x and of A per 32 k.  TM = 16: the waves take the k steps in turn and their sums are joined in LDS;
-// TM = 64: each wave has 16 rows of its own.
-template <typename TX, int NX, int RT, int TM>
+// ------------------------------------------------------------------ h = A x, short sequences
+// Workgroup: (tile of 16 rows, slice of K); its waves take the k steps in turn and their sums are joined in LDS.  Lane (row
+// or rank column = lane % 16, k group = lane / 16) loads 16 bytes of its row of x and of A per 32 k.
+template <typename TX, int NX, int RT>
 __global__ void __launch_bounds__(256) lora_shrink_kernel(LoraArgs p) {
-  constexpr bool ROWS4 = TM == LO_ROWS;
-  __shared__ float sm[ROWS4 ? 1 : 4][ROWS4 ? 1 : 16][16 * RT + 1];
+  constexpr int AHEAD = RT * NX >= 8 ? 2 : 4;                // steps whose loads are requested together
+  __shared__ float sm[4][16][16 * RT + 1];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
+  int b, row0;
+  const SeqRows sr = find_row_tile<LO_STEP>(p.r, blockIdx.x, &b, &row0);
+  if (b < 0) return;
+  const int i = p.which[b];
+  if ((unsigned)i >= (unsigned)p.n) return;
+  const int k0 = blockIdx.y * p.kslice, k1 = min(p.k, k0 + p.kslice);
+  const bf16_t* A = p.a + (size_t)i * p.rank * p.k;
+  // Rows behind the tile's last and ranks behind the adapter's repeat the last one: what comes of them is not stored.
+  const TX* x = reinterpret_cast<const TX*>(p.x) + (long)(sr.r0 + min(row0 + col, sr.n - 1)) * p.x_row;
+  const bf16_t* ar[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) ar[t] = A + (size_t)min(16 * t + col, p.rank - 1) * p.k;
+  f32x4 acc[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto step = [&](int kk, bool whole) {                      // k kk .. kk + 31, of which those below k1
+    const int k = kk + 8 * grp;
+    const bool in = whole || k < k1;
+    const int at = in ? k : 0;
+    Frag8 f[NX], a[RT];
+    split_raw<NX>(load_raw_x(x + at), f);
+#pragma unroll
+    for (int t = 0; t < RT; ++t) a[t] = *reinterpret_cast<const Frag8*>(ar[t] + at);
+    if (!whole) {
+#pragma unroll
+      for (int n = 0; n < NX; ++n) f[n] = in ? f[n] : zero_frag();
+#pragma unroll
+      for (int t = 0; t < RT; ++t) a[t] = in ? a[t] : zero_frag();
+    }
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int n = 0; n < NX; ++n) acc[t] = mfma16(f[n], a[t], acc[t]);
+  };
+  int kk = k0 + 32 * wave;
+#pragma unroll AHEAD
+  for (; kk + 32 <= k1; kk += 128) step(kk, true);
+  if (kk < k1) step(kk, false);
+  // acc[t][e]: row 4 grp + e, rank column 16 t + col
+#pragma unroll
+  for (int t = 0; t < RT; ++t)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sm[wave][4 * grp + e][16 * t + col] = acc[t][e];
+  __syncthreads();
+  float* h = p.part + ((size_t)blockIdx.y * p.r.rows + sr.r0 + row0) * p.rank;
+  for (int w = threadIdx.x; w < 16 * 16 * RT; w += 256) {
+    const int rr = w / (16 * RT), c = w % (16 * RT);
+    if (row0 + rr < sr.n && c < p.rank) h[(size_t)rr * p.rank + c] = (sm[0][rr][c] + sm[1][rr][c]) + (sm[2][rr][c] + sm[3][rr][c]);
+  }
+}
+
+// ------------------------------------------------------------------ h = A x, long sequences
+// Workgroup: (tile of 64 RW rows, slice of K), RW blocks of 16 rows a wave.  64 of K at a time go through LDS, loaded a
+// step ahead: an MFMA operand has neighbouring lanes in different rows, and read straight from memory each of its 16 bytes
+// is an access of its own to the address unit (54 of 64 a load, busy for 78% of the time; 4500 rows of 3584 to rank 64
+// took 27 us).  16-byte chunks of a row are turned by its number (chunk c of row r at c ^ (r & 7)): no bank conflicts.
+template <typename TX, int NX, int RT, int RW>
+__global__ void __launch_bounds__(256) lora_down_kernel(LoraArgs p) {
+  constexpr int TM = 64 * RW, XC = TM * 8 / 256, AC = (16 * RT * 8 + 255) / 256;   // chunks of a thread: x, A
+  constexpr int NB = NX == 1 ? 2 : 1;                        // buffers; x in parts leaves room for one
+  __shared__ __align__(16) Frag8 sm_x[NB][NX][TM][8];
+  __shared__ __align__(16) Frag8 sm_a[NB][16 * RT][8];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
   int b, row0;
   const SeqRows sr = find_row_tile<TM>(p.r, blockIdx.x, &b, &row0);
   if (b < 0) return;
   const int i = p.which[b];
   if ((unsigned)i >= (unsigned)p.n) return;
-  if (ROWS4) row0 += 16 * wave;
   const int k0 = blockIdx.y * p.kslice, k1 = min(p.k, k0 + p.kslice);
+  // Rows behind the tile's last and ranks behind the adapter's repeat the last one: what comes of them is not stored.
+  const TX* x = reinterpret_cast<const TX*>(p.x) + (long)(sr.r0 + row0) * p.x_row;
   const bf16_t* A = p.a + (size_t)i * p.rank * p.k;
-  const TX* x = reinterpret_cast<const TX*>(p.x) + (sr.r0 + row0 + col) * p.x_row;
-  const bool live = row0 + col < sr.n;
-  f32x4 acc[RT];
+  const int rows = min(TM, sr.n - row0), chunk = threadIdx.x & 7, first = threadIdx.x >> 3;
+  Raw<TX> rx[XC];
+  Frag8 ra[AC];
+  auto request = [&](int kk) {
+    const int k = min(kk + 8 * chunk, k1 - 8);
 #pragma unroll
-  for (int t = 0; t < RT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (row0 < sr.n) {
-    constexpr int STEP = ROWS4 ? 32 : 128;
-#pragma unroll 2
-    for (int kk = k0 + (ROWS4 ? 0 : 32 * wave); kk < k1; kk += STEP) {
-      const int k = kk + 8 * grp;
-      const bool in = k < k1;
-      Frag8 f[NX], a[RT];
+    for (int j = 0; j < XC; ++j) rx[j] = load_raw_x(x + (long)min(first + 32 * j, rows - 1) * p.x_row + k);
 #pragma unroll
-      for (int n = 0; n < NX; ++n) f[n] = zero_frag();
-      if (in && live) load_x<NX>(x + k, f);
+    for (int j = 0; j < AC; ++j) ra[j] = *reinterpret_cast<const Frag8*>(A + (size_t)min(first + 32 * j, p.rank - 1) * p.k + k);
+  };
+  auto keep = [&](int kk, int buf) {
+    const bool in = kk + 8 * chunk < k1;                     // what lies behind the slice is zero
 #pragma unroll
-      for (int t = 0; t < RT; ++t)
-        a[t] = in && 16 * t + col < p.rank ? *reinterpret_cast<const Frag8*>(A + (size_t)(16 * t + col) * p.k + k) : zero_frag();
+    for (int j = 0; j < XC; ++j) {
+      const int r = first + 32 * j;
+      Frag8 f[NX];
+      split_raw<NX>(rx[j], f);
 #pragma unroll
-      for (int t = 0; t < RT; ++t)
+      for (int n = 0; n < NX; ++n) sm_x[buf][n][r][chunk ^ (r & 7)] = in ? f[n] : zero_frag();
+    }
 #pragma unroll
-        for (int n = 0; n < NX; ++n) acc[t] = mfma16(f[n], a[t], acc[t]);
+    for (int j = 0; j < AC; ++j) {
+      const int r = first + 32 * j;
+      if (16 * RT % 32 == 0 || r < 16 * RT) sm_a[buf][r][chunk ^ (r & 7)] = in ? ra[j] : zero_frag();
+    }
+  };
+  f32x4 acc[RW][RT];
+#pragma unroll
+  for (int w = 0; w < RW; ++w)
+#pragma unroll
+    for (int t = 0; t < RT; ++t) acc[w][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (k0 < k1) request(k0);
+  for (int kk = k0, buf = 0; kk < k1; kk += 64, buf ^= NB - 1) {
+    if (NB == 1 && kk > k0) __syncthreads();
+    keep(kk, buf);
+    if (kk + 64 < k1) request(kk + 64);
+    __syncthreads();                       // of two buffers a wave one step ahead writes the other
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      Frag8 a[RT];
+#pragma unroll
+      for (int t = 0; t < RT; ++t) a[t] = sm_a[buf][16 * t + col][(4 * s + grp) ^ (col & 7)];
+#pragma unroll
+      for (int w = 0; w < RW; ++w)
+#pragma unroll
+        for (int n = 0; n < NX; ++n) {
+          const Frag8 f = sm_x[buf][n][16 * (RW * wave + w) + col][(4 * s + grp) ^ (col & 7)];
+#pragma unroll
+          for (int t = 0; t < RT; ++t) acc[w][t] = mfma16(f, a[t], acc[w][t]);
+        }
     }
   }
-  // acc[t][e]: row 4 grp + e, rank column 16 t + col
+  // acc[w][t][e]: row 16 (RW wave + w) + 4 grp + e, rank column 16 t + col
   float* h = p.part + ((size_t)blockIdx.y * p.r.rows + sr.r0 + row0) * p.rank;
-  if constexpr (ROWS4) {
 #pragma unroll
-    for (int t = 0; t < RT; ++t)
+  for (int w = 0; w < RW; ++w)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (row0 + 4 * grp + e < sr.n && 16 * t + col < p.rank) h[(size_t)(4 * grp + e) * p.rank + 16 * t + col] = acc[t][e];
-  } else {
+    for (int e = 0; e < 4; ++e) {
+      const int r = 16 * (RW * wave + w) + 4 * grp + e;
 #pragma unroll
-    for (int t = 0; t < RT; ++t)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sm[wave][4 * grp + e][16 * t + col] = acc[t][e];
-    __syncthreads();
-    for (int w = threadIdx.x; w < 16 * 16 * RT; w += 256) {
-      const int rr = w / (16 * RT), c = w % (16 * RT);
-      if (row0 + rr < sr.n && c < p.rank) h[(size_t)rr * p.rank + c] = (sm[0][rr][c] + sm[1][rr][c]) + (sm[2][rr][c] + sm[3][rr][c]);
+      for (int t = 0; t < RT; ++t)
+        if (r < rows && 16 * t + col < p.rank) h[(size_t)r * p.rank + 16 * t + col] = acc[w][t][e];
     }
+}
+
+// ------------------------------------------------------------------ h joined
+// Thread: four ranks of a row, as the expand's operands [part][row][32 KS], zeros behind the rank.  Rows without an adapter
+// (whose partials nobody wrote) give what nobody reads.
+template <int KS, int NH>
+__global__ void __launch_bounds__(256) lora_join_kernel(LoraArgs p) {
+  const long i = (long)blockIdx.x * 256 + threadIdx.x, row = i / (8 * KS);
+  const int c = (int)(i % (8 * KS)) * 4;
+  if (row >= p.r.rows) return;
+  f32x4 h{0.f, 0.f, 0.f, 0.f};
+  if (c < p.rank) {
+#pragma unroll 4
+    for (int s = 0; s < p.slices; ++s) h += *reinterpret_cast<const f32x4*>(p.part + ((size_t)s * p.r.rows + row) * p.rank + c);
+  }
+#pragma unroll
+  for (int n = 0; n < NH; ++n) {
+    const uint2 w = make_uint2(pack2(h[0], h[1]), pack2(h[2], h[3]));
+    *reinterpret_cast<uint2*>(p.parts + ((size_t)n * p.r.rows + row) * (32 * KS) + c) = w;
+    h[0] = rest_of(h[0], __uint_as_float(w.x << 16));
+    h[1] = rest_of(h[1], __uint_as_float(w.x & 0xFFFF0000u));
+    h[2] = rest_of(h[2], __uint_as_float(w.y << 16));
+    h[3] = rest_of(h[3], __uint_as_float(w.y & 0xFFFF0000u));
   }
 }
 
@@ -161,34 +279,35 @@ template <typename T> NOVA_DEV void store_out8(T* p, const float* x) {
   }
 }
 
-// Workgroup: (tile of TM rows, `cols` columns); a wave takes 64 columns at a time.  Which column of B is which MFMA row
-// is free, so two tiles give a lane 8 consecutive columns of its row of out, and the four lane groups 32: 64 bytes of a
-// row side by side in one instruction.  The rows of base of all row tiles are requested before the first product.  K (here the rank) is 32 a
-// step.
-template <typename TO, int RT, int TM>
+// ---- short sequences
+// Workgroup: (tile of 16 rows, `cols` columns); a wave takes 64 columns at a time.  Which column of B is which MFMA row
+// is free, so two tiles give a lane 8 consecutive columns of its row of out, and the four lane groups 32.  K (here the
+// rank) is 32 a step.
+template <typename TO, int RT>
 __global__ void __launch_bounds__(256) lora_expand_kernel(LoraArgs p) {
   constexpr int KS = (RT + 1) / 2;                           // steps of 32 of the rank
   constexpr int LD = 32 * KS + 8;                            // row pitch in LDS (16 bytes more: rows on other banks)
   constexpr int NH = sizeof(TO) == 4 ? 3 : 2;                // parts of h
-  __shared__ __align__(16) bf16_t sm[NH][TM][LD];
+  __shared__ __align__(16) bf16_t sm[NH][LO_STEP][LD];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
   int b, row0;
-  const SeqRows sr = find_row_tile<TM>(p.r, blockIdx.x, &b, &row0);
+  const SeqRows sr = find_row_tile<LO_STEP>(p.r, blockIdx.x, &b, &row0);
   if (b < 0) return;
-  const int i = p.which[b], rows = min(TM, sr.n - row0);
+  const int i = p.which[b], rows = min(LO_STEP, sr.n - row0);
   const bool has = (unsigned)i < (unsigned)p.n;
   const long r0 = sr.r0 + row0;
   const TO* base = reinterpret_cast<const TO*>(p.base);
   TO* out = reinterpret_cast<TO*>(p.out);
   if (!has && base == out) return;                           // nothing is added
+  const float scale = has && p.scale ? p.scale[i] : 1.f;
   if (has) {
-    const float scale = p.scale ? p.scale[i] : 1.f;
-    for (int w = threadIdx.x; w < TM * 32 * KS; w += 256) {
+    for (int w = threadIdx.x; w < LO_STEP * 32 * KS; w += 256) {
       const int rr = w / (32 * KS), c = w % (32 * KS);
       float h = 0.f;
-      if (rr < rows && c < p.rank)
+      if (rr < rows && c < p.rank) {
+#pragma unroll 8
         for (int s = 0; s < p.slices; ++s) h += p.part[((size_t)s * p.r.rows + r0 + rr) * p.rank + c];
-      h *= scale;
+      }
 #pragma unroll
       for (int n = 0; n < NH; ++n) {
         const bf16_t part = f2bf(h);
@@ -201,101 +320,262 @@ __global__ void __launch_bounds__(256) lora_expand_kernel(LoraArgs p) {
   const bf16_t* B = p.b + (has ? (size_t)i * p.nout * p.rank : 0);
   const int n_end = min(p.nout, (int)(blockIdx.y + 1) * p.cols);
   for (int n0 = blockIdx.y * p.cols + 64 * wave; n0 < n_end; n0 += 256) {
-    Out8<TO> old[TM / 16][2];
+    // Rows behind the tile's last and columns behind the last repeat what is there: nothing of them is stored.
+    Out8<TO> old[2];
+    if (base) {
 #pragma unroll
-    for (int rt = 0; rt < TM / 16; ++rt)
+      for (int q = 0; q < 2; ++q) old[q] = load_out8(base + (r0 + min(col, rows - 1)) * p.base_row + min(n0 + 32 * q + 8 * grp, p.nout - 8));
+    } else {
+      old[0] = old[1] = Out8<TO>{};
+    }
+    f32x4 acc[4];
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const int rr = 16 * rt + col, n = n0 + 32 * q + 8 * grp;
-        old[rt][q] = base && rr < rows && n < p.nout ? load_out8(base + (r0 + rr) * p.base_row + n) : Out8<TO>{};
-      }
-    // tile t = 2 q + h, MFMA row m: column n0 + 32 q + 8 (m / 4) + 4 h + m % 4, so that lane group g holds 32 q + 8 g ..
-    Frag8 bf[KS][4];
+    for (int t = 0; t < 4; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (has) {
+      // tile t = 2 q + h, MFMA row m: column n0 + 32 q + 8 (m / 4) + 4 h + m % 4, so that lane group g holds 32 q + 8 g ..
+      Frag8 bf[KS][4];
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const int n = n0 + 32 * (t >> 1) + 8 * (col >> 2) + 4 * (t & 1) + (col & 3), k = 32 * ks + 8 * grp;
+          const Frag8 w = *reinterpret_cast<const Frag8*>(B + (size_t)min(n, p.nout - 1) * p.rank + min(k, p.rank - 8));
+          bf[ks][t] = k < p.rank ? w : zero_frag();
+        }
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int q = 0; q < NH; ++q) {
+          const Frag8 h = *reinterpret_cast<const Frag8*>(&sm[q][col][32 * ks + 8 * grp]);
+#pragma unroll
+          for (int t = 0; t < 4; ++t) acc[t] = mfma16(bf[ks][t], h, acc[t]);
+        }
+    }
+    if (col >= rows) continue;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int n = n0 + 32 * q + 8 * grp;
+      if (n >= p.nout) continue;
+      float y[8];
+      unpack_out8(old[q], y);
+      if (has)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] += scale * acc[2 * q + (e >> 2)][e & 3];
+      store_out8(out + (r0 + col) * p.out_row + n, y);
+    }
+  }
+}
+
+// ---- long sequences
+// 16 bytes of base as loaded, and as floats.
+template <typename T> NOVA_DEV void unpack16(const u32x4& w, float* x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      x[i] = __uint_as_float(w[i]);
+    } else {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  }
+}
+template <typename T> NOVA_DEV u32x4 pack16(const float* x) {
+  u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = sizeof(T) == 4 ? __float_as_uint(x[i]) : pack2(x[2 * i], x[2 * i + 1]);
+  return w;
+}
+
+// Workgroup: (tile of 64 RW rows, `cols` columns), RW blocks of 16 rows a wave, whose h stays in registers.  64 columns of
+// B at a time go through LDS for all four waves, loaded a step ahead (turned as in the kernel above), and what they give
+// goes back through LDS, so that base and out are read and written in runs of a row's 64 columns: see there.
+template <typename TO, int RT, int RW>
+__global__ void __launch_bounds__(256) lora_up_kernel(LoraArgs p) {
+  constexpr int KS = (RT + 1) / 2, TM = 64 * RW;
+  constexpr int NH = sizeof(TO) == 4 ? 3 : 2;
+  constexpr int CH = 2 * RT, BC = 64 * CH / 256 > 0 ? 64 * CH / 256 : 1;   // chunks of a column of B; of a thread
+  constexpr int E = 16 / sizeof(TO), LPR = 64 / E, RPI = 64 / LPR, IT = 16 / RPI;   // of out: elements and lanes of a row, rows of an instruction
+  constexpr int LD = 68;                                     // floats of a row in LDS
+  __shared__ __align__(16) Frag8 sm_b[2][64][CH];
+  __shared__ __align__(16) float sm_o[4][16][LD];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
+  int b, row0;
+  const SeqRows sr = find_row_tile<TM>(p.r, blockIdx.x, &b, &row0);
+  if (b < 0) return;
+  const int i = p.which[b], rows = min(TM, sr.n - row0);
+  const bool has = (unsigned)i < (unsigned)p.n;
+  const long r0 = sr.r0 + row0;
+  const TO* base = reinterpret_cast<const TO*>(p.base);
+  TO* out = reinterpret_cast<TO*>(p.out);
+  if (!has && base == out) return;                           // nothing is added
+  const float scale = has && p.scale ? p.scale[i] : 1.f;
+  const bf16_t* B = p.b + (has ? (size_t)i * p.nout * p.rank : 0);
+  Frag8 h[RW][KS][NH];
+#pragma unroll
+  for (int w = 0; w < RW; ++w)
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const int n = n0 + 32 * (t >> 1) + 8 * (col >> 2) + 4 * (t & 1) + (col & 3), k = 32 * ks + 8 * grp;
-        bf[ks][t] = has && n < p.nout && k < p.rank ? *reinterpret_cast<const Frag8*>(B + (size_t)n * p.rank + k) : zero_frag();
+      for (int n = 0; n < NH; ++n)
+        h[w][ks][n] = has ? *reinterpret_cast<const Frag8*>(p.parts + ((size_t)n * p.r.rows + r0 + min(16 * (RW * wave + w) + col, rows - 1)) * (32 * KS) + 32 * ks + 8 * grp)
+                          : zero_frag();
+  // Chunk c of column n lies so that eight neighbouring columns' chunks are on different banks, whatever a column's size.
+  auto turn = [](int n, int c) { return CH >= 8 ? c ^ (n & 7) : CH == 4 ? c ^ ((n >> 1) & 3) : c ^ ((n >> 2) & 1); };
+  const int bn = threadIdx.x / CH, bc = threadIdx.x % CH;    // the thread's first column and chunk
+  Frag8 rb[BC];
+  u32x4 old[RW][IT], next[RW][IT];
+  const int orow = lane / LPR, ocol = lane % LPR * E;        // of an instruction
+  auto request = [&](int n0) {
+    if (has) {
+#pragma unroll
+      for (int j = 0; j < BC; ++j) {
+        const int n = bn + 256 / CH * j;
+        rb[j] = *reinterpret_cast<const Frag8*>(B + (size_t)min(n0 + n, p.nout - 1) * p.rank + min(8 * bc, p.rank - 8));
       }
+    }
+    if (base) {
 #pragma unroll
-    for (int rt = 0; rt < TM / 16; ++rt) {
-      if (16 * rt >= rows) break;
-      const int rr = 16 * rt + col;
-      f32x4 acc[4];
+      for (int w = 0; w < RW; ++w)
 #pragma unroll
-      for (int t = 0; t < 4; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (has) {
+        for (int j = 0; j < IT; ++j)
+          next[w][j] = *reinterpret_cast<const u32x4*>(base + (r0 + min(16 * (RW * wave + w) + RPI * j + orow, rows - 1)) * p.base_row + min(n0 + ocol, p.nout - E));
+    } else {
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          Frag8 h[NH];
+      for (int w = 0; w < RW; ++w)
 #pragma unroll
-          for (int q = 0; q < NH; ++q) h[q] = *reinterpret_cast<const Frag8*>(&sm[q][rr][32 * ks + 8 * grp]);
+        for (int j = 0; j < IT; ++j) next[w][j] = u32x4{0u, 0u, 0u, 0u};
+    }
+  };
+  const int n_begin = blockIdx.y * p.cols, n_end = min(p.nout, n_begin + p.cols);
+  request(n_begin);
+  for (int n0 = n_begin, buf = 0; n0 < n_end; n0 += 64, buf ^= 1) {
+    if (has && (64 * CH >= 256 || threadIdx.x < 64 * CH)) {
 #pragma unroll
-          for (int t = 0; t < 4; ++t)
+      for (int j = 0; j < BC; ++j) {
+        const int n = bn + 256 / CH * j;
+        sm_b[buf][n][turn(n, bc)] = 8 * bc < p.rank ? rb[j] : zero_frag();
+      }
+    }
 #pragma unroll
-            for (int q = 0; q < NH; ++q) acc[t] = mfma16(bf[ks][t], h[q], acc[t]);
+    for (int w = 0; w < RW; ++w)
+#pragma unroll
+      for (int j = 0; j < IT; ++j) old[w][j] = next[w][j];
+    if (n0 + 64 < n_end) request(n0 + 64);
+    __syncthreads();                       // a wave one step ahead writes the other buffer
+    f32x4 acc[RW][4];
+#pragma unroll
+    for (int w = 0; w < RW; ++w)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) acc[w][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (has) {
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const int n = 16 * t + col, c = 4 * ks + grp;
+          const Frag8 f = CH >= 4 || grp < 2 ? sm_b[buf][n][turn(n, CH >= 4 ? c : c & 1)] : zero_frag();
+#pragma unroll
+          for (int w = 0; w < RW; ++w)
+#pragma unroll
+            for (int q = 0; q < NH; ++q) acc[w][t] = mfma16(f, h[w][ks][q], acc[w][t]);
         }
-      }
-      if (rr >= rows) continue;
+    }
+    // acc[w][t][e]: row 16 (RW wave + w) + col, column 16 t + 4 grp + e
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const int n = n0 + 32 * q + 8 * grp;
-        if (n >= p.nout) continue;
-        float y[8];
-        unpack_out8(old[rt][q], y);
+    for (int w = 0; w < RW; ++w) {
+      if (16 * (RW * wave + w) >= rows) break;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4*>(&sm_o[wave][col][16 * t + 4 * grp]) = acc[w][t];
+      wave_fence();
+#pragma unroll
+      for (int j = 0; j < IT; ++j) {
+        const int rr = RPI * j + orow, r = 16 * (RW * wave + w) + rr;
+        float y[E];
+        unpack16<TO>(old[w][j], y);
         if (has)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] += acc[2 * q + (e >> 2)][e & 3];
-        store_out8(out + (r0 + rr) * p.out_row + n, y);
+          for (int e = 0; e < E; e += 4) {
+            const f32x4 d = *reinterpret_cast<const f32x4*>(&sm_o[wave][rr][ocol + e]);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) y[e + x] += scale * d[x];
+          }
+        if (r < rows && n0 + ocol < p.nout) *reinterpret_cast<u32x4*>(out + (r0 + r) * p.out_row + n0 + ocol) = pack16<TO>(y);
       }
+      wave_fence();
     }
   }
 }
 
 // ------------------------------------------------------------------ launch
-// Tiles of 64 rows where the sequences have that many on average, else of 16.
-static bool lora_long(const LoraArgs& p) { return p.r.rows >= LO_ROWS / 2 * (long)p.r.batch; }
+// Blocks of 16 rows a wave of the kernels for long sequences takes (0: those for short ones): by the rows that a sequence
+// has on average.
+static int lora_blocks(const LoraArgs& p) {
+  const long rows = p.r.rows, batch = p.r.batch;
+  return rows >= 128 * batch ? 2 : rows >= 32 * batch ? 1 : 0;
+}
 static long lora_tiles(const LoraArgs& p) {
-  const int tm = lora_long(p) ? LO_ROWS : LO_STEP;
+  const int rw = lora_blocks(p), tm = rw ? 64 * rw : LO_STEP;
   return std::min<long>(p.r.rows, p.r.rows / tm + p.r.batch);
 }
-// Slices of K: two workgroups for each compute unit, each of at least 512 of K.
-int lora_slices(const LoraArgs& p, int cus) {
-  const long want = (2l * cus + lora_tiles(p) - 1) / std::max(1l, lora_tiles(p));
-  return (int)std::max(1l, std::min<long>(want, (p.k + 511) / 512));
+// Slices of K: four workgroups for each compute unit, each of at least 256 of K where h is joined, 512 where every
+// workgroup of the expand sums the slices.
+static int lora_slices(const LoraArgs& p, int cus) {
+  const long tiles = std::max(1l, lora_tiles(p)), want = (4l * cus + tiles - 1) / tiles, least = lora_blocks(p) ? 256 : 512;
+  return (int)std::max(1l, std::min<long>(want, (p.k + least - 1) / least));
+}
+static size_t parts_at(const LoraArgs& p, int slices) { return ((size_t)slices * p.r.rows * p.rank * sizeof(float) + 255) / 256 * 256; }
+size_t lora_bytes(const LoraArgs& p, int cus) {
+  // three parts (of an fp32 out) of the rank, rounded up to the widths that the kernels have
+  const int wide = p.rank <= 32 ? 32 : p.rank <= 64 ? 64 : 128;
+  return parts_at(p, lora_slices(p, cus)) + (lora_blocks(p) ? (size_t)3 * p.r.rows * wide * sizeof(bf16_t) : 0);
 }
 
-template <typename TX, typename TO, int RT, int TM>
+template <typename TX, typename TO, int RT, int RW>
 static hipError_t lora_launch(const LoraArgs& p, int cus, hipStream_t s) {
-  const unsigned tiles = (unsigned)lora_tiles(p);
   constexpr int NX = sizeof(TX) == 2 ? 1 : sizeof(TO) == 2 ? 2 : 3;
-  hipLaunchKernelGGL((lora_shrink_kernel<TX, NX, RT, TM>), dim3(tiles, p.slices), dim3(256), 0, s, p);
+  const unsigned tiles = (unsigned)lora_tiles(p);
+  const dim3 slices(tiles, p.slices);
+  if constexpr (RW == 0) {
+    hipLaunchKernelGGL((lora_shrink_kernel<TX, NX, RT>), slices, dim3(256), 0, s, p);
+  } else {
+    constexpr int KS = (RT + 1) / 2, NH = sizeof(TO) == 4 ? 3 : 2;
+    hipLaunchKernelGGL((lora_down_kernel<TX, NX, RT, RW>), slices, dim3(256), 0, s, p);
+    if (hipError_t e = hipGetLastError()) return e;
+    hipLaunchKernelGGL((lora_join_kernel<KS, NH>), dim3((unsigned)(((long)p.r.rows * 8 * KS + 255) / 256)), dim3(256), 0, s, p);
+  }
   if (hipError_t e = hipGetLastError()) return e;
-  // columns of a workgroup: eight workgroups for each compute unit, whole steps of 256
+  // columns of a workgroup: eight workgroups for each compute unit, whole steps
   LoraArgs q = p;
-  const long steps = (p.nout + 255) / 256, groups = std::min(steps, std::max(1l, 8l * cus / tiles));
-  q.cols = (int)((steps + groups - 1) / groups * 256);
-  hipLaunchKernelGGL((lora_expand_kernel<TO, RT, TM>), dim3(tiles, (p.nout + q.cols - 1) / q.cols), dim3(256), 0, s, q);
+  const int step = RW ? 64 : 256;
+  const long steps = (p.nout + step - 1) / step, groups = std::min(steps, std::max(1l, 8l * cus / tiles));
+  q.cols = (int)((steps + groups - 1) / groups * step);
+  const dim3 grid(tiles, (p.nout + q.cols - 1) / q.cols);
+  if constexpr (RW == 0) hipLaunchKernelGGL((lora_expand_kernel<TO, RT>), grid, dim3(256), 0, s, q);
+  else hipLaunchKernelGGL((lora_up_kernel<TO, RT, RW>), grid, dim3(256), 0, s, q);
   return hipGetLastError();
 }
-template <typename TX, typename TO, int TM>
+template <typename TX, typename TO, int RW>
 static hipError_t lora_rank(const LoraArgs& p, int cus, hipStream_t s) {
-  if (p.rank <= 16) return lora_launch<TX, TO, 1, TM>(p, cus, s);
-  if (p.rank <= 32) return lora_launch<TX, TO, 2, TM>(p, cus, s);
-  if (p.rank <= 64) return lora_launch<TX, TO, 4, TM>(p, cus, s);
-  return lora_launch<TX, TO, 8, TM>(p, cus, s);
+  if (p.rank <= 16) return lora_launch<TX, TO, 1, RW>(p, cus, s);
+  if (p.rank <= 32) return lora_launch<TX, TO, 2, RW>(p, cus, s);
+  if (p.rank <= 64) return lora_launch<TX, TO, 4, RW>(p, cus, s);
+  return lora_launch<TX, TO, 8, RW>(p, cus, s);
 }
 template <typename TX, typename TO>
 static hipError_t lora_types(const LoraArgs& p, int cus, hipStream_t s) {
-  return lora_long(p) ? lora_rank<TX, TO, LO_ROWS>(p, cus, s) : lora_rank<TX, TO, LO_STEP>(p, cus, s);
+  switch (lora_blocks(p)) {
+    case 0: return lora_rank<TX, TO, 0>(p, cus, s);
+    case 1: return lora_rank<TX, TO, 1>(p, cus, s);
+    default: return lora_rank<TX, TO, 2>(p, cus, s);
+  }
 }
 hipError_t lora(const LoraArgs& p, int cus, hipStream_t s) {
   if (p.r.rows <= 0) return hipSuccess;
   if (p.rank <= 0 || p.rank > 128 || p.rank % 8 || p.k % 8 || p.nout % 8) return hipErrorInvalidValue;
   LoraArgs q = p;
   q.slices = lora_slices(p, cus);
-  q.kslice = ((p.k + q.slices - 1) / q.slices + 31) / 32 * 32;
+  q.parts = (bf16_t*)((char*)p.part + parts_at(p, q.slices));
+  q.kslice = ((p.k + q.slices - 1) / q.slices + 63) / 64 * 64;
   if (p.x_f32) return p.out_f32 ? lora_types<float, float>(q, cus, s) : lora_types<float, bf16_t>(q, cus, s);
   return p.out_f32 ? lora_types<bf16_t, float>(q, cus, s) : lora_types<bf16_t, bf16_t>(q, cus, s);
 }

@@ -323,10 +323,11 @@ struct LoraArgs {
   const void* x; long x_row; bool x_f32;
   const void* base; long base_row;
   void* out; long out_row; bool out_f32;
-  float* part;                                          // [slices][rows][rank]
-  int slices, kslice, cols;                             // set by the launcher
+  float* part;                                          // lora_bytes(): partials [slices][rows][rank], then
+  bf16_t* parts;                                        // the joined h; set by the launcher, like those below
+  int slices, kslice, cols;
 };
-int lora_slices(const LoraArgs& p, int cus);
+size_t lora_bytes(const LoraArgs& p, int cus);
 hipError_t lora(const LoraArgs& p, int cus, hipStream_t s);
 bool logprobs_fits(int vocab, int n_top);
 void logprobs_part_sizes(int rows, int vocab, int n_top, size_t* sum_floats, size_t* max_floats);

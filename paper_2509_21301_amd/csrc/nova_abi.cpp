@@ -1248,7 +1248,7 @@ nova::LoraArgs lora_args(const nova_adapters& d, const nova_rows& r) {
 extern "C" size_t nova_lora_workspace_bytes(const nova_adapters* adapters, const nova_rows* rows) {
   if (check_adapters(adapters) || check_row_starts(rows, 0)) return 0;
   const nova::LoraArgs a = lora_args(*adapters, *rows);
-  return align256((size_t)nova::lora_slices(a, device_cus()) * rows->rows * adapters->rank * sizeof(float));
+  return align256(nova::lora_bytes(a, device_cus()));
 }
 
 extern "C" int nova_lora(const nova_adapters* adapters, const nova_rows* rows, const int32_t* which, int x_type, const void* x,
