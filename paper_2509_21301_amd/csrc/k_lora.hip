@@ -279,16 +279,23 @@ template <typename T> NOVA_DEV void store_out8(T* p, const float* x) {
   }
 }
 
+// Chunk c of column n of B in LDS (CH chunks of 16 bytes a column) lies so that eight neighbouring columns' chunks are on
+// different banks.
+template <int CH> NOVA_DEV int turn_chunk(int n, int c) { return CH >= 8 ? c ^ (n & 7) : CH == 4 ? c ^ ((n >> 1) & 3) : c ^ ((n >> 2) & 1); }
+
 // ---- short sequences
-// Workgroup: (tile of 16 rows, `cols` columns); a wave takes 64 columns at a time.  Which column of B is which MFMA row
-// is free, so two tiles give a lane 8 consecutive columns of its row of out, and the four lane groups 32.  K (here the
+// Workgroup: (tile of 16 rows, `cols` columns); a wave takes 64 columns at a time, whose B it loads in one run and turns
+// into MFMA operands in LDS of its own, a step ahead; the first step's loads are on their way while h is summed.  Which
+// column of B is which MFMA row is free, so two tiles give a lane 8 consecutive columns of its row of out.  K (here the
 // rank) is 32 a step.
 template <typename TO, int RT>
 __global__ void __launch_bounds__(256) lora_expand_kernel(LoraArgs p) {
   constexpr int KS = (RT + 1) / 2;                           // steps of 32 of the rank
-  constexpr int LD = 32 * KS + 8;                            // row pitch in LDS (16 bytes more: rows on other banks)
+  constexpr int LD = 32 * KS + 8;                            // row pitch of h in LDS (16 bytes more: rows on other banks)
   constexpr int NH = sizeof(TO) == 4 ? 3 : 2;                // parts of h
+  constexpr int CH = 2 * RT;                                 // chunks of a column of B, and of a lane
   __shared__ __align__(16) bf16_t sm[NH][LO_STEP][LD];
+  __shared__ __align__(16) Frag8 sm_b[4][64][CH];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
   int b, row0;
   const SeqRows sr = find_row_tile<LO_STEP>(p.r, blockIdx.x, &b, &row0);
@@ -299,6 +306,27 @@ __global__ void __launch_bounds__(256) lora_expand_kernel(LoraArgs p) {
   const TO* base = reinterpret_cast<const TO*>(p.base);
   TO* out = reinterpret_cast<TO*>(p.out);
   if (!has && base == out) return;                           // nothing is added
+  const bf16_t* B = p.b + (has ? (size_t)i * p.nout * p.rank : 0);
+  Frag8 rb[CH];
+  Out8<TO> next[2], old[2];
+  // Rows behind the tile's last and columns and ranks behind the last repeat what is there.
+  auto request = [&](int n0) {
+    if (has)
+#pragma unroll
+      for (int j = 0; j < CH; ++j) {
+        const int w = lane + 64 * j;
+        rb[j] = *reinterpret_cast<const Frag8*>(B + (size_t)min(n0 + w / CH, p.nout - 1) * p.rank + min(8 * (w % CH), p.rank - 8));
+      }
+    if (base) {
+#pragma unroll
+      for (int q = 0; q < 2; ++q) next[q] = load_out8(base + (r0 + min(col, rows - 1)) * p.base_row + min(n0 + 32 * q + 8 * grp, p.nout - 8));
+    } else {
+      next[0] = next[1] = Out8<TO>{};
+    }
+  };
+  const int n_end = min(p.nout, (int)(blockIdx.y + 1) * p.cols);
+  int n0 = blockIdx.y * p.cols + 64 * wave;
+  if (n0 < n_end) request(n0);
   const float scale = has && p.scale ? p.scale[i] : 1.f;
   if (has) {
     for (int w = threadIdx.x; w < LO_STEP * 32 * KS; w += 256) {
@@ -317,51 +345,49 @@ __global__ void __launch_bounds__(256) lora_expand_kernel(LoraArgs p) {
     }
     __syncthreads();
   }
-  const bf16_t* B = p.b + (has ? (size_t)i * p.nout * p.rank : 0);
-  const int n_end = min(p.nout, (int)(blockIdx.y + 1) * p.cols);
-  for (int n0 = blockIdx.y * p.cols + 64 * wave; n0 < n_end; n0 += 256) {
-    // Rows behind the tile's last and columns behind the last repeat what is there: nothing of them is stored.
-    Out8<TO> old[2];
-    if (base) {
+  for (; n0 < n_end; n0 += 256) {
+    if (has) {
 #pragma unroll
-      for (int q = 0; q < 2; ++q) old[q] = load_out8(base + (r0 + min(col, rows - 1)) * p.base_row + min(n0 + 32 * q + 8 * grp, p.nout - 8));
-    } else {
-      old[0] = old[1] = Out8<TO>{};
+      for (int j = 0; j < CH; ++j) {
+        const int w = lane + 64 * j, n = w / CH, c = w % CH;
+        sm_b[wave][n][turn_chunk<CH>(n, c)] = 8 * c < p.rank ? rb[j] : zero_frag();
+      }
     }
+    old[0] = next[0], old[1] = next[1];
+    if (n0 + 256 < n_end) request(n0 + 256);
+    wave_fence();
     f32x4 acc[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (has) {
-      // tile t = 2 q + h, MFMA row m: column n0 + 32 q + 8 (m / 4) + 4 h + m % 4, so that lane group g holds 32 q + 8 g ..
-      Frag8 bf[KS][4];
+      // tile t = 2 q + h, MFMA row m: column 32 q + 8 (m / 4) + 4 h + m % 4 of the step, so that lane group g holds 32 q + 8 g ..
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
+      for (int ks = 0; ks < KS; ++ks) {
+        Frag8 h[NH];
+#pragma unroll
+        for (int q = 0; q < NH; ++q) h[q] = *reinterpret_cast<const Frag8*>(&sm[q][col][32 * ks + 8 * grp]);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-          const int n = n0 + 32 * (t >> 1) + 8 * (col >> 2) + 4 * (t & 1) + (col & 3), k = 32 * ks + 8 * grp;
-          const Frag8 w = *reinterpret_cast<const Frag8*>(B + (size_t)min(n, p.nout - 1) * p.rank + min(k, p.rank - 8));
-          bf[ks][t] = k < p.rank ? w : zero_frag();
+          const int n = 32 * (t >> 1) + 8 * (col >> 2) + 4 * (t & 1) + (col & 3), c = 4 * ks + grp;
+          const Frag8 f = CH >= 4 || grp < 2 ? sm_b[wave][n][turn_chunk<CH>(n, CH >= 4 ? c : c & 1)] : zero_frag();
+#pragma unroll
+          for (int q = 0; q < NH; ++q) acc[t] = mfma16(f, h[q], acc[t]);
         }
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-        for (int q = 0; q < NH; ++q) {
-          const Frag8 h = *reinterpret_cast<const Frag8*>(&sm[q][col][32 * ks + 8 * grp]);
-#pragma unroll
-          for (int t = 0; t < 4; ++t) acc[t] = mfma16(bf[ks][t], h, acc[t]);
-        }
+      }
     }
-    if (col >= rows) continue;
+    wave_fence();                          // the next step writes there
+    if (col < rows) {
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const int n = n0 + 32 * q + 8 * grp;
-      if (n >= p.nout) continue;
-      float y[8];
-      unpack_out8(old[q], y);
-      if (has)
+      for (int q = 0; q < 2; ++q) {
+        const int n = n0 + 32 * q + 8 * grp;
+        if (n >= p.nout) continue;
+        float y[8];
+        unpack_out8(old[q], y);
+        if (has)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] += scale * acc[2 * q + (e >> 2)][e & 3];
-      store_out8(out + (r0 + col) * p.out_row + n, y);
+          for (int e = 0; e < 8; ++e) y[e] += scale * acc[2 * q + (e >> 2)][e & 3];
+        store_out8(out + (r0 + col) * p.out_row + n, y);
+      }
     }
   }
 }
@@ -419,8 +445,6 @@ __global__ void __launch_bounds__(256) lora_up_kernel(LoraArgs p) {
       for (int n = 0; n < NH; ++n)
         h[w][ks][n] = has ? *reinterpret_cast<const Frag8*>(p.parts + ((size_t)n * p.r.rows + r0 + min(16 * (RW * wave + w) + col, rows - 1)) * (32 * KS) + 32 * ks + 8 * grp)
                           : zero_frag();
-  // Chunk c of column n lies so that eight neighbouring columns' chunks are on different banks, whatever a column's size.
-  auto turn = [](int n, int c) { return CH >= 8 ? c ^ (n & 7) : CH == 4 ? c ^ ((n >> 1) & 3) : c ^ ((n >> 2) & 1); };
   const int bn = threadIdx.x / CH, bc = threadIdx.x % CH;    // the thread's first column and chunk
   Frag8 rb[BC];
   u32x4 old[RW][IT], next[RW][IT];
@@ -453,7 +477,7 @@ __global__ void __launch_bounds__(256) lora_up_kernel(LoraArgs p) {
 #pragma unroll
       for (int j = 0; j < BC; ++j) {
         const int n = bn + 256 / CH * j;
-        sm_b[buf][n][turn(n, bc)] = 8 * bc < p.rank ? rb[j] : zero_frag();
+        sm_b[buf][n][turn_chunk<CH>(n, bc)] = 8 * bc < p.rank ? rb[j] : zero_frag();
       }
     }
 #pragma unroll
@@ -473,7 +497,7 @@ __global__ void __launch_bounds__(256) lora_up_kernel(LoraArgs p) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const int n = 16 * t + col, c = 4 * ks + grp;
-          const Frag8 f = CH >= 4 || grp < 2 ? sm_b[buf][n][turn(n, CH >= 4 ? c : c & 1)] : zero_frag();
+          const Frag8 f = CH >= 4 || grp < 2 ? sm_b[buf][n][turn_chunk<CH>(n, CH >= 4 ? c : c & 1)] : zero_frag();
 #pragma unroll
           for (int w = 0; w < RW; ++w)
 #pragma unroll
