@@ -373,7 +373,7 @@ int nova_logprobs(const void* logits, int type, int64_t pitch, int rows, int voc
  *  path:   device int32 [batch][max_rows]: the kept rows' numbers in their sequence, ascending; -1 behind
  *  tokens: device int32 [batch][max_rows]: the token after each kept row (the last of them is new); -1 behind
  *  lp:     device fp32 [batch][max_rows]: their log probabilities under p (0 at temperature 0 and behind)
- * vocab <= 2^21, and rows (twice with draft) and batch times ceil(vocab / 4096) are below 2^24.
+ * vocab <= 2^21, and rows (twice with draft) and batch times ceil(vocab / 8192) are below 2^24.
  *  ws: device, nova_accept_workspace_bytes(), 256-byte aligned, as for nova_tree_attention */
 size_t nova_accept_workspace_bytes(const nova_rows* rows, int vocab, int with_draft);
 int nova_accept(const nova_rows* rows, const int32_t* ids, const uint64_t* mask, const void* logits, int type, int64_t pitch,

@@ -8,7 +8,7 @@
 // A draw is the first token whose running sum exceeds u times the total.  The running sums reach over the whole
 // vocabulary and are compared with a number that may lie next to any of them, so weights and sums are in 64 bits (an
 // fp32 sum would move about one draw in a thousand at 152064 logits).
-// Two launches: the first reads every logit once (maximum, sum and largest id of chunks of 4096), the second
+// Two launches: the first reads every logit once (maximum, sum and largest id of chunks of 8192), the second
 // decides and draws, reading again only chunks of the rows where something is drawn.
 #include <algorithm>
 
@@ -16,7 +16,7 @@
 
 namespace nova {
 
-constexpr int AC_CHUNK = 4096;             // logits of a workgroup
+constexpr int AC_CHUNK = 8192;             // logits of a workgroup
 constexpr int AC_THREADS = 256;
 constexpr int AC_PER = AC_CHUNK / AC_THREADS;
 
@@ -45,16 +45,27 @@ NOVA_DEV double wave_scan64(double v) {
 }
 NOVA_DEV double wave_sum64(double v) { return lane_of(wave_scan64(v), 63); }
 
-// The sequence of a row (batch: none).
-NOVA_DEV int seq_of_row(const BatchRows& p, int r) {
-  if (!p.row_start) return r / p.max_rows;
-  int lo = 0, hi = p.batch;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (p.row_start[mid + 1] <= r) lo = mid + 1;
-    else hi = mid;
+// The sequence of a row in *b (batch: none) and its rows; a wave looks at 64 row starts at a time.
+NOVA_DEV SeqRows seq_of_row(const BatchRows& p, int r, int* b) {
+  *b = p.batch;
+  if (!p.row_start) {
+    *b = r / p.max_rows;
+    return seq_rows(p, *b);
   }
-  return lo;
+  const int lane = threadIdx.x & 63;
+  for (int base = 0; base < p.batch; base += 64) {
+    const int i = min(base + lane, p.batch - 1), from = p.row_start[i], to = p.row_start[i + 1];
+    const unsigned long long m = __ballot(to > r);
+    if (!m) continue;
+    const int l = __ffsll(m) - 1;
+    *b = min(base + l, p.batch - 1);
+    SeqRows s;
+    s.r0 = min(max(__builtin_amdgcn_readlane(from, l), 0), p.rows);
+    s.n = min(min(max(__builtin_amdgcn_readlane(to, l), s.r0), p.rows) - s.r0, p.max_rows);
+    s.ctx = 0;
+    return s;
+  }
+  return SeqRows{0, 0, 0};
 }
 
 // log2(e) / T, 0 for T = 0 (the largest logit takes all), negative where T gives no distribution.
@@ -71,11 +82,13 @@ NOVA_DEV double inv_temperature(const AcceptArgs& p, int b) {
 struct Exp2Table { double t[256]; };       // in LDS
 NOVA_DEV void fill_table(Exp2Table& tab) { // by the workgroup's threads; a barrier has to follow
   for (int j = threadIdx.x; j < 256; j += blockDim.x) {
-    const double r = j * (0.6931471805599453 / 256);
-    double y = 1.0;                        // Taylor series of e^r, r < ln 2, from its 20th power on
+    const double r = (j - 128) * (0.6931471805599453 / 256);
+    double y = 1.0 / 6227020800.0;         // Taylor series of e^r to r^13, |r| <= ln 2 / 2: its rest is below 5e-18
+    constexpr double C[13] = {1.0, 1.0, 1.0 / 2, 1.0 / 6, 1.0 / 24, 1.0 / 120, 1.0 / 720, 1.0 / 5040, 1.0 / 40320, 1.0 / 362880,
+                              1.0 / 3628800, 1.0 / 39916800, 1.0 / 479001600};
 #pragma unroll
-    for (int n = 20; n >= 1; --n) y = fma(y, r * (1.0 / n), 1.0);
-    tab.t[j] = y;
+    for (int n = 12; n >= 0; --n) y = fma(y, r, C[n]);
+    tab.t[j] = j ? y * 1.4142135623730951 : 1.0;   // the largest logit's weight is 1 exactly
   }
 }
 NOVA_DEV double exp2_neg(const Exp2Table& tab, double z) {
@@ -96,6 +109,19 @@ template <typename T> NOVA_DEV float logit(const T* row, int i) { return to_f<T>
 
 // The larger of two values, NaN where either is.
 NOVA_DEV float nan_max(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+template <int CTRL, int ROWS> NOVA_DEV float dpp_max(float v) {
+  return nan_max(v, __int_as_float(__builtin_amdgcn_update_dpp((int)0xFF800000u, __float_as_int(v), CTRL, ROWS, 0xf, false)));
+}
+NOVA_DEV float wave_nan_max(float v) {
+  v = dpp_max<0x111, 0xf>(v);
+  v = dpp_max<0x112, 0xf>(v);
+  v = dpp_max<0x114, 0xf>(v);
+  v = dpp_max<0x118, 0xf>(v);
+  v = dpp_max<0x142, 0xa>(v);
+  v = dpp_max<0x143, 0xc>(v);
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
 
 // A thread's logits of a chunk: 16 bytes at a time where the row allows it (x[i]: number place_of(.., i) of the chunk);
 // -infinity behind the vocabulary.
@@ -140,14 +166,14 @@ __global__ void __launch_bounds__(256) accept_stats_kernel(AcceptArgs p) {
   const int item = blockIdx.x / p.chunks, chunk = blockIdx.x % p.chunks;
   if (item >= p.items) return;
   const bool draft = item >= p.r.rows;
-  const int r = draft ? item - p.r.rows : item, b = seq_of_row(p.r, r);
-  if (b >= p.r.batch) return;
-  const SeqRows sr = seq_rows(p.r, b);
-  if (r < sr.r0 + (draft ? 1 : 0) || r >= sr.r0 + sr.n) return;   // a sequence's first row was drawn by nobody
+  const int r = draft ? item - p.r.rows : item;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c0 = chunk * AC_CHUNK;
   float x[AC_PER];
+  if (!draft) load_chunk((const TL*)p.logits + (long)r * p.row, c0, p.vocab, x);
+  int b;
+  const SeqRows sr = seq_of_row(p.r, r, &b);
+  if (b >= p.r.batch || r < sr.r0 + (draft ? 1 : 0) || r >= sr.r0 + sr.n) return;   // a sequence's first row was drawn by nobody
   if (draft) load_chunk((const TD*)p.draft + (long)r * p.draft_row, c0, p.vocab, x);
-  else load_chunk((const TL*)p.logits + (long)r * p.row, c0, p.vocab, x);
   __shared__ Exp2Table tab;
   __shared__ float sm_m[4];
   __shared__ int sm_arg[4];
@@ -157,8 +183,7 @@ __global__ void __launch_bounds__(256) accept_stats_kernel(AcceptArgs p) {
   float m = x[0];
 #pragma unroll
   for (int i = 1; i < AC_PER; ++i) m = nan_max(m, x[i]);
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) m = nan_max(m, __shfl_xor(m, o, 64));
+  m = wave_nan_max(m);
   if (lane == 0) sm_m[wave] = m;
   __syncthreads();
   m = nan_max(nan_max(sm_m[0], sm_m[1]), nan_max(sm_m[2], sm_m[3]));
@@ -192,33 +217,36 @@ __global__ void __launch_bounds__(256) accept_stats_kernel(AcceptArgs p) {
 struct RowStats { float m; int arg; double s; };
 NOVA_DEV bool has_dist(const RowStats& a, double inv) { return a.m > -INFINITY && inv >= 0.0; }   // NaN compares false
 
-// By one wave; every lane returns the same.
-NOVA_DEV RowStats join_row(const AcceptArgs& p, const Exp2Table& tab, int item, double inv) {
-  const int lane = threadIdx.x & 63;
+// A lane's chunks of a row: a request for all that is known of them (of more than 64 chunks those before are joined).
+struct LaneParts { float m; int arg; double s; };
+NOVA_DEV LaneParts lane_parts(const AcceptArgs& p, const Exp2Table& tab, int item, double inv) {
   const long at = (long)item * p.chunks;
-  RowStats a{-INFINITY, 0x7FFFFFFF, 0.0};
-  bool bad = false;
-  for (int c = lane; c < p.chunks; c += 64) {
-    const float m = p.part_max[at + c];
-    bad |= m != m;
-    if (m > a.m) a.m = m, a.arg = p.part_arg[at + c];
+  LaneParts a{-INFINITY, 0x7FFFFFFF, 0.0};
+  for (int c = threadIdx.x & 63; c < p.chunks; c += 64) {
+    const LaneParts n{p.part_max[at + c], p.part_arg[at + c], p.part_sum[at + c]};
+    if (c < 64) {
+      a = n;
+      continue;
+    }
+    const float m = nan_max(a.m, n.m);
+    const double of_a = a.m > -INFINITY ? a.s * exp2_neg(tab, ((double)a.m - (double)m) * inv) : 0.0;
+    const double of_n = n.m > -INFINITY ? n.s * exp2_neg(tab, ((double)n.m - (double)m) * inv) : 0.0;
+    a.arg = n.m > a.m ? n.arg : a.arg;
+    a.m = m, a.s = of_a + of_n;
   }
+  return a;
+}
+// By one wave; every lane returns the same.
+NOVA_DEV RowStats join_parts(const Exp2Table& tab, const LaneParts& l, double inv) {
+  RowStats a{wave_nan_max(l.m), 0x7FFFFFFF, 0.0};
+  if (!(a.m > -INFINITY)) return a;
+  if (inv == 0.0) {
+    a.arg = l.m == a.m ? l.arg : 0x7FFFFFFF;
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) {
-    const float om = __shfl_xor(a.m, o, 64);
-    const int oa = __shfl_xor(a.arg, o, 64);
-    if (om > a.m || (om == a.m && oa < a.arg)) a.m = om, a.arg = oa;
+    for (int o = 32; o >= 1; o >>= 1) a.arg = min(a.arg, __shfl_xor(a.arg, o, 64));
+  } else if (inv > 0.0) {
+    a.s = wave_sum64(l.m > -INFINITY ? l.s * exp2_neg(tab, ((double)l.m - (double)a.m) * inv) : 0.0);
   }
-  if (__ballot(bad)) {
-    a.m = __uint_as_float(0x7FC00000u);
-    return a;
-  }
-  if (a.m == -INFINITY || !(inv > 0.0)) return a;
-  for (int c = lane; c < p.chunks; c += 64) {
-    const float m = p.part_max[at + c];
-    if (m > -INFINITY) a.s += p.part_sum[at + c] * exp2_neg(tab, ((double)m - (double)a.m) * inv);
-  }
-  a.s = wave_sum64(a.s);
   return a;
 }
 
@@ -307,15 +335,15 @@ template <typename T> NOVA_DEV T get(const T* at) { return __hip_atomic_load(at,
 // Workgroup: a row, which draws its token; the last of a sequence walks from its first row on.
 template <typename TL>
 __global__ void __launch_bounds__(256) accept_follow_kernel(AcceptArgs p) {
-  const int r = blockIdx.x, b = seq_of_row(p.r, r);
-  if (b >= p.r.batch) return;
-  const SeqRows sr = seq_rows(p.r, b);
-  if (r < sr.r0 || r >= sr.r0 + sr.n) return;
-  const double inv = inv_temperature(p, b);
   __shared__ Exp2Table tab;
   fill_table(tab);
+  const int r = blockIdx.x;
+  int b;
+  const SeqRows sr = seq_of_row(p.r, r, &b);
+  if (b >= p.r.batch || r < sr.r0 || r >= sr.r0 + sr.n) return;
+  const double inv = inv_temperature(p, b);
   __syncthreads();
-  const RowStats a = join_row(p, tab, r, inv);
+  const RowStats a = join_parts(tab, lane_parts(p, tab, r, inv), inv);
   const int token = draw_row<TL>(p, tab, r, a, inv, p.u[r]);
   if (threadIdx.x == 0) {
     put(p.row_token + r, token);
@@ -380,23 +408,23 @@ __global__ void __launch_bounds__(AC_TEST) accept_draft_kernel(AcceptArgs p) {
     // wave w: row j0 + w against its draft, the target's row before it
     const int j = j0 + wave;
     if (j <= sr.n) {
-      const int r = sr.r0 + j - 1;
-      const RowStats a = join_row(p, tab, r, inv);
-      RowStats q{__uint_as_float(0x7FC00000u), 0, 0.0};
+      // everything that is known of the two rows at once
+      const int r = sr.r0 + j - 1, next = j < sr.n ? r + 1 : r, x = p.ids[next];
+      const bool test = j < sr.n, in = (unsigned)x < (unsigned)p.vocab;
+      const float u = p.u[next], lx = logit((const TL*)p.logits + (long)r * p.row, in ? x : 0),
+                  dx = test ? logit((const TD*)p.draft + (long)next * p.draft_row, in ? x : 0) : 0.f;
+      const LaneParts lp_ = lane_parts(p, tab, r, inv), lq = test ? lane_parts(p, tab, p.r.rows + next, inv) : LaneParts{-INFINITY, 0, 0.0};
+      const RowStats a = join_parts(tab, lp_, inv), q = join_parts(tab, lq, inv);
       bool kept = false, some = false;
       float lp = 0.f;
-      if (j < sr.n && has_dist(a, inv)) {
-        const int x = p.ids[r + 1];
-        const bool in = (unsigned)x < (unsigned)p.vocab;
+      if (test && has_dist(a, inv)) {
         if (inv == 0.0) {
           kept = x == a.arg;
         } else {
-          q = join_row(p, tab, p.r.rows + r + 1, inv);
           some = has_dist(q, inv);
           if (in && some) {
-            const double zp = ((double)logit((const TL*)p.logits + (long)r * p.row, x) - (double)a.m) * inv;
-            const double zq = ((double)logit((const TD*)p.draft + (long)(r + 1) * p.draft_row, x) - (double)q.m) * inv;
-            kept = uniform(p.u[r + 1]) * (exp2_neg(tab, zq) / q.s) < exp2_neg(tab, zp) / a.s;
+            const double zp = ((double)lx - (double)a.m) * inv, zq = ((double)dx - (double)q.m) * inv;
+            kept = uniform(u) * (exp2_neg(tab, zq) / q.s) < exp2_neg(tab, zp) / a.s;
             lp = (float)(zp * LN2 - log(a.s));
           }
         }
