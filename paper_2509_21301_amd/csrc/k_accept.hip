@@ -19,6 +19,7 @@ namespace nova {
 constexpr int AC_CHUNK = 8192;             // logits of a workgroup
 constexpr int AC_THREADS = 256;
 constexpr int AC_PER = AC_CHUNK / AC_THREADS;
+constexpr int AC_PART = AC_CHUNK / AC_PARTS;
 
 // A value of another lane by a data-parallel move: 0 where there is no such lane (or its row is left out of ROWS).
 template <int CTRL, int ROWS> NOVA_DEV double dpp64(double v) {
@@ -123,18 +124,18 @@ NOVA_DEV float wave_nan_max(float v) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
-// A thread's logits of a chunk: 16 bytes at a time where the row allows it (x[i]: number place_of(.., i) of the chunk);
-// -infinity behind the vocabulary.
-NOVA_DEV int place_of(bool f32, int i) {
-  const int n = f32 ? 4 : 8;
-  return (i / n * AC_THREADS + threadIdx.x) * n + i % n;
+// A thread's logits of a chunk, of which every wave has a part: 16 bytes at a time where the row allows it (x[i]: number
+// place_of(i) of the chunk); -infinity behind the vocabulary.
+template <typename T> NOVA_DEV int place_of(int i) {
+  constexpr int N = 16 / sizeof(T);
+  return (threadIdx.x >> 6) * AC_PART + (i / N * 64 + (threadIdx.x & 63)) * N + i % N;
 }
 template <typename T> NOVA_DEV void load_chunk(const T* row, int c0, int vocab, float* x) {
   constexpr int N = 16 / sizeof(T);
   if (((uintptr_t)row & 15) == 0 && c0 + AC_CHUNK <= vocab) {
     u32x4 w[AC_PER / N];
 #pragma unroll
-    for (int i = 0; i < AC_PER / N; ++i) w[i] = reinterpret_cast<const u32x4*>(row + c0)[i * AC_THREADS + threadIdx.x];
+    for (int i = 0; i < AC_PER / N; ++i) w[i] = *reinterpret_cast<const u32x4*>(row + c0 + place_of<T>(i * N));
 #pragma unroll
     for (int i = 0; i < AC_PER; ++i) {
       if constexpr (N == 4) x[i] = __uint_as_float(w[i / 4][i % 4]);
@@ -144,7 +145,7 @@ template <typename T> NOVA_DEV void load_chunk(const T* row, int c0, int vocab, 
   }
 #pragma unroll
   for (int i = 0; i < AC_PER; ++i) {
-    const int at = c0 + place_of(N == 4, i);
+    const int at = c0 + place_of<T>(i);
     x[i] = at < vocab ? logit(row, at) : -INFINITY;
   }
 }
@@ -177,7 +178,6 @@ __global__ void __launch_bounds__(256) accept_stats_kernel(AcceptArgs p) {
   __shared__ Exp2Table tab;
   __shared__ float sm_m[4];
   __shared__ int sm_arg[4];
-  __shared__ double sm_s[4];
   const double inv = inv_temperature(p, b);
   fill_table(tab);                         // while the logits are on their way
   float m = x[0];
@@ -198,17 +198,19 @@ __global__ void __launch_bounds__(256) accept_stats_kernel(AcceptArgs p) {
   if (inv == 0.0) {                        // greedy: the first of the largest
 #pragma unroll
     for (int i = 0; i < AC_PER; ++i)
-      if (x[i] == m) arg = min(arg, c0 + place_of(draft ? (sizeof(TD) == 4) : (sizeof(TL) == 4), i));
+      if (x[i] == m) arg = min(arg, c0 + (draft ? place_of<TD>(i) : place_of<TL>(i)));
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) arg = min(arg, __shfl_xor(arg, o, 64));
   }
-  if (lane == 0) sm_s[wave] = sum, sm_arg[wave] = arg;
+  const long at = (long)item * p.chunks + chunk;
+  if (lane == 0) {
+    p.part_sum[at * AC_PARTS + wave] = sum;
+    sm_arg[wave] = arg;
+  }
   __syncthreads();
   if (threadIdx.x == 0) {
-    const long at = (long)item * p.chunks + chunk;
     p.part_max[at] = m < INFINITY ? m : __uint_as_float(0x7FC00000u);   // NaN or +infinity: no distribution
     p.part_arg[at] = min(min(sm_arg[0], sm_arg[1]), min(sm_arg[2], sm_arg[3]));
-    p.part_sum[at] = ((sm_s[0] + sm_s[1]) + sm_s[2]) + sm_s[3];
   }
 }
 
@@ -223,7 +225,8 @@ NOVA_DEV LaneParts lane_parts(const AcceptArgs& p, const Exp2Table& tab, int ite
   const long at = (long)item * p.chunks;
   LaneParts a{-INFINITY, 0x7FFFFFFF, 0.0};
   for (int c = threadIdx.x & 63; c < p.chunks; c += 64) {
-    const LaneParts n{p.part_max[at + c], p.part_arg[at + c], p.part_sum[at + c]};
+    const double* sums = p.part_sum + (at + c) * AC_PARTS;
+    const LaneParts n{p.part_max[at + c], p.part_arg[at + c], ((sums[0] + sums[1]) + sums[2]) + sums[3]};
     if (c < 64) {
       a = n;
       continue;
@@ -279,27 +282,30 @@ template <typename F> NOVA_DEV int first_above(int n, double target, double* bef
   return last;
 }
 
-// The token of a chunk whose running sum of weight(i) exceeds `target`; by the whole workgroup.  First the thread's
-// range of consecutive logits, then the logit in it, one a lane.
-template <typename F> NOVA_DEV int draw_in_chunk(int c0, int vocab, double target, F&& weight) {
-  const int per = AC_CHUNK / blockDim.x;
-  __shared__ double sm_sum[1024];
-  const int first = c0 + threadIdx.x * per;
+// The token of SIZE logits from c0 on whose running sum of weight(i) exceeds `target`; by the whole workgroup of THREADS.
+// First the thread's range of consecutive logits, then the logit in it, one a lane.
+template <int SIZE, int THREADS, typename F> NOVA_DEV int draw_in_part(int c0, int vocab, double target, F&& weight) {
+  constexpr int PER = SIZE / THREADS;
+  __shared__ double sm_sum[THREADS];
+  const int first = c0 + threadIdx.x * PER;
   double sum = 0.0;
-#pragma unroll 4
-  for (int i = 0; i < per; ++i) sum += first + i < vocab ? weight(first + i) : 0.0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const double w = weight(min(first + i, vocab - 1));      // the loads together
+    sum += first + i < vocab ? w : 0.0;
+  }
   __syncthreads();
   sm_sum[threadIdx.x] = sum;
   __syncthreads();
   double before = 0.0;
-  const int t = first_above(blockDim.x, target, &before, [&](int i) { return sm_sum[i]; });
-  const int from = c0 + t * per;
+  const int t = first_above(THREADS, target, &before, [&](int i) { return sm_sum[i]; });
+  const int from = c0 + t * PER;
   double none;
-  return from + first_above(min(per, vocab - from), target - before, &none, [&](int i) { return weight(from + i); });
+  return from + first_above(min(PER, vocab - from), target - before, &none, [&](int i) { return weight(from + i); });
 }
 
 // A token drawn from a target row by its number u; by the whole workgroup.  -1: the row has no distribution.
-template <typename TL> NOVA_DEV int draw_row(const AcceptArgs& p, const Exp2Table& tab, int r, const RowStats& a, double inv, float u) {
+template <int THREADS, typename TL> NOVA_DEV int draw_row(const AcceptArgs& p, const Exp2Table& tab, int r, const RowStats& a, double inv, float u) {
   if (!has_dist(a, inv)) return -1;
   if (inv == 0.0) return a.arg;
   const TL* row = (const TL*)p.logits + (long)r * p.row;
@@ -307,8 +313,9 @@ template <typename TL> NOVA_DEV int draw_row(const AcceptArgs& p, const Exp2Tabl
   double before = 0.0;
   const double target = uniform(u) * a.s;
   auto scale = [&](float m) { return m > -INFINITY ? exp2_neg(tab, ((double)m - (double)a.m) * inv) : 0.0; };
-  const int c = first_above(p.chunks, target, &before, [&](int i) { return p.part_sum[at + i] * scale(p.part_max[at + i]); });
-  return draw_in_chunk(c * AC_CHUNK, p.vocab, target - before, [&](int i) { return exp2_neg(tab, ((double)logit(row, i) - (double)a.m) * inv); });
+  const int c = first_above(p.chunks * AC_PARTS, target, &before,
+                            [&](int i) { return p.part_sum[at * AC_PARTS + i] * scale(p.part_max[at + i / AC_PARTS]); });
+  return draw_in_part<AC_PART, THREADS>(c * AC_PART, p.vocab, target - before, [&](int i) { return exp2_neg(tab, ((double)logit(row, i) - (double)a.m) * inv); });
 }
 
 // log p of a token of a row.
@@ -341,10 +348,11 @@ __global__ void __launch_bounds__(256) accept_follow_kernel(AcceptArgs p) {
   int b;
   const SeqRows sr = seq_of_row(p.r, r, &b);
   if (b >= p.r.batch || r < sr.r0 || r >= sr.r0 + sr.n) return;
+  const float u = p.u[r];
   const double inv = inv_temperature(p, b);
   __syncthreads();
   const RowStats a = join_parts(tab, lane_parts(p, tab, r, inv), inv);
-  const int token = draw_row<TL>(p, tab, r, a, inv, p.u[r]);
+  const int token = draw_row<AC_THREADS, TL>(p, tab, r, a, inv, u);
   if (threadIdx.x == 0) {
     put(p.row_token + r, token);
     put(p.row_lp + r, log_p<TL>(p, r, a, inv, token));
@@ -388,6 +396,7 @@ __global__ void __launch_bounds__(256) accept_follow_kernel(AcceptArgs p) {
 // drawn from what the target has more than the draft, it sums that over its chunk, and the last to arrive draws.  Else
 // the first chunk's workgroup draws from the target's row.
 constexpr int AC_TEST = 512, AC_WAVES = AC_TEST / 64;
+static_assert(AC_PARTS == AC_THREADS / 64 && AC_SHARES == AC_WAVES);
 template <typename TL, typename TD>
 __global__ void __launch_bounds__(AC_TEST) accept_draft_kernel(AcceptArgs p) {
   const int b = blockIdx.x / p.chunks, chunk = blockIdx.x % p.chunks;
@@ -460,37 +469,34 @@ __global__ void __launch_bounds__(AC_TEST) accept_draft_kernel(AcceptArgs p) {
       const double d = exp2_neg(tab, ((double)logit(rp, i) - (double)tp.m) * inv) - exp2_neg(tab, ((double)logit(rq, i) - (double)tq.m) * inv) * iq;
       return d > 0.0 ? d : 0.0;
     };
-    __shared__ double sm_s[AC_WAVES];
+    // a wave's part of the chunk: its share of 8, in runs
+    constexpr int SHARE = AC_CHUNK / AC_WAVES;
     double sum = 0.0;
-    const int first = chunk * AC_CHUNK + threadIdx.x;
+    const int first = chunk * AC_CHUNK + wave * SHARE + lane;
 #pragma unroll
-    for (int i = 0; i < AC_CHUNK / AC_TEST; ++i)
-      if (first + AC_TEST * i < p.vocab) sum += more(first + AC_TEST * i);
-    sum = wave_sum64(sum);
-    if (lane == 0) sm_s[wave] = sum;
-    __syncthreads();
-    double* parts = p.rest_sum + (long)b * p.chunks;
-    if (threadIdx.x == 0) {
-      sum = 0.0;
-#pragma unroll
-      for (int w = 0; w < AC_WAVES; ++w) sum += sm_s[w];
-      put(parts + chunk, sum);
+    for (int i = 0; i < SHARE / 64; ++i) {
+      const double w = more(min(first + 64 * i, p.vocab - 1));
+      sum += first + 64 * i < p.vocab ? w : 0.0;
     }
+    sum = wave_sum64(sum);
+    const int shares = p.chunks * AC_WAVES;
+    double* parts = p.rest_sum + (long)b * shares;
+    if (lane == 0) put(parts + chunk * AC_WAVES + wave, sum);
     if (arrive(p.counters + b) != (unsigned)p.chunks) return;
     double total = 0.0;
-    for (int c = lane; c < p.chunks; c += 64) total += get(parts + c);
+    for (int c = lane; c < shares; c += 64) total += get(parts + c);
     total = wave_sum64(total);
     if (total > 0.0) {
       const double target = uniform(u) * total;
       double before = 0.0;
-      const int c = first_above(p.chunks, target, &before, [&](int i) { return get(parts + i); });
-      token = draw_in_chunk(c * AC_CHUNK, p.vocab, target - before, more);
+      const int c = first_above(shares, target, &before, [&](int i) { return get(parts + i); });
+      token = draw_in_part<SHARE, AC_TEST>(c * SHARE, p.vocab, target - before, more);
     } else {                               // nothing is left by rounding: p and q are alike
-      token = draw_row<TL>(p, tab, r, tp, inv, u);
+      token = draw_row<AC_TEST, TL>(p, tab, r, tp, inv, u);
     }
   } else {
     if (chunk != 0) return;
-    token = draw_row<TL>(p, tab, r, tp, inv, u);
+    token = draw_row<AC_TEST, TL>(p, tab, r, tp, inv, u);
   }
   const int i = threadIdx.x;
   if (i == 0) p.n_keep[b] = at + 1;

@@ -276,11 +276,12 @@ struct AcceptArgs {
   int* n_keep; int* path; int* tokens; float* lp;       // [batch], [batch][max_rows]
   // workspace: of each item (row of logits, then of the draft) and chunk
   int items, chunks;
-  float* part_max; int* part_arg; double* part_sum;
+  float* part_max; int* part_arg; double* part_sum;     // part_sum: of the chunk's AC_PARTS parts
   int* row_token; float* row_lp;                        // [rows]
-  double* rest_sum;                                     // [batch][chunks]
+  double* rest_sum;                                     // [batch][chunks][AC_SHARES]
   unsigned* counters;                                   // [batch]
 };
+constexpr int AC_PARTS = 4, AC_SHARES = 8;              // of a chunk, each with a sum of its own
 int accept_chunks(int vocab);
 hipError_t accept(const AcceptArgs& p, hipStream_t s);
 // Plans over the pages of a pool: refs [num_blocks], tables [batch][max_blocks], n requests.

@@ -1023,12 +1023,12 @@ int check_accept(const nova_rows* rows, int vocab, bool draft) {
 size_t accept_ws(nova::AcceptArgs* a, void* base) {
   Carve w(base);
   const size_t parts = (size_t)a->items * a->chunks;
-  a->part_sum = w.take<double>(parts);
+  a->part_sum = w.take<double>(parts * nova::AC_PARTS);
   a->part_max = w.take<float>(parts);
   a->part_arg = w.take<int>(parts);
   a->row_token = w.take<int>(a->r.rows);
   a->row_lp = w.take<float>(a->r.rows);
-  a->rest_sum = w.take<double>(a->items > a->r.rows ? (size_t)a->r.batch * a->chunks : 0);
+  a->rest_sum = w.take<double>(a->items > a->r.rows ? (size_t)a->r.batch * a->chunks * nova::AC_SHARES : 0);
   a->counters = w.take<unsigned>(a->r.batch);
   return w.used;
 }
