@@ -281,25 +281,25 @@ hipError_t kv_append(const AppendArgs& p, int cus, hipStream_t s) {
 }
 
 // ------------------------------------------------------------------ rotary embedding of dense rows
-// Workgroup: R rows of a group of heads.  The rows' sines and cosines are formed once in LDS; then a lane takes an item at a
+// Workgroup: some rows (as many as make a round of items) of a group of heads.  The rows' sines and cosines are formed once in LDS; then a lane takes an item at a
 // time: 8 pairs of the half layout (two loads of 8 elements, rot/2 apart), 8 elements of the interleaved one or 8 that
 // are not turned.  Items are numbered over rows and heads so that neighbouring lanes read neighbouring memory, and four
 // are requested before the first is turned.
-constexpr int ROT_ROWS = 8, ROT_AHEAD = 4;
+constexpr int ROT_AHEAD = 4;
 
 // n / d for n < 2^32 / d, from m = 2^32 / d + 1 (0 for d = 1).
 NOVA_DEV uint32_t div_by(uint32_t n, uint32_t m) { return m ? __umulhi(n, m) : n; }
 inline uint32_t reciprocal(uint32_t d) { return d == 1 ? 0u : (uint32_t)((1ull << 32) / d + 1); }
 
-// Items of a head, heads of a workgroup (at most ROT_ITEMS items a row, so that div_by is exact over its rows), and the
-// reciprocals of the items of a head and of a row.
-constexpr int ROT_ITEMS = 4096;
-struct RotateSplit { int items, heads; uint32_t per_item, per_row; };
+// Items of a head, rows and heads of a workgroup (at most 16 rows of ROT_ITEMS items, so that div_by is exact over them),
+// and the reciprocals of the items of a head and of a row.
+constexpr int ROT_ITEMS = 4096, ROT_ROWS = 16;
+struct RotateSplit { int items, heads, rows; uint32_t per_item, per_row; };
 
-template <typename TI, typename TO, int R, bool INTER>
+template <typename TI, typename TO, bool INTER>
 __global__ void __launch_bounds__(256) rotate_kernel(RotateArgs p, RotateSplit d) {
   extern __shared__ __align__(16) float sm[];             // [R][half] cosines, then sines
-  const int half = p.rot >> 1, r0 = blockIdx.x * R, n = min(R, p.rows - r0);
+  const int half = p.rot >> 1, R = d.rows, r0 = blockIdx.x * R, n = min(R, p.rows - r0);
   const int turned = INTER ? p.rot >> 3 : p.rot >> 4;     // items of a head that are turned
   const int h0 = blockIdx.y * d.heads;
   const uint32_t row_items = d.items * d.heads, live = d.items * min(d.heads, p.heads - h0);   // of a row; those of heads that there are
@@ -378,18 +378,13 @@ static hipError_t rotate_types(const RotateArgs& p, int cus, hipStream_t s) {
   d.heads = std::min(p.heads, ROT_ITEMS / d.items);
   d.per_item = reciprocal(d.items);
   d.per_row = reciprocal(d.items * d.heads);
-  // few rows: a workgroup each
-  const bool many = p.rows >= 2 * ROT_ROWS * cus;
-  const int R = many ? ROT_ROWS : 1;
-  const size_t lds = (size_t)R * p.rot * sizeof(float);
-  const dim3 grid((p.rows + R - 1) / R, (p.heads + d.heads - 1) / d.heads);
-  if (p.interleaved) {
-    if (many) hipLaunchKernelGGL((rotate_kernel<TI, TO, ROT_ROWS, true>), grid, dim3(256), lds, s, p, d);
-    else hipLaunchKernelGGL((rotate_kernel<TI, TO, 1, true>), grid, dim3(256), lds, s, p, d);
-  } else {
-    if (many) hipLaunchKernelGGL((rotate_kernel<TI, TO, ROT_ROWS, false>), grid, dim3(256), lds, s, p, d);
-    else hipLaunchKernelGGL((rotate_kernel<TI, TO, 1, false>), grid, dim3(256), lds, s, p, d);
-  }
+  // Rows that give every thread ROT_AHEAD items, fewer while that leaves fewer than two workgroups for each compute unit.
+  const long row = (long)d.items * d.heads, groups = (p.heads + d.heads - 1) / d.heads;
+  d.rows = (int)std::max(1l, std::min<long>({ROT_ROWS, 256 * ROT_AHEAD / row, p.rows * groups / (2l * cus)}));
+  const size_t lds = (size_t)d.rows * p.rot * sizeof(float);
+  const dim3 grid((p.rows + d.rows - 1) / d.rows, (unsigned)groups);
+  if (p.interleaved) hipLaunchKernelGGL((rotate_kernel<TI, TO, true>), grid, dim3(256), lds, s, p, d);
+  else hipLaunchKernelGGL((rotate_kernel<TI, TO, false>), grid, dim3(256), lds, s, p, d);
   return hipGetLastError();
 }
 

@@ -84,7 +84,7 @@ def test_rotate(gpu_lib, which, types):
 
 
 def test_rotate_many_rows(gpu_lib):
-    """Rows beyond one workgroup's, in the 16-row kernel, its last workgroup in part, and 900 heads (more than a group)."""
+    """Rows beyond one workgroup's, its last workgroup in part, and 900 heads (more than a group)."""
     nova = gpu_lib
     a = AXES[-1]
     rope, turn, fp = _rope_of(nova, a)
