@@ -470,6 +470,17 @@ int nova_llm_verify(const nova_llm* llm, const int32_t* ids, const int32_t* pos,
                     const nova_rows* rows, const nova_cache* cache, int32_t* next_ids, float* logits, void* ws,
                     size_t ws_bytes, nova_stream_t stream);
 
+/* The same calls with rotary positions of the rows' own, for prompts with images or video: rope in place of the
+ * model's (rope_theta over the whole head at the tokens' numbers), with axes (or NULL: one position a row), and pos
+ * device int32 [n_axes][rows] ([n_axes][n_vis + n_text] of a prompt; [rows] with axes NULL).  What a row sees goes by
+ * its place in the sequence as before.  Workspaces are those of nova_llm_prefill and nova_llm_verify. */
+int nova_llm_prefill_axes(const nova_llm* llm, const void* vis, int n_vis, const int32_t* ids, int n_text,
+                          const int32_t* block_table, const nova_cache* cache, const nova_rope* rope, const nova_rope_axes* axes,
+                          const int32_t* pos, int32_t* next_id, float* logits, void* ws, size_t ws_bytes, nova_stream_t stream);
+int nova_llm_verify_axes(const nova_llm* llm, const int32_t* ids, const nova_rope* rope, const nova_rope_axes* axes,
+                         const int32_t* pos, const uint64_t* mask, const nova_rows* rows, const nova_cache* cache,
+                         int32_t* next_ids, float* logits, void* ws, size_t ws_bytes, nova_stream_t stream);
+
 /* ------------------------------------------------------------------ linear co-run study
  * The two-linear experiment behind the paper's choice of inter-CU partitioning (Sec. 3.2.1, its
  * linear co-run table, and Sec. 3.2.3): one linear layer out[M, N] += x[M, K] w[N, K]^T

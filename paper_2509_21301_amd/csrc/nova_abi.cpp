@@ -1290,10 +1290,18 @@ extern "C" size_t nova_llm_decode_workspace_bytes(const nova_llm* m, int batch, 
 }
 
 namespace {
+// Rotary positions of the rows' own, in place of the model's (rope null: those).
+struct Positions {
+  const nova_rope* rope;
+  const nova_rope_axes* axes;
+  const int32_t* pos;
+};
+
 // `pool`: the cache is a nova_cache pool (kv is null then).
 template <typename T>
 int llm_prefill_t(const nova_llm* m, const T* vis, int n_vis, const int* ids, int n_text, const int* table,
-                  const nova_kv* kv, const nova_cache* pool, int* next_id, float* logits_out, void* ws, hipStream_t s) {
+                  const nova_kv* kv, const nova_cache* pool, int* next_id, float* logits_out, void* ws, hipStream_t s,
+                  const Positions& at = {}) {
   const nova_llm_config& c = m->d.cfg;
   const int S = n_vis + n_text, H = c.hidden, D = c.head_dim, qd = c.n_q * D;
   const int skp = round_up(S, 64);
@@ -1336,6 +1344,14 @@ int llm_prefill_t(const nova_llm* m, const T* vis, int n_vis, const int* ids, in
       CALL(NOVA_KIND_MISC, s, nova::norm_rows<T>(xr, p.M, H, gain, nullptr, c.eps, 0, a, H, 1, 0, 0, s));
     return (int)NOVA_OK;
   };
+  nova::RotateArgs turn{};                // q and k of the packed projection, in place: the same in every layer
+  if (at.rope) {
+    turn.x = turn.out = qkv, turn.x_row = turn.out_row = m->qkvw;
+    turn.in_f32 = turn.out_f32 = sizeof(T) == 4;
+    turn.rows = S, turn.heads = c.n_q + c.n_kv, turn.D = D;
+    turn.pos = at.pos;
+    set_rope(turn, *at.rope, at.axes, S);
+  }
   for (int l = 0; l < c.layers; ++l) {
     const char* lw = (const char*)m->d.layers + (size_t)l * m->lay.bytes;
     auto W = [&](int i) { return (const bf16_t*)(lw + m->lay.off[i]); };
@@ -1352,7 +1368,8 @@ int llm_prefill_t(const nova_llm* m, const T* vis, int n_vis, const int* ids, in
       const GemmArgs p = with_split(GemmArgs{a, H, W(1), H, S, m->qkvw, H, nullptr, qkv, m->qkvw, nullptr, 0});
       CALL(NOVA_KIND_GEMM, s, (nova::gemm<T, T>(p, nova::EPI_STORE, s)));
     }
-    CALL(NOVA_KIND_MISC, s, nova::qkv_prefill<T>(qkv, S, 1, c.n_q, c.n_kv, D, c.rope_theta, 0, vt, skp, kp, vp, kv ? table : nullptr,
+    if (at.rope) CALL(NOVA_KIND_MISC, s, nova::rotate(turn, cus, s));
+    CALL(NOVA_KIND_MISC, s, nova::qkv_prefill<T>(qkv, S, 1, c.n_q, c.n_kv, D, at.rope ? 0.f : c.rope_theta, 0, vt, skp, kp, vp, kv ? table : nullptr,
                                                   c.block, s, att_cnt, n_cnt));
     if (pool) {
       // K as the attention below reads it, rotated and rounded to bf16: so an 8-bit cache holds the 16-bit one's values,
@@ -1405,6 +1422,7 @@ struct Verify {
   const nova_rows* rows;
   const nova_cache* pool;
   const uint64_t* mask;
+  Positions at;
 };
 // Its buffers beside a decode step's of as many rows: the rotated q and the attention's partials.
 template <typename T>
@@ -1448,7 +1466,8 @@ int llm_decode_t(const nova_llm* m, const int* ids, const int* pos, const int* t
     app.q_row = app.k_row = app.v_row = m->qkvw, app.n_q = c.n_q;
     app.q_out = vb.q, app.q_out_row = qd;
     app.in_f32 = true, app.q_out_f32 = f32;
-    set_rope(app, nova_rope{D, 0, c.rope_theta, 1.f, 0, 1.f, 32.f, 1.f});
+    if (vf->at.rope) set_rope(app, *vf->at.rope, vf->at.axes, vf->rows->rows);
+    else set_rope(app, nova_rope{D, 0, c.rope_theta, 1.f, 0, 1.f, 32.f, 1.f});
   }
   auto attention_block = [&](int l) -> int {
     if (vf) {
@@ -1639,21 +1658,45 @@ int check_model_cache(const nova_llm* m, const nova_cache* c) {
 }
 }  // namespace
 
-extern "C" int nova_llm_prefill_cache(const nova_llm* m, const void* vis, int n_vis, const int32_t* ids, int n_text,
-                                      const int32_t* table, const nova_cache* cache, int32_t* next_id, float* logits, void* ws,
-                                      size_t ws_bytes, nova_stream_t stream) {
+namespace {
+int check_positions(const nova_llm* m, const Positions& at) {
+  if (!at.rope) return at.axes ? fail(NOVA_EINVAL, "axes without a rope") : NOVA_OK;
+  if (int rc = check_rope(at.rope, m->d.cfg.head_dim)) return rc;
+  if (at.axes)
+    if (int rc = check_axes(at.axes, at.rope->rot / 2)) return rc;
+  if (!at.pos || !aligned4(at.pos)) return fail(NOVA_EINVAL, "pos null or misaligned");
+  return NOVA_OK;
+}
+
+int prefill_cache(const nova_llm* m, const void* vis, int n_vis, const int32_t* ids, int n_text, const int32_t* table,
+                  const nova_cache* cache, const Positions& at, int32_t* next_id, float* logits, void* ws, size_t ws_bytes, hipStream_t s) {
   if (int rc = check_model_cache(m, cache)) return rc;
   if (int rc = check_prompt(n_vis, n_text)) return rc;
   if ((n_vis > 0 && (!vis || !aligned(vis))) || (n_text > 0 && !ids) || !table || !next_id || !ws || !aligned(ws))
     return fail(NOVA_EINVAL, "null or misaligned pointer");
   const int S = n_vis + n_text;
   if ((S + 15) / 16 > cache->num_blocks) return fail(NOVA_ENOKV, "prompt needs more blocks than the pool holds");
+  if (int rc = check_positions(m, at)) return rc;
+  if (at.rope && S > MAX_ROWS) return fail(NOVA_EUNSUPPORTED, "prompt of %d tokens with positions (at most %d)", S, MAX_ROWS);
   const size_t need = nova_llm_prefill_workspace_bytes(m, S);
   if (ws_bytes < need) return fail(NOVA_ENOSPACE, "workspace %zu < required %zu bytes", ws_bytes, need);
-  hipStream_t s = (hipStream_t)stream;
   return m->d.cfg.act == NOVA_ACT_F32
-             ? llm_prefill_t<float>(m, (const float*)vis, n_vis, ids, n_text, table, nullptr, cache, next_id, logits, ws, s)
-             : llm_prefill_t<bf16_t>(m, (const bf16_t*)vis, n_vis, ids, n_text, table, nullptr, cache, next_id, logits, ws, s);
+             ? llm_prefill_t<float>(m, (const float*)vis, n_vis, ids, n_text, table, nullptr, cache, next_id, logits, ws, s, at)
+             : llm_prefill_t<bf16_t>(m, (const bf16_t*)vis, n_vis, ids, n_text, table, nullptr, cache, next_id, logits, ws, s, at);
+}
+}  // namespace
+
+extern "C" int nova_llm_prefill_cache(const nova_llm* m, const void* vis, int n_vis, const int32_t* ids, int n_text,
+                                      const int32_t* table, const nova_cache* cache, int32_t* next_id, float* logits, void* ws,
+                                      size_t ws_bytes, nova_stream_t stream) {
+  return prefill_cache(m, vis, n_vis, ids, n_text, table, cache, Positions{}, next_id, logits, ws, ws_bytes, (hipStream_t)stream);
+}
+
+extern "C" int nova_llm_prefill_axes(const nova_llm* m, const void* vis, int n_vis, const int32_t* ids, int n_text,
+                                     const int32_t* table, const nova_cache* cache, const nova_rope* rope, const nova_rope_axes* axes,
+                                     const int32_t* pos, int32_t* next_id, float* logits, void* ws, size_t ws_bytes, nova_stream_t stream) {
+  if (!rope) return fail(NOVA_EINVAL, "null rope");
+  return prefill_cache(m, vis, n_vis, ids, n_text, table, cache, Positions{rope, axes, pos}, next_id, logits, ws, ws_bytes, (hipStream_t)stream);
 }
 
 extern "C" size_t nova_llm_verify_workspace_bytes(const nova_llm* m, const nova_cache* cache, const nova_rows* rows) {
@@ -1661,21 +1704,37 @@ extern "C" size_t nova_llm_verify_workspace_bytes(const nova_llm* m, const nova_
   return m->d.cfg.act == NOVA_ACT_F32 ? verify_bufs<float>(m, cache, rows, nullptr).used : verify_bufs<bf16_t>(m, cache, rows, nullptr).used;
 }
 
-extern "C" int nova_llm_verify(const nova_llm* m, const int32_t* ids, const int32_t* pos, const uint64_t* mask, const nova_rows* rows,
-                               const nova_cache* cache, int32_t* next_ids, float* logits, void* ws, size_t ws_bytes, nova_stream_t stream) {
+namespace {
+int verify(const nova_llm* m, const int32_t* ids, const Positions& at, const uint64_t* mask, const nova_rows* rows, const nova_cache* cache,
+           int32_t* next_ids, float* logits, void* ws, size_t ws_bytes, nova_stream_t stream) {
+  const int32_t* pos = at.pos;
   if (int rc = check_model_cache(m, cache)) return rc;
   if (int rc = check_tree(cache, rows, m->d.cfg.n_q)) return rc;
   if (rows->rows < 1 || rows->rows > 32) return fail(NOVA_EINVAL, "%d rows outside 1..32", rows->rows);
   if (!ids || !pos || !next_ids) return fail(NOVA_EINVAL, "null pointer");
+  if (int rc = check_positions(m, at)) return rc;
   if ((uintptr_t)mask & 7) return fail(NOVA_EINVAL, "mask must be 8-byte aligned");
   if (!ws || !aligned(ws)) return fail(NOVA_EINVAL, "null or misaligned workspace");
   const size_t need = nova_llm_verify_workspace_bytes(m, cache, rows);
   if (ws_bytes < need) return fail(NOVA_ENOSPACE, "workspace %zu < required %zu bytes", ws_bytes, need);
-  const Verify vf{rows, cache, mask};
+  const Verify vf{rows, cache, mask, at};
   hipStream_t s = (hipStream_t)stream;
   return m->d.cfg.act == NOVA_ACT_F32
              ? llm_decode_t<float>(m, ids, pos, nullptr, 0, rows->rows, 1, nullptr, &vf, next_ids, logits, ws, s)
              : llm_decode_t<bf16_t>(m, ids, pos, nullptr, 0, rows->rows, 1, nullptr, &vf, next_ids, logits, ws, s);
+}
+}  // namespace
+
+extern "C" int nova_llm_verify(const nova_llm* m, const int32_t* ids, const int32_t* pos, const uint64_t* mask, const nova_rows* rows,
+                               const nova_cache* cache, int32_t* next_ids, float* logits, void* ws, size_t ws_bytes, nova_stream_t stream) {
+  return verify(m, ids, Positions{nullptr, nullptr, pos}, mask, rows, cache, next_ids, logits, ws, ws_bytes, stream);
+}
+
+extern "C" int nova_llm_verify_axes(const nova_llm* m, const int32_t* ids, const nova_rope* rope, const nova_rope_axes* axes,
+                                    const int32_t* pos, const uint64_t* mask, const nova_rows* rows, const nova_cache* cache,
+                                    int32_t* next_ids, float* logits, void* ws, size_t ws_bytes, nova_stream_t stream) {
+  if (!rope) return fail(NOVA_EINVAL, "null rope");
+  return verify(m, ids, Positions{rope, axes, pos}, mask, rows, cache, next_ids, logits, ws, ws_bytes, stream);
 }
 
 // ------------------------------------------------------------------ allocation-free decode

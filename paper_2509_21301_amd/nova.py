@@ -148,6 +148,10 @@ _SIG = {
     "nova_llm_verify_workspace_bytes": (C.c_size_t, [C.c_void_p, C.c_void_p, C.c_void_p]),
     "nova_llm_verify": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                   C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "nova_llm_prefill_axes": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                        C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "nova_llm_verify_axes": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                       C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "nova_linear": (C.c_int, [C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p]),
     "nova_make_cu_mask": (C.c_int, [C.c_int, C.c_int, C.POINTER(C.c_uint32)]),
     "nova_set_stage_partition": (C.c_int, [C.c_int, C.POINTER(C.c_uint32), C.c_int, C.POINTER(C.c_void_p)]),
@@ -443,7 +447,9 @@ class Llm:
             need = max(lib.nova_llm_decode_workspace_bytes(self.h, b, decode_ctx) for b in range(1, decode_batch + 1))
             self._workspace("decode", need)
 
-    def prefill(self, vis, ids, table, kv, logits=None, next_id=None, stream=None):
+    def prefill(self, vis, ids, table, kv, logits=None, next_id=None, stream=None, rope=None, pos=None):
+        """One prompt, [vis ; ids], into a ``KvPool`` or a ``Cache``; on a Cache with ``rope`` the rotary positions are
+        ``pos`` (int32 [rows], or [axes, rows] of a Rope with axes) in place of the tokens' numbers."""
         n_vis = 0 if vis is None else vis.shape[0]
         n_text = ids.shape[0]
         ws = self._workspace("prefill", lib.nova_llm_prefill_workspace_bytes(self.h, n_vis + n_text), stream)
@@ -453,9 +459,21 @@ class Llm:
             kv._check_layers(self.cfg.layers)
             _check_device(kv.device, vis, ids, table, next_id, logits)
             _check_vector("table", table, torch.int32, (n_vis + n_text + 15) // 16)
+            if rope is not None:
+                if pos is None:
+                    raise ValueError("a rope needs pos")
+                _check_device(kv.device, pos)
+                rope._check_pos(pos, n_vis + n_text)
+                _check(lib.nova_llm_prefill_axes(self.h, _ptr(vis), n_vis, _ptr(ids), n_text, _ptr(table), kv.layer(0), rope.ref, rope.axes_ref,
+                                                 _ptr(pos), _ptr(next_id), _ptr(logits), _ptr(ws), ws.numel(), _stream(stream)))
+                return next_id
+            if pos is not None:
+                raise ValueError("pos goes with a rope")
             _check(lib.nova_llm_prefill_cache(self.h, _ptr(vis), n_vis, _ptr(ids), n_text, _ptr(table), kv.layer(0),
                                               _ptr(next_id), _ptr(logits), _ptr(ws), ws.numel(), _stream(stream)))
             return next_id
+        if rope is not None or pos is not None:
+            raise ValueError("positions of the rows' own need a Cache")
         _check(lib.nova_llm_prefill(self.h, _ptr(vis), n_vis, _ptr(ids), n_text, _ptr(table), C.byref(kv.c),
                                     _ptr(next_id), _ptr(logits), _ptr(ws), ws.numel(), _stream(stream)))
         return next_id
@@ -471,14 +489,19 @@ class Llm:
                                    _stream(stream)))
         return next_ids
 
-    def verify(self, ids, pos, rows, cache, mask=None, next_ids=None, logits=None, stream=None):
+    def verify(self, ids, pos, rows, cache, mask=None, next_ids=None, logits=None, stream=None, rope=None):
         """A decode step over drafted tokens on a ``Cache``: ids, pos int32 [rows.rows] (at most 32 rows), ``mask``
         int64 [rows] as for ``tree_attention``; the greedy id after every row.  One row per sequence decodes.  Rows
-        behind the last sequence need valid ids too; what comes back for them means nothing."""
+        behind the last sequence need valid ids too; what comes back for them means nothing.  ``rope`` replaces the
+        model's rotary embedding (pos [axes, rows] of a Rope with axes)."""
         cache._check_layers(self.cfg.layers)
         _check_device(cache.device, rows.tables, ids, pos, mask, next_ids, logits)
-        for what, t, dt in (("ids", ids, torch.int32), ("pos", pos, torch.int32), ("mask", mask, torch.int64)):
+        for what, t, dt in (("ids", ids, torch.int32), ("mask", mask, torch.int64)):
             _check_vector(what, t, dt, rows.rows)
+        if rope is None:
+            _check_vector("pos", pos, torch.int32, rows.rows)
+        else:
+            rope._check_pos(pos, rows.rows)
         if logits is not None and (logits.dtype != torch.float32 or not logits.is_contiguous() or
                                    logits.shape != (rows.rows, self.cfg.vocab)):
             raise ValueError(f"logits must be contiguous float32 {(rows.rows, self.cfg.vocab)}")
@@ -488,6 +511,10 @@ class Llm:
         if next_ids is None:
             next_ids = _empty(self.embed, rows.rows, torch.int32, stream)
         _check_vector("next_ids", next_ids, torch.int32, rows.rows)
+        if rope is not None:
+            _check(lib.nova_llm_verify_axes(self.h, _ptr(ids), rope.ref, rope.axes_ref, _ptr(pos), _ptr(mask), rows.ref, cache.layer(0),
+                                            _ptr(next_ids), _ptr(logits), _ptr(ws), ws.numel(), _stream(stream)))
+            return next_ids
         _check(lib.nova_llm_verify(self.h, _ptr(ids), _ptr(pos), _ptr(mask), rows.ref, cache.layer(0), _ptr(next_ids),
                                    _ptr(logits), _ptr(ws), ws.numel(), _stream(stream)))
         return next_ids
@@ -908,6 +935,7 @@ class Pages:
         self.refs, self.num_blocks, self.device = refs, refs.shape[0], refs.get_device()
         self._c = PagesC(_ptr(refs), self.num_blocks)
         self.ref = C.addressof(self._c)
+        self._ws = {}
 
     def _tables(self, tables, what="tables"):
         if tables.dtype != torch.int32 or tables.dim() != 2 or not tables.is_contiguous():
@@ -915,7 +943,10 @@ class Pages:
         return tables.shape
 
     def _workspace(self, batch, n, stream):
-        return _empty(self.refs, max(256, lib.nova_pages_workspace_bytes(self.ref, batch, n)), torch.uint8, stream)
+        nbytes = self._ws.get((batch, n))
+        if nbytes is None:
+            nbytes = self._ws[batch, n] = max(256, lib.nova_pages_workspace_bytes(self.ref, batch, n))
+        return _empty(self.refs, nbytes, torch.uint8, stream)
 
     def extend(self, tables, tokens, stream=None):
         """Blocks for the first ``tokens`` (int32 [batch]) tokens of every sequence, those that it lacks."""
