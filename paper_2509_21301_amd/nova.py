@@ -860,29 +860,33 @@ def accept(rows, ids, logits, u, mask=None, draft=None, temperature=None, stream
     n, batch, width = rows.rows, rows.batch, rows.max_rows
     dev = logits.get_device()
     _check_device(dev, rows.tables, ids, logits, u, mask, draft, temperature)
-    for what, t in (("logits", logits), ("draft", draft)):
-        if t is not None and (t.dtype not in _ACT or t.dim() != 2 or t.shape[0] != n or t.shape != logits.shape or t.stride(1) != 1):
-            raise ValueError(f"{what} must be float32 or bfloat16 [{n}, vocab] with contiguous rows, got {t.dtype} {tuple(t.shape)}")
+    if act is None or logits.dim() != 2 or logits.shape[0] != n or logits.stride(1) != 1:
+        raise ValueError(f"logits must be float32 or bfloat16 [{n}, vocab] with contiguous rows, got {logits.dtype} {tuple(logits.shape)}")
+    vocab = logits.shape[1]
+    draft_act = draft_pitch = 0
+    if draft is not None:
+        draft_act, draft_pitch = _check_matrix("draft", draft, n, vocab)
     _check_vector("ids", ids, torch.int32, n)
     _check_vector("u", u, torch.float32, n)
     _check_vector("mask", mask, torch.int64, n)
     _check_vector("temperature", temperature, torch.float32, batch)
-    vocab = logits.shape[1]
     key = (vocab, draft is not None)
     nbytes = rows._ws.get(key)
     if nbytes is None:
         nbytes = rows._ws[key] = lib.nova_accept_workspace_bytes(rows.ref, vocab, int(draft is not None))
-    ws = _empty(logits, max(nbytes, 256), torch.uint8, stream)
-    # one allocation for what is returned
-    buf = _empty(logits, batch * (1 + 3 * width), torch.int32, stream)
+    # one allocation for what is returned, and for a small workspace behind it
+    out = batch * (1 + 3 * width)
+    at = (out + 63) // 64 * 64
+    small = 0 < nbytes <= 1 << 16
+    buf = _empty(logits, at + nbytes // 4 if small else out, torch.int32, stream)
+    apart = None if small else _empty(logits, max(nbytes, 256), torch.uint8, stream)
+    ws = buf.data_ptr() + 4 * at if small else apart.data_ptr()
     n_keep = buf.as_strided((batch,), (1,), 0)
     path, tokens, lp = (buf.as_strided((batch, width), (width, 1), batch * (1 + i * width)) for i in range(3))
-    lp = lp.view(torch.float32)
     _check(lib.nova_accept(rows.ref, ids.data_ptr(), _ptr(mask), logits.data_ptr(), act, logits.stride(0) if n > 1 else vocab, _ptr(draft),
-                           _ACT[draft.dtype] if draft is not None else 0, 0 if draft is None else draft.stride(0) if n > 1 else vocab,
-                           vocab, _ptr(temperature), u.data_ptr(), n_keep.data_ptr(), path.data_ptr(), tokens.data_ptr(), lp.data_ptr(),
-                           ws.data_ptr(), nbytes, _stream_on(dev, stream)))
-    return n_keep, path, tokens, lp
+                           draft_act, draft_pitch, vocab, _ptr(temperature), u.data_ptr(), n_keep.data_ptr(), path.data_ptr(),
+                           tokens.data_ptr(), lp.data_ptr(), ws, nbytes, _stream_on(dev, stream)))
+    return n_keep, path, tokens, lp.view(torch.float32)
 
 
 def kv_keep(cache, rows, path, n_keep, ctx_out=None, stream=None):
