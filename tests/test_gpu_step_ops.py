@@ -457,7 +457,7 @@ def test_copy(gpu_lib, kind):
 def test_extend(gpu_lib):
     nova = gpu_lib
     r = _rng(2)
-    for blocks, batch, width in [(1, 1, 1), (50, 7, 9), (5000, 40, 130), (9000, 1500, 7)]:
+    for blocks, batch, width in [(1, 1, 1), (50, 7, 9), (5000, 40, 130), (9000, 1500, 7), (40011, 50, 700)]:
         refs = (r.random(blocks) < 0.3) * r.integers(1, 4, blocks)
         tables = np.full((batch, width), -1)
         tables[r.random((batch, width)) < 0.2] = 0
@@ -516,7 +516,7 @@ def test_fork_refusals_and_exhaustion(gpu_lib):
 
 
 @pytest.mark.parametrize("kind", TYPES)
-@pytest.mark.parametrize("blocks", [1, 2, 37, 1023, 3001])
+@pytest.mark.parametrize("blocks", [1, 2, 37, 1023, 3001, 5003, 20011])
 def test_compact(gpu_lib, kind, blocks):
     nova = gpu_lib
     r = _rng(blocks)
