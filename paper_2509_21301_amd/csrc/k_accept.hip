@@ -20,6 +20,7 @@ constexpr int AC_CHUNK = 8192;             // logits of a workgroup
 constexpr int AC_THREADS = 256;
 constexpr int AC_PER = AC_CHUNK / AC_THREADS;
 constexpr int AC_PART = AC_CHUNK / AC_PARTS;
+constexpr int AC_MAX_CHUNKS = (1 << 21) / AC_CHUNK;   // of the largest vocabulary
 
 // A value of another lane by a data-parallel move: 0 where there is no such lane (or its row is left out of ROWS).
 template <int CTRL, int ROWS> NOVA_DEV double dpp64(double v) {
@@ -77,7 +78,7 @@ NOVA_DEV double inv_temperature(const AcceptArgs& p, int b) {
 }
 
 // 2^z for z <= 0 in 64 bits (0 below 2^-1074 and for -infinity): z = k + j / 256 + f with |f| <= 2^-9, the table's
-// 2^(j/256), and the Taylor series of 2^f to f^4 (its rest is below 4e-17): 17 instructions, where a series without a
+// 2^(j/256), and the Taylor series of 2^f to f^4 (its rest is below 4e-17): 16 instructions, where a series without a
 // table takes 30, and 64-bit ones issue as slowly as they come: the first pass over 480 rows of 152064 logits took 96 us
 // with the longer one, 62 us with this.
 struct Exp2Table { double t[256]; };       // in LDS
@@ -92,10 +93,10 @@ NOVA_DEV void fill_table(Exp2Table& tab) { // by the workgroup's threads; a barr
     tab.t[j] = j ? y * 1.4142135623730951 : 1.0;   // the largest logit's weight is 1 exactly
   }
 }
-NOVA_DEV double exp2_neg(const Exp2Table& tab, double z) {
+// 2^(d inv), d <= 0 and at least -1100 / inv.
+NOVA_DEV double exp2_times(const Exp2Table& tab, double d, double inv) {
   constexpr double MAGIC = 0x1.8p44;       // a sum with it ends at the 8th binary place
-  z = fmax(z, -1100.0);
-  const double t = z + MAGIC, f = z - (t - MAGIC);
+  const double t = fma(d, inv, MAGIC), f = fma(d, inv, -(t - MAGIC));
   const int n = (int)(uint32_t)__builtin_bit_cast(uint64_t, t);
   double y = fma(f, 9.6181291076284772e-3, 5.5504108664821580e-2);
   y = fma(y, f, 2.4022650695910072e-1);
@@ -103,6 +104,15 @@ NOVA_DEV double exp2_neg(const Exp2Table& tab, double z) {
   const double b = tab.t[n & 255];
   return ldexp(fma(b, y * f, b), n >> 8);
 }
+NOVA_DEV double exp2_neg(const Exp2Table& tab, double z) { return exp2_times(tab, fmax(z, -1100.0), 1.0); }
+
+// Weights of logits relative to a maximum m at log2(e) / T = inv: the difference first (it is exact, where a product with a
+// small temperature's inverse would not cancel at the maximum).
+struct Weigh {
+  double m, inv, least;
+  NOVA_DEV Weigh(float m, double inv) : m(m), inv(inv), least(-1100.0 / inv) {}
+  NOVA_DEV double operator()(const Exp2Table& tab, float x) const { return exp2_times(tab, fmax((double)x - m, least), inv); }
+};
 constexpr double LN2 = 0.6931471805599453;
 
 // A logit of a row, from memory in its type.
@@ -189,9 +199,9 @@ __global__ void __launch_bounds__(256) accept_stats_kernel(AcceptArgs p) {
   m = nan_max(nan_max(sm_m[0], sm_m[1]), nan_max(sm_m[2], sm_m[3]));
   double sum = 0.0;
   if (inv > 0.0 && m > -INFINITY && m < INFINITY) {
-    // the difference first: it is exact, where a product with a small temperature's inverse would not cancel at the maximum
+    const Weigh weight(m, inv);
 #pragma unroll
-    for (int i = 0; i < AC_PER; ++i) sum += exp2_neg(tab, ((double)x[i] - (double)m) * inv);
+    for (int i = 0; i < AC_PER; ++i) sum += weight(tab, x[i]);
   }
   sum = wave_sum64(sum);
   int arg = 0x7FFFFFFF;
@@ -312,10 +322,14 @@ template <int THREADS, typename TL> NOVA_DEV int draw_row(const AcceptArgs& p, c
   const long at = (long)r * p.chunks;
   double before = 0.0;
   const double target = uniform(u) * a.s;
-  auto scale = [&](float m) { return m > -INFINITY ? exp2_neg(tab, ((double)m - (double)a.m) * inv) : 0.0; };
-  const int c = first_above(p.chunks * AC_PARTS, target, &before,
-                            [&](int i) { return p.part_sum[at * AC_PARTS + i] * scale(p.part_max[at + i / AC_PARTS]); });
-  return draw_in_part<AC_PART, THREADS>(c * AC_PART, p.vocab, target - before, [&](int i) { return exp2_neg(tab, ((double)logit(row, i) - (double)a.m) * inv); });
+  const Weigh weight(a.m, inv);
+  auto scale = [&](float m) { return m > -INFINITY ? weight(tab, m) : 0.0; };
+  // the parts' sums side by side in LDS, requested together
+  __shared__ double sm_parts[AC_MAX_CHUNKS * AC_PARTS];
+  for (int i = threadIdx.x; i < p.chunks * AC_PARTS; i += THREADS) sm_parts[i] = p.part_sum[at * AC_PARTS + i] * scale(p.part_max[at + i / AC_PARTS]);
+  __syncthreads();
+  const int c = first_above(p.chunks * AC_PARTS, target, &before, [&](int i) { return sm_parts[i]; });
+  return draw_in_part<AC_PART, THREADS>(c * AC_PART, p.vocab, target - before, [&](int i) { return weight(tab, logit(row, i)); });
 }
 
 // log p of a token of a row.
@@ -465,8 +479,9 @@ __global__ void __launch_bounds__(AC_TEST) accept_draft_kernel(AcceptArgs p) {
     const TD* rq = (const TD*)p.draft + (long)(r + 1) * p.draft_row;
     // times p's sum, so that equal logits of the target weigh exactly 1 and their running sums are exact
     const double iq = tp.s / tq.s;
+    const Weigh wp(tp.m, inv), wq(tq.m, inv);
     auto more = [&](int i) {
-      const double d = exp2_neg(tab, ((double)logit(rp, i) - (double)tp.m) * inv) - exp2_neg(tab, ((double)logit(rq, i) - (double)tq.m) * inv) * iq;
+      const double d = wp(tab, logit(rp, i)) - wq(tab, logit(rq, i)) * iq;
       return d > 0.0 ? d : 0.0;
     };
     // a wave's part of the chunk: its share of 8, in runs
@@ -483,13 +498,16 @@ __global__ void __launch_bounds__(AC_TEST) accept_draft_kernel(AcceptArgs p) {
     double* parts = p.rest_sum + (long)b * shares;
     if (lane == 0) put(parts + chunk * AC_WAVES + wave, sum);
     if (arrive(p.counters + b) != (unsigned)p.chunks) return;
+    __shared__ double sm_shares[AC_MAX_CHUNKS * AC_SHARES];
+    for (int i = threadIdx.x; i < shares; i += AC_TEST) sm_shares[i] = get(parts + i);
+    __syncthreads();
     double total = 0.0;
-    for (int c = lane; c < shares; c += 64) total += get(parts + c);
+    for (int c = lane; c < shares; c += 64) total += sm_shares[c];
     total = wave_sum64(total);
     if (total > 0.0) {
       const double target = uniform(u) * total;
       double before = 0.0;
-      const int c = first_above(shares, target, &before, [&](int i) { return get(parts + i); });
+      const int c = first_above(shares, target, &before, [&](int i) { return sm_shares[i]; });
       token = draw_in_part<SHARE, AC_TEST>(c * SHARE, p.vocab, target - before, more);
     } else {                               // nothing is left by rounding: p and q are alike
       token = draw_row<AC_TEST, TL>(p, tab, r, tp, inv, u);
@@ -523,7 +541,7 @@ static hipError_t accept_types(const AcceptArgs& p, hipStream_t s) {
 }
 
 hipError_t accept(const AcceptArgs& p, hipStream_t s) {
-  if (p.r.max_rows <= 0 || p.r.max_rows > 64 || p.vocab <= 0) return hipErrorInvalidValue;
+  if (p.r.max_rows <= 0 || p.r.max_rows > 64 || p.vocab <= 0 || p.vocab > AC_MAX_CHUNKS * AC_CHUNK) return hipErrorInvalidValue;
   if (p.f32) return p.draft_f32 ? accept_types<float, float>(p, s) : accept_types<float, bf16_t>(p, s);
   return p.draft_f32 ? accept_types<bf16_t, float>(p, s) : accept_types<bf16_t, bf16_t>(p, s);
 }

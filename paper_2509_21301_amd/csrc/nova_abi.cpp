@@ -1084,8 +1084,9 @@ extern "C" int nova_kv_keep(const nova_cache* cache, int layers, const nova_rows
   if ((int64_t)rows->batch * layers > (1 << 24) / cache->n_kv) return fail(NOVA_EUNSUPPORTED, "keep: %d sequences, %d layers and %d heads", rows->batch, layers, cache->n_kv);
   if (!n_keep || !aligned4(n_keep) || !aligned4(path) || !aligned4(ctx_out)) return fail(NOVA_EINVAL, "n_keep null, or an array misaligned");
   const size_t bytes = (size_t)rows->batch * sizeof(int32_t);
-  if (ctx_out && ((rows->ctx && overlap(ctx_out, bytes, rows->ctx, bytes)) || overlap(ctx_out, bytes, n_keep, bytes)))
-    return fail(NOVA_EINVAL, "ctx_out may not lie over ctx or n_keep");
+  if (ctx_out && ((rows->ctx && overlap(ctx_out, bytes, rows->ctx, bytes)) || overlap(ctx_out, bytes, n_keep, bytes) ||
+                  (path && overlap(ctx_out, bytes, path, bytes * rows->max_rows))))
+    return fail(NOVA_EINVAL, "ctx_out may not lie over ctx, n_keep or path");
   hipStream_t s = (hipStream_t)stream;
   const nova::KeepArgs a{pool_layer(*cache, 0), layers, batch_rows(*rows), path, n_keep, ctx_out};
   CALL(NOVA_KIND_MISC, s, nova::kv_keep(a, s));

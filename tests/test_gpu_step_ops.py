@@ -83,6 +83,17 @@ def test_rotate(gpu_lib, which, types):
             assert torch.equal(x, out) and torch.equal(wide[:, [0, heads + 1]], beside)
 
 
+def test_rotate_back(gpu_lib):
+    """Positions below 0 turn the other way: there and back is where it was, up to the two rotations' roundings."""
+    nova = gpu_lib
+    for a in (AXES[0], AXES[5]):
+        rope, _, fp = _rope_of(nova, dict(a, mscale=1.0))
+        x = torch.randn(50, 3, 2 * sum(a["pairs"]), device="cuda")
+        pos = torch.randint(0, 1 << 20, (len(a["pairs"]), 50), device="cuda", dtype=torch.int32)
+        y = nova.rotate(nova.rotate(x, pos, rope), -pos, rope)
+        assert ((y - x).abs() <= 4 * 2 * fp * 2 * x.abs().amax(-1, keepdim=True)).all()
+
+
 def test_rotate_many_rows(gpu_lib):
     """Rows beyond one workgroup's, its last workgroup in part, and 900 heads (more than a group)."""
     nova = gpu_lib
@@ -259,6 +270,17 @@ def test_accept_at_the_real_vocabulary(gpu_lib, kind):
     """152064 logits, 64 rows of one sequence, nearly flat distributions (the running sums have many borders)."""
     rows = [64, 3]
     _check_accept(gpu_lib, rows, *_accept_case(rows, 152064, 3, F32, kind, spread=0.5))
+
+
+@pytest.mark.parametrize("kind", ["tree", "draft"])
+def test_accept_many_chunks(gpu_lib, kind):
+    """More chunks than lanes (700001 logits: 86), equal large logits among them, a greedy sequence."""
+    rows = [3, 2, 2]
+    starts, logits, draft, ids, masks, t, u = _accept_case(rows, 700001, 12, F32, kind, spread=1.0)
+    logits[3] = 0.0
+    logits[3, [5, 650000, 700000]] = 40.0
+    u[3] = 0.6
+    _check_accept(gpu_lib, rows, starts, logits, draft, ids, masks, t, u)
 
 
 def test_accept_keeps_everything_when_draft_and_target_agree(gpu_lib):

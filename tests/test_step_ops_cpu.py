@@ -81,7 +81,7 @@ def test_keep_refusals():
     def call(c=None, layers=3, r=None, path=FAKE, n=FAKE + 256, out=FAKE + 512):
         return LIB.nova_kv_keep(C.byref(c or _cache()), layers, C.byref(r or _rows(ctx=FAKE + 1024)), path, n, out, None)
     for bad in [dict(c=_cache(type=9)), dict(c=_cache(v=None)), dict(layers=0), dict(r=_rows(tables=None)), dict(r=_rows(max_rows=65, max_ctx=64)),
-                dict(n=None), dict(n=FAKE + 2), dict(path=FAKE + 1), dict(out=FAKE + 3), dict(out=FAKE + 1024), dict(out=FAKE + 1020), dict(out=FAKE + 260)]:
+                dict(n=None), dict(n=FAKE + 2), dict(path=FAKE + 1), dict(out=FAKE + 3), dict(out=FAKE + 1024), dict(out=FAKE + 1020), dict(out=FAKE + 260), dict(out=FAKE + 4)]:
         assert call(**bad) == nova.EINVAL, bad
     assert call(r=_rows(max_ctx=65)) == nova.ENOKV
     for bad in [dict(r=_rows(max_rows=65, max_ctx=1000, max_blocks=70)), dict(layers=1 << 24), dict(c=_cache(n_kv=8192), layers=2000)]:
