@@ -142,8 +142,9 @@ __global__ void __launch_bounds__(256) lora_shrink_kernel(LoraArgs p) {
 // ------------------------------------------------------------------ h = A x, long sequences
 // Workgroup: (tile of 64 RW rows, slice of K), RW blocks of 16 rows a wave.  64 of K at a time go through LDS, loaded a
 // step ahead: an MFMA operand has neighbouring lanes in different rows, and read straight from memory each of its 16 bytes
-// is an access of its own to the address unit (54 of 64 a load, busy for 78% of the time; 4500 rows of 3584 to rank 64
-// took 27 us).  16-byte chunks of a row are turned by its number (chunk c of row r at c ^ (r & 7)): no bank conflicts.
+// is an access of its own to the address unit (54 of 64 a load, and the unit busy for 78% of the time).  16-byte chunks of
+// a row are turned by its number (chunk c of row r at c ^ (r & 7)): no bank conflicts.  3751 rows of 3584 to rank 64: 13.4
+// us, 27 from memory; the floor, reading x, is 5.3.
 template <typename TX, int NX, int RT, int RW>
 __global__ void __launch_bounds__(256) lora_down_kernel(LoraArgs p) {
   constexpr int TM = 64 * RW, XC = TM * 8 / 256, AC = (16 * RT * 8 + 255) / 256;   // chunks of a thread: x, A
@@ -287,7 +288,8 @@ template <int CH> NOVA_DEV int turn_chunk(int n, int c) { return CH >= 8 ? c ^ (
 // Workgroup: (tile of 16 rows, `cols` columns); a wave takes 64 columns at a time, whose B it loads in one run and turns
 // into MFMA operands in LDS of its own, a step ahead; the first step's loads are on their way while h is summed.  Which
 // column of B is which MFMA row is free, so two tiles give a lane 8 consecutive columns of its row of out.  K (here the
-// rank) is 32 a step.
+// rank) is 32 a step.  Bound by latency: 32 tokens with an adapter each of rank 16 onto 4608 columns 5.3 us (the kernel above
+// 3.5), onto 37888 columns 14.6 us, 2.7 TB/s of adapters.
 template <typename TO, int RT>
 __global__ void __launch_bounds__(256) lora_expand_kernel(LoraArgs p) {
   constexpr int KS = (RT + 1) / 2;                           // steps of 32 of the rank
@@ -414,7 +416,10 @@ template <typename T> NOVA_DEV u32x4 pack16(const float* x) {
 
 // Workgroup: (tile of 64 RW rows, `cols` columns), RW blocks of 16 rows a wave, whose h stays in registers.  64 columns of
 // B at a time go through LDS for all four waves, loaded a step ahead (turned as in the kernel above), and what they give
-// goes back through LDS, so that base and out are read and written in runs of a row's 64 columns: see there.
+// goes back through LDS, so that base and out are read and written in runs of a row's 64 columns: see there.  3751 rows onto
+// 37888 columns in bf16, rank 64: 115 to 127 us, 4.5 to 4.9 TB/s of 5.1 that a large copy reaches (162 us with operands
+// and rows straight from memory); rank 16 109, rank 128 149, fp32 233 us.  Rows that start off a line of 128 bytes (37896
+// columns) share each line between two steps: 180 us.
 template <typename TO, int RT, int RW>
 __global__ void __launch_bounds__(256) lora_up_kernel(LoraArgs p) {
   constexpr int KS = (RT + 1) / 2, TM = 64 * RW;
@@ -568,7 +573,7 @@ static hipError_t lora_launch(const LoraArgs& p, int cus, hipStream_t s) {
     hipLaunchKernelGGL((lora_join_kernel<KS, NH>), dim3((unsigned)(((long)p.r.rows * 8 * KS + 255) / 256)), dim3(256), 0, s, p);
   }
   if (hipError_t e = hipGetLastError()) return e;
-  // columns of a workgroup: whole steps, twelve workgroups for each compute unit (4500 rows onto 37888 columns at rank 64:
+  // columns of a workgroup: whole steps, twelve workgroups for each compute unit (3751 rows onto 37888 columns at rank 64:
   // 115 us, 118 with eight, 140 with four)
   LoraArgs q = p;
   const int step = RW ? 64 : 256;
