@@ -323,12 +323,13 @@ __global__ void __launch_bounds__(256) compact_move_kernel(CopyArgs p, PagesArgs
 // Workgroup: a KV head of a layer of a sequence.  Row path[i] of the sequence's rows becomes row i, for i below n_keep:
 // what is read, K and V, is held in LDS until every read is done, so a path may have any order.  Bound by a chain of
 // dependent loads (sequence and path, table, rows): 32 sequences with trees of 64 rows over 28 layers of 4 heads in
-// 9.6 us.
+// 7.8 us (9.6 with all 64 rows in LDS).
+constexpr int KEEP_ROWS = 16;              // rows in LDS: a workgroup of 64 would leave room for four on a compute unit
 template <typename CT, int D>
 __global__ void __launch_bounds__(128) kv_keep_kernel(KeepArgs p) {
   extern __shared__ __align__(16) char sm_raw[];
-  CT* sm_k = reinterpret_cast<CT*>(sm_raw);                 // [rows][D], K then V
-  CT* sm_v = sm_k + (size_t)p.r.max_rows * D;
+  CT* sm_k = reinterpret_cast<CT*>(sm_raw);                 // [KEEP_ROWS][D], K then V
+  CT* sm_v = sm_k + KEEP_ROWS * D;
   __shared__ long sm_from[64], sm_to[64];                   // places of the rows that move: block * 16 + slot in the layer
   __shared__ int sm_moves;
   __shared__ uint8_t sm_exp[2][64];
@@ -370,13 +371,20 @@ __global__ void __launch_bounds__(128) kv_keep_kernel(KeepArgs p) {
   auto k_at = [&](long at, int w) { return reinterpret_cast<u32x4*>(kc + (((base + at / PAGE) * n_kv + h) * PAGE + at % PAGE) * D) + w; };
   auto v_at = [&](long at, int d) { return vc + (((base + at / PAGE) * n_kv + h) * D + d) * PAGE + at % PAGE; };
   auto exp_at = [&](int side, long at) { return (side ? p.c.v_exp : p.c.k_exp) + ((base + at / PAGE) * n_kv + h) * PAGE + at % PAGE; };
-  for (int w = threadIdx.x; w < n * WORDS; w += 128) reinterpret_cast<u32x4*>(sm_k)[w] = *k_at(sm_from[w / WORDS], w % WORDS);
-  for (int w = threadIdx.x; w < n * D; w += 128) sm_v[w] = *v_at(sm_from[w / D], w % D);
-  if (sizeof(CT) == 1 && (int)threadIdx.x < 2 * n) sm_exp[threadIdx.x & 1][threadIdx.x >> 1] = *exp_at(threadIdx.x & 1, sm_from[threadIdx.x >> 1]);
-  __syncthreads();
-  for (int w = threadIdx.x; w < n * WORDS; w += 128) *k_at(sm_to[w / WORDS], w % WORDS) = reinterpret_cast<const u32x4*>(sm_k)[w];
-  for (int w = threadIdx.x; w < n * D; w += 128) *v_at(sm_to[w / D], w % D) = sm_v[w];
-  if (sizeof(CT) == 1 && (int)threadIdx.x < 2 * n) *exp_at(threadIdx.x & 1, sm_to[threadIdx.x >> 1]) = sm_exp[threadIdx.x & 1][threadIdx.x >> 1];
+  // More rows than the LDS holds go by parts of their columns, which do not depend on one another.
+  const int parts = n <= KEEP_ROWS ? 0 : n <= 2 * KEEP_ROWS ? 1 : 2;      // 2^parts of them
+  const int words = WORDS >> parts, dims = D >> parts, wl = __builtin_ctz(words), dl = __builtin_ctz(dims);
+  for (int part = 0; part < 1 << parts; ++part) {
+    const int w0 = part * words, d0 = part * dims;
+    if (part) __syncthreads();
+    for (int i = threadIdx.x; i < n * words; i += 128) reinterpret_cast<u32x4*>(sm_k)[i] = *k_at(sm_from[i >> wl], w0 + (i & (words - 1)));
+    for (int i = threadIdx.x; i < n * dims; i += 128) sm_v[i] = *v_at(sm_from[i >> dl], d0 + (i & (dims - 1)));
+    if (sizeof(CT) == 1 && part == 0 && (int)threadIdx.x < 2 * n) sm_exp[threadIdx.x & 1][threadIdx.x >> 1] = *exp_at(threadIdx.x & 1, sm_from[threadIdx.x >> 1]);
+    __syncthreads();
+    for (int i = threadIdx.x; i < n * words; i += 128) *k_at(sm_to[i >> wl], w0 + (i & (words - 1))) = reinterpret_cast<const u32x4*>(sm_k)[i];
+    for (int i = threadIdx.x; i < n * dims; i += 128) *v_at(sm_to[i >> dl], d0 + (i & (dims - 1))) = sm_v[i];
+    if (sizeof(CT) == 1 && part == 0 && (int)threadIdx.x < 2 * n) *exp_at(threadIdx.x & 1, sm_to[threadIdx.x >> 1]) = sm_exp[threadIdx.x & 1][threadIdx.x >> 1];
+  }
 }
 
 // ------------------------------------------------------------------ launch
@@ -419,7 +427,7 @@ hipError_t compact_move(const CopyArgs& p, const PagesArgs& g, int cus, hipStrea
 
 template <typename CT> static hipError_t keep_launch(const KeepArgs& p, hipStream_t s) {
   const dim3 grid((unsigned)((long)p.r.batch * p.layers * p.c.n_kv));
-  const size_t lds = (size_t)2 * p.r.max_rows * p.c.D * sizeof(CT);
+  const size_t lds = (size_t)2 * KEEP_ROWS * p.c.D * sizeof(CT);
   if (p.c.D == 64) hipLaunchKernelGGL((kv_keep_kernel<CT, 64>), grid, dim3(128), lds, s, p);
   else hipLaunchKernelGGL((kv_keep_kernel<CT, 128>), grid, dim3(128), lds, s, p);
   return hipGetLastError();

@@ -651,3 +651,71 @@ def test_lora_keeps_sequences_apart(gpu_lib):
     out = torch.full_like(want, 3.0)
     nova.lora(nova.Adapters(a, b), short, _i32([0, 1, 2]), x, out=out)
     assert torch.equal(out[:8], want[:8]) and (out[8:23] == 3.0).all() and torch.equal(out[23:], want[23:])
+
+
+# ----------------------------------------------------------------------------- offsets beyond 32 bits
+def test_far_rows(gpu_lib):
+    """Rows, logits and outputs whose elements lie past 2^32: the last ones against the same rows by themselves."""
+    nova = gpu_lib
+    rope = nova.Rope(32, axes=(8, 8))
+    x = torch.zeros(70000, 1 << 16, dtype=BF16, device="cuda")                            # 4.6e9 elements
+    x[-3:, :64] = torch.randn(3, 64, device="cuda")
+    pos = _i32(np.stack([np.arange(70000) % 97, np.arange(70000) % 89]))
+    rows = x[:, :64].unflatten(1, (2, 32))
+    want = nova.rotate(rows[-3:].contiguous(), pos[:, -3:].contiguous(), rope)
+    nova.rotate(rows, pos, rope, out=rows)
+    assert torch.equal(rows[-3:], want)
+    del x, rows
+    n, vocab = 32768, 152064                                                              # 5.0e9 logits
+    logits = torch.zeros(n, vocab, dtype=BF16, device="cuda")
+    logits[-64:] = (torch.randn(64, vocab, device="cuda") * 4).to(BF16)
+    ids, u = torch.randint(0, vocab, (n,), device="cuda", dtype=torch.int32), torch.rand(n, device="cuda")
+    ids[-63] = logits[-64].argmax()
+    temperature = torch.full((512,), 0.0, device="cuda")
+    temperature[-1] = 0.2
+    tables = torch.zeros(512, 4, dtype=torch.int32, device="cuda")
+    got = nova.accept(nova.Rows(None, None, tables, max_rows=64, max_ctx=64), ids, logits, u, temperature=temperature)
+    want = nova.accept(nova.Rows(None, None, tables[:1], max_rows=64, max_ctx=64), ids[-64:].contiguous(), logits[-64:], u[-64:].contiguous(),
+                       temperature=temperature[-1:].contiguous())
+    for a, b in zip(got, want):
+        assert torch.equal(a[-1:], b)
+    wp, wt, _ = st.accept(_np(logits[-64:]), ids[-64:].tolist(), u[-64:].double().tolist(), t=0.2)
+    assert got[1][-1, :len(wp)].tolist() == wp and got[2][-1, :len(wt)].tolist() == wt
+    del logits, got, want
+    n, wide = 120000, 37888                                                               # 4.5e9 results
+    ad = nova.Adapters(torch.randn(2, 8, 16, device="cuda").to(BF16), torch.randn(2, wide, 8, device="cuda").to(BF16))
+    x = torch.randn(n, 16, device="cuda").to(BF16)
+    many = nova.Rows(_i32([0, 100000, n]), None, tables[:2], rows=n, max_rows=n, max_ctx=64)
+    out = nova.lora(ad, many, _i32([0, 1]), x)
+    few = nova.Rows(_i32([0, 32 * 4]), None, tables[:1], rows=128, max_rows=128, max_ctx=64)
+    assert torch.equal(out[-32:], nova.lora(ad, few, _i32([1]), x[-128:].contiguous())[-32:])
+
+
+def test_far_blocks(gpu_lib):
+    """A pool of more than 2^32 bytes of K: copies, forks, kept rows and a compaction among its last blocks."""
+    nova = gpu_lib
+    blocks = 140000
+    c = nova.Cache(blocks, 4, 128, nova.CACHE_F32)
+    last = c.k[0, -6:], c.v[0, -6:]
+    for t in last:
+        t.normal_()
+    k0, v0 = (t.clone() for t in last)
+    nova.kv_copy(c, _i32([blocks - 1]), _i32([blocks - 6]))
+    assert torch.equal(c.k[0, -6], k0[5]) and torch.equal(c.v[0, -6], v0[5])
+    tables = _i32([[blocks - 4, blocks - 3, -1], [-1, -1, -1]])
+    desc = nova.Rows(None, _i32([10, 10]), tables, max_rows=12, max_ctx=32)
+    ctx = nova.kv_keep(c, desc, _i32([[0, 3, 11] + [-1] * 9, [-1] * 12]), _i32([3, 0]))
+    assert ctx.tolist() == [13, 10]
+    assert torch.equal(c.k[0, -4, :, 11], k0[2, :, 13]) and torch.equal(c.k[0, -4, :, 12], k0[3, :, 5])
+    assert torch.equal(c.v[0, -4, :, :, 11], v0[2, :, :, 13]) and torch.equal(c.v[0, -4, :, :, 12], v0[3, :, :, 5])
+    pages = nova.Pages(blocks)
+    pages.refs[:-2] = 1
+    pages.refs[-4:-2] = 1
+    pages.refs[7] = 0
+    assert pages.fork(c, tables, _i32([0]), _i32([1]), _i32([20])).tolist() == [1]
+    assert tables[1].tolist() == [blocks - 4, 7, -1] and torch.equal(c.k[0, 7], c.k[0, -3]) and torch.equal(c.v[0, 7], c.v[0, -3])
+    pages.refs[3] = 0
+    kept = c.k[0, -3].clone(), c.v[0, -3].clone()
+    assert pages.compact(c, tables).tolist() == [blocks - 3]
+    assert tables.tolist() == [[blocks - 4, 3, -1], [blocks - 4, 7, -1]]
+    assert torch.equal(c.k[0, 3], kept[0]) and torch.equal(c.v[0, 3], kept[1])
