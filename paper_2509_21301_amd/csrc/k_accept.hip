@@ -71,11 +71,14 @@ NOVA_DEV SeqRows seq_of_row(const BatchRows& p, int r, int* b) {
   return SeqRows{0, 0, 0};
 }
 
-// log2(e) / T, 0 for T = 0 (the largest logit takes all), negative where T gives no distribution.
-NOVA_DEV double inv_temperature(const AcceptArgs& p, int b) {
+// A sequence's temperature T: inv = log2(e) / T, 0 for T = 0 (the largest logit takes all), negative where T gives no
+// distribution; least: the difference of logits below which every weight is 0.
+struct Heat { double inv, least; };
+NOVA_DEV Heat heat_of(const AcceptArgs& p, int b) {
   const float t = p.temperature ? p.temperature[b] : 1.f;
-  if (t == 0.f) return 0.0;
-  return t > 0.f && t < INFINITY ? 1.4426950408889634 / (double)t : -1.0;
+  if (t == 0.f) return Heat{0.0, 0.0};
+  if (!(t > 0.f && t < INFINITY)) return Heat{-1.0, 0.0};
+  return Heat{1.4426950408889634 / (double)t, -762.4618986159398 * (double)t};     // 2^-1100 and below
 }
 
 // 2^z for z <= 0 in 64 bits (0 below 2^-1074 and for -infinity): z = k + j / 256 + f with |f| <= 2^-9, the table's
@@ -94,7 +97,7 @@ NOVA_DEV void fill_table(Exp2Table& tab) { // by the workgroup's threads; a barr
     tab.t[j] = j ? y * 1.4142135623730951 : 1.0;   // the largest logit's weight is 1 exactly
   }
 }
-// 2^(d inv), d <= 0 and at least -1100 / inv.
+// 2^(d inv), d <= 0 and d inv at least -1100.
 NOVA_DEV double exp2_times(const Exp2Table& tab, double d, double inv) {
   constexpr double MAGIC = 0x1.8p44;       // a sum with it ends at the 8th binary place
   const double t = fma(d, inv, MAGIC), f = fma(d, inv, -(t - MAGIC));
@@ -110,9 +113,10 @@ NOVA_DEV double exp2_neg(const Exp2Table& tab, double z) { return exp2_times(tab
 // Weights of logits relative to a maximum m at log2(e) / T = inv: the difference first (it is exact, where a product with a
 // small temperature's inverse would not cancel at the maximum).
 struct Weigh {
-  double m, inv, least;
-  NOVA_DEV Weigh(float m, double inv) : m(m), inv(inv), least(-1100.0 / inv) {}
-  NOVA_DEV double operator()(const Exp2Table& tab, float x) const { return exp2_times(tab, fmax((double)x - m, least), inv); }
+  double m;
+  Heat h;
+  NOVA_DEV Weigh(float m, const Heat& h) : m(m), h(h) {}
+  NOVA_DEV double operator()(const Exp2Table& tab, float x) const { return exp2_times(tab, fmax((double)x - m, h.least), h.inv); }
 };
 constexpr double LN2 = 0.6931471805599453;
 
@@ -191,7 +195,7 @@ __global__ void __launch_bounds__(256) accept_stats_kernel(AcceptArgs p) {
   __shared__ Exp2Table tab;
   __shared__ float sm_m[4];
   __shared__ int sm_arg[4];
-  const double inv = inv_temperature(p, b);
+  const Heat h = heat_of(p, b);
   fill_table(tab);                         // while the logits are on their way
   float m = x[0];
 #pragma unroll
@@ -201,14 +205,14 @@ __global__ void __launch_bounds__(256) accept_stats_kernel(AcceptArgs p) {
   __syncthreads();
   m = nan_max(nan_max(sm_m[0], sm_m[1]), nan_max(sm_m[2], sm_m[3]));
   double sum = 0.0;
-  if (inv > 0.0 && m > -INFINITY && m < INFINITY) {
-    const Weigh weight(m, inv);
+  if (h.inv > 0.0 && m > -INFINITY && m < INFINITY) {
+    const Weigh weight(m, h);
 #pragma unroll
     for (int i = 0; i < AC_PER; ++i) sum += weight(tab, x[i]);
   }
   sum = wave_sum64(sum);
   int arg = 0x7FFFFFFF;
-  if (inv == 0.0) {                        // greedy: the first of the largest
+  if (h.inv == 0.0) {                        // greedy: the first of the largest
 #pragma unroll
     for (int i = 0; i < AC_PER; ++i)
       if (x[i] == m) arg = min(arg, c0 + (draft ? place_of<TD>(i) : place_of<TL>(i)));
@@ -230,11 +234,11 @@ __global__ void __launch_bounds__(256) accept_stats_kernel(AcceptArgs p) {
 // ------------------------------------------------------------------ a row's chunks joined
 // m: the row's maximum (NaN: no distribution), s: its sum relative to it, arg: the first of the largest logits.
 struct RowStats { float m; int arg; double s; };
-NOVA_DEV bool has_dist(const RowStats& a, double inv) { return a.m > -INFINITY && inv >= 0.0; }   // NaN compares false
+NOVA_DEV bool has_dist(const RowStats& a, const Heat& h) { return a.m > -INFINITY && h.inv >= 0.0; }   // NaN compares false
 
 // A lane's chunks of a row: a request for all that is known of them (of more than 64 chunks those before are joined).
 struct LaneParts { float m; int arg; double s; };
-NOVA_DEV LaneParts lane_parts(const AcceptArgs& p, const Exp2Table& tab, int item, double inv) {
+NOVA_DEV LaneParts lane_parts(const AcceptArgs& p, const Exp2Table& tab, int item, const Heat& h) {
   const long at = (long)item * p.chunks;
   LaneParts a{-INFINITY, 0x7FFFFFFF, 0.0};
   for (int c = threadIdx.x & 63; c < p.chunks; c += 64) {
@@ -245,23 +249,23 @@ NOVA_DEV LaneParts lane_parts(const AcceptArgs& p, const Exp2Table& tab, int ite
       continue;
     }
     const float m = nan_max(a.m, n.m);
-    const double of_a = a.m > -INFINITY ? a.s * exp2_neg(tab, ((double)a.m - (double)m) * inv) : 0.0;
-    const double of_n = n.m > -INFINITY ? n.s * exp2_neg(tab, ((double)n.m - (double)m) * inv) : 0.0;
+    const double of_a = a.m > -INFINITY ? a.s * exp2_neg(tab, ((double)a.m - (double)m) * h.inv) : 0.0;
+    const double of_n = n.m > -INFINITY ? n.s * exp2_neg(tab, ((double)n.m - (double)m) * h.inv) : 0.0;
     a.arg = n.m > a.m ? n.arg : a.arg;
     a.m = m, a.s = of_a + of_n;
   }
   return a;
 }
 // By one wave; every lane returns the same.
-NOVA_DEV RowStats join_parts(const Exp2Table& tab, const LaneParts& l, double inv) {
+NOVA_DEV RowStats join_parts(const Exp2Table& tab, const LaneParts& l, const Heat& h) {
   RowStats a{wave_nan_max(l.m), 0x7FFFFFFF, 0.0};
   if (!(a.m > -INFINITY)) return a;
-  if (inv == 0.0) {
+  if (h.inv == 0.0) {
     a.arg = l.m == a.m ? l.arg : 0x7FFFFFFF;
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) a.arg = min(a.arg, __shfl_xor(a.arg, o, 64));
-  } else if (inv > 0.0) {
-    a.s = wave_sum64(l.m > -INFINITY ? l.s * exp2_neg(tab, ((double)l.m - (double)a.m) * inv) : 0.0);
+  } else if (h.inv > 0.0) {
+    a.s = wave_sum64(l.m > -INFINITY ? l.s * exp2_neg(tab, ((double)l.m - (double)a.m) * h.inv) : 0.0);
   }
   return a;
 }
@@ -318,14 +322,14 @@ template <int SIZE, int THREADS, typename F> NOVA_DEV int draw_in_part(int c0, i
 }
 
 // A token drawn from a target row by its number u; by the whole workgroup.  -1: the row has no distribution.
-template <int THREADS, typename TL> NOVA_DEV int draw_row(const AcceptArgs& p, const Exp2Table& tab, int r, const RowStats& a, double inv, float u) {
-  if (!has_dist(a, inv)) return -1;
-  if (inv == 0.0) return a.arg;
+template <int THREADS, typename TL> NOVA_DEV int draw_row(const AcceptArgs& p, const Exp2Table& tab, int r, const RowStats& a, const Heat& h, float u) {
+  if (!has_dist(a, h)) return -1;
+  if (h.inv == 0.0) return a.arg;
   const TL* row = (const TL*)p.logits + (long)r * p.row;
   const long at = (long)r * p.chunks;
   double before = 0.0;
   const double target = uniform(u) * a.s;
-  const Weigh weight(a.m, inv);
+  const Weigh weight(a.m, h);
   auto scale = [&](float m) { return m > -INFINITY ? weight(tab, m) : 0.0; };
   // the parts' sums side by side in LDS, requested together
   __shared__ double sm_parts[AC_MAX_CHUNKS * AC_PARTS];
@@ -336,10 +340,10 @@ template <int THREADS, typename TL> NOVA_DEV int draw_row(const AcceptArgs& p, c
 }
 
 // log p of a token of a row.
-template <typename TL> NOVA_DEV float log_p(const AcceptArgs& p, int r, const RowStats& a, double inv, int token) {
+template <typename TL> NOVA_DEV float log_p(const AcceptArgs& p, int r, const RowStats& a, const Heat& h, int token) {
   if (token < 0) return __uint_as_float(0x7FC00000u);
-  if (inv == 0.0) return 0.f;
-  return (float)(((double)logit((const TL*)p.logits + (long)r * p.row, token) - (double)a.m) * inv * LN2 - log(a.s));
+  if (h.inv == 0.0) return 0.f;
+  return (float)(((double)logit((const TL*)p.logits + (long)r * p.row, token) - (double)a.m) * h.inv * LN2 - log(a.s));
 }
 
 // The workgroups of a sequence that have come this far, this one included; what each stored before (with
@@ -367,13 +371,13 @@ __global__ void __launch_bounds__(256) accept_follow_kernel(AcceptArgs p) {
   const SeqRows sr = seq_of_row(p.r, r, &b);
   if (b >= p.r.batch || r < sr.r0 || r >= sr.r0 + sr.n) return;
   const float u = p.u[r];
-  const double inv = inv_temperature(p, b);
+  const Heat h = heat_of(p, b);
   __syncthreads();
-  const RowStats a = join_parts(tab, lane_parts(p, tab, r, inv), inv);
-  const int token = draw_row<AC_THREADS, TL>(p, tab, r, a, inv, u);
+  const RowStats a = join_parts(tab, lane_parts(p, tab, r, h), h);
+  const int token = draw_row<AC_THREADS, TL>(p, tab, r, a, h, u);
   if (threadIdx.x == 0) {
     put(p.row_token + r, token);
-    put(p.row_lp + r, log_p<TL>(p, r, a, inv, token));
+    put(p.row_lp + r, log_p<TL>(p, r, a, h, token));
   }
   if (arrive(p.counters + b) != (unsigned)sr.n) return;
   if (threadIdx.x >= 64) return;
@@ -422,8 +426,8 @@ __global__ void __launch_bounds__(AC_TEST) accept_draft_kernel(AcceptArgs p) {
   const SeqRows sr = seq_rows(p.r, b);
   if (sr.n <= 0) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const double inv = inv_temperature(p, b);
-  __shared__ float sm_lp[64];
+  const Heat h = heat_of(p, b);
+  __shared__ double sm_z[64], sm_s[64];    // of a kept row's token: its logit relative to the maximum, and the row's sum
   __shared__ int sm_kept[AC_WAVES], sm_rest[AC_WAVES];   // of a wave's row: its token is kept; else what remains of p is drawn from
   __shared__ RowStats sm_p[AC_WAVES], sm_q[AC_WAVES];
   __shared__ Exp2Table tab;
@@ -441,26 +445,25 @@ __global__ void __launch_bounds__(AC_TEST) accept_draft_kernel(AcceptArgs p) {
       const bool test = j < sr.n, in = (unsigned)x < (unsigned)p.vocab;
       const float u = p.u[next], lx = logit((const TL*)p.logits + (long)r * p.row, in ? x : 0),
                   dx = test ? logit((const TD*)p.draft + (long)next * p.draft_row, in ? x : 0) : 0.f;
-      const LaneParts lp_ = lane_parts(p, tab, r, inv), lq = test ? lane_parts(p, tab, p.r.rows + next, inv) : LaneParts{-INFINITY, 0, 0.0};
-      const RowStats a = join_parts(tab, lp_, inv), q = join_parts(tab, lq, inv);
+      const LaneParts lp_ = lane_parts(p, tab, r, h), lq = test ? lane_parts(p, tab, p.r.rows + next, h) : LaneParts{-INFINITY, 0, 0.0};
+      const RowStats a = join_parts(tab, lp_, h), q = join_parts(tab, lq, h);
       bool kept = false, some = false;
-      float lp = 0.f;
-      if (test && has_dist(a, inv)) {
-        if (inv == 0.0) {
+      double zp = 0.0;
+      if (test && has_dist(a, h)) {
+        if (h.inv == 0.0) {
           kept = x == a.arg;
         } else {
-          some = has_dist(q, inv);
-          if (in && some) {
-            const double zp = ((double)lx - (double)a.m) * inv, zq = ((double)dx - (double)q.m) * inv;
-            kept = uniform(u) * (exp2_neg(tab, zq) / q.s) < exp2_neg(tab, zp) / a.s;
-            lp = (float)(zp * LN2 - log(a.s));
+          some = has_dist(q, h);
+          if (in && some) {                // u q(x) < p(x), times both sums
+            zp = ((double)lx - (double)a.m) * h.inv;
+            kept = uniform(u) * exp2_neg(tab, ((double)dx - (double)q.m) * h.inv) * a.s < exp2_neg(tab, zp) * q.s;
           }
         }
       }
       if (lane == 0) {
         sm_kept[wave] = kept, sm_rest[wave] = some && !kept;
         sm_p[wave] = a, sm_q[wave] = q;
-        if (kept) sm_lp[j - 1] = lp;
+        if (kept) sm_z[j - 1] = zp, sm_s[j - 1] = a.s;
       }
     } else if (lane == 0) {
       sm_kept[wave] = 0;
@@ -484,7 +487,7 @@ __global__ void __launch_bounds__(AC_TEST) accept_draft_kernel(AcceptArgs p) {
     const TD* rq = (const TD*)p.draft + (long)(r + 1) * p.draft_row;
     // times p's sum, so that equal logits of the target weigh exactly 1 and their running sums are exact
     const double iq = tp.s / tq.s;
-    const Weigh wp(tp.m, inv), wq(tq.m, inv);
+    const Weigh wp(tp.m, h), wq(tq.m, h);
     auto more = [&](int i) {
       const double d = wp(tab, logit(rp, i)) - wq(tab, logit(rq, i)) * iq;
       return d > 0.0 ? d : 0.0;
@@ -515,11 +518,11 @@ __global__ void __launch_bounds__(AC_TEST) accept_draft_kernel(AcceptArgs p) {
       const int c = first_above(shares, target, &before, [&](int i) { return sm_shares[i]; });
       token = draw_in_part<SHARE, AC_TEST>(c * SHARE, p.vocab, target - before, more);
     } else {                               // nothing is left by rounding: p and q are alike
-      token = draw_row<AC_TEST, TL>(p, tab, r, tp, inv, u);
+      token = draw_row<AC_TEST, TL>(p, tab, r, tp, h, u);
     }
   } else {
     if (chunk != 0) return;
-    token = draw_row<AC_TEST, TL>(p, tab, r, tp, inv, u);
+    token = draw_row<AC_TEST, TL>(p, tab, r, tp, h, u);
   }
   const int i = threadIdx.x;
   if (i == 0) p.n_keep[b] = at + 1;
@@ -527,7 +530,7 @@ __global__ void __launch_bounds__(AC_TEST) accept_draft_kernel(AcceptArgs p) {
     const long o = (long)b * p.r.max_rows + i;
     p.path[o] = i <= at ? i : -1;
     p.tokens[o] = i < at ? p.ids[sr.r0 + i + 1] : i == at ? token : -1;
-    p.lp[o] = i < at ? sm_lp[i] : i == at ? log_p<TL>(p, r, tp, inv, token) : 0.f;
+    p.lp[o] = i < at ? (h.inv == 0.0 ? 0.f : (float)(sm_z[i] * LN2 - log(sm_s[i]))) : i == at ? log_p<TL>(p, r, tp, h, token) : 0.f;
   }
 }
 
