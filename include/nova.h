@@ -411,7 +411,8 @@ int nova_pages_extend(const nova_pages* pages, int32_t* tables, int max_blocks, 
 /* Row dst[i] of the tables becomes the first tokens[i] tokens of row src[i] (device int32 [n] each): whole blocks are
  * shared, the last one, if tokens[i] fills it only in part, is copied in `layers` layers to a block that is taken.  What
  * row dst[i] named before is overwritten (give it up first).  Refused (done[i] 0): rows outside the tables, a target
- * that is another request's source, or of an earlier request, tokens beyond the source's blocks. */
+ * that is a request's source (its own or another's: no source is overwritten) or an earlier request's target (served or
+ * not), tokens beyond the source's blocks. */
 int nova_pages_fork(const nova_pages* pages, const nova_cache* cache, int layers, int32_t* tables, int max_blocks, int batch,
                     const int32_t* src, const int32_t* dst, const int32_t* tokens, int n, int32_t* done, void* ws,
                     size_t ws_bytes, nova_stream_t stream);

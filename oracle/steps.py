@@ -174,7 +174,7 @@ class Pool:
         inside = lambda r: 0 <= r < batch  # noqa: E731
         for i, (a, b, n) in enumerate(zip(src, dst, tokens)):
             blocks = -(-int(n) // PAGE)
-            ok = inside(a) and inside(b) and 0 <= n and blocks <= width and b not in dst[:i] and a not in [d for d in dst if inside(d)]
+            ok = inside(a) and inside(b) and 0 <= n and blocks <= width and b not in dst[:i] and b not in src
             ok = ok and all(self._named(x) for x in self.tables[a, :blocks])
             if ok and n % PAGE:
                 asked += 1

@@ -141,21 +141,28 @@ template <int E> __global__ void __launch_bounds__(PLAN) pages_extend_kernel(Pag
 
 // ------------------------------------------------------------------ forks
 // Fork i: row dst[i] of the tables becomes the first lens[i] tokens of row src[i].  Refused (done 0, nothing changed):
-// rows outside the tables, a row that is another fork's target too (the first of them counts) or a target that is a
-// source, lengths that the source's pages do not cover, and forks behind the pool's last free block.
+// rows outside the tables, a target that is any request's source (so no source is overwritten, whatever the order) or an
+// earlier request's target (be that one served or not), lengths that the source's pages do not cover, and forks behind the
+// pool's last free block.
+constexpr int MAX_BATCH = 1 << 16;
 template <int E> __global__ void __launch_bounds__(PLAN) pages_fork_kernel(PagesArgs p) {
+  __shared__ unsigned sm_source[MAX_BATCH / 32];            // a bit for every row: it is a source
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for (int b = threadIdx.x; b < p.batch; b += PLAN) __hip_atomic_store(p.claim + b, 0x7FFFFFFF, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  for (int w = threadIdx.x; w < (p.batch + 31) / 32; w += PLAN) sm_source[w] = 0u;
   __syncthreads();
-  for (int i = threadIdx.x; i < p.n; i += PLAN)
-    if ((unsigned)p.dst[i] < (unsigned)p.batch) __hip_atomic_fetch_min(p.claim + p.dst[i], i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  for (int i = threadIdx.x; i < p.n; i += PLAN) {
+    const int src = p.src[i], dst = p.dst[i];
+    if ((unsigned)src < (unsigned)p.batch) atomicOr(sm_source + (src >> 5), 1u << (src & 31));
+    if ((unsigned)dst < (unsigned)p.batch) __hip_atomic_fetch_min(p.claim + dst, i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
   __syncthreads();
   for (int i = wave; i < p.n; i += PLAN / 64) {
     const int src = p.src[i], dst = p.dst[i], len = p.lens[i];
     const long blocks = ((long)len + PAGE - 1) / PAGE;
     bool ok = (unsigned)src < (unsigned)p.batch && (unsigned)dst < (unsigned)p.batch && len >= 0 && blocks <= p.max_blocks;
     if (ok) ok = __hip_atomic_load(p.claim + dst, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == i &&
-                 __hip_atomic_load(p.claim + src, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 0x7FFFFFFF;
+                 !(sm_source[dst >> 5] >> (dst & 31) & 1);
     bool miss = false;
     if (ok)
       for (int e = lane; e < blocks; e += 64) miss |= !in_pool(p.tables[(long)src * p.max_blocks + e], p.num_blocks);
@@ -399,7 +406,10 @@ __global__ void __launch_bounds__(128) kv_keep_kernel(KeepArgs p) {
     return hipGetLastError();                                                                                          \
   } while (0)
 hipError_t pages_extend(const PagesArgs& p, hipStream_t s) { PLAN_LAUNCH(pages_extend_kernel); }
-hipError_t pages_fork(const PagesArgs& p, hipStream_t s) { PLAN_LAUNCH(pages_fork_kernel); }
+hipError_t pages_fork(const PagesArgs& p, hipStream_t s) {
+  if (p.batch > MAX_BATCH) return hipErrorInvalidValue;
+  PLAN_LAUNCH(pages_fork_kernel);
+}
 hipError_t pages_compact(const PagesArgs& p, hipStream_t s) { PLAN_LAUNCH(pages_compact_kernel); }
 hipError_t pages_free(const PagesArgs& p, hipStream_t s) {
   const int x = std::min(64, (p.max_blocks + 255) / 256);

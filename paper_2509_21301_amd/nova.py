@@ -965,7 +965,8 @@ class Pages:
 
     def fork(self, cache, tables, src, dst, tokens, stream=None):
         """Rows ``dst`` of the tables become the first ``tokens`` tokens of rows ``src`` (int32 [n] each): whole blocks are
-        shared, a last one in part is copied in every layer of ``cache``.  What the rows named before is overwritten."""
+        shared, a last one in part is copied in every layer of ``cache``.  What the rows named before is overwritten.  Not
+        served: a target that is a source of the call, or an earlier request's target."""
         batch, width = self._tables(tables)
         _check_device(self.device, cache.k, tables, src, dst, tokens)
         n = dst.shape[0] if dst.dim() == 1 else 0
