@@ -398,6 +398,9 @@ int nova_kv_copy(const nova_cache* src, const nova_cache* dst, int layers, const
  * [batch][max_blocks], an entry outside the pool names no block.  What is taken are always the lowest free blocks, in the
  * order of the requests; a request is served (done 1) if it and the requests before it find enough, and else left as it
  * was (done 0).  Calls on one pool are made one after the other (on one stream, say).  At most 65535 requests.
+ * Rows share whole pages only, and none of these calls leaves a row ending inside a page that another names: rows append
+ * behind what they share.  (A program that lowers a row's ctx by itself, or forks more tokens than the source holds, has
+ * to see to that.)
  *  ws: device, nova_pages_workspace_bytes(), 256-byte aligned, as for nova_tree_attention */
 typedef struct {
   int32_t* refs;    /* device [num_blocks], all 0 at first */
@@ -416,10 +419,15 @@ int nova_pages_extend(const nova_pages* pages, int32_t* tables, int max_blocks, 
 int nova_pages_fork(const nova_pages* pages, const nova_cache* cache, int layers, int32_t* tables, int max_blocks, int batch,
                     const int32_t* src, const int32_t* dst, const int32_t* tokens, int n, int32_t* done, void* ws,
                     size_t ws_bytes, nova_stream_t stream);
-/* Rows seqs[i] give up what lies behind their first tokens[i] tokens (device int32 [n] each; tokens NULL: everything);
- * the entries become -1. */
+/* Rows seqs[i] (device int32 [n]) give up everything; their entries become -1.  tokens: NULL (see nova_pages_trim). */
 int nova_pages_free(const nova_pages* pages, int32_t* tables, int max_blocks, int batch, const int32_t* seqs,
                     const int32_t* tokens, int n, nova_stream_t stream);
+/* Rows seqs[i] give up what lies behind their first tokens[i] tokens (device int32 [n] each); the entries become -1.  The
+ * row goes on in the page that it keeps in part, so a request whose page is named by other entries too (counts as they
+ * were before the call) is refused: done[i] 0, the row left as it was (device int32 [n]; 0 also for rows outside the
+ * tables).  nova_pages_fork gives such tokens to another row with a copy of that page, after which this one can be freed. */
+int nova_pages_trim(const nova_pages* pages, int32_t* tables, int max_blocks, int batch, const int32_t* seqs,
+                    const int32_t* tokens, int n, int32_t* done, nova_stream_t stream);
 /* Move the pool's used blocks to its front: of `live` of them those at live and above go to the free ones below, in order,
  * in `layers` layers, and tables and refs follow (refs_out, tables_out: of their shapes, or refs and tables themselves;
  * entries that name no used block become -1).  live_out: device int32 [1], or NULL.  Every table that names blocks of the

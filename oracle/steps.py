@@ -195,14 +195,19 @@ class Pool:
         return done, copies
 
     def free(self, seqs, tokens=None):
-        for i, row in enumerate(seqs):
-            if not 0 <= row < len(self.tables):
-                continue
-            keep = 0 if tokens is None else -(-max(0, int(tokens[i])) // PAGE)
-            for e in range(keep, self.tables.shape[1]):
+        """With tokens: which requests are served; one whose page kept in part others name too (before the call) is not."""
+        keeps = [0] * len(seqs) if tokens is None else [max(0, int(n)) for n in tokens]
+        done = [int(0 <= row < len(self.tables)) for row in seqs]
+        for i, (row, n) in enumerate(zip(seqs, keeps)):
+            if done[i] and n % PAGE and n // PAGE < self.tables.shape[1]:
+                block = self.tables[row, n // PAGE]
+                done[i] = int(not self._named(block) or self.refs[block] <= 1)
+        for row, n, ok in zip(seqs, keeps, done):
+            for e in range(-(-n // PAGE), self.tables.shape[1]) if ok else ():
                 if self._named(self.tables[row, e]):
                     self.refs[self.tables[row, e]] -= 1
                 self.tables[row, e] = -1
+        return done
 
     def compact(self):
         used = self.refs > 0

@@ -189,11 +189,26 @@ template <int E> __global__ void __launch_bounds__(PLAN) pages_fork_kernel(Pages
 }
 
 // ------------------------------------------------------------------ pages given up
-// Row seqs[i] of the tables keeps the pages of its first lens[i] tokens (lens null: none).  An entry is taken out of
+// Request i with lens keeps the pages of row src[i]'s first lens[i] tokens.  What the row appends next goes into the page
+// that is kept in part, so that has to be the row's own: one that other entries name too is refused, by the counts
+// before anything is given up (a launch of its own, since requests of one call may share pages).
+__global__ void __launch_bounds__(256) pages_trim_kernel(PagesArgs p) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= p.n) return;
+  const int row = p.src[i], len = max(p.lens[i], 0), last = len / PAGE;     // the page that holds token len
+  bool ok = (unsigned)row < (unsigned)p.batch;
+  if (ok && len % PAGE && last < p.max_blocks) {
+    const int block = p.tables[(long)row * p.max_blocks + last];
+    ok = !in_pool(block, p.num_blocks) || p.refs[block] <= 1;
+  }
+  p.done[i] = ok;
+}
+
+// Row src[i] of the tables keeps the pages of its first lens[i] tokens (lens null: none).  An entry is taken out of
 // the table by one thread, whoever else is at it.
 __global__ void __launch_bounds__(256) pages_free_kernel(PagesArgs p) {
   const int row = p.src[blockIdx.y];
-  if ((unsigned)row >= (unsigned)p.batch) return;
+  if ((unsigned)row >= (unsigned)p.batch || (p.lens && !p.done[blockIdx.y])) return;
   const int len = p.lens ? max(p.lens[blockIdx.y], 0) : 0;
   const int keep = (int)(((long)len + PAGE - 1) / PAGE);
   for (int e = keep + blockIdx.x * 256 + threadIdx.x; e < p.max_blocks; e += gridDim.x * 256) {
@@ -412,6 +427,10 @@ hipError_t pages_fork(const PagesArgs& p, hipStream_t s) {
 }
 hipError_t pages_compact(const PagesArgs& p, hipStream_t s) { PLAN_LAUNCH(pages_compact_kernel); }
 hipError_t pages_free(const PagesArgs& p, hipStream_t s) {
+  if (p.lens) {
+    hipLaunchKernelGGL(pages_trim_kernel, dim3((p.n + 255) / 256), dim3(256), 0, s, p);
+    if (hipError_t e = hipGetLastError()) return e;
+  }
   const int x = std::min(64, (p.max_blocks + 255) / 256);
   hipLaunchKernelGGL(pages_free_kernel, dim3(x, p.n), dim3(256), 0, s, p);
   return hipGetLastError();

@@ -1193,16 +1193,32 @@ extern "C" int nova_pages_fork(const nova_pages* pages, const nova_cache* cache,
   return NOVA_OK;
 }
 
+namespace {
+int give_up(const nova_pages* pages, int32_t* tables, int max_blocks, int batch, const int32_t* seqs, const int32_t* tokens, int n,
+            int32_t* done, hipStream_t s) {
+  nova::PagesArgs a = pages_args(pages, tables, max_blocks, batch);
+  a.src = seqs, a.lens = tokens, a.n = n, a.done = done;
+  CALL(NOVA_KIND_MISC, s, nova::pages_free(a, s));
+  return NOVA_OK;
+}
+}  // namespace
+
+extern "C" int nova_pages_trim(const nova_pages* pages, int32_t* tables, int max_blocks, int batch, const int32_t* seqs,
+                               const int32_t* tokens, int n, int32_t* done, nova_stream_t stream) {
+  if (int rc = check_pages(pages, tables, max_blocks, batch, n)) return rc;
+  if (n == 0) return NOVA_OK;
+  for (const void* o : {(const void*)seqs, (const void*)tokens, (const void*)done})
+    if (!o || !aligned4(o)) return fail(NOVA_EINVAL, "seqs, tokens and done must be non-null and aligned");
+  return give_up(pages, tables, max_blocks, batch, seqs, tokens, n, done, (hipStream_t)stream);
+}
+
 extern "C" int nova_pages_free(const nova_pages* pages, int32_t* tables, int max_blocks, int batch, const int32_t* seqs,
                                const int32_t* tokens, int n, nova_stream_t stream) {
   if (int rc = check_pages(pages, tables, max_blocks, batch, n)) return rc;
   if (n == 0) return NOVA_OK;
   if (!seqs || !aligned4(seqs) || !aligned4(tokens)) return fail(NOVA_EINVAL, "seqs null, or an array misaligned");
-  nova::PagesArgs a = pages_args(pages, tables, max_blocks, batch);
-  a.src = seqs, a.lens = tokens, a.n = n;
-  hipStream_t s = (hipStream_t)stream;
-  CALL(NOVA_KIND_MISC, s, nova::pages_free(a, s));
-  return NOVA_OK;
+  if (tokens) return fail(NOVA_EUNSUPPORTED, "free: keeping tokens can be refused row by row, which nova_pages_trim reports");
+  return give_up(pages, tables, max_blocks, batch, seqs, nullptr, n, nullptr, (hipStream_t)stream);
 }
 
 extern "C" int nova_pages_compact(const nova_pages* pages, const nova_cache* cache, int layers, const int32_t* tables, int max_blocks,

@@ -138,6 +138,7 @@ _SIG = {
     "nova_pages_fork": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p,
                                   C.c_int, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "nova_pages_free": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p]),
+    "nova_pages_trim": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p]),
     "nova_pages_compact": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p,
                                      C.c_void_p, C.c_size_t, C.c_void_p]),
     "nova_lora_workspace_bytes": (C.c_size_t, [C.c_void_p, C.c_void_p]),
@@ -922,7 +923,8 @@ def kv_copy(cache, src, dst, to=None, stream=None):
 class Pages:
     """Which blocks of a pool are in use: ``refs`` int32 [num_blocks], how many table entries name each.  Tables are int32
     [batch, max_blocks], -1 where there is no block.  The lowest free blocks are taken, in the order of the requests; a
-    request that finds too few is left as it was and says 0 in what the call returns (int32, 1: served)."""
+    request that finds too few is left as it was and says 0 in what the call returns (int32, 1: served).  Rows share whole
+    pages only and append behind them; a program that lowers a row's context by itself has to see to that."""
 
     def __init__(self, num_blocks, device="cuda"):
         self._own(torch.zeros(num_blocks, dtype=torch.int32, device=device))
@@ -979,13 +981,21 @@ class Pages:
         return done
 
     def free(self, tables, seqs, tokens=None, stream=None):
-        """Rows ``seqs`` (int32 [n]) give up what lies behind their first ``tokens`` (int32 [n]; None: 0) tokens."""
+        """Rows ``seqs`` (int32 [n]) give up everything.  With ``tokens`` (int32 [n]): what lies behind their first tokens;
+        returns which were served.  A row that would end inside a page that others name too is not, since it would go on in
+        their page: it is left as it was (``fork`` its tokens to another row, which copies that page, and free this one)."""
         batch, width = self._tables(tables)
         _check_device(self.device, tables, seqs, tokens)
         n = seqs.shape[0] if seqs.dim() == 1 else 0
         _check_vector("seqs", seqs, torch.int32, n)
         _check_vector("tokens", tokens, torch.int32, n)
-        _check(lib.nova_pages_free(self.ref, tables.data_ptr(), width, batch, seqs.data_ptr(), _ptr(tokens), n, _stream_on(self.device, stream)))
+        if tokens is None:
+            _check(lib.nova_pages_free(self.ref, tables.data_ptr(), width, batch, seqs.data_ptr(), None, n, _stream_on(self.device, stream)))
+            return None
+        done = _empty(tokens, n, torch.int32, stream)
+        _check(lib.nova_pages_trim(self.ref, tables.data_ptr(), width, batch, seqs.data_ptr(), tokens.data_ptr(), n, done.data_ptr(),
+                                   _stream_on(self.device, stream)))
+        return done
 
     def compact(self, cache, tables, refs_out=None, tables_out=None, stream=None):
         """The pool's used blocks moved to its front in every layer of ``cache``; the tables (all that name its blocks)
