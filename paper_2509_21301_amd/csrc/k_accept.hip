@@ -422,7 +422,7 @@ constexpr int AC_TEST = 512, AC_WAVES = AC_TEST / 64;
 static_assert(AC_PARTS == AC_THREADS / 64 && AC_SHARES == AC_WAVES);
 template <typename TL, typename TD>
 __global__ void __launch_bounds__(AC_TEST) accept_draft_kernel(AcceptArgs p) {
-  const int b = blockIdx.x / p.chunks, chunk = blockIdx.x % p.chunks;
+  const int b = blockIdx.y, chunk = blockIdx.x;
   const SeqRows sr = seq_rows(p.r, b);
   if (sr.n <= 0) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -543,7 +543,8 @@ static hipError_t accept_types(const AcceptArgs& p, hipStream_t s) {
   hipLaunchKernelGGL((accept_stats_kernel<TL, TD>), dim3((unsigned)blocks), dim3(256), 0, s, p);
   if (hipError_t e = hipGetLastError()) return e;
   if (p.r.rows == 0) return hipSuccess;
-  if (p.draft) hipLaunchKernelGGL((accept_draft_kernel<TL, TD>), dim3((unsigned)((long)p.r.batch * p.chunks)), dim3(AC_TEST), 0, s, p);
+  // in two dimensions: sequences times chunks times 512 threads may pass the 2^32 of one
+  if (p.draft) hipLaunchKernelGGL((accept_draft_kernel<TL, TD>), dim3((unsigned)p.chunks, (unsigned)p.r.batch), dim3(AC_TEST), 0, s, p);
   else hipLaunchKernelGGL((accept_follow_kernel<TL>), dim3((unsigned)p.r.rows), dim3(256), 0, s, p);
   return hipGetLastError();
 }

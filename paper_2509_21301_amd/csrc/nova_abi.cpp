@@ -1009,7 +1009,9 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
 }
 
-constexpr int64_t MAX_ACCEPT_BLOCKS = 1 << 24;    // workgroups of 256 threads: a grid dimension has fewer than 2^32
+// Rows times chunks: workgroups of 256 threads in one grid dimension, which has fewer than 2^32 (sequences times chunks are
+// two dimensions; their limit is the workspace's size).
+constexpr int64_t MAX_ACCEPT_BLOCKS = 1 << 24;
 
 int check_accept(const nova_rows* rows, int vocab, bool draft) {
   if (int rc = check_row_starts(rows, 64)) return rc;
