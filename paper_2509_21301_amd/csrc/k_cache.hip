@@ -9,6 +9,7 @@
 #include <algorithm>
 
 #include "paged.hpp"
+#include "rotate_plan.hpp"
 
 namespace nova {
 
@@ -282,21 +283,14 @@ hipError_t kv_append(const AppendArgs& p, int cus, hipStream_t s) {
 }
 
 // ------------------------------------------------------------------ rotary embedding of dense rows
-// Workgroup: some rows (as many as make a round of items) of a group of heads.  The rows' sines and cosines are formed once in LDS; then a lane takes an item at a
-// time: 8 pairs of the half layout (two loads of 8 elements, rot/2 apart), 8 elements of the interleaved one or 8 that
-// are not turned.  Items are numbered over rows and heads so that neighbouring lanes read neighbouring memory, and four
-// are requested before the first is turned.  Bound by HBM: 13416 patches of 32 heads of 80 in bf16, 137 MB, in 30 us, 4.6
+// Workgroup: some rows (as many as make a round of items) of a group of heads.  The rows' sines and cosines are formed
+// once in LDS; then a lane takes an item at a time: 8 pairs of the half layout (two loads of 8 elements, rot/2 apart), 8
+// elements of the interleaved one or 8 that are not turned.  Items are numbered over rows and heads so that neighbouring
+// lanes read neighbouring memory, and four are requested before the first is turned.  Bound by HBM: 13416 patches of 32 heads of 80 in bf16, 137 MB, in 30 us, 4.6
 // TB/s of 5.1 that a large copy reaches (42 us with one item at a time, 33 with 8 rows a workgroup).
-constexpr int ROT_AHEAD = 4;
 
-// n / d for n < 2^32 / d, from m = 2^32 / d + 1 (0 for d = 1).
+// n / d from reciprocal(d), as far as that is exact.
 NOVA_DEV uint32_t div_by(uint32_t n, uint32_t m) { return m ? __umulhi(n, m) : n; }
-inline uint32_t reciprocal(uint32_t d) { return d == 1 ? 0u : (uint32_t)((1ull << 32) / d + 1); }
-
-// Items of a head, rows and heads of a workgroup (at most 16 rows of ROT_ITEMS items, so that div_by is exact over them),
-// and the reciprocals of the items of a head and of a row.
-constexpr int ROT_ITEMS = 4096, ROT_ROWS = 16;
-struct RotateSplit { int items, heads, rows; uint32_t per_item, per_row; };
 
 template <typename TI, typename TO, bool INTER>
 __global__ void __launch_bounds__(256) rotate_kernel(RotateArgs p, RotateSplit d) {
@@ -375,16 +369,9 @@ __global__ void __launch_bounds__(256) rotate_kernel(RotateArgs p, RotateSplit d
 
 template <typename TI, typename TO>
 static hipError_t rotate_types(const RotateArgs& p, int cus, hipStream_t s) {
-  RotateSplit d;
-  d.items = (p.interleaved ? p.rot / 8 : p.rot / 16) + (p.D - p.rot) / 8;
-  d.heads = std::min(p.heads, ROT_ITEMS / d.items);
-  d.per_item = reciprocal(d.items);
-  d.per_row = reciprocal(d.items * d.heads);
-  // Rows that give every thread ROT_AHEAD items, fewer while that leaves fewer than two workgroups for each compute unit.
-  const long row = (long)d.items * d.heads, groups = (p.heads + d.heads - 1) / d.heads;
-  d.rows = (int)std::max(1l, std::min<long>({ROT_ROWS, 256 * ROT_AHEAD / row, p.rows * groups / (2l * cus)}));
+  const RotateSplit d = split_rotate(p.rows, p.heads, p.D, p.rot, p.interleaved, cus);
   const size_t lds = (size_t)d.rows * p.rot * sizeof(float);
-  const dim3 grid((p.rows + d.rows - 1) / d.rows, (unsigned)groups);
+  const dim3 grid(d.row_groups, d.head_groups);
   if (p.interleaved) hipLaunchKernelGGL((rotate_kernel<TI, TO, true>), grid, dim3(256), lds, s, p, d);
   else hipLaunchKernelGGL((rotate_kernel<TI, TO, false>), grid, dim3(256), lds, s, p, d);
   return hipGetLastError();
