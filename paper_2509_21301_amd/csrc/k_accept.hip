@@ -299,8 +299,8 @@ template <typename F> NOVA_DEV int first_above(int n, double target, double* bef
   return last;
 }
 
-// The token of SIZE logits from c0 on whose running sum of weight(i) exceeds `target`; by the whole workgroup of THREADS.
-// First the thread's range of consecutive logits, then the logit in it, one a lane.
+// The token of SIZE logits from c0 on whose running sum of weight(i) exceeds `target` (-1: none has a weight); by the whole
+// workgroup of THREADS.  First the thread's range of consecutive logits, then the logit in it, one a lane.
 template <int SIZE, int THREADS, typename F> NOVA_DEV int draw_in_part(int c0, int vocab, double target, F&& weight) {
   constexpr int PER = SIZE / THREADS;
   __shared__ double sm_sum[THREADS];
@@ -316,6 +316,7 @@ template <int SIZE, int THREADS, typename F> NOVA_DEV int draw_in_part(int c0, i
   __syncthreads();
   double before = 0.0;
   const int t = first_above(THREADS, target, &before, [&](int i) { return sm_sum[i]; });
+  if (!(sm_sum[t] > 0.0)) return -1;
   const int from = c0 + t * PER;
   double none;
   return from + first_above(min(PER, vocab - from), target - before, &none, [&](int i) { return weight(from + i); });
@@ -335,8 +336,16 @@ template <int THREADS, typename TL> NOVA_DEV int draw_row(const AcceptArgs& p, c
   __shared__ double sm_parts[AC_MAX_CHUNKS * AC_PARTS];
   for (int i = threadIdx.x; i < p.chunks * AC_PARTS; i += THREADS) sm_parts[i] = p.part_sum[at * AC_PARTS + i] * scale(p.part_max[at + i / AC_PARTS]);
   __syncthreads();
-  const int c = first_above(p.chunks * AC_PARTS, target, &before, [&](int i) { return sm_parts[i]; });
-  return draw_in_part<AC_PART, THREADS>(c * AC_PART, p.vocab, target - before, [&](int i) { return weight(tab, logit(row, i)); });
+  // A part's sum, which was formed relative to its chunk's maximum, may be positive where each of its weights underflows
+  // (met by numbers of 0 only): then the draw goes on behind it.  The part of the largest logit has a weight of 1.
+  while (true) {
+    const int c = first_above(p.chunks * AC_PARTS, target, &before, [&](int i) { return sm_parts[i]; });
+    const int token = draw_in_part<AC_PART, THREADS>(c * AC_PART, p.vocab, target - before, [&](int i) { return weight(tab, logit(row, i)); });
+    if (token >= 0) return token;
+    __syncthreads();
+    if (threadIdx.x == 0) sm_parts[c] = 0.0;
+    __syncthreads();
+  }
 }
 
 // log p of a token of a row.
