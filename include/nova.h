@@ -439,7 +439,8 @@ int nova_pages_compact(const nova_pages* pages, const nova_cache* cache, int lay
 /* ------------------------------------------------------------------ adapters
  * Low-rank adapters of many requests beside a projection that they share:
  *   out[row] = base[row] + scale[i] b[i] (a[i] x[row]),  i = which[sequence of the row]
- * (fp32 sums, rounded once; which outside 0 .. n - 1: no adapter, out is base).  Rows outside the sequences are left as
+ * (fp32 sums, a[i] x[row] taken on in all its 24 bits, rounded once; which outside 0 .. n - 1: no adapter, out is base;
+ * an infinite weight gives infinity or NaN).  Rows outside the sequences are left as
  * they were.
  *  which: device int32 [batch];  x: device, x_type;  base: device, out_type, NULL: 0;  out: device, out_type, may be
  *         base itself (same pitch); pitches in elements, a multiple of 16 bytes

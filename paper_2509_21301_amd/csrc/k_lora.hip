@@ -1,11 +1,11 @@
 // Low-rank adapters of many requests beside a projection that they share: with i the adapter of a row's sequence,
 //   out = base + s_i B_i (A_i x),   A_i [rank][K], B_i [N][rank].
 //  * shrink: h = A_i x per row, tiles of a sequence's rows times a slice of K, fp32 partials [slice][row][rank];
-//  * join (long sequences): the slices summed in order, as the operands that expand takes;
+//  * join (long sequences): the slices summed in order;
 //  * expand: B_i h, times s_i, onto base, rounded once.  Short tiles sum the slices themselves (a launch less).
 // The ranks are far below what would make this compute-bound: it is bound by reading x, base and the adapters and by
-// writing out.  The matrix cores take bf16, so h goes to them as a sum of bf16 parts, an MFMA each: two (a relative error
-// of 2^-16 instead of a bf16 rounding's 2^-8) where out is bf16, three (all 24 bits) where it is fp32.  x in fp32 likewise.
+// writing out.  The matrix cores take bf16, so h, and x in fp32, go to them as a sum of three bf16 parts, which hold all 24
+// bits, an MFMA each.
 #include <algorithm>
 
 #include "paged.hpp"
@@ -52,20 +52,29 @@ template <int TM> NOVA_DEV SeqRows find_row_tile(const BatchRows& p, int tile, i
   return SeqRows{0, 0, 0};
 }
 
-// What a bf16 rounding of v leaves; nothing of what is not finite.
-NOVA_DEV float rest_of(float v, float rounded) { return fabsf(rounded) < INFINITY ? v - rounded : 0.f; }
+// An fp32 number is the sum of three of bf16, 8 of its 24 bits each: cut off, not rounded, so that no part of a finite
+// number is infinite.  The upper halves of two floats in a dword (a's in the low half), those halves as floats, and what
+// they leave (of infinity nothing; of NaN NaN).
+constexpr int LO_PARTS = 3;
+NOVA_DEV uint32_t top2(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); }
+NOVA_DEV float top(float v) { return __uint_as_float(__float_as_uint(v) & 0xFFFF0000u); }
+NOVA_DEV float rest_of(float v) {
+  const float t = top(v);
+  return v == t ? 0.f : v - t;
+}
 
-// Eight floats as a sum of N operands of bf16, each the rounded rest of those before it.
+// Eight floats as a sum of N operands of bf16.
 template <int N> NOVA_DEV void split_parts(float* x, Frag8* f) {
 #pragma unroll
   for (int n = 0; n < N; ++n)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      f[n].w[i] = pack2(x[2 * i], x[2 * i + 1]);
-      x[2 * i] = rest_of(x[2 * i], __uint_as_float(f[n].w[i] << 16));
-      x[2 * i + 1] = rest_of(x[2 * i + 1], __uint_as_float(f[n].w[i] & 0xFFFF0000u));
+      f[n].w[i] = top2(x[2 * i], x[2 * i + 1]);
+      x[2 * i] = rest_of(x[2 * i]);
+      x[2 * i + 1] = rest_of(x[2 * i + 1]);
     }
 }
+
 // Eight elements of x as loaded, and as N operands.
 template <typename T> struct Raw;
 template <> struct Raw<bf16_t> { Frag8 f; };
@@ -227,9 +236,10 @@ __global__ void __launch_bounds__(256) lora_down_kernel(LoraArgs p) {
 }
 
 // ------------------------------------------------------------------ h joined
-// Thread: four ranks of a row, as the expand's operands [part][row][32 KS], zeros behind the rank.  Rows without an adapter
-// (whose partials nobody wrote) give what nobody reads.
-template <int KS, int NH>
+// Thread: four ranks of a row, [row][32 KS] with zeros behind the rank, in fp32: the expand reads every row once for each of
+// its columns' workgroups, and parts would be half as much again.  Rows without an adapter (whose partials nobody wrote) give
+// what nobody reads.
+template <int KS>
 __global__ void __launch_bounds__(256) lora_join_kernel(LoraArgs p) {
   const long i = (long)blockIdx.x * 256 + threadIdx.x, row = i / (8 * KS);
   const int c = (int)(i % (8 * KS)) * 4;
@@ -239,15 +249,7 @@ __global__ void __launch_bounds__(256) lora_join_kernel(LoraArgs p) {
 #pragma unroll 4
     for (int s = 0; s < p.slices; ++s) h += *reinterpret_cast<const f32x4*>(p.part + ((size_t)s * p.r.rows + row) * p.rank + c);
   }
-#pragma unroll
-  for (int n = 0; n < NH; ++n) {
-    const uint2 w = make_uint2(pack2(h[0], h[1]), pack2(h[2], h[3]));
-    *reinterpret_cast<uint2*>(p.parts + ((size_t)n * p.r.rows + row) * (32 * KS) + c) = w;
-    h[0] = rest_of(h[0], __uint_as_float(w.x << 16));
-    h[1] = rest_of(h[1], __uint_as_float(w.x & 0xFFFF0000u));
-    h[2] = rest_of(h[2], __uint_as_float(w.y << 16));
-    h[3] = rest_of(h[3], __uint_as_float(w.y & 0xFFFF0000u));
-  }
+  *reinterpret_cast<f32x4*>(p.joined + row * (32 * KS) + c) = h;
 }
 
 // ------------------------------------------------------------------ out = base + s B h
@@ -294,9 +296,8 @@ template <typename TO, int RT>
 __global__ void __launch_bounds__(256) lora_expand_kernel(LoraArgs p) {
   constexpr int KS = (RT + 1) / 2;                           // steps of 32 of the rank
   constexpr int LD = 32 * KS + 8;                            // row pitch of h in LDS (16 bytes more: rows on other banks)
-  constexpr int NH = sizeof(TO) == 4 ? 3 : 2;                // parts of h
   constexpr int CH = 2 * RT;                                 // chunks of a column of B, and of a lane
-  __shared__ __align__(16) bf16_t sm[NH][LO_STEP][LD];
+  __shared__ __align__(16) bf16_t sm[LO_PARTS][LO_STEP][LD];
   __shared__ __align__(16) Frag8 sm_b[4][64][CH];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
   int b, row0;
@@ -339,10 +340,9 @@ __global__ void __launch_bounds__(256) lora_expand_kernel(LoraArgs p) {
         for (int s = 0; s < p.slices; ++s) h += p.part[((size_t)s * p.r.rows + r0 + rr) * p.rank + c];
       }
 #pragma unroll
-      for (int n = 0; n < NH; ++n) {
-        const bf16_t part = f2bf(h);
-        sm[n][rr][c] = part;
-        h = rest_of(h, bf2f(part));
+      for (int n = 0; n < LO_PARTS; ++n) {
+        sm[n][rr][c] = (bf16_t)(__float_as_uint(h) >> 16);
+        h = rest_of(h);
       }
     }
     __syncthreads();
@@ -365,15 +365,15 @@ __global__ void __launch_bounds__(256) lora_expand_kernel(LoraArgs p) {
       // tile t = 2 q + h, MFMA row m: column 32 q + 8 (m / 4) + 4 h + m % 4 of the step, so that lane group g holds 32 q + 8 g ..
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        Frag8 h[NH];
+        Frag8 h[LO_PARTS];
 #pragma unroll
-        for (int q = 0; q < NH; ++q) h[q] = *reinterpret_cast<const Frag8*>(&sm[q][col][32 * ks + 8 * grp]);
+        for (int q = 0; q < LO_PARTS; ++q) h[q] = *reinterpret_cast<const Frag8*>(&sm[q][col][32 * ks + 8 * grp]);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const int n = 32 * (t >> 1) + 8 * (col >> 2) + 4 * (t & 1) + (col & 3), c = 4 * ks + grp;
           const Frag8 f = CH >= 4 || grp < 2 ? sm_b[wave][n][turn_chunk<CH>(n, CH >= 4 ? c : c & 1)] : zero_frag();
 #pragma unroll
-          for (int q = 0; q < NH; ++q) acc[t] = mfma16(f, h[q], acc[t]);
+          for (int q = 0; q < LO_PARTS; ++q) acc[t] = mfma16(f, h[q], acc[t]);
         }
       }
     }
@@ -423,7 +423,6 @@ template <typename T> NOVA_DEV u32x4 pack16(const float* x) {
 template <typename TO, int RT, int RW>
 __global__ void __launch_bounds__(256) lora_up_kernel(LoraArgs p) {
   constexpr int KS = (RT + 1) / 2, TM = 64 * RW;
-  constexpr int NH = sizeof(TO) == 4 ? 3 : 2;
   constexpr int CH = 2 * RT, BC = 64 * CH / 256 > 0 ? 64 * CH / 256 : 1;   // chunks of a column of B; of a thread
   constexpr int E = 16 / sizeof(TO), LPR = 64 / E, RPI = 64 / LPR, IT = 16 / RPI;   // of out: elements and lanes of a row, rows of an instruction
   constexpr int LD = 68;                                     // floats of a row in LDS
@@ -441,15 +440,15 @@ __global__ void __launch_bounds__(256) lora_up_kernel(LoraArgs p) {
   if (!has && base == out) return;                           // nothing is added
   const float scale = has && p.scale ? p.scale[i] : 1.f;
   const bf16_t* B = p.b + (has ? (size_t)i * p.nout * p.rank : 0);
-  Frag8 h[RW][KS][NH];
+  Frag8 h[RW][KS][LO_PARTS];
 #pragma unroll
   for (int w = 0; w < RW; ++w)
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-      for (int n = 0; n < NH; ++n)
-        h[w][ks][n] = has ? *reinterpret_cast<const Frag8*>(p.parts + ((size_t)n * p.r.rows + r0 + min(16 * (RW * wave + w) + col, rows - 1)) * (32 * KS) + 32 * ks + 8 * grp)
-                          : zero_frag();
+    for (int ks = 0; ks < KS; ++ks) {
+      float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (has) unpack_out8(load_out8(p.joined + (r0 + min(16 * (RW * wave + w) + col, rows - 1)) * (32 * KS) + 32 * ks + 8 * grp), y);
+      split_parts<LO_PARTS>(y, h[w][ks]);
+    }
   const int bn = threadIdx.x / CH, bc = threadIdx.x % CH;    // the thread's first column and chunk
   Frag8 rb[BC];
   u32x4 old[RW][IT], next[RW][IT];
@@ -506,7 +505,7 @@ __global__ void __launch_bounds__(256) lora_up_kernel(LoraArgs p) {
 #pragma unroll
           for (int w = 0; w < RW; ++w)
 #pragma unroll
-            for (int q = 0; q < NH; ++q) acc[w][t] = mfma16(f, h[w][ks][q], acc[w][t]);
+            for (int q = 0; q < LO_PARTS; ++q) acc[w][t] = mfma16(f, h[w][ks][q], acc[w][t]);
         }
     }
     // acc[w][t][e]: row 16 (RW wave + w) + col, column 16 t + 4 grp + e
@@ -553,25 +552,25 @@ static int lora_slices(const LoraArgs& p, int cus) {
   const long tiles = std::max(1l, lora_tiles(p)), want = (4l * cus + tiles - 1) / tiles, least = lora_blocks(p) ? 256 : 512;
   return (int)std::max(1l, std::min<long>(want, (p.k + least - 1) / least));
 }
-static size_t parts_at(const LoraArgs& p, int slices) { return ((size_t)slices * p.r.rows * p.rank * sizeof(float) + 255) / 256 * 256; }
+static size_t joined_at(const LoraArgs& p, int slices) { return ((size_t)slices * p.r.rows * p.rank * sizeof(float) + 255) / 256 * 256; }
 size_t lora_bytes(const LoraArgs& p, int cus) {
-  // three parts (of an fp32 out) of the rank, rounded up to the widths that the kernels have
+  // and h, of the rank rounded up to the widths that the kernels have
   const int wide = p.rank <= 32 ? 32 : p.rank <= 64 ? 64 : 128;
-  return parts_at(p, lora_slices(p, cus)) + (lora_blocks(p) ? (size_t)3 * p.r.rows * wide * sizeof(bf16_t) : 0);
+  return joined_at(p, lora_slices(p, cus)) + (lora_blocks(p) ? (size_t)p.r.rows * wide * sizeof(float) : 0);
 }
 
 template <typename TX, typename TO, int RT, int RW>
 static hipError_t lora_launch(const LoraArgs& p, int cus, hipStream_t s) {
-  constexpr int NX = sizeof(TX) == 2 ? 1 : sizeof(TO) == 2 ? 2 : 3;
+  constexpr int NX = sizeof(TX) == 2 ? 1 : LO_PARTS;
   const unsigned tiles = (unsigned)lora_tiles(p);
   const dim3 slices(tiles, p.slices);
   if constexpr (RW == 0) {
     hipLaunchKernelGGL((lora_shrink_kernel<TX, NX, RT>), slices, dim3(256), 0, s, p);
   } else {
-    constexpr int KS = (RT + 1) / 2, NH = sizeof(TO) == 4 ? 3 : 2;
+    constexpr int KS = (RT + 1) / 2;
     hipLaunchKernelGGL((lora_down_kernel<TX, NX, RT, RW>), slices, dim3(256), 0, s, p);
     if (hipError_t e = hipGetLastError()) return e;
-    hipLaunchKernelGGL((lora_join_kernel<KS, NH>), dim3((unsigned)(((long)p.r.rows * 8 * KS + 255) / 256)), dim3(256), 0, s, p);
+    hipLaunchKernelGGL((lora_join_kernel<KS>), dim3((unsigned)(((long)p.r.rows * 8 * KS + 255) / 256)), dim3(256), 0, s, p);
   }
   if (hipError_t e = hipGetLastError()) return e;
   // columns of a workgroup: whole steps, twelve workgroups for each compute unit (3751 rows onto 37888 columns at rank 64:
@@ -605,7 +604,7 @@ hipError_t lora(const LoraArgs& p, int cus, hipStream_t s) {
   if (p.rank <= 0 || p.rank > 128 || p.rank % 8 || p.k % 8 || p.nout % 8) return hipErrorInvalidValue;
   LoraArgs q = p;
   q.slices = lora_slices(p, cus);
-  q.parts = (bf16_t*)((char*)p.part + parts_at(p, q.slices));
+  q.joined = (float*)((char*)p.part + joined_at(p, q.slices));
   q.kslice = ((p.k + q.slices - 1) / q.slices + 63) / 64 * 64;
   if (p.x_f32) return p.out_f32 ? lora_types<float, float>(q, cus, s) : lora_types<float, bf16_t>(q, cus, s);
   return p.out_f32 ? lora_types<bf16_t, float>(q, cus, s) : lora_types<bf16_t, bf16_t>(q, cus, s);

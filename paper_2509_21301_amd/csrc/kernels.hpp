@@ -325,7 +325,7 @@ struct LoraArgs {
   const void* base; long base_row;
   void* out; long out_row; bool out_f32;
   float* part;                                          // lora_bytes(): partials [slices][rows][rank], then
-  bf16_t* parts;                                        // the joined h; set by the launcher, like those below
+  float* joined;                                        // their sums; set by the launcher, like those below
   int slices, kslice, cols;
 };
 size_t lora_bytes(const LoraArgs& p, int cus);
