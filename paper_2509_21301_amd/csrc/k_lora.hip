@@ -535,12 +535,17 @@ __global__ void __launch_bounds__(256) lora_up_kernel(LoraArgs p) {
 }
 
 // ------------------------------------------------------------------ launch
-// Blocks of 16 rows a wave of the kernels for long sequences takes (0: those for short ones): by the rows that a sequence
-// has on average.  Onto 37888 columns, us with 0 / 1 / 2: 8 sequences of 24 rows 21 / 21 / 24; one of 2000 at rank 64 155 /
-// 94 / 84, with 31 of one row beside it 161 / 132 / 123, with 127 197 / 220 / 228; 64 of one row 24 / 45 / 61.
+// Blocks of 16 rows a wave of the kernels for long sequences takes (0: those for short ones): long ones by the rows that a
+// sequence has on average, two blocks, which read B half as often, where the result is large and h of both leaves registers
+// enough.  us of a call in a graph with 0 / 1 / 2:
+//  * onto 37888 columns: 8 sequences of 24 rows at rank 16 20 / 21 / 29; one of 2000 at rank 64 147 / 84 / 86, with 31 of one
+//    row beside it 157 / 110 / 120, with 127 187 / 181 / 241; 64 of one row at rank 16 24 / 45 / 73;
+//  * with 1 / 2 onto 37888 columns: one of 600 rows at rank 64 35 / 38, of 4000 153 / 147, at rank 128 191 / 184 (fp32 285 /
+//    308); 8 of 140 63 / 74; 3751 rows at rank 64 onto 3584 33 / 36, in fp32 onto 4608 60 / 66.
 static int lora_blocks(const LoraArgs& p) {
   const long rows = p.r.rows, batch = p.r.batch;
-  return rows >= 128 * batch ? 2 : rows >= 32 * batch ? 1 : 0;
+  if (rows < 32 * batch) return 0;
+  return rows >= 128 * batch && rows * p.nout >= 100000000 && p.rank <= 64 ? 2 : 1;
 }
 static long lora_tiles(const LoraArgs& p) {
   const int rw = lora_blocks(p), tm = rw ? 64 * rw : LO_STEP;
@@ -574,7 +579,7 @@ static hipError_t lora_launch(const LoraArgs& p, int cus, hipStream_t s) {
   }
   if (hipError_t e = hipGetLastError()) return e;
   // columns of a workgroup: whole steps, twelve workgroups for each compute unit (3751 rows onto 37888 columns at rank 64:
-  // 115 us, 118 with eight, 140 with four)
+  // 147 us a call, 150 with eight, 168 with four)
   LoraArgs q = p;
   const int step = RW ? 64 : 256;
   const long steps = (p.nout + step - 1) / step, groups = std::min(steps, std::max(1l, 12l * cus / tiles));
@@ -589,7 +594,7 @@ static hipError_t lora_rank(const LoraArgs& p, int cus, hipStream_t s) {
   if (p.rank <= 16) return lora_launch<TX, TO, 1, RW>(p, cus, s);
   if (p.rank <= 32) return lora_launch<TX, TO, 2, RW>(p, cus, s);
   if (p.rank <= 64) return lora_launch<TX, TO, 4, RW>(p, cus, s);
-  return lora_launch<TX, TO, 8, RW>(p, cus, s);
+  return lora_launch<TX, TO, 8, RW == 2 ? 1 : RW>(p, cus, s);   // lora_blocks(): two up to rank 64
 }
 template <typename TX, typename TO>
 static hipError_t lora_types(const LoraArgs& p, int cus, hipStream_t s) {

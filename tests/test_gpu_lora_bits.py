@@ -73,3 +73,32 @@ def test_range_of_fp32(gpu_lib, out, rows):
     sign[3] = -1
     assert torch.equal(got[2], sign * float("inf")) and torch.equal(got[3], -sign * float("inf")) and torch.isnan(got[4]).all()
     assert (got[[0, 1, *range(5, total)]] == 0).all()
+
+
+@pytest.mark.parametrize("types", [(BF16, BF16), (F32, BF16), (BF16, F32), (F32, F32)])
+@pytest.mark.parametrize("rank", [8, 32, 64, 72])
+def test_large_results(gpu_lib, types, rank):
+    """More than 10^8 numbers of result, whose tiles are the largest; sequences that end inside them, and one without an adapter."""
+    nova = gpu_lib
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rank)
+    rows, k, n_out = [9000, 40, 0, 3000, 1001], 72, 8192
+    which, scale = [1, 0, 1, -1, 0], torch.tensor([1.0, -0.5], device="cuda")
+    total = sum(rows)
+    assert total * n_out > 10 ** 8
+    whole = lambda lo, hi, *s: torch.randint(lo, hi, s, generator=g, device="cuda").to(F32)  # noqa: E731
+    # sums of 72 numbers below 2^8, then of at most 72 of those times 3: below 2^22; in fp32 below 2^12, and two: below 2^21
+    top = 1 << (12 if types[0] == F32 else 8)
+    x, a, b = whole(1 - top, top, total, k).to(types[0]), whole(-1, 2, 2, rank, k).to(BF16), whole(-3, 4, 2, n_out, rank).to(BF16)
+    if types[0] == F32:                      # two ranks of a column only
+        b[:, :, 2:] = 0
+    base = whole(-100, 101, total, n_out).to(types[1])
+    got = nova.lora(nova.Adapters(a, b, scale), _rows(nova, rows), _i32(which), x, base=base)
+    at = 0
+    for n, i in zip(rows, which):
+        sl = slice(at, at + n)
+        at += n
+        want = base[sl].double()
+        if i >= 0:
+            want = want + float(scale[i]) * ((x[sl].double() @ a[i].double().T.contiguous()) @ b[i].double().T.contiguous())
+        assert torch.equal(got[sl], want.to(F32).to(types[1]))
