@@ -104,10 +104,11 @@ NOVA_DEV void wave_lds_fence() {
 // workgroup into LDS.  Pairs of the half layout lie D/8 or fewer lanes apart and are exchanged by a
 // shuffle; the maximum of a row is a shuffle reduction over its lanes.  V is turned to [D][16]
 // through wave-private LDS: a whole block leaves as 16 tokens per lane, a part of one per element.
-// Bound by HBM for prompts (3579 tokens of 28 + 2 x 4 heads of 128 in bf16 into an e4m3 cache: 62 MB in 16.5 to
-// 17.8 us, 3.6 TB/s where a large copy reaches 5.0), by latency for a decode step (32 tokens: 7.3 us, a chain
-// of row starts, table, rows and stores; six sequences' drafts of 8 to 13: 6.4 us).  Positions with several axes cost the
-// pair's axis and a load of its own: 17.1 to 18.4 and 7.5 us for those prompts and that step.
+// Prompts run between HBM and what is formed beside it: 3579 tokens of 28 + 2 x 4 heads of 128 in bf16 into an e4m3
+// cache, 62 MB, in 16.5 to 17.8 us, 3.6 TB/s where a large copy reaches 5.0 (every group of heads forms its block's
+// 64-bit sines again).  A decode step is bound by latency (32 tokens: 7.3 us, a chain of row starts, table, rows and
+// stores; six sequences' drafts of 8 to 13: 6.4 us).  Positions with several axes cost the pair's axis and a load of its
+// own: 16.6 to 18.6 and 7.5 us for those prompts and that step.
 template <typename TI, typename TO, typename CT, int D>
 __global__ void __launch_bounds__(256) kv_append_kernel(AppendArgs p, int heads_per_wg) {
   constexpr int LPR = D / 8, RPI = 64 / LPR, NI = PAGE / RPI;

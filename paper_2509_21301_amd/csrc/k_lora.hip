@@ -290,8 +290,8 @@ template <int CH> NOVA_DEV int turn_chunk(int n, int c) { return CH >= 8 ? c ^ (
 // Workgroup: (tile of 16 rows, `cols` columns); a wave takes 64 columns at a time, whose B it loads in one run and turns
 // into MFMA operands in LDS of its own, a step ahead; the first step's loads are on their way while h is summed.  Which
 // column of B is which MFMA row is free, so two tiles give a lane 8 consecutive columns of its row of out.  K (here the
-// rank) is 32 a step.  Bound by latency: 32 tokens with an adapter each of rank 16 onto 4608 columns 5.3 us (the kernel above
-// 3.5), onto 37888 columns 14.6 us, 2.7 TB/s of adapters.
+// rank) is 32 a step.  Bound by latency: 32 tokens with an adapter each of rank 16 onto 4608 columns 5.3 to 6.3 us (the kernel
+// above 3.6), onto 37888 columns 14.7 us, 2.7 TB/s of adapters.
 template <typename TO, int RT>
 __global__ void __launch_bounds__(256) lora_expand_kernel(LoraArgs p) {
   constexpr int KS = (RT + 1) / 2;                           // steps of 32 of the rank
@@ -417,9 +417,9 @@ template <typename T> NOVA_DEV u32x4 pack16(const float* x) {
 // Workgroup: (tile of 64 RW rows, `cols` columns), RW blocks of 16 rows a wave, whose h stays in registers.  64 columns of
 // B at a time go through LDS for all four waves, loaded a step ahead (turned as in the kernel above), and what they give
 // goes back through LDS, so that base and out are read and written in runs of a row's 64 columns: see there.  3751 rows onto
-// 37888 columns in bf16, rank 64: 115 to 127 us, 4.5 to 4.9 TB/s of 5.1 that a large copy reaches (162 us with operands
-// and rows straight from memory); rank 16 109, rank 128 149, fp32 233 us.  Rows that start off a line of 128 bytes (37896
-// columns) share each line between two steps: 180 us.
+// 37888 columns in bf16, rank 64: 117 to 132 us, 4.3 to 4.9 TB/s of 5.1 that a large copy reaches (162 us with operands
+// and rows straight from memory); rank 16 110, rank 128 (one block) 156 to 181, fp32 228 us.  Rows that start off a line of
+// 128 bytes (37896 columns) share each line between two steps: 182 us.
 template <typename TO, int RT, int RW>
 __global__ void __launch_bounds__(256) lora_up_kernel(LoraArgs p) {
   constexpr int KS = (RT + 1) / 2, TM = 64 * RW;
