@@ -52,8 +52,8 @@ template <int TM> NOVA_DEV SeqRows find_row_tile(const BatchRows& p, int tile, i
   return SeqRows{0, 0, 0};
 }
 
-// An fp32 number is the sum of three of bf16, 8 of its 24 bits each: cut off, not rounded, so that no part of a finite
-// number is infinite.  The upper halves of two floats in a dword (a's in the low half), those halves as floats, and what
+// An fp32 number is the sum of three of bf16, 8 of its 24 bits each (what is below bf16's smallest number, 2^-133, is left
+// out): cut off, not rounded, so that no part of a finite number is infinite.  The upper halves of two floats in a dword (a's in the low half), those halves as floats, and what
 // they leave (of infinity nothing; of NaN NaN).
 constexpr int LO_PARTS = 3;
 NOVA_DEV uint32_t top2(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); }
